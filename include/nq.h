@@ -63,7 +63,8 @@ typedef enum {
     NQ_ERR_TIMEOUT = 6      /* a bounded on-device wait expired (reported by nq_device_status)   */
 } nq_status;
 
-typedef enum { NQ_F32 = 0, NQ_BF16 = 1 } nq_dtype;
+/* NQ_E4M3 (8-bit floating point, 4 exponent and 3 mantissa bits, no infinities) and NQ_I8 only where an entry point names them. */
+typedef enum { NQ_F32 = 0, NQ_BF16 = 1, NQ_E4M3 = 2, NQ_I8 = 3 } nq_dtype;
 
 /* Text for a status code (host, static storage). */
 NQ_API const char *nq_status_str(int status);
@@ -318,6 +319,87 @@ NQ_API int nq_maxpool_nhwc_i8(const int8_t *X, int B, int H, int W, int C, int k
  */
 NQ_API int nq_avgpool_requant_nhwc_i8(const int8_t *X, int B, int H, int W, int C, float in_scale, float out_scale,
                                int8_t *Y, void *stream);
+
+/*
+ * 8-bit floating point with a scale for each block of 128 -- the layers of a network that is trained or served in
+ * e4m3 beside the nested INT8 ones.  (The paper has no counterpart; definitions are the library's own.)
+ *
+ * A matrix [rows, cols] is stored as e4m3 bytes (row pitch a multiple of 16, base 16-byte aligned) and fp32 scales,
+ * GROUPS FIRST: block_rows == 1: scales [ceil(cols/128), rows], one for each row and group of 128 columns;
+ * block_rows == 128: scales [ceil(cols/128), ceil(rows/128)], one for each block of 128 x 128.  Scale pitches (of one
+ * group's scales, in elements) are lds >= rows or >= ceil(rows/128).  A stored value is worth e4m3 * scale.
+ *
+ * Quantiser.  Per group, with one fp32 rounding per operation:
+ *   a = max |x|;  s = max(fl(a / 448), 2^-126);  i = fl(1 / s);  q = e4m3_nearest_even(min(max(fl(x * i), -448), 448))
+ *   A group that holds a NaN gets scale NaN, one that holds an infinity gets scale +inf: its values read as NaN.
+ *   X (device) [rows, cols] of x_dtype (NQ_F32, NQ_BF16), pitch ldx, any element alignment (32-byte aligned rows are
+ *     fastest)
+ *   Q, S  (device, out) the quantised matrix, or both NULL
+ *   Qt, St (device, out) the quantised TRANSPOSE [cols, rows] -- its groups run along the rows of X, as the product
+ *     for a weight gradient (block_rows 1) or an input gradient (block_rows 128) needs them -- or both NULL; written
+ *     in the same pass.  For block_rows == 128 its bytes and scales are those of Q and S, transposed.
+ *   Only the rows x cols values are written, never a pitch's padding.  rows, cols < 2^31 - 128.
+ */
+NQ_API int nq_fp8_quantize(const void *X, int64_t ldx, int x_dtype, int64_t rows, int64_t cols, int block_rows,
+                    void *Q, int64_t ldq, float *S, int64_t lds, void *Qt, int64_t ldqt, float *St, int64_t ldst,
+                    void *stream);
+
+/*
+ * Block norm -- what stands between two blocks of a transformer, in one pass over the rows: the norm after a block,
+ * its gate and residual scale, the residual sum, and the norm before the next block.  Per row, in fp32:
+ *   u = N_post(y);   r = skip_scale * x + branch_scale * gate * u;   h = N_pre(r)
+ *   N(v) = v^ * weight + bias,  v^ = v / sqrt(mean(v^2) + eps)                  NQ_NORM_RMS
+ *                               v^ = (v - mean) / sqrt(mean((v - mean)^2) + eps) NQ_NORM_LAYER
+ *                               N(v) = v                                        NQ_NORM_NONE
+ *   The statistics are those of the unrounded fp32 values; r is rounded once to its type, h once to its own.
+ *   X, R (device) [rows, cols] of x_dtype: the residual stream in and out.  R may be X itself (in place), or NULL (not
+ *     wanted).
+ *   Y (device) [rows, cols] of y_dtype: the block's output; NULL = no block: r = skip_scale * x, and post and gate
+ *     must be absent (NQ_NORM_NONE, NULL).  (x_dtype, y_dtype): (F32, F32), (F32, BF16) or (BF16, BF16).
+ *   gate (device) fp32 rows of cols values, dense: row m uses gate row m / rows_per_gate (one for each sequence, say),
+ *     or gate row 0 throughout when rows_per_gate == 0.  NULL = 1.
+ *   weights, biases (device) fp32 [cols] or NULL (1, 0); NULL where the norm is NQ_NORM_NONE.
+ *   H (device, out) by h_dtype; with pre == NQ_NORM_NONE it must be NULL, otherwise it must be given:
+ *     NQ_F32, NQ_BF16   [rows, cols]
+ *     NQ_E4M3           the operand of nq_fp8_gemm: quantised as nq_fp8_quantize does with block_rows 1; Hs (device, out)
+ *                       its scales [ceil(cols/128), rows], pitch ldhs; ldh a multiple of 16, H 16-byte aligned
+ *     NQ_I8             the activations of the INT8 layers: clip(round_half_even(fl(h * fl(1 / h_scale))), -128, 127), a
+ *                       NaN as 0; ldh a multiple of 16, H 16-byte aligned
+ *   Any other tensor may have any element alignment and pitch (16-byte aligned rows with cols a multiple of 8 are
+ *   fastest).  cols in [1, 16384].
+ */
+enum { NQ_NORM_NONE = 0, NQ_NORM_RMS = 1, NQ_NORM_LAYER = 2 };
+typedef struct {
+    int64_t rows, cols;
+    int64_t ldx, ldy, ldr, ldh;         /* pitches in elements: X, Y, R, H */
+    int64_t lddx, lddy, lddr, lddh;     /* ... of the gradients (backward only) */
+    int64_t rows_per_gate;
+    int32_t x_dtype, y_dtype, h_dtype;
+    int32_t post, pre;
+    float skip_scale, branch_scale, eps, h_scale;
+} nq_block_norm_desc;
+
+NQ_API int nq_block_norm(const nq_block_norm_desc *desc, const void *X, const void *Y, const float *post_weight,
+                  const float *post_bias, const float *gate, const float *pre_weight, const float *pre_bias,
+                  void *R, void *H, float *Hs, int64_t ldhs, void *stream);
+
+/*
+ * Its backward pass, from the r and y of the forward pass (r as it is held; the statistics are computed again):
+ *   R (x_dtype), Y (y_dtype; NULL as in the forward pass)
+ *   dR (x_dtype) gradient that arrives at r from further on, or NULL;  dH (y_dtype, whatever h was rounded to: the
+ *     rounding to 8 bits is passed straight through), NULL exactly when pre == NQ_NORM_NONE.  One of them is needed.
+ *   dX (x_dtype), dY (y_dtype), dgate (fp32, the gate's shape), dpost_weight, dpost_bias, dpre_weight, dpre_bias (fp32
+ *     [cols]) (device, out): any may be NULL; dY, dgate and the post pair only with Y, a norm's pair only with that
+ *     norm.  dX may be dR, dY may be dH (in place).
+ *   post_bias is read for dgate; pre_bias is not needed.
+ *   workspace (device) nq_block_norm_backward_workspace_bytes(desc, gate != NULL) bytes, 16-byte aligned: the column
+ *     sums of each thread block, which a second kernel joins in a fixed order (no atomics: results repeat bit for bit).
+ */
+NQ_API int64_t nq_block_norm_backward_workspace_bytes(const nq_block_norm_desc *desc, int has_gate);
+NQ_API int nq_block_norm_backward(const nq_block_norm_desc *desc, const void *R, const void *Y, const void *dR, const void *dH,
+                           const float *post_weight, const float *post_bias, const float *gate, const float *pre_weight,
+                           void *dX, void *dY, float *dgate, float *dpost_weight, float *dpost_bias,
+                           float *dpre_weight, float *dpre_bias, void *workspace, int64_t workspace_bytes, void *stream);
 
 /*
  * The convolution again, for callers that must not allocate.  (The paper has no counterpart; this is a

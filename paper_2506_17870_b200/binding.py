@@ -19,7 +19,8 @@ _LIB_PATH = _PKG / "libnq_b200.so"
 _lib = None
 
 NQ_OK = 0
-NQ_F32, NQ_BF16 = 0, 1
+NQ_F32, NQ_BF16, NQ_E4M3, NQ_I8 = 0, 1, 2, 3
+NQ_NORM_NONE, NQ_NORM_RMS, NQ_NORM_LAYER = 0, 1, 2
 
 EXPORTS = (
     "nq_status_str", "nq_low_bits", "nq_packed_row_bytes", "nq_packed_bytes",
@@ -32,6 +33,7 @@ EXPORTS = (
     "nq_conv_implicit_gemm_nested_q8",
     "nq_i8_mma_ceiling", "nq_debug_set",
     "nq_conv_implicit_gemm_q8_res", "nq_conv_implicit_gemm_nested_q8_res", "nq_maxpool_nhwc_i8", "nq_avgpool_requant_nhwc_i8",
+    "nq_fp8_quantize", "nq_block_norm", "nq_block_norm_backward", "nq_block_norm_backward_workspace_bytes",
     "nq_device_status",
 )
 
@@ -56,6 +58,24 @@ class nq_conv_desc(ctypes.Structure):
                 ("B", "Cin", "H", "W", "Cout", "R", "S", "stride", "pad", "x_nchw")]
 
 
+class nq_block_norm_desc(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_int64) for k in
+                 ("rows", "cols", "ldx", "ldy", "ldr", "ldh", "lddx", "lddy", "lddr", "lddh", "rows_per_gate")] +
+                [(k, ctypes.c_int32) for k in ("x_dtype", "y_dtype", "h_dtype", "post", "pre")] +
+                [(k, ctypes.c_float) for k in ("skip_scale", "branch_scale", "eps", "h_scale")])
+
+
+# Argument types of the entry points whose calls pass plain numbers: a call of a few microseconds is not spent on
+# wrapping each of them.
+_P, _L, _I, _F = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_float
+_ARGTYPES = {
+    "nq_fp8_quantize": (_P, _L, _I, _L, _L, _I, _P, _L, _P, _L, _P, _L, _P, _L, _P),
+    "nq_block_norm": (_P,) * 11 + (_L, _P),
+    "nq_block_norm_backward": (_P,) * 17 + (_L, _P),
+    "nq_block_norm_backward_workspace_bytes": (_P, _I),
+}
+
+
 def lib() -> ctypes.CDLL:
     """The loaded C library.  Raises NqLibraryError when it has not been built."""
     global _lib
@@ -70,8 +90,10 @@ def lib() -> ctypes.CDLL:
             raise NqLibraryError(f"cannot load {_LIB_PATH}: {e}") from e
         L.nq_status_str.restype = ctypes.c_char_p
         for name in ("nq_packed_row_bytes", "nq_packed_bytes", "nq_batch_table_bytes", "nq_conv_workspace_bytes",
-                     "nq_word64_row_words"):
+                     "nq_word64_row_words", "nq_block_norm_backward_workspace_bytes"):
             getattr(L, name).restype = ctypes.c_int64
+        for name, types in _ARGTYPES.items():
+            getattr(L, name).argtypes = types
         _lib = L
     return _lib
 
@@ -593,6 +615,212 @@ def nq_avgpool_requant_nhwc_i8(X: torch.Tensor, in_scale: float, out_scale: floa
     _check(lib().nq_avgpool_requant_nhwc_i8(_ptr(X), B, H, W, C, ctypes.c_float(in_scale), ctypes.c_float(out_scale),
                                             _ptr(y), _stream()), "nq_avgpool_requant_nhwc_i8")
     return y
+
+
+# --------------------------------------------------------------------------- e4m3 with a scale for each block of 128
+_FLOATS = {torch.float32: NQ_F32, torch.bfloat16: NQ_BF16}
+
+
+def _raw_stream(device: torch.device) -> int:
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def _matrix(t: torch.Tensor, name: str, dtype=None, shape=None) -> int:
+    """Checks a [rows, cols] CUDA tensor with neighbouring columns; -> its row pitch."""
+    if t.dim() != 2 or (shape is not None and t.shape != shape):
+        raise ValueError(f"{name} must be a {'[rows, cols]' if shape is None else list(shape)} tensor, got {list(t.shape)}")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    ld, step = t.stride()
+    rows, cols = t.shape
+    if step != 1 and cols > 1 and rows > 0:
+        raise ValueError(f"{name} must be contiguous in its last dimension")
+    if rows > 1:
+        if ld < cols:
+            raise ValueError(f"{name} must have rows that do not overlap (row pitch {ld}, {cols} columns)")
+        return ld
+    return max(cols, 1)
+
+
+def _fp8_pitch(cols: int) -> int:
+    return (cols + 15) & ~15
+
+
+def _fp8_ld(t: torch.Tensor, name: str, shape=None) -> int:
+    """The row pitch of an e4m3 (or INT8) matrix: of a single row, the one that its columns need."""
+    ld = _matrix(t, name, t.dtype, shape)
+    return ld if t.shape[0] > 1 else _fp8_pitch(t.shape[1])
+
+
+def _fp8_empty(rows: int, cols: int, device, dtype=torch.float8_e4m3fn) -> torch.Tensor:
+    """[rows, cols] with a row pitch that is a multiple of 16."""
+    pitch = _fp8_pitch(cols)
+    t = torch.empty((rows, pitch), dtype=dtype, device=device)
+    return t if pitch == cols else t[:, :cols]
+
+
+def _scales(t: torch.Tensor, name: str, groups: int, count: int) -> int:
+    return _matrix(t, name, torch.float32, (groups, count))
+
+
+def nq_fp8_quantize(x: torch.Tensor, block_rows: int = 1, rowwise: bool = True, transposed: bool = False):
+    """[rows, cols] fp32 / bf16 -> (q, s, qt, st): e4m3 [rows, cols] and its scales, groups first
+    ([ceil(cols / 128), rows], or [ceil(cols / 128), ceil(rows / 128)] for block_rows == 128); the same of the transpose
+    x^T (groups along the rows of x).  A pair that is not asked for is (None, None)."""
+    ld = _matrix(x, "x")
+    if x.dtype not in _FLOATS:
+        raise ValueError(f"x must be float32 or bfloat16, got {x.dtype}")
+    if block_rows not in (1, 128):
+        raise ValueError("block_rows must be 1 or 128")
+    if not (rowwise or transposed):
+        raise ValueError("ask for the matrix (rowwise), its transpose (transposed) or both")
+    rows, cols = x.shape
+    device = x.device
+    q = s = qt = st = None
+    if rowwise:
+        q = _fp8_empty(rows, cols, device)
+        s = torch.empty(((cols + 127) // 128, -(-rows // block_rows)), dtype=torch.float32, device=device)
+    if transposed:
+        qt = _fp8_empty(cols, rows, device)
+        st = torch.empty(((rows + 127) // 128, -(-cols // block_rows)), dtype=torch.float32, device=device)
+    _check(lib().nq_fp8_quantize(x.data_ptr(), ld, _FLOATS[x.dtype], rows, cols, block_rows,
+                                 q.data_ptr() if rowwise else None, _fp8_pitch(cols), s.data_ptr() if rowwise else None,
+                                 s.shape[1] if rowwise else 0, qt.data_ptr() if transposed else None, _fp8_pitch(rows),
+                                 st.data_ptr() if transposed else None, st.shape[1] if transposed else 0, _raw_stream(device)),
+           "nq_fp8_quantize")
+    return q, s, qt, st
+
+
+# --------------------------------------------------------------------------- block norm
+def _vector(t: Optional[torch.Tensor], name: str, cols: int):
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.shape != (cols,) or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a dense float32 CUDA vector of {cols}")
+    return t.data_ptr()
+
+
+def _norm_desc(rows, cols, gate, rows_per_gate, post, pre, skip_scale, branch_scale, eps):
+    if post not in (NQ_NORM_NONE, NQ_NORM_RMS, NQ_NORM_LAYER) or pre not in (NQ_NORM_NONE, NQ_NORM_RMS, NQ_NORM_LAYER):
+        raise ValueError("post and pre are NQ_NORM_NONE, NQ_NORM_RMS or NQ_NORM_LAYER")
+    if rows_per_gate < 0:
+        raise ValueError("rows_per_gate must not be negative")
+    if gate is not None:
+        need = -(-rows // rows_per_gate) if rows_per_gate else 1
+        if gate.dtype != torch.float32 or not gate.is_cuda or not gate.is_contiguous() or gate.shape != (need, cols):
+            raise ValueError(f"gate must be a dense float32 CUDA tensor [{need}, {cols}]")
+    d = nq_block_norm_desc()
+    d.rows, d.cols, d.rows_per_gate = rows, cols, rows_per_gate
+    d.post, d.pre, d.skip_scale, d.branch_scale, d.eps = post, pre, skip_scale, branch_scale, eps
+    return d
+
+
+def _norm_types(x: torch.Tensor, y: Optional[torch.Tensor], names) -> None:
+    if x.dtype not in _FLOATS:
+        raise ValueError(f"{names[0]} must be float32 or bfloat16, got {x.dtype}")
+    if y is not None and (y.dtype not in _FLOATS or (x.dtype == torch.bfloat16 and y.dtype != torch.bfloat16)):
+        raise ValueError(f"({names[0]}, {names[1]}) must be (float32, float32), (float32, bfloat16) or (bfloat16, bfloat16), "
+                         f"got ({x.dtype}, {y.dtype})")
+
+
+def nq_block_norm(x: torch.Tensor, y: Optional[torch.Tensor] = None, *, post: int = NQ_NORM_NONE,
+                  post_weight: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None,
+                  gate: Optional[torch.Tensor] = None, rows_per_gate: int = 0, skip_scale: float = 1.0,
+                  branch_scale: float = 1.0, pre: int = NQ_NORM_RMS, pre_weight: Optional[torch.Tensor] = None,
+                  pre_bias: Optional[torch.Tensor] = None, eps: float = 1e-6, h_dtype: Optional[torch.dtype] = None,
+                  h_scale: float = 1.0, want_r: Optional[bool] = None, r_out: Optional[torch.Tensor] = None):
+    """r = skip_scale * x + branch_scale * gate * N_post(y), h = N_pre(r); -> (r, h, hs).
+
+    x, r: the residual stream [rows, cols]; y: the block's output, None for the plain norm of x (then r is returned only
+    when want_r).  gate: [1, cols], or one row for each rows_per_gate rows.  h_dtype: float32, bfloat16 (default: y's
+    type, without y x's), float8_e4m3fn (hs: its scales, groups first) or int8 (static scale h_scale).  r_out may be x."""
+    ldx = _matrix(x, "x")
+    _norm_types(x, y, ("x", "y"))
+    rows, cols = x.shape
+    device = x.device
+    d = _norm_desc(rows, cols, gate, rows_per_gate, post, pre, skip_scale, branch_scale, eps)
+    d.ldx, d.x_dtype = ldx, _FLOATS[x.dtype]
+    d.y_dtype = _FLOATS[(x if y is None else y).dtype]
+    if y is not None:
+        d.ldy = _matrix(y, "y", shape=x.shape)
+    r = h = hs = None
+    if r_out is not None:
+        r = r_out
+        d.ldr = _matrix(r, "r_out", x.dtype, x.shape)
+    elif want_r or (want_r is None and y is not None):
+        r = torch.empty((rows, cols), dtype=x.dtype, device=device)
+        d.ldr = cols
+    if pre != NQ_NORM_NONE:
+        if h_dtype is None:
+            h_dtype = (x if y is None else y).dtype
+        if h_dtype in _FLOATS:
+            h = torch.empty((rows, cols), dtype=h_dtype, device=device)
+            d.h_dtype, d.ldh = _FLOATS[h_dtype], cols
+        elif h_dtype in (torch.float8_e4m3fn, torch.int8):
+            h = _fp8_empty(rows, cols, device, h_dtype)
+            d.h_dtype, d.ldh, d.h_scale = NQ_E4M3 if h_dtype == torch.float8_e4m3fn else NQ_I8, _fp8_pitch(cols), h_scale
+            if d.h_dtype == NQ_E4M3:
+                hs = torch.empty(((cols + 127) // 128, rows), dtype=torch.float32, device=device)
+        else:
+            raise ValueError(f"h_dtype must be float32, bfloat16, float8_e4m3fn or int8, got {h_dtype}")
+    _check(lib().nq_block_norm(ctypes.addressof(d), x.data_ptr(), None if y is None else y.data_ptr(),
+                               _vector(post_weight, "post_weight", cols), _vector(post_bias, "post_bias", cols),
+                               None if gate is None else gate.data_ptr(), _vector(pre_weight, "pre_weight", cols),
+                               _vector(pre_bias, "pre_bias", cols), None if r is None else r.data_ptr(),
+                               None if h is None else h.data_ptr(), None if hs is None else hs.data_ptr(), rows,
+                               _raw_stream(device)), "nq_block_norm")
+    return r, h, hs
+
+
+def nq_block_norm_backward_workspace_bytes(desc: nq_block_norm_desc, has_gate: bool) -> int:
+    return int(lib().nq_block_norm_backward_workspace_bytes(ctypes.addressof(desc), int(bool(has_gate))))
+
+
+def nq_block_norm_backward(r: torch.Tensor, y: Optional[torch.Tensor] = None, *, dr: Optional[torch.Tensor] = None,
+                           dh: Optional[torch.Tensor] = None, post: int = NQ_NORM_NONE,
+                           post_weight: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None,
+                           gate: Optional[torch.Tensor] = None, rows_per_gate: int = 0, skip_scale: float = 1.0,
+                           branch_scale: float = 1.0, pre: int = NQ_NORM_RMS, pre_weight: Optional[torch.Tensor] = None,
+                           pre_bias: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                           workspace: Optional[torch.Tensor] = None):
+    """Gradients of nq_block_norm from the r and y of the forward pass and the gradients dr, dh of its outputs (dh in
+    y's type, without y in any that goes with x; one of the two may be None).
+    -> (dx, dy, dgate, dpost_weight, dpost_bias, dpre_weight, dpre_bias), None for each input that was absent."""
+    ldr = _matrix(r, "r")
+    rows, cols = r.shape
+    device = r.device
+    like = y if y is not None else dh if dh is not None else r
+    _norm_types(r, like, ("r", "y" if y is not None else "dh"))
+    if (pre == NQ_NORM_NONE) != (dh is None):
+        raise ValueError("dh goes with the pre norm: give both or neither")
+    if dr is None and dh is None:
+        raise ValueError("give dr, dh or both")
+    d = _norm_desc(rows, cols, gate, rows_per_gate, post, pre, skip_scale, branch_scale, eps)
+    d.ldr, d.x_dtype, d.y_dtype = ldr, _FLOATS[r.dtype], _FLOATS[like.dtype]
+    if y is not None:
+        d.ldy = _matrix(y, "y", shape=r.shape)
+    if dr is not None:
+        d.lddr = _matrix(dr, "dr", r.dtype, r.shape)
+    if dh is not None:
+        d.lddh = _matrix(dh, "dh", like.dtype, r.shape)
+    dx = torch.empty((rows, cols), dtype=r.dtype, device=device)
+    dy = torch.empty((rows, cols), dtype=like.dtype, device=device) if y is not None else None
+    d.lddx = d.lddy = cols
+    dgate = None if gate is None else torch.empty_like(gate)
+    vec = [None if t is None else torch.empty(cols, dtype=torch.float32, device=device)
+           for t in (post_weight, post_bias, pre_weight, pre_bias)]
+    if workspace is None:
+        workspace = torch.empty(max(nq_block_norm_backward_workspace_bytes(d, gate is not None), 16), dtype=torch.uint8, device=device)
+    _check(lib().nq_block_norm_backward(
+        ctypes.addressof(d), r.data_ptr(), None if y is None else y.data_ptr(), None if dr is None else dr.data_ptr(),
+        None if dh is None else dh.data_ptr(), _vector(post_weight, "post_weight", cols), _vector(post_bias, "post_bias", cols),
+        None if gate is None else gate.data_ptr(), _vector(pre_weight, "pre_weight", cols), dx.data_ptr(),
+        None if dy is None else dy.data_ptr(), None if dgate is None else dgate.data_ptr(),
+        *[None if t is None else t.data_ptr() for t in vec], workspace.data_ptr(), workspace.numel(), _raw_stream(device)),
+        "nq_block_norm_backward")
+    return dx, dy, dgate, vec[0], vec[1], vec[2], vec[3]
 
 
 def nq_i8_mma_ceiling(stage_iters: int) -> float:
