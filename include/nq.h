@@ -345,6 +345,25 @@ NQ_API int nq_fp8_quantize(const void *X, int64_t ldx, int x_dtype, int64_t rows
                     void *stream);
 
 /*
+ * Product of two such matrices, both K-major:
+ *   Y[m, n] = sum_g sa[g, m] * sb[g, n] * (sum_{k in group g} A[m, k] * B[n, k])  (+ bias[n])  (+ Y[m, n] before the call)
+ *   The inner sum of a group of 128 is the tensor core's (exact products, fp32 accumulation), the outer one fp32 with
+ *   one rounding a term; a group's scales are multiplied in fp32 before or after the inner sum's factor, so their
+ *   product must stay inside fp32's normal range.
+ *   A (device) e4m3 [M, K], pitch lda, SA scales of block_rows 1: [ceil(K/128), M], pitch ldsa
+ *   B (device) e4m3 [N, K], pitch ldb, SB scales of block_rows b_block_rows (1 or 128), pitch ldsb
+ *     A, B 16-byte aligned, lda, ldb multiples of 16.  bias (device) fp32 [N] or NULL.
+ *   Y (device, out) [M, N] of y_dtype (NQ_F32, NQ_BF16), pitch ldy, any element alignment (16-byte aligned base and
+ *     pitch is fastest).  accumulate != 0 (NQ_F32 only) adds to what Y holds: gradients over several passes.
+ *   A linear layer y = x W^T with W quantised in 128 x 128 blocks: forward A = x, B = W; input gradient A = dy,
+ *     B = W^T (nq_fp8_quantize's Qt, St); weight gradient A = dy^T, B = x^T, both transposes with block_rows 1.
+ *   M, N, K < 2^30.  Allocates nothing and needs no workspace; results repeat bit for bit.
+ */
+NQ_API int nq_fp8_gemm(const void *A, int64_t lda, const float *SA, int64_t ldsa, const void *B, int64_t ldb, const float *SB,
+                int64_t ldsb, int b_block_rows, const float *bias, int64_t M, int64_t N, int64_t K,
+                void *Y, int64_t ldy, int y_dtype, int accumulate, void *stream);
+
+/*
  * Block norm -- what stands between two blocks of a transformer, in one pass over the rows: the norm after a block,
  * its gate and residual scale, the residual sum, and the norm before the next block.  Per row, in fp32:
  *   u = N_post(y);   r = skip_scale * x + branch_scale * gate * u;   h = N_pre(r)

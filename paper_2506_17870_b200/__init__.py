@@ -14,7 +14,7 @@ from .binding import (  # noqa: F401
     nq_conv_implicit_gemm_nested_q8,
     nq_i8_mma_ceiling, nq_debug_set, NQ_DEBUG_PLAIN_STORES, NQ_DEBUG_PACKED_RING,
     nq_conv_implicit_gemm_q8_res, nq_conv_implicit_gemm_nested_q8_res, nq_maxpool_nhwc_i8, nq_avgpool_requant_nhwc_i8,
-    NQ_E4M3, NQ_I8, NQ_NORM_NONE, NQ_NORM_RMS, NQ_NORM_LAYER, nq_fp8_quantize, nq_block_norm_desc, nq_block_norm,
+    NQ_E4M3, NQ_I8, NQ_NORM_NONE, NQ_NORM_RMS, NQ_NORM_LAYER, nq_fp8_quantize, nq_fp8_gemm, nq_block_norm_desc, nq_block_norm,
     nq_block_norm_backward, nq_block_norm_backward_workspace_bytes,
     nq_rounding_mask, NQ_ROUND_DOWN, NQ_ROUND_UP, NQ_ROUND_NEAREST,
 )

@@ -33,7 +33,7 @@ EXPORTS = (
     "nq_conv_implicit_gemm_nested_q8",
     "nq_i8_mma_ceiling", "nq_debug_set",
     "nq_conv_implicit_gemm_q8_res", "nq_conv_implicit_gemm_nested_q8_res", "nq_maxpool_nhwc_i8", "nq_avgpool_requant_nhwc_i8",
-    "nq_fp8_quantize", "nq_block_norm", "nq_block_norm_backward", "nq_block_norm_backward_workspace_bytes",
+    "nq_fp8_quantize", "nq_fp8_gemm", "nq_block_norm", "nq_block_norm_backward", "nq_block_norm_backward_workspace_bytes",
     "nq_device_status",
 )
 
@@ -70,6 +70,7 @@ class nq_block_norm_desc(ctypes.Structure):
 _P, _L, _I, _F = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_float
 _ARGTYPES = {
     "nq_fp8_quantize": (_P, _L, _I, _L, _L, _I, _P, _L, _P, _L, _P, _L, _P, _L, _P),
+    "nq_fp8_gemm": (_P, _L, _P, _L, _P, _L, _P, _L, _I, _P, _L, _L, _L, _P, _L, _I, _I, _P),
     "nq_block_norm": (_P,) * 11 + (_L, _P),
     "nq_block_norm_backward": (_P,) * 17 + (_L, _P),
     "nq_block_norm_backward_workspace_bytes": (_P, _I),
@@ -691,6 +692,41 @@ def nq_fp8_quantize(x: torch.Tensor, block_rows: int = 1, rowwise: bool = True, 
                                  st.data_ptr() if transposed else None, st.shape[1] if transposed else 0, _raw_stream(device)),
            "nq_fp8_quantize")
     return q, s, qt, st
+
+
+def nq_fp8_gemm(a: torch.Tensor, sa: torch.Tensor, b: torch.Tensor, sb: torch.Tensor, b_block_rows: int = 128,
+                bias: Optional[torch.Tensor] = None, y_dtype: torch.dtype = torch.bfloat16,
+                y_out: Optional[torch.Tensor] = None, accumulate: bool = False) -> torch.Tensor:
+    """y[m, n] = sum over groups of 128 of sa * sb * (a . b) (+ bias) for e4m3 a [M, K], b [N, K] as nq_fp8_quantize
+    writes them: sa [ceil(K / 128), M]; sb [ceil(K / 128), N], or [ceil(K / 128), ceil(N / 128)] for b_block_rows == 128.
+    -> y [M, N] fp32 or bf16, or y_out, to which an fp32 product may be added (accumulate)."""
+    if a.dtype != torch.float8_e4m3fn or b.dtype != torch.float8_e4m3fn:
+        raise ValueError(f"a and b must be float8_e4m3fn, got {a.dtype} and {b.dtype}")
+    lda, ldb = _fp8_ld(a, "a"), _fp8_ld(b, "b")
+    M, K = a.shape
+    N = b.shape[0]
+    if b.shape[1] != K:
+        raise ValueError(f"a and b differ in K: {K} and {b.shape[1]}")
+    if b_block_rows not in (1, 128):
+        raise ValueError("b_block_rows must be 1 or 128")
+    groups = (K + 127) // 128
+    ldsa = _scales(sa, "sa", groups, M)
+    ldsb = _scales(sb, "sb", groups, -(-N // b_block_rows))
+    device = a.device
+    if y_out is not None:
+        y = y_out
+        ldy = _matrix(y, "y_out", None, (M, N))
+    else:
+        if accumulate:
+            raise ValueError("accumulate needs y_out")
+        y = torch.empty((M, N), dtype=y_dtype, device=device)
+        ldy = max(N, 1)
+    if y.dtype not in _FLOATS:
+        raise ValueError(f"the output must be float32 or bfloat16, got {y.dtype}")
+    _check(lib().nq_fp8_gemm(a.data_ptr(), lda, sa.data_ptr(), ldsa, b.data_ptr(), ldb, sb.data_ptr(), ldsb, b_block_rows,
+                             _vector(bias, "bias", N), M, N, K, y.data_ptr(), ldy, _FLOATS[y.dtype], accumulate,
+                             _raw_stream(device)), "nq_fp8_gemm")
+    return y
 
 
 # --------------------------------------------------------------------------- block norm

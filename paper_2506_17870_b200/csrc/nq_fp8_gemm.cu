@@ -1,0 +1,320 @@
+// Product of e4m3 matrices with a scale for each block of 128: kernels and the entry point.
+//
+//   Y[m, n] = sum_g sa[g, m] * sb[g, n] * D_g[m, n] (+ bias[n]),   D_g = the 128-long inner products of group g
+//
+// tcgen05.mma (kind::f8f6f4) computes each D_g afresh in tensor memory; the epilogue warps read it, scale it and add it to
+// accumulators that stay in registers for the whole of K ("promotion").  Two or more D buffers let the tensor core
+// compute group g + 1 while group g is promoted.
+//
+// fp8_tile_kernel<NT>: one CTA per 128 (rows of B) x NT (rows of A) tile, K split over a cluster of up to 8 CTAs that join
+//   their sums through distributed shared memory.  For few rows of A (the weights stream through shared memory once,
+//   as the MMA's 128-row operand, so a single token wastes no bandwidth) and for outputs too small to fill the machine.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/nq.h"
+#include "nq_internal.cuh"
+#include "nq_sm100.cuh"
+
+namespace nq {
+namespace {
+
+using namespace sm100;
+
+constexpr int kGroup = 128;              // K values of a scale group = bytes of a shared-memory row
+
+struct Fp8Args {
+    int M, N, k_blocks;
+    const float* sa;
+    const float* sb;
+    long long ldsa, ldsb;
+    int b_shift;                         // log2 of the rows of B that share a scale: 0 or 7
+    const float* bias;
+    void* y;
+    long long ldy;
+    int y_is_bf16, accumulate;
+    unsigned int* status;
+    int m_tiles, n_tiles;                // in tiles of the kernel that runs
+    int split;                           // tile kernel: CTAs of a cluster, which share K
+};
+
+__device__ __forceinline__ void store_out(const Fp8Args& p, long long m, int n, float v) {
+    if (p.bias) v += __ldg(p.bias + n);
+    const long long at = m * p.ldy + n;
+    if (p.y_is_bf16) {
+        static_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(v);
+    } else {
+        float* y = static_cast<float*>(p.y) + at;
+        *y = p.accumulate ? *y + v : v;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------ tile kernel
+constexpr int kTileThreads = 192;        // warp 0 TMA, warp 1 MMA and TMEM, warps 2-5 promotion (a 32-lane quarter each)
+template <int NT>
+struct TileShape {
+    static constexpr int kStageBytes = (128 + NT) * kGroup;
+    static constexpr int kStages = NT <= 16 ? 6 : NT <= 32 ? 5 : NT <= 64 ? 4 : 3;      // two CTAs an SM: about 100 KB each
+    static constexpr int kBufs = NT <= 64 ? 4 : 2;                                      // D buffers: 64 .. 256 TMEM columns
+    static constexpr int kSmem = kStages * kStageBytes + 4 * 2 * NT * 4 + 512 + 1024;
+    static_assert(NT * 128 * 4 <= kStages * kStageBytes, "the joined tile lies where the stages were");
+};
+
+template <int NT>
+__global__ void __launch_bounds__(kTileThreads, 2)
+fp8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const Fp8Args p) {
+    using S = TileShape<NT>;
+    constexpr int STAGES = S::kStages, BUFS = S::kBufs;
+    constexpr uint32_t COLS = BUFS * NT;
+    constexpr uint32_t IDESC = idesc_e4m3(128, NT);
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t* sW = smem;                                       // [STAGES][128 rows of B][128 B]
+    uint8_t* sX = sW + STAGES * 128 * kGroup;                 // [STAGES][NT rows of A][128 B]
+    float* sScale = reinterpret_cast<float*>(sX + STAGES * NT * kGroup);     // [4 warps][2][NT]
+    uint64_t* full = reinterpret_cast<uint64_t*>(sScale + 4 * 2 * NT);
+    uint64_t* empty = full + STAGES;
+    uint64_t* tfull = empty + STAGES;
+    uint64_t* tempty = tfull + BUFS;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tempty + BUFS);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = (int)(blockIdx.x % (unsigned)p.split);
+    const int tile = (int)(blockIdx.x / (unsigned)p.split);
+    const int n0 = (tile % p.n_tiles) * 128, m0 = (tile / p.n_tiles) * NT;
+    const int kb0 = (int)((long long)p.k_blocks * rank / p.split), kb1 = (int)((long long)p.k_blocks * (rank + 1) / p.split);
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) { mbar_init(smem_u32(&full[s]), 1); mbar_init(smem_u32(&empty[s]), 1); }
+        for (int b = 0; b < BUFS; ++b) { mbar_init(smem_u32(&tfull[b]), 1); mbar_init(smem_u32(&tempty[b]), 4); }
+        *abort_flag = 0;
+        fence_barrier_init();
+        prefetch_tensormap(&tmA);
+        prefetch_tensormap(&tmB);
+    }
+    if (warp == 1) {
+        tmem_alloc(smem_u32(tmem_slot), COLS);
+        tmem_relinquish();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem_base = *tmem_slot;
+
+    float acc[NT];
+#pragma unroll
+    for (int c = 0; c < NT; ++c) acc[c] = 0.0f;
+    const int quarter = warp & 3;
+    const int nl = quarter * 32 + lane;                        // this lane's row of the B tile (promotion warps)
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t it = 0;
+            bool ok = true;
+            for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                const uint32_t s = it % STAGES, use = it / STAGES;
+                if (!(ok = mbar_wait(smem_u32(&empty[s]), (use & 1) ^ 1, abort_flag, p.status, 0x210u))) break;
+                const uint32_t bar = smem_u32(&full[s]);
+                mbar_arrive_expect_tx(bar, S::kStageBytes);
+                tma_load_2d(smem_u32(sW + s * 128 * kGroup), &tmB, kb * kGroup, n0, bar);
+                tma_load_2d(smem_u32(sX + s * NT * kGroup), &tmA, kb * kGroup, m0, bar);
+            }
+            if (!ok) {
+                const long long t0 = clock64();                // let copies in flight land before shared memory is released
+                while (clock64() - t0 < (1ll << 22)) { }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            uint32_t it = 0;
+            for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                const uint32_t s = it % STAGES, use = it / STAGES, b = it % BUFS, buse = it / BUFS;
+                if (!mbar_wait(smem_u32(&tempty[b]), (buse & 1) ^ 1, abort_flag, p.status, 0x220u)) break;
+                if (!mbar_wait(smem_u32(&full[s]), use & 1, abort_flag, p.status, 0x221u)) break;
+                tc_fence_after_sync();
+                const uint64_t dw = smem_desc_sw128(smem_u32(sW + s * 128 * kGroup));
+                const uint64_t dx = smem_desc_sw128(smem_u32(sX + s * NT * kGroup));
+#pragma unroll
+                for (int k = 0; k < kGroup / 32; ++k) mma_e4m3(tmem_base + b * NT, dw + 2 * k, dx + 2 * k, IDESC, k != 0);
+                mma_commit(smem_u32(&empty[s]));
+                mma_commit(smem_u32(&tfull[b]));
+            }
+        }
+    } else {
+        // Promotion: this lane holds one row of B against the NT rows of A.  The scales of A's rows are needed by every
+        // lane: each warp keeps a group's NT of them in shared memory, fetched one group ahead.
+        float* mine = sScale + (warp - 2) * 2 * NT;
+        constexpr int PER = (NT + 31) / 32;
+        const long long sb_row = (n0 + nl < p.N) ? (long long)((n0 + nl) >> p.b_shift) : -1;
+        float next_b = 0.0f, next_a[PER];
+        const auto fetch = [&](int kb) {
+            next_b = sb_row >= 0 ? __ldg(p.sb + (long long)kb * p.ldsb + sb_row) : 0.0f;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int c = i * 32 + lane;
+                next_a[i] = (c < NT && m0 + c < p.M) ? __ldg(p.sa + (long long)kb * p.ldsa + m0 + c) : 0.0f;
+            }
+        };
+        if (kb0 < kb1) fetch(kb0);
+        uint32_t it = 0;
+        for (int kb = kb0; kb < kb1; ++kb, ++it) {
+            const uint32_t b = it % BUFS, buse = it / BUFS;
+            float* sc = mine + (it & 1) * NT;
+            const float scale_b = next_b;
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if (i * 32 + lane < NT) sc[i * 32 + lane] = next_a[i];
+            __syncwarp();
+            if (kb + 1 < kb1) fetch(kb + 1);
+            bool ok = mbar_wait(smem_u32(&tfull[b]), buse & 1, abort_flag, p.status, 0x230u);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tc_fence_after_sync();
+#pragma unroll
+            for (int c0 = 0; c0 < NT; c0 += 16) {
+                uint32_t d[16];
+                tmem_ld_32x16(tmem_base + b * NT + c0 + ((uint32_t)(quarter * 32) << 16), d);
+                tmem_ld_wait();
+                if (c0 + 16 == NT) {
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&tempty[b]));
+                }
+#pragma unroll
+                for (int j = 0; j < 16; ++j) acc[c0 + j] = fmaf(__uint_as_float(d[j]) * scale_b, sc[c0 + j], acc[c0 + j]);
+            }
+        }
+        if (p.split == 1) {
+            if (n0 + nl < p.N)
+#pragma unroll
+                for (int c = 0; c < NT; ++c)
+                    if (m0 + c < p.M) store_out(p, m0 + c, n0 + nl, acc[c]);
+        } else {
+            // every stage has been read by then: the last group's MMAs are complete, and so are all before them
+            float* red = reinterpret_cast<float*>(smem);
+#pragma unroll
+            for (int c = 0; c < NT; ++c) red[c * 128 + nl] = acc[c];
+        }
+    }
+
+    __syncwarp();
+    if (p.split > 1) {
+        cluster_sync_all();
+        if (warp >= 2) {
+            // CTA `rank` joins its share of the tile's rows of A, adding the ranks in order
+            const int c0 = NT * rank / p.split, c1 = NT * (rank + 1) / p.split;
+            const uint32_t red = smem_u32(smem) + nl * 4;
+            for (int c = c0; c < c1; ++c) {
+                if (m0 + c >= p.M) break;
+                float v = 0.0f;
+                for (int r = 0; r < p.split; ++r) {
+                    float t;
+                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(t) : "r"(map_to_cta(red + c * 512, r)) : "memory");
+                    v += t;
+                }
+                if (n0 + nl < p.N) store_out(p, m0 + c, n0 + nl, v);
+            }
+        }
+        __syncwarp();
+        cluster_sync_all();                                    // nobody leaves while its sums are being read
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after_sync();
+        tmem_dealloc(tmem_base, COLS);
+    }
+}
+
+// K == 0: no groups
+__global__ void fp8_empty_kernel(const Fp8Args p) {
+    const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+    if (i < (long long)p.M * p.N) store_out(p, i / p.N, (int)(i % p.N), 0.0f);
+}
+
+// ------------------------------------------------------------------------------------------------------------ host
+template <int NT>
+int launch_tile(const CUtensorMap& tmB, const void* A, int64_t lda, int64_t K, Fp8Args& a, cudaStream_t stream) {
+    a.m_tiles = (a.M + NT - 1) / NT;
+    a.n_tiles = (a.N + 127) / 128;
+    const long long tiles = (long long)a.m_tiles * a.n_tiles;
+    // Split K while that still adds CTAs that run at once (two fit on an SM); a CTA keeps two groups at least.
+    int split = 1;
+    while (split < 8 && tiles * split * 2 <= 2 * sm_count() && a.k_blocks >= 4 * split) split *= 2;
+    a.split = split;
+    if (tiles * split > 0x7fffffffll) return NQ_ERR_UNSUPPORTED;
+    CUtensorMap tmA;
+    const int st = encode_tensor_map_2d(&tmA, A, (uint64_t)K, (uint64_t)a.M, (uint64_t)lda, kGroup, NT, 128);
+    if (st != NQ_OK) return st;
+    static int configured[64] = {0};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return NQ_ERR_CUDA;
+    if (!configured[dev]) {
+        if (cudaFuncSetAttribute(fp8_tile_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, TileShape<NT>::kSmem) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return NQ_ERR_CUDA;
+        }
+        configured[dev] = 1;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(tiles * split), 1, 1);
+    cfg.blockDim = dim3(kTileThreads, 1, 1);
+    cfg.dynamicSmemBytes = TileShape<NT>::kSmem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = split;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, fp8_tile_kernel<NT>, tmA, tmB, a) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return NQ_ERR_CUDA;
+    }
+    return NQ_OK;
+}
+
+int run_fp8_gemm(const void* A, int64_t lda, const void* B, int64_t ldb, int64_t K, Fp8Args& a, cudaStream_t stream) {
+    CUtensorMap tmB;
+    const int st = encode_tensor_map_2d(&tmB, B, (uint64_t)K, (uint64_t)a.N, (uint64_t)ldb, kGroup, 128, 128);
+    if (st != NQ_OK) return st;
+    if (a.M <= 16) return launch_tile<16>(tmB, A, lda, K, a, stream);
+    if (a.M <= 32) return launch_tile<32>(tmB, A, lda, K, a, stream);
+    if (a.M <= 64) return launch_tile<64>(tmB, A, lda, K, a, stream);
+    return launch_tile<128>(tmB, A, lda, K, a, stream);
+}
+
+}  // namespace
+}  // namespace nq
+
+extern "C" int nq_fp8_gemm(const void* A, int64_t lda, const float* SA, int64_t ldsa, const void* B, int64_t ldb, const float* SB,
+                           int64_t ldsb, int b_block_rows, const float* bias, int64_t M, int64_t N, int64_t K, void* Y, int64_t ldy,
+                           int y_dtype, int accumulate, void* stream) {
+    if (M < 0 || N < 0 || K < 0 || (y_dtype != NQ_F32 && y_dtype != NQ_BF16) || (b_block_rows != 1 && b_block_rows != 128))
+        return NQ_ERR_INVALID_ARG;
+    if (accumulate && y_dtype != NQ_F32) return NQ_ERR_UNSUPPORTED;
+    if (M >= (1ll << 30) || N >= (1ll << 30) || K >= (1ll << 30)) return NQ_ERR_UNSUPPORTED;
+    if (M == 0 || N == 0) return NQ_OK;
+    if (!Y || ldy < N) return NQ_ERR_INVALID_ARG;
+    const auto at = [](const void* p) { return reinterpret_cast<uintptr_t>(p); };
+    if (at(Y) % (y_dtype == NQ_BF16 ? 2 : 4) || (at(bias) & 3)) return NQ_ERR_ALIGNMENT;
+    nq::Fp8Args a{};
+    a.M = (int)M; a.N = (int)N; a.k_blocks = (int)((K + 127) / 128);
+    a.sa = SA; a.sb = SB; a.ldsa = ldsa; a.ldsb = ldsb; a.b_shift = b_block_rows == 128 ? 7 : 0;
+    a.bias = bias; a.y = Y; a.ldy = ldy; a.y_is_bf16 = y_dtype == NQ_BF16; a.accumulate = accumulate != 0;
+    const cudaStream_t s = (cudaStream_t)stream;
+    if (K == 0) {
+        if ((M * N + 255) / 256 > 0x7fffffffll) return NQ_ERR_UNSUPPORTED;
+        nq::fp8_empty_kernel<<<(unsigned)((M * N + 255) / 256), 256, 0, s>>>(a);
+        return cudaGetLastError() == cudaSuccess ? NQ_OK : NQ_ERR_CUDA;
+    }
+    if (!A || !B || !SA || !SB || lda < K || ldb < K || ldsa < M || ldsb < (b_block_rows == 128 ? (N + 127) / 128 : N)) return NQ_ERR_INVALID_ARG;
+    if ((at(A) & 15) || (at(B) & 15) || (lda & 15) || (ldb & 15) || (at(SA) & 3) || (at(SB) & 3)) return NQ_ERR_ALIGNMENT;
+    a.status = nq::status_word();
+    if (!a.status) return NQ_ERR_CUDA;
+    return nq::run_fp8_gemm(A, lda, B, ldb, K, a, s);
+}
