@@ -9,6 +9,7 @@
 // fp8_tile_kernel<NT>: one CTA per 128 (rows of B) x NT (rows of A) tile, K split over a cluster of up to 8 CTAs that join
 //   their sums through distributed shared memory.  For few rows of A (the weights stream through shared memory once,
 //   as the MMA's 128-row operand, so a single token wastes no bandwidth) and for outputs too small to fill the machine.
+// fp8_pair_kernel<ROW_SCALES>: persistent CTA pairs (cta_group::2) on 256 x 256 tiles, for everything larger.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -38,6 +39,8 @@ struct Fp8Args {
     unsigned int* status;
     int m_tiles, n_tiles;                // in tiles of the kernel that runs
     int split;                           // tile kernel: CTAs of a cluster, which share K
+    int group_m;                         // pair kernel: M-tiles that share a band of N-tiles
+    int y_tma;                           // pair kernel: Y is written with tile stores
 };
 
 __device__ __forceinline__ void store_out(const Fp8Args& p, long long m, int n, float v) {
@@ -229,6 +232,340 @@ fp8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     }
 }
 
+// ------------------------------------------------------------------------------------------------------ pair kernel
+// 256 x 256 tiles on CTA pairs: a CTA stages its 128 rows of A and half of the B tile (32 KB a group of K), which is what
+// keeps shared memory out of the way of the tensor core (one CTA with a 128 x 256 tile moves 1.5 times as much a
+// multiply).  One group of 128 takes the tensor core 512 cycles; both D buffers of 128 x 256 fill the CTA's tensor
+// memory.  In those 512 cycles eight promotion warps, two to a scheduler, read 128 x 256 sums back and add them to
+// 128 accumulators a thread with packed fp32 FMAs: about 160 issue slots a warp.
+// Barriers (at the same offsets in both CTAs): full[s] in the leader counts the bytes of both CTAs' loads; done[s], one
+// per CTA, is arrived on by the commit of group `it` = s mod STAGES: it frees the stage for the producer AND hands the
+// sums to the promotion warps (a waiter is never more than one phase behind: the next use of the stage needs the D
+// buffer back first); tempty[b] in the leader: its own promotion warps arrive, the partner's send 4 announced bytes each.
+constexpr int kPairThreads = 320;        // warp 0 TMA, warp 1 MMA and TMEM, warps 2-9 promotion
+constexpr int kPairWarps = 8;
+constexpr int kPairStages = 6;
+constexpr int kPairStageBytes = 2 * 128 * kGroup;
+constexpr int kOutPiece = 32 * 64;       // 32 rows x 64 bytes of output, in the 64-byte swizzle
+template <bool ROW_SCALES>
+struct PairShape {
+    static constexpr int kPieces = ROW_SCALES ? 1 : 2;                                   // output pieces in flight per warp
+    static constexpr int kScaleBytes = ROW_SCALES ? kPairWarps * 2 * 128 * 4 : 0;        // a group's 128 column scales, twice, per warp
+    static constexpr int kSmem = kPairStages * kPairStageBytes + kPairWarps * kPieces * kOutPiece + kScaleBytes + 512 + 1024;
+};
+
+__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ uint64_t pack2(uint32_t lo, uint32_t hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+template <int N>
+__device__ __forceinline__ void bulk_wait_read() {
+    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
+}
+
+// Tiles in groups of M-tiles that share a band of N-tiles, so that a group's rows of A stay in L2 while B goes by.
+__device__ __forceinline__ void pair_tile(int tile, const Fp8Args& p, int& mt, int& nt) {
+    const int per_group = p.group_m * p.n_tiles;
+    const int first = tile / per_group * p.group_m;
+    const int local = tile - first * p.n_tiles;
+    const int height = min(p.group_m, p.m_tiles - first);
+    nt = local / height;
+    mt = first + local - nt * height;
+}
+
+// 32 rows x (64 bytes of columns) of finished values: through this warp's piece of shared memory to a tile store, or to
+// ordinary stores that coalesce along the rows.
+struct PairOut {
+    uint8_t* piece;        // kPieces of them
+    int used;              // pieces written so far
+    long long row0;        // of the warp's 32 rows
+};
+template <int PIECES>
+__device__ __forceinline__ void store_piece(const Fp8Args& p, const CUtensorMap* tmY, PairOut& o, int col0, const uint32_t (&w)[16], int lane) {
+    uint8_t* piece = o.piece + (PIECES > 1 ? (o.used % PIECES) * kOutPiece : 0);
+    ++o.used;
+    if (p.y_tma) {
+        if (lane == 0) bulk_wait_read<PIECES - 1>();
+        __syncwarp();
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<uint4*>(piece + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4)) = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+    if (p.y_tma) {
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+            tma_store_4d(tmY, smem_u32(piece), col0 * (p.y_is_bf16 ? 2 : 4), (int)o.row0, 0, 0);
+            bulk_commit_group();
+        }
+        return;
+    }
+    __syncwarp();
+    const long long rows = p.M - o.row0;
+    if (p.y_is_bf16) {
+        if (col0 + lane < p.N)
+#pragma unroll 8
+            for (int r = 0; r < 32; ++r)
+                if (r < rows)
+                    static_cast<uint16_t*>(p.y)[(o.row0 + r) * p.ldy + col0 + lane] =
+                        *reinterpret_cast<const uint16_t*>(piece + r * 64 + (((lane >> 3) ^ ((r >> 1) & 3)) << 4) + (lane & 7) * 2);
+    } else {
+        const int c = lane & 15;
+        if (col0 + c < p.N)
+#pragma unroll 8
+            for (int i = 0; i < 16; ++i) {
+                const int r = 2 * i + (lane >> 4);
+                if (r < rows) {
+                    float* y = static_cast<float*>(p.y) + (o.row0 + r) * p.ldy + col0 + c;
+                    const float v = *reinterpret_cast<const float*>(piece + r * 64 + (((c >> 2) ^ ((r >> 1) & 3)) << 4) + (c & 3) * 4);
+                    *y = p.accumulate ? *y + v : v;
+                }
+            }
+    }
+    __syncwarp();                                              // the piece may be written again
+}
+
+template <bool ROW_SCALES>
+__global__ void __launch_bounds__(kPairThreads, 1)
+fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmY,
+                const Fp8Args p) {
+    using S = PairShape<ROW_SCALES>;
+    constexpr int STAGES = kPairStages;
+    constexpr uint32_t IDESC = idesc_e4m3(256, 256);
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t* sA = smem;
+    uint8_t* sB = sA + STAGES * 128 * kGroup;
+    uint8_t* sOut = sB + STAGES * 128 * kGroup;
+    float* sScale = reinterpret_cast<float*>(sOut + kPairWarps * S::kPieces * kOutPiece);
+    uint64_t* full = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(sScale) + S::kScaleBytes);
+    uint64_t* done = full + STAGES;
+    uint64_t* tempty = done + STAGES;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tempty + 2);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    uint32_t* signal_sink = tmem_slot + 2;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_ctarank();
+    const int pair = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
+    const int num_tiles = p.m_tiles * p.n_tiles;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) { mbar_init(smem_u32(&full[s]), 1); mbar_init(smem_u32(&done[s]), 1); }
+        for (int b = 0; b < 2; ++b) mbar_init(smem_u32(&tempty[b]), kPairWarps + 1);
+        *abort_flag = 0;
+        fence_barrier_init();
+        prefetch_tensormap(&tmA);
+        prefetch_tensormap(&tmB);
+        if (p.y_tma) prefetch_tensormap(&tmY);
+    }
+    if (warp == 1) {
+        tmem_alloc_pair(smem_u32(tmem_slot), 512);
+        tmem_relinquish_pair();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    cluster_sync_all();                                        // both CTAs' barriers exist before anyone signals across
+    tc_fence_after_sync();
+    const uint32_t tmem_base = *tmem_slot;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t it = 0;
+            bool ok = true;
+            for (int tile = pair; ok && tile < num_tiles; tile += num_pairs) {
+                int mt, nt;
+                pair_tile(tile, p, mt, nt);
+                const int row = mt * 256 + (int)rank * 128, brow = nt * 256 + (int)rank * 128;
+                for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
+                    const uint32_t s = it % STAGES, use = it / STAGES;
+                    if (!(ok = mbar_wait_cluster(smem_u32(&done[s]), (use & 1) ^ 1, abort_flag, p.status, 0x310u))) break;
+                    const uint32_t bar = map_to_cta(smem_u32(&full[s]), 0);
+                    if (rank == 0) mbar_arrive_expect_tx(smem_u32(&full[s]), 2 * kPairStageBytes);
+                    tma_load_2d_pair(smem_u32(sA + s * 128 * kGroup), &tmA, kb * kGroup, row, bar);
+                    tma_load_2d_pair(smem_u32(sB + s * 128 * kGroup), &tmB, kb * kGroup, brow, bar);
+                }
+            }
+            if (!ok) {
+                const long long t0 = clock64();                // let copies in flight land before shared memory is released
+                while (clock64() - t0 < (1ll << 22)) { }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            uint32_t it = 0;
+            bool ok = true;
+            for (int tile = pair; ok && tile < num_tiles; tile += num_pairs) {
+                for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
+                    const uint32_t s = it % STAGES, use = it / STAGES, b = it & 1, buse = it >> 1;
+                    if (!(ok = mbar_wait_cluster(smem_u32(&full[s]), use & 1, abort_flag, p.status, 0x321u))) break;
+                    if (!(ok = mbar_wait_cluster(smem_u32(&tempty[b]), (buse & 1) ^ 1, abort_flag, p.status, 0x320u))) break;
+                    mbar_arrive_expect_tx(smem_u32(&tempty[b]), 4 * kPairWarps);
+                    tc_fence_after_sync();
+                    const uint64_t da = smem_desc_sw128(smem_u32(sA + s * 128 * kGroup));
+                    const uint64_t db = smem_desc_sw128(smem_u32(sB + s * 128 * kGroup));
+#pragma unroll
+                    for (int k = 0; k < kGroup / 32; ++k) mma_e4m3_pair(tmem_base + b * 256, da + 2 * k, db + 2 * k, IDESC, k != 0);
+                    mma_commit_pair(smem_u32(&done[s]));
+                }
+            }
+        }
+    } else {
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        const uint32_t tmem_mine = tmem_base + half * 128 + ((uint32_t)(quarter * 32) << 16);
+        const uint32_t remote_sink = map_to_cta(smem_u32(signal_sink), 0);
+        float* sc = sScale + (warp - 2) * 2 * 128;
+        PairOut out;
+        out.piece = sOut + (warp - 2) * S::kPieces * kOutPiece;
+        out.used = 0;
+
+        // scales of the next group, fetched while this one is worked on
+        float next_a = 0.0f, next_b = 0.0f, next_c[4];
+        const auto fetch = [&](int mt, int nt, int kb) {
+            const long long row = (long long)mt * 256 + rank * 128 + quarter * 32 + lane;
+            next_a = row < p.M ? __ldg(p.sa + (long long)kb * p.ldsa + row) : 0.0f;
+            const int col = nt * 256 + half * 128;
+            if (ROW_SCALES) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    next_c[i] = col + 32 * i + lane < p.N ? __ldg(p.sb + (long long)kb * p.ldsb + col + 32 * i + lane) : 0.0f;
+            } else {
+                next_b = col < p.N ? __ldg(p.sb + (long long)kb * p.ldsb + (col >> 7)) : 0.0f;
+            }
+        };
+        uint32_t it = 0;
+        bool ok = true;
+        int mt = 0, nt = 0;
+        if (pair < num_tiles) {
+            pair_tile(pair, p, mt, nt);
+            fetch(mt, nt, 0);
+        }
+        for (int tile = pair; ok && tile < num_tiles; tile += num_pairs) {
+            uint64_t acc[64];
+#pragma unroll
+            for (int i = 0; i < 64; ++i) acc[i] = 0ull;
+            const int mt_now = mt, nt_now = nt;
+            for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
+                const uint32_t s = it % STAGES, use = it / STAGES, b = it & 1;
+                const uint64_t scale = ROW_SCALES ? pack2(next_a, next_a) : pack2(next_a * next_b, next_a * next_b);
+                float* col_scales = sc + (it & 1) * 128;
+                if (ROW_SCALES) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) col_scales[32 * i + lane] = next_c[i];
+                    __syncwarp();
+                }
+                if (kb + 1 < p.k_blocks) {
+                    fetch(mt, nt, kb + 1);
+                } else if (tile + num_pairs < num_tiles) {
+                    pair_tile(tile + num_pairs, p, mt, nt);
+                    fetch(mt, nt, 0);
+                }
+                ok = mbar_wait_cluster(smem_u32(&done[s]), use & 1, abort_flag, p.status, 0x330u);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tc_fence_after_sync();
+                uint32_t d[2][16];
+                tmem_ld_32x16(tmem_mine + b * 256, d[0]);
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    tmem_ld_wait();
+                    if (c < 7) {
+                        tmem_ld_32x16(tmem_mine + b * 256 + (c + 1) * 16, d[(c + 1) & 1]);
+                    } else {
+                        tc_fence_before_sync();
+                        __syncwarp();
+                        if (lane == 0) {
+                            if (rank == 0) mbar_arrive(smem_u32(&tempty[b]));
+                            else signal_remote_tx4(remote_sink, map_to_cta(smem_u32(&tempty[b]), 0));
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        uint64_t v = pack2(d[c & 1][2 * j], d[c & 1][2 * j + 1]);
+                        if (ROW_SCALES) v = mul2(v, *reinterpret_cast<const uint64_t*>(col_scales + c * 16 + 2 * j));
+                        acc[c * 8 + j] = fma2(v, scale, acc[c * 8 + j]);
+                    }
+                }
+            }
+            if (!ok) break;
+            const int col = nt_now * 256 + half * 128;
+            out.row0 = (long long)mt_now * 256 + rank * 128 + quarter * 32;
+            if (out.row0 >= p.M) continue;
+            const bool bias4 = p.bias && (reinterpret_cast<uintptr_t>(p.bias) & 15) == 0 && col + 128 <= p.N;
+            if (p.y_is_bf16) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    if (col + 32 * c >= p.N) break;
+                    uint32_t w[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        float lo, hi;
+                        unpack2(acc[c * 16 + j], lo, hi);
+                        if (p.bias) {
+                            const int n = col + 32 * c + 2 * j;
+                            if (bias4) {
+                                const float2 bb = __ldg(reinterpret_cast<const float2*>(p.bias + n));
+                                lo += bb.x; hi += bb.y;
+                            } else {
+                                if (n < p.N) lo += __ldg(p.bias + n);
+                                if (n + 1 < p.N) hi += __ldg(p.bias + n + 1);
+                            }
+                        }
+                        const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
+                        w[j] = *reinterpret_cast<const uint32_t*>(&t);
+                    }
+                    store_piece<S::kPieces>(p, &tmY, out, col + 32 * c, w, lane);
+                }
+            } else {
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    if (col + 16 * c >= p.N) break;
+                    uint32_t w[16];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        float lo, hi;
+                        unpack2(acc[c * 8 + j], lo, hi);
+                        if (p.bias) {
+                            const int n = col + 16 * c + 2 * j;
+                            if (n < p.N) lo += __ldg(p.bias + n);
+                            if (n + 1 < p.N) hi += __ldg(p.bias + n + 1);
+                        }
+                        w[2 * j] = __float_as_uint(lo);
+                        w[2 * j + 1] = __float_as_uint(hi);
+                    }
+                    store_piece<S::kPieces>(p, &tmY, out, col + 16 * c, w, lane);
+                }
+            }
+        }
+        if (lane == 0) bulk_wait_all();                        // this lane's tile stores are done before the block leaves
+    }
+
+    tc_fence_before_sync();
+    __syncthreads();
+    cluster_sync_all();          // the partner's shared memory and TMEM stay alive until both CTAs are done
+    if (warp == 1) {
+        tc_fence_after_sync();
+        tmem_dealloc_pair(tmem_base, 512);
+    }
+}
+
 // K == 0: no groups
 __global__ void fp8_empty_kernel(const Fp8Args p) {
     const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
@@ -278,8 +615,61 @@ int launch_tile(const CUtensorMap& tmB, const void* A, int64_t lda, int64_t K, F
     return NQ_OK;
 }
 
+template <bool ROW_SCALES>
+int launch_pair(const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensorMap& tmY, const Fp8Args& a, cudaStream_t stream) {
+    using S = PairShape<ROW_SCALES>;
+    static int configured[64] = {0};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return NQ_ERR_CUDA;
+    if (!configured[dev]) {
+        if (cudaFuncSetAttribute(fp8_pair_kernel<ROW_SCALES>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return NQ_ERR_CUDA;
+        }
+        configured[dev] = 1;
+    }
+    const long long tiles = (long long)a.m_tiles * a.n_tiles;
+    const int max_pairs = sm_count() / 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(2 * (tiles < max_pairs ? tiles : max_pairs)), 1, 1);
+    cfg.blockDim = dim3(kPairThreads, 1, 1);
+    cfg.dynamicSmemBytes = S::kSmem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, fp8_pair_kernel<ROW_SCALES>, tmA, tmB, tmY, a) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return NQ_ERR_CUDA;
+    }
+    return NQ_OK;
+}
+
 int run_fp8_gemm(const void* A, int64_t lda, const void* B, int64_t ldb, int64_t K, Fp8Args& a, cudaStream_t stream) {
     CUtensorMap tmB;
+    const long long pair_tiles = (long long)((a.M + 255) / 256) * ((a.N + 255) / 256);
+    if (a.M > 128 && a.N > 128 && pair_tiles * 2 > sm_count() / 2) {
+        if (pair_tiles > 0x3fffffffll) return NQ_ERR_UNSUPPORTED;
+        CUtensorMap tmA, tmY;
+        int st = encode_tensor_map_2d(&tmA, A, (uint64_t)K, (uint64_t)a.M, (uint64_t)lda, kGroup, 128, 128);
+        if (st != NQ_OK) return st;
+        st = encode_tensor_map_2d(&tmB, B, (uint64_t)K, (uint64_t)a.N, (uint64_t)ldb, kGroup, 128, 128);
+        if (st != NQ_OK) return st;
+        a.m_tiles = (a.M + 255) / 256;
+        a.n_tiles = (a.N + 255) / 256;
+        // a group's rows of A stay within about 32 MB of L2
+        a.group_m = 16;
+        while (a.group_m > 4 && 256.0 * a.group_m * (double)K > 34.0e6) a.group_m /= 2;
+        tmY = tmA;
+        const uint64_t esize = a.y_is_bf16 ? 2 : 4, pitch = (uint64_t)a.ldy * esize;
+        a.y_tma = !a.accumulate && (reinterpret_cast<uintptr_t>(a.y) & 15) == 0 && (pitch & 15) == 0 && pitch < (1ull << 40) &&
+                  encode_tensor_map_out(&tmY, a.y, (uint64_t)a.N * esize, pitch, (uint64_t)a.M, 1, 1, 32, 1, 1, 64) == NQ_OK;
+        return a.b_shift == 0 ? launch_pair<true>(tmA, tmB, tmY, a, stream) : launch_pair<false>(tmA, tmB, tmY, a, stream);
+    }
     const int st = encode_tensor_map_2d(&tmB, B, (uint64_t)K, (uint64_t)a.N, (uint64_t)ldb, kGroup, 128, 128);
     if (st != NQ_OK) return st;
     if (a.M <= 16) return launch_tile<16>(tmB, A, lda, K, a, stream);
