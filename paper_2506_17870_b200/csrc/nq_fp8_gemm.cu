@@ -15,6 +15,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/nq.h"
 #include "nq_internal.cuh"
 #include "nq_sm100.cuh"
@@ -233,47 +235,36 @@ fp8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
 }
 
 // ------------------------------------------------------------------------------------------------------ pair kernel
-// 256 x 256 tiles on CTA pairs: a CTA stages its 128 rows of A and half of the B tile (32 KB a group of K), which is what
-// keeps shared memory out of the way of the tensor core (one CTA with a 128 x 256 tile moves 1.5 times as much a
-// multiply).  One group of 128 takes the tensor core 512 cycles; both D buffers of 128 x 256 fill the CTA's tensor
-// memory.  In those 512 cycles eight promotion warps, two to a scheduler, read 128 x 256 sums back and add them to
-// 128 accumulators a thread with packed fp32 FMAs: about 160 issue slots a warp.
-// Barriers (at the same offsets in both CTAs): full[s] in the leader counts the bytes of both CTAs' loads; done[s], one
-// per CTA, is arrived on by the commit of group `it` = s mod STAGES: it frees the stage for the producer AND hands the
-// sums to the promotion warps (a waiter is never more than one phase behind: the next use of the stage needs the D
-// buffer back first); tempty[b] in the leader: its own promotion warps arrive, the partner's send 4 announced bytes each.
-constexpr int kPairThreads = 320;        // warp 0 TMA, warp 1 MMA and TMEM, warps 2-9 promotion
+// 256 x 256 tiles on CTA pairs, in two halves of 128 columns: a CTA stages its 128 rows of A and half of the rows of each
+// half of B (32 KB a group of K) and gets 128 x 128 sums a half; four such buffers fill its tensor memory.  What bounds the
+// rate is the hand-over of a buffer -- commit, promotion warps in BOTH CTAs read it, their signal travels to the
+// leader's MMA thread: about a thousand cycles, against 512 in which the tensor core computes a group of 256 x 256.  With
+// two buffers of 256 columns the tensor core waited for it every group; with four of 128 it has three others to fill
+// meanwhile, at the price of reading A from shared memory twice.
+// Eight promotion warps, two to a scheduler: a warp reads 32 rows x 64 columns of a half with two loads, gives the buffer
+// back as soon as they have arrived, and then adds them to 128 accumulators a thread; the loads of the second half are
+// issued between the FMAs of the first.  (Sixteen warps of 64 accumulators have no registers to take in 64 columns before they
+// add: they held the buffers longer, and 8192^3 took 637 us.)
+// Barriers (at the same offsets in both CTAs): full[s] in the leader counts the bytes of both CTAs' loads; done[s][h], in
+// each CTA, is arrived on by the commit of half h of the group in stage s: it hands the sums to the promotion warps, and
+// both halves together free the stage for the producer (a waiter is never more than one phase behind: the next use of the
+// stage needs the buffers back first); tempty[b] in the leader: the sixteen promotion warps of both CTAs arrive;
+// sfull[s] / sempty[s], private to a CTA (ROW_SCALES): the ring of column scales, filled by warp 2 with asynchronous copies.
+constexpr int kPairThreads = 384;        // warp 0 TMA, warps 1 and 3 MMA (1 also TMEM), warp 2 column scales, warps 4-11 promotion
 constexpr int kPairWarps = 8;
 constexpr int kPairStages = 6;
 constexpr int kPairStageBytes = 2 * 128 * kGroup;
 constexpr int kOutPiece = 32 * 64;       // 32 rows x 64 bytes of output, in the 64-byte swizzle
 template <bool ROW_SCALES>
 struct PairShape {
-    static constexpr int kPieces = ROW_SCALES ? 1 : 2;                                   // output pieces in flight per warp
-    static constexpr int kScaleBytes = ROW_SCALES ? kPairWarps * 2 * 128 * 4 : 0;        // a group's 128 column scales, twice, per warp
-    static constexpr int kSmem = kPairStages * kPairStageBytes + kPairWarps * kPieces * kOutPiece + kScaleBytes + 512 + 1024;
+    static constexpr int kPieces = 1;                                                    // output pieces in flight per warp
+    static constexpr int kScales = ROW_SCALES ? 256 : 0;                                 // of a group: rows of B
+    static constexpr int kSmem = kPairStages * (kPairStageBytes + kScales * 4) + kPairWarps * kPieces * kOutPiece + 512 + 1024;
 };
 
-__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ uint64_t pack2(uint32_t lo, uint32_t hi) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
-    return r;
-}
-__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
+// one scale to shared memory, asynchronously; zero where there is none (`any`: some readable address)
+__device__ __forceinline__ void copy_scale(uint32_t dst, const float* src, bool present, const float* any) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(present ? src : any), "r"(present ? 4 : 0) : "memory");
 }
 template <int N>
 __device__ __forceinline__ void bulk_wait_read() {
@@ -348,19 +339,20 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 const Fp8Args p) {
     using S = PairShape<ROW_SCALES>;
     constexpr int STAGES = kPairStages;
-    constexpr uint32_t IDESC = idesc_e4m3(256, 256);
+    constexpr uint32_t IDESC = idesc_e4m3(256, 128);
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t* sA = smem;
     uint8_t* sB = sA + STAGES * 128 * kGroup;
     uint8_t* sOut = sB + STAGES * 128 * kGroup;
     float* sScale = reinterpret_cast<float*>(sOut + kPairWarps * S::kPieces * kOutPiece);
-    uint64_t* full = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(sScale) + S::kScaleBytes);
+    uint64_t* full = reinterpret_cast<uint64_t*>(sScale + STAGES * S::kScales);
     uint64_t* done = full + STAGES;
-    uint64_t* tempty = done + STAGES;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tempty + 2);
+    uint64_t* sfull = done + 2 * STAGES;
+    uint64_t* sempty = sfull + STAGES;
+    uint64_t* tempty = sempty + STAGES;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tempty + 4);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    uint32_t* signal_sink = tmem_slot + 2;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
@@ -368,8 +360,13 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     const int num_tiles = p.m_tiles * p.n_tiles;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < STAGES; ++s) { mbar_init(smem_u32(&full[s]), 1); mbar_init(smem_u32(&done[s]), 1); }
-        for (int b = 0; b < 2; ++b) mbar_init(smem_u32(&tempty[b]), kPairWarps + 1);
+        for (int s = 0; s < STAGES; ++s) {
+            mbar_init(smem_u32(&full[s]), 1);
+            mbar_init(smem_u32(&sfull[s]), 32);
+            mbar_init(smem_u32(&sempty[s]), kPairWarps);
+        }
+        for (int s = 0; s < 2 * STAGES; ++s) mbar_init(smem_u32(&done[s]), 1);
+        for (int b = 0; b < 4; ++b) mbar_init(smem_u32(&tempty[b]), 2 * kPairWarps);
         *abort_flag = 0;
         fence_barrier_init();
         prefetch_tensormap(&tmA);
@@ -385,6 +382,9 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     cluster_sync_all();                                        // both CTAs' barriers exist before anyone signals across
     tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_slot;
+    // 384 threads are launched with 168 registers each (64512); the promotion warps take 224 (256 x 224 = 57344), the
+    // other four 56 (128 x 56 = 7168): together what was launched.
+    if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
 
     if (warp == 0) {
         if (lane == 0) {
@@ -393,14 +393,16 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             for (int tile = pair; ok && tile < num_tiles; tile += num_pairs) {
                 int mt, nt;
                 pair_tile(tile, p, mt, nt);
-                const int row = mt * 256 + (int)rank * 128, brow = nt * 256 + (int)rank * 128;
+                const int row = mt * 256 + (int)rank * 128, brow = nt * 256 + (int)rank * 64;
                 for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
                     const uint32_t s = it % STAGES, use = it / STAGES;
-                    if (!(ok = mbar_wait_cluster(smem_u32(&done[s]), (use & 1) ^ 1, abort_flag, p.status, 0x310u))) break;
+                    if (!(ok = mbar_wait(smem_u32(&done[2 * s]), (use & 1) ^ 1, abort_flag, p.status, 0x310u))) break;
+                    if (!(ok = mbar_wait(smem_u32(&done[2 * s + 1]), (use & 1) ^ 1, abort_flag, p.status, 0x311u))) break;
                     const uint32_t bar = map_to_cta(smem_u32(&full[s]), 0);
                     if (rank == 0) mbar_arrive_expect_tx(smem_u32(&full[s]), 2 * kPairStageBytes);
                     tma_load_2d_pair(smem_u32(sA + s * 128 * kGroup), &tmA, kb * kGroup, row, bar);
                     tma_load_2d_pair(smem_u32(sB + s * 128 * kGroup), &tmB, kb * kGroup, brow, bar);
+                    tma_load_2d_pair(smem_u32(sB + s * 128 * kGroup + 64 * kGroup), &tmB, kb * kGroup, brow + 128, bar);
                 }
             }
             if (!ok) {
@@ -408,149 +410,184 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 while (clock64() - t0 < (1ll << 22)) { }
             }
         }
-    } else if (warp == 1) {
+    } else if (warp == 1 || warp == 3) {
+        // One thread issues the first halves, another the second: what a thread pays between two batches (a probe of a
+        // barrier that is ready costs about 115 cycles, a commit 70) passes while the other's products are computed.
         if (lane == 0 && rank == 0) {
+            const int h = warp >> 1;
             uint32_t it = 0;
             bool ok = true;
             for (int tile = pair; ok && tile < num_tiles; tile += num_pairs) {
                 for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
-                    const uint32_t s = it % STAGES, use = it / STAGES, b = it & 1, buse = it >> 1;
-                    if (!(ok = mbar_wait_cluster(smem_u32(&full[s]), use & 1, abort_flag, p.status, 0x321u))) break;
-                    if (!(ok = mbar_wait_cluster(smem_u32(&tempty[b]), (buse & 1) ^ 1, abort_flag, p.status, 0x320u))) break;
-                    mbar_arrive_expect_tx(smem_u32(&tempty[b]), 4 * kPairWarps);
+                    const uint32_t s = it % STAGES, use = it / STAGES, b = (2 * it + h) & 3;
+                    if (!(ok = mbar_wait(smem_u32(&full[s]), use & 1, abort_flag, p.status, 0x321u))) break;
+                    if (!(ok = mbar_wait(smem_u32(&tempty[b]), ((it >> 1) & 1) ^ 1, abort_flag, p.status, 0x320u))) break;
                     tc_fence_after_sync();
                     const uint64_t da = smem_desc_sw128(smem_u32(sA + s * 128 * kGroup));
-                    const uint64_t db = smem_desc_sw128(smem_u32(sB + s * 128 * kGroup));
+                    const uint64_t db = smem_desc_sw128(smem_u32(sB + s * 128 * kGroup + h * 64 * kGroup));
 #pragma unroll
-                    for (int k = 0; k < kGroup / 32; ++k) mma_e4m3_pair(tmem_base + b * 256, da + 2 * k, db + 2 * k, IDESC, k != 0);
-                    mma_commit_pair(smem_u32(&done[s]));
+                    for (int k = 0; k < kGroup / 32; ++k) mma_e4m3_pair(tmem_base + b * 128, da + 2 * k, db + 2 * k, IDESC, k != 0);
+                    mma_commit_pair(smem_u32(&done[2 * s + h]));
                 }
             }
         }
-    } else {
-        const int quarter = warp & 3, half = (warp - 2) >> 2;
-        const uint32_t tmem_mine = tmem_base + half * 128 + ((uint32_t)(quarter * 32) << 16);
-        const uint32_t remote_sink = map_to_cta(smem_u32(signal_sink), 0);
-        float* sc = sScale + (warp - 2) * 2 * 128;
-        PairOut out;
-        out.piece = sOut + (warp - 2) * S::kPieces * kOutPiece;
-        out.used = 0;
-
-        // scales of the next group, fetched while this one is worked on
-        float next_a = 0.0f, next_b = 0.0f, next_c[4];
-        const auto fetch = [&](int mt, int nt, int kb) {
-            const long long row = (long long)mt * 256 + rank * 128 + quarter * 32 + lane;
-            next_a = row < p.M ? __ldg(p.sa + (long long)kb * p.ldsa + row) : 0.0f;
-            const int col = nt * 256 + half * 128;
-            if (ROW_SCALES) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    next_c[i] = col + 32 * i + lane < p.N ? __ldg(p.sb + (long long)kb * p.ldsb + col + 32 * i + lane) : 0.0f;
-            } else {
-                next_b = col < p.N ? __ldg(p.sb + (long long)kb * p.ldsb + (col >> 7)) : 0.0f;
-            }
-        };
+    } else if (warp == 2) {
+        // column scales of each group, as many groups ahead as there are stages; outside the matrix they read as zero
         uint32_t it = 0;
         bool ok = true;
-        int mt = 0, nt = 0;
-        if (pair < num_tiles) {
-            pair_tile(pair, p, mt, nt);
-            fetch(mt, nt, 0);
-        }
-        for (int tile = pair; ok && tile < num_tiles; tile += num_pairs) {
-            uint64_t acc[64];
-#pragma unroll
-            for (int i = 0; i < 64; ++i) acc[i] = 0ull;
-            const int mt_now = mt, nt_now = nt;
+        for (int tile = pair; ROW_SCALES && ok && tile < num_tiles; tile += num_pairs) {
+            int mt, nt;
+            pair_tile(tile, p, mt, nt);
+            const int col = nt * 256 + lane;
             for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
-                const uint32_t s = it % STAGES, use = it / STAGES, b = it & 1;
-                const uint64_t scale = ROW_SCALES ? pack2(next_a, next_a) : pack2(next_a * next_b, next_a * next_b);
-                float* col_scales = sc + (it & 1) * 128;
-                if (ROW_SCALES) {
+                const uint32_t s = it % STAGES, use = it / STAGES;
+                ok = mbar_wait(smem_u32(&sempty[s]), (use & 1) ^ 1, abort_flag, p.status, 0x340u);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                const uint32_t to = smem_u32(sScale + s * S::kScales + lane);
+                const float* from = p.sb + (long long)kb * p.ldsb + col;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) col_scales[32 * i + lane] = next_c[i];
+                for (int i = 0; i < 8; ++i) copy_scale(to + 128 * i, from + 32 * i, col + 32 * i < p.N, p.sb);
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sfull[s])) : "memory");
+            }
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+    } else if (warp >= 4) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        const int quarter = warp & 3, part = (warp - 4) >> 2;  // 32 rows, and 64 of the columns of each half
+        const uint32_t tmem_mine = tmem_base + part * 64 + ((uint32_t)(quarter * 32) << 16);
+        PairOut out;
+        out.piece = sOut + (warp - 4) * S::kPieces * kOutPiece;
+        out.used = 0;
+        uint32_t it = 0;
+        bool ok = true;
+        for (int tile = pair; ok && tile < num_tiles; tile += num_pairs) {
+            int mt, nt;
+            pair_tile(tile, p, mt, nt);
+            // this row's scales and (blocks) those of the two column blocks, one group ahead
+            const long long row = (long long)mt * 256 + rank * 128 + quarter * 32 + lane;
+            const float* from_a = p.sa + (row < p.M ? row : 0);
+            const float* from_b = p.sb + 2 * nt;
+            const bool second = !ROW_SCALES && nt * 256 + 128 < p.N;
+            float next_a, next_b0 = 0.0f, next_b1 = 0.0f;
+            const auto fetch = [&]() {
+                next_a = __ldg(from_a);
+                from_a += p.ldsa;
+                if (!ROW_SCALES) {
+                    next_b0 = __ldg(from_b);
+                    if (second) next_b1 = __ldg(from_b + 1);
+                    from_b += p.ldsb;
+                }
+            };
+            fetch();
+            float acc[2][64];
+#pragma unroll
+            for (int i = 0; i < 64; ++i) acc[0][i] = acc[1][i] = 0.0f;
+            for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
+                const uint32_t s = it % STAGES, parity = (it / STAGES) & 1;
+                const uint32_t bar = smem_u32(&done[2 * s]);
+                const float* col_scales = sScale + s * S::kScales + part * 64;
+                const float scale0 = ROW_SCALES ? next_a : next_a * next_b0, scale1 = ROW_SCALES ? next_a : next_a * next_b1;
+                if (kb + 1 < p.k_blocks) fetch();
+                uint32_t d[2][32];
+                const auto add = [&](int h, int c, float scale) {
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4) {
+                        float w[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+                        if (ROW_SCALES) *reinterpret_cast<float4*>(w) = *reinterpret_cast<const float4*>(col_scales + h * 128 + c * 32 + j);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float v = __uint_as_float(d[c][j + i]);
+                            if (ROW_SCALES) v *= w[i];
+                            acc[h][c * 32 + j + i] = fmaf(v, scale, acc[h][c * 32 + j + i]);
+                        }
+                    }
+                };
+                const auto give_back = [&](int h) {
+                    tc_fence_before_sync();
                     __syncwarp();
-                }
-                if (kb + 1 < p.k_blocks) {
-                    fetch(mt, nt, kb + 1);
-                } else if (tile + num_pairs < num_tiles) {
-                    pair_tile(tile + num_pairs, p, mt, nt);
-                    fetch(mt, nt, 0);
-                }
-                ok = mbar_wait_cluster(smem_u32(&done[s]), use & 1, abort_flag, p.status, 0x330u);
+                    if (lane == 0) {
+                        const uint32_t to = smem_u32(&tempty[(2 * it + h) & 3]);
+                        if (rank == 0) mbar_arrive(to);
+                        else mbar_arrive_cluster_relaxed(map_to_cta(to, 0));
+                    }
+                };
+                const uint32_t from = tmem_mine + ((2 * it) & 3) * 128;
+                ok = mbar_wait(bar, parity, abort_flag, p.status, 0x330u);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after_sync();
-                uint32_t d[2][16];
-                tmem_ld_32x16(tmem_mine + b * 256, d[0]);
-#pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    tmem_ld_wait();
-                    if (c < 7) {
-                        tmem_ld_32x16(tmem_mine + b * 256 + (c + 1) * 16, d[(c + 1) & 1]);
-                    } else {
-                        tc_fence_before_sync();
-                        __syncwarp();
-                        if (lane == 0) {
-                            if (rank == 0) mbar_arrive(smem_u32(&tempty[b]));
-                            else signal_remote_tx4(remote_sink, map_to_cta(smem_u32(&tempty[b]), 0));
-                        }
-                    }
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        uint64_t v = pack2(d[c & 1][2 * j], d[c & 1][2 * j + 1]);
-                        if (ROW_SCALES) v = mul2(v, *reinterpret_cast<const uint64_t*>(col_scales + c * 16 + 2 * j));
-                        acc[c * 8 + j] = fma2(v, scale, acc[c * 8 + j]);
-                    }
+                tmem_ld_32x32(from, d[0]);
+                tmem_ld_32x32(from + 32, d[1]);
+                if (ROW_SCALES) ok = mbar_wait(smem_u32(&sfull[s]), parity, abort_flag, p.status, 0x331u);
+                bool ready = mbar_try_wait(bar + 8, parity);
+                ready = __all_sync(0xffffffffu, ready);
+                tmem_ld_wait();
+                give_back(0);
+                if (!ready) {
+                    ok = mbar_wait(bar + 8, parity, abort_flag, p.status, 0x332u) && ok;
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                }
+                tc_fence_after_sync();
+                add(0, 0, scale0);
+                tmem_ld_32x32(from + 128, d[0]);
+                add(0, 1, scale0);
+                tmem_ld_32x32(from + 160, d[1]);
+                tmem_ld_wait();
+                give_back(1);
+                add(1, 0, scale1);
+                add(1, 1, scale1);
+                if (ROW_SCALES) {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&sempty[s]));
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
                 }
             }
             if (!ok) break;
-            const int col = nt_now * 256 + half * 128;
-            out.row0 = (long long)mt_now * 256 + rank * 128 + quarter * 32;
+            out.row0 = (long long)mt * 256 + rank * 128 + quarter * 32;
             if (out.row0 >= p.M) continue;
-            const bool bias4 = p.bias && (reinterpret_cast<uintptr_t>(p.bias) & 15) == 0 && col + 128 <= p.N;
-            if (p.y_is_bf16) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    if (col + 32 * c >= p.N) break;
-                    uint32_t w[16];
+            for (int h = 0; h < 2; ++h) {
+                const int col = nt * 256 + h * 128 + part * 64;
+                if (p.bias) {
+                    const bool whole = (reinterpret_cast<uintptr_t>(p.bias) & 15) == 0 && col + 64 <= p.N;
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        float lo, hi;
-                        unpack2(acc[c * 16 + j], lo, hi);
-                        if (p.bias) {
-                            const int n = col + 32 * c + 2 * j;
-                            if (bias4) {
-                                const float2 bb = __ldg(reinterpret_cast<const float2*>(p.bias + n));
-                                lo += bb.x; hi += bb.y;
-                            } else {
-                                if (n < p.N) lo += __ldg(p.bias + n);
-                                if (n + 1 < p.N) hi += __ldg(p.bias + n + 1);
-                            }
+                    for (int i = 0; i < 64; i += 4) {
+                        float4 b = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        if (whole) {
+                            b = __ldg(reinterpret_cast<const float4*>(p.bias + col + i));
+                        } else {
+                            if (col + i < p.N) b.x = __ldg(p.bias + col + i);
+                            if (col + i + 1 < p.N) b.y = __ldg(p.bias + col + i + 1);
+                            if (col + i + 2 < p.N) b.z = __ldg(p.bias + col + i + 2);
+                            if (col + i + 3 < p.N) b.w = __ldg(p.bias + col + i + 3);
                         }
-                        const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
-                        w[j] = *reinterpret_cast<const uint32_t*>(&t);
+                        acc[h][i] += b.x; acc[h][i + 1] += b.y; acc[h][i + 2] += b.z; acc[h][i + 3] += b.w;
                     }
-                    store_piece<S::kPieces>(p, &tmY, out, col + 32 * c, w, lane);
                 }
-            } else {
+                if (p.y_is_bf16) {
 #pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    if (col + 16 * c >= p.N) break;
-                    uint32_t w[16];
+                    for (int c = 0; c < 2; ++c) {
+                        if (col + 32 * c >= p.N) break;
+                        uint32_t w[16];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        float lo, hi;
-                        unpack2(acc[c * 8 + j], lo, hi);
-                        if (p.bias) {
-                            const int n = col + 16 * c + 2 * j;
-                            if (n < p.N) lo += __ldg(p.bias + n);
-                            if (n + 1 < p.N) hi += __ldg(p.bias + n + 1);
+                        for (int j = 0; j < 16; ++j) {
+                            const __nv_bfloat162 t = __floats2bfloat162_rn(acc[h][c * 32 + 2 * j], acc[h][c * 32 + 2 * j + 1]);
+                            w[j] = *reinterpret_cast<const uint32_t*>(&t);
                         }
-                        w[2 * j] = __float_as_uint(lo);
-                        w[2 * j + 1] = __float_as_uint(hi);
+                        store_piece<S::kPieces>(p, &tmY, out, col + 32 * c, w, lane);
                     }
-                    store_piece<S::kPieces>(p, &tmY, out, col + 16 * c, w, lane);
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        if (col + 16 * c >= p.N) break;
+                        uint32_t w[16];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) w[j] = __float_as_uint(acc[h][c * 16 + j]);
+                        store_piece<S::kPieces>(p, &tmY, out, col + 16 * c, w, lane);
+                    }
                 }
             }
         }
@@ -657,7 +694,7 @@ int run_fp8_gemm(const void* A, int64_t lda, const void* B, int64_t ldb, int64_t
         CUtensorMap tmA, tmY;
         int st = encode_tensor_map_2d(&tmA, A, (uint64_t)K, (uint64_t)a.M, (uint64_t)lda, kGroup, 128, 128);
         if (st != NQ_OK) return st;
-        st = encode_tensor_map_2d(&tmB, B, (uint64_t)K, (uint64_t)a.N, (uint64_t)ldb, kGroup, 128, 128);
+        st = encode_tensor_map_2d(&tmB, B, (uint64_t)K, (uint64_t)a.N, (uint64_t)ldb, kGroup, 64, 128);
         if (st != NQ_OK) return st;
         a.m_tiles = (a.M + 255) / 256;
         a.n_tiles = (a.N + 255) / 256;

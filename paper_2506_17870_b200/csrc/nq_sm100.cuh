@@ -250,6 +250,11 @@ __device__ __forceinline__ uint32_t map_to_cta(uint32_t addr, uint32_t rank) {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
+// The same without ordering the thread's memory accesses before it (none to protect: tensor memory reads that a
+// tcgen05.wait has completed); it does not stall the issuing warp.
+__device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t cluster_addr) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
 // Fire-and-forget signal to a barrier in another CTA of the cluster: an asynchronous 4-byte store to `sink`
 // there that counts 4 bytes on `bar` when it lands (both are cluster addresses).  Ordered after the issuing
 // thread's earlier generic-proxy writes by a preceding fence.proxy.async; unlike a cluster-scope release
