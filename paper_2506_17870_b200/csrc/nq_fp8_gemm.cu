@@ -241,14 +241,14 @@ fp8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
 // leader's MMA thread: about a thousand cycles, against 512 in which the tensor core computes a group of 256 x 256.  With
 // two buffers of 256 columns the tensor core waited for it every group; with four of 128 it has three others to fill
 // meanwhile, at the price of reading A from shared memory twice.
-// Eight promotion warps, two to a scheduler: a warp reads 32 rows x 64 columns of a half with two loads, gives the buffer
-// back as soon as they have arrived, and then adds them to 128 accumulators a thread; the loads of the second half are
-// issued between the FMAs of the first.  (Sixteen warps of 64 accumulators have no registers to take in 64 columns before they
-// add: they held the buffers longer, and 8192^3 took 637 us.)
+// Eight promotion warps, two to a scheduler, one for each half: a warp reads 32 rows x 128 columns in four loads of 32, two in
+// flight, and adds them to 128 accumulators a thread.  The two warps of a scheduler work half a group apart, so that the
+// FMAs of one fall into the waits of the other (both on the same half, 64 columns each, they waited together: 8192^3 took
+// 656 us; sixteen warps of 64 accumulators have no registers to take in what they add: 637 us).
 // Barriers (at the same offsets in both CTAs): full[s] in the leader counts the bytes of both CTAs' loads; done[s][h], in
 // each CTA, is arrived on by the commit of half h of the group in stage s: it hands the sums to the promotion warps, and
 // both halves together free the stage for the producer (a waiter is never more than one phase behind: the next use of the
-// stage needs the buffers back first); tempty[b] in the leader: the sixteen promotion warps of both CTAs arrive;
+// stage needs the buffers back first); tempty[b] in the leader: the half's four promotion warps of both CTAs arrive;
 // sfull[s] / sempty[s], private to a CTA (ROW_SCALES): the ring of column scales, filled by warp 2 with asynchronous copies.
 constexpr int kPairThreads = 384;        // warp 0 TMA, warps 1 and 3 MMA (1 also TMEM), warp 2 column scales, warps 4-11 promotion
 constexpr int kPairWarps = 8;
@@ -366,7 +366,7 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             mbar_init(smem_u32(&sempty[s]), kPairWarps);
         }
         for (int s = 0; s < 2 * STAGES; ++s) mbar_init(smem_u32(&done[s]), 1);
-        for (int b = 0; b < 4; ++b) mbar_init(smem_u32(&tempty[b]), 2 * kPairWarps);
+        for (int b = 0; b < 4; ++b) mbar_init(smem_u32(&tempty[b]), kPairWarps);
         *abort_flag = 0;
         fence_barrier_init();
         prefetch_tensormap(&tmA);
@@ -454,8 +454,8 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         asm volatile("cp.async.wait_all;" ::: "memory");
     } else if (warp >= 4) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
-        const int quarter = warp & 3, part = (warp - 4) >> 2;  // 32 rows, and 64 of the columns of each half
-        const uint32_t tmem_mine = tmem_base + part * 64 + ((uint32_t)(quarter * 32) << 16);
+        const int quarter = warp & 3, h = (warp - 4) >> 2;     // 32 rows of one half
+        const uint32_t tmem_mine = tmem_base + h * 128 + ((uint32_t)(quarter * 32) << 16);
         PairOut out;
         out.piece = sOut + (warp - 4) * S::kPieces * kOutPiece;
         out.used = 0;
@@ -464,80 +464,66 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         for (int tile = pair; ok && tile < num_tiles; tile += num_pairs) {
             int mt, nt;
             pair_tile(tile, p, mt, nt);
-            // this row's scales and (blocks) those of the two column blocks, one group ahead
+            const int col = nt * 256 + h * 128;
+            // this row's scales and (blocks) the column block's, one group ahead
             const long long row = (long long)mt * 256 + rank * 128 + quarter * 32 + lane;
             const float* from_a = p.sa + (row < p.M ? row : 0);
-            const float* from_b = p.sb + 2 * nt;
-            const bool second = !ROW_SCALES && nt * 256 + 128 < p.N;
-            float next_a, next_b0 = 0.0f, next_b1 = 0.0f;
+            const float* from_b = p.sb + (col < p.N ? col >> 7 : 0);
+            float next_a, next_b = 1.0f;
             const auto fetch = [&]() {
                 next_a = __ldg(from_a);
                 from_a += p.ldsa;
                 if (!ROW_SCALES) {
-                    next_b0 = __ldg(from_b);
-                    if (second) next_b1 = __ldg(from_b + 1);
+                    next_b = __ldg(from_b);
                     from_b += p.ldsb;
                 }
             };
             fetch();
-            float acc[2][64];
+            float acc[128];
 #pragma unroll
-            for (int i = 0; i < 64; ++i) acc[0][i] = acc[1][i] = 0.0f;
+            for (int i = 0; i < 128; ++i) acc[i] = 0.0f;
             for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
                 const uint32_t s = it % STAGES, parity = (it / STAGES) & 1;
-                const uint32_t bar = smem_u32(&done[2 * s]);
-                const float* col_scales = sScale + s * S::kScales + part * 64;
-                const float scale0 = ROW_SCALES ? next_a : next_a * next_b0, scale1 = ROW_SCALES ? next_a : next_a * next_b1;
+                const float* col_scales = sScale + s * S::kScales + h * 128;
+                const float scale = ROW_SCALES ? next_a : next_a * next_b;
                 if (kb + 1 < p.k_blocks) fetch();
                 uint32_t d[2][32];
-                const auto add = [&](int h, int c, float scale) {
+                const auto add = [&](int c) {
 #pragma unroll
                     for (int j = 0; j < 32; j += 4) {
                         float w[4] = {1.0f, 1.0f, 1.0f, 1.0f};
-                        if (ROW_SCALES) *reinterpret_cast<float4*>(w) = *reinterpret_cast<const float4*>(col_scales + h * 128 + c * 32 + j);
+                        if (ROW_SCALES) *reinterpret_cast<float4*>(w) = *reinterpret_cast<const float4*>(col_scales + c * 32 + j);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            float v = __uint_as_float(d[c][j + i]);
+                            float v = __uint_as_float(d[c & 1][j + i]);
                             if (ROW_SCALES) v *= w[i];
-                            acc[h][c * 32 + j + i] = fmaf(v, scale, acc[h][c * 32 + j + i]);
+                            acc[c * 32 + j + i] = fmaf(v, scale, acc[c * 32 + j + i]);
                         }
                     }
                 };
-                const auto give_back = [&](int h) {
-                    tc_fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) {
-                        const uint32_t to = smem_u32(&tempty[(2 * it + h) & 3]);
-                        if (rank == 0) mbar_arrive(to);
-                        else mbar_arrive_cluster_relaxed(map_to_cta(to, 0));
-                    }
-                };
-                const uint32_t from = tmem_mine + ((2 * it) & 3) * 128;
-                ok = mbar_wait(bar, parity, abort_flag, p.status, 0x330u);
+                const uint32_t b = (2 * it) & 3, from = tmem_mine + b * 128;
+                ok = mbar_wait(smem_u32(&done[2 * s + h]), parity, abort_flag, p.status, 0x330u);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after_sync();
                 tmem_ld_32x32(from, d[0]);
                 tmem_ld_32x32(from + 32, d[1]);
                 if (ROW_SCALES) ok = mbar_wait(smem_u32(&sfull[s]), parity, abort_flag, p.status, 0x331u);
-                bool ready = mbar_try_wait(bar + 8, parity);
-                ready = __all_sync(0xffffffffu, ready);
                 tmem_ld_wait();
-                give_back(0);
-                if (!ready) {
-                    ok = mbar_wait(bar + 8, parity, abort_flag, p.status, 0x332u) && ok;
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
+                add(0);
+                tmem_ld_32x32(from + 64, d[0]);
+                add(1);
+                tmem_ld_32x32(from + 96, d[1]);
+                tmem_ld_wait();
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) {                               // the buffer goes back before its last sums are added
+                    const uint32_t to = smem_u32(&tempty[b + h]);
+                    if (rank == 0) mbar_arrive(to);
+                    else mbar_arrive_cluster_relaxed(map_to_cta(to, 0));
                 }
-                tc_fence_after_sync();
-                add(0, 0, scale0);
-                tmem_ld_32x32(from + 128, d[0]);
-                add(0, 1, scale0);
-                tmem_ld_32x32(from + 160, d[1]);
-                tmem_ld_wait();
-                give_back(1);
-                add(1, 0, scale1);
-                add(1, 1, scale1);
+                add(2);
+                add(3);
                 if (ROW_SCALES) {
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_u32(&sempty[s]));
@@ -548,46 +534,42 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             if (!ok) break;
             out.row0 = (long long)mt * 256 + rank * 128 + quarter * 32;
             if (out.row0 >= p.M) continue;
+            if (p.bias) {
+                const bool whole = (reinterpret_cast<uintptr_t>(p.bias) & 15) == 0 && col + 128 <= p.N;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int col = nt * 256 + h * 128 + part * 64;
-                if (p.bias) {
-                    const bool whole = (reinterpret_cast<uintptr_t>(p.bias) & 15) == 0 && col + 64 <= p.N;
-#pragma unroll
-                    for (int i = 0; i < 64; i += 4) {
-                        float4 b = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                        if (whole) {
-                            b = __ldg(reinterpret_cast<const float4*>(p.bias + col + i));
-                        } else {
-                            if (col + i < p.N) b.x = __ldg(p.bias + col + i);
-                            if (col + i + 1 < p.N) b.y = __ldg(p.bias + col + i + 1);
-                            if (col + i + 2 < p.N) b.z = __ldg(p.bias + col + i + 2);
-                            if (col + i + 3 < p.N) b.w = __ldg(p.bias + col + i + 3);
-                        }
-                        acc[h][i] += b.x; acc[h][i + 1] += b.y; acc[h][i + 2] += b.z; acc[h][i + 3] += b.w;
+                for (int i = 0; i < 128; i += 4) {
+                    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    if (whole) {
+                        v = __ldg(reinterpret_cast<const float4*>(p.bias + col + i));
+                    } else {
+                        if (col + i < p.N) v.x = __ldg(p.bias + col + i);
+                        if (col + i + 1 < p.N) v.y = __ldg(p.bias + col + i + 1);
+                        if (col + i + 2 < p.N) v.z = __ldg(p.bias + col + i + 2);
+                        if (col + i + 3 < p.N) v.w = __ldg(p.bias + col + i + 3);
                     }
+                    acc[i] += v.x; acc[i + 1] += v.y; acc[i + 2] += v.z; acc[i + 3] += v.w;
                 }
-                if (p.y_is_bf16) {
+            }
+            if (p.y_is_bf16) {
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        if (col + 32 * c >= p.N) break;
-                        uint32_t w[16];
+                for (int c = 0; c < 4; ++c) {
+                    if (col + 32 * c >= p.N) break;
+                    uint32_t w[16];
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            const __nv_bfloat162 t = __floats2bfloat162_rn(acc[h][c * 32 + 2 * j], acc[h][c * 32 + 2 * j + 1]);
-                            w[j] = *reinterpret_cast<const uint32_t*>(&t);
-                        }
-                        store_piece<S::kPieces>(p, &tmY, out, col + 32 * c, w, lane);
+                    for (int j = 0; j < 16; ++j) {
+                        const __nv_bfloat162 t = __floats2bfloat162_rn(acc[c * 32 + 2 * j], acc[c * 32 + 2 * j + 1]);
+                        w[j] = *reinterpret_cast<const uint32_t*>(&t);
                     }
-                } else {
+                    store_piece<S::kPieces>(p, &tmY, out, col + 32 * c, w, lane);
+                }
+            } else {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        if (col + 16 * c >= p.N) break;
-                        uint32_t w[16];
+                for (int c = 0; c < 8; ++c) {
+                    if (col + 16 * c >= p.N) break;
+                    uint32_t w[16];
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) w[j] = __float_as_uint(acc[h][c * 16 + j]);
-                        store_piece<S::kPieces>(p, &tmY, out, col + 16 * c, w, lane);
-                    }
+                    for (int j = 0; j < 16; ++j) w[j] = __float_as_uint(acc[c * 16 + j]);
+                    store_piece<S::kPieces>(p, &tmY, out, col + 16 * c, w, lane);
                 }
             }
         }
