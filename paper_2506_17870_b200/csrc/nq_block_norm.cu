@@ -205,6 +205,8 @@ __global__ void __launch_bounds__(512) block_norm_kernel(const NormArgs p, int t
     const int team = threadIdx.x / threads, teams = blockDim.x / threads;
     const Cols<NV, VEC> c{(int)threadIdx.x - team * threads, threads, p.cols};
     TeamSum<1> sum{box, 0, threads >> 5};
+    start_next();
+    wait_previous();
     for (long long row = (long long)blockIdx.x * teams + team; row < p.rows; row += (long long)gridDim.x * teams) {
         float r[NV][8];
         load_row(c, static_cast<const TX*>(p.x) + row * p.ldx, r);
@@ -325,6 +327,8 @@ __global__ void __launch_bounds__(512) block_norm_backward_kernel(const BackArgs
 #pragma unroll
         for (int j = 0; j < 8; ++j) P0[k][j] = P1[k][j] = 0.0f;
     bool first = true;
+    start_next();
+    wait_previous();
 
     for (long long item = blockIdx.x; item < p.items; item += gridDim.x) {
         const long long group = item / p.chunks;
@@ -501,15 +505,17 @@ struct JoinArgs {
     const float* gate_part;
     float* out[4];                         // dpre_weight, dpre_bias, dpost_weight, dpost_bias
     float* dgate;
-    int cols, blocks, chunks;
+    int cols, col_blocks, blocks, chunks;
     long long groups;
 };
 constexpr int kJoinCols = 32, kJoinSlices = 8;
 __global__ void __launch_bounds__(kJoinCols* kJoinSlices) block_norm_join_kernel(const JoinArgs p) {
     __shared__ float box[kJoinSlices][kJoinCols];
     const int lane = threadIdx.x % kJoinCols, slice = threadIdx.x / kJoinCols;
-    const int col = blockIdx.x * kJoinCols + lane;
-    for (long long z = blockIdx.y; z < 4 + p.groups; z += gridDim.y) {
+    const int col = (int)(blockIdx.x % p.col_blocks) * kJoinCols + lane;
+    start_next();
+    wait_previous();
+    for (long long z = blockIdx.x / p.col_blocks; z < 4 + p.groups; z += gridDim.x / p.col_blocks) {
         float* out = z < 4 ? p.out[z] : p.dgate + (z - 4) * p.cols;
         if (!out) continue;                                          // the same for the whole block
         const int n = z < 4 ? p.blocks : p.chunks;
@@ -572,8 +578,7 @@ int launch_norm(const NormArgs& a, bool vec, cudaStream_t stream) {
     const long long most = (long long)sm_count() * (2048 / block);
     if (grid > most) grid = most;
     const auto run = [&](auto kernel) {
-        kernel<<<(unsigned)grid, block, 0, stream>>>(a, sh.threads);
-        return cudaGetLastError() == cudaSuccess ? NQ_OK : NQ_ERR_CUDA;
+        return launch_chained(kernel, (unsigned)grid, block, 0, 1, stream, a, sh.threads);
     };
     if (vec) {
         if (sh.nv == 1) return run(block_norm_kernel<TX, TY, 1, true>);
@@ -612,8 +617,7 @@ BackPlan plan_backward(const nq_block_norm_desc* d, bool has_gate) {
 template <typename TX, typename TY>
 int launch_back(const BackArgs& a, const BackPlan& pl, bool vec, cudaStream_t stream) {
     const auto run = [&](auto kernel) {
-        kernel<<<(unsigned)pl.blocks, pl.shape.threads, 0, stream>>>(a);
-        return cudaGetLastError() == cudaSuccess ? NQ_OK : NQ_ERR_CUDA;
+        return launch_chained(kernel, (unsigned)pl.blocks, pl.shape.threads, 0, 1, stream, a);
     };
     if (vec) {
         if (pl.shape.nv == 1) return run(block_norm_backward_kernel<TX, TY, 1, true>);
@@ -726,9 +730,8 @@ int nq_block_norm_backward(const nq_block_norm_desc* d, const void* R, const voi
     j.out[0] = dpre_weight; j.out[1] = dpre_bias; j.out[2] = dpost_weight; j.out[3] = dpost_bias;
     j.groups = join_gate ? pl.groups : 0;
     const long long planes = 4 + j.groups;
-    const dim3 grid((unsigned)((d->cols + kJoinCols - 1) / kJoinCols), (unsigned)(planes < 1024 ? planes : 1024));
-    block_norm_join_kernel<<<grid, kJoinCols * kJoinSlices, 0, s>>>(j);
-    return cudaGetLastError() == cudaSuccess ? NQ_OK : NQ_ERR_CUDA;
+    j.col_blocks = (int)((d->cols + kJoinCols - 1) / kJoinCols);
+    return launch_chained(block_norm_join_kernel, (unsigned)(j.col_blocks * (planes < 1024 ? planes : 1024)), kJoinCols * kJoinSlices, 0, 1, s, j);
 }
 
 }  // extern "C"

@@ -108,6 +108,8 @@ fp8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_slot;
+    start_next();
+    wait_previous();
 
     float acc[NT];
 #pragma unroll
@@ -397,6 +399,8 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     cluster_sync_all();                                        // both CTAs' barriers exist before anyone signals across
     tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_slot;
+    start_next();
+    wait_previous();
     // 384 threads are launched with 168 registers each (64512); the promotion warps take 224 (256 x 224 = 57344), the
     // other four 56 (128 x 56 = 7168): together what was launched.
     if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
@@ -627,6 +631,8 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
 
 // K == 0: no groups
 __global__ void fp8_empty_kernel(const Fp8Args p) {
+    start_next();
+    wait_previous();
     const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
     if (i < (long long)p.M * p.N) store_out(p, i / p.N, (int)(i % p.N), 0.0f);
 }
@@ -655,23 +661,7 @@ int launch_tile(const CUtensorMap& tmB, const void* A, int64_t lda, int64_t K, F
         }
         configured[dev] = 1;
     }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(tiles * split), 1, 1);
-    cfg.blockDim = dim3(kTileThreads, 1, 1);
-    cfg.dynamicSmemBytes = TileShape<NT>::kSmem;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = split;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, fp8_tile_kernel<NT>, tmA, tmB, a) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return NQ_ERR_CUDA;
-    }
-    return NQ_OK;
+    return launch_chained(fp8_tile_kernel<NT>, (unsigned)(tiles * split), kTileThreads, TileShape<NT>::kSmem, (unsigned)split, stream, tmA, tmB, a);
 }
 
 template <bool ROW_SCALES>
@@ -689,23 +679,7 @@ int launch_pair(const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensorMa
     }
     const long long tiles = (long long)a.m_tiles * a.n_tiles;
     const int max_pairs = sm_count() / 2;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(2 * (tiles < max_pairs ? tiles : max_pairs)), 1, 1);
-    cfg.blockDim = dim3(kPairThreads, 1, 1);
-    cfg.dynamicSmemBytes = S::kSmem;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 2;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, fp8_pair_kernel<ROW_SCALES>, tmA, tmB, tmY, a) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return NQ_ERR_CUDA;
-    }
-    return NQ_OK;
+    return launch_chained(fp8_pair_kernel<ROW_SCALES>, (unsigned)(2 * (tiles < max_pairs ? tiles : max_pairs)), kPairThreads, S::kSmem, 2u, stream, tmA, tmB, tmY, a);
 }
 
 int run_fp8_gemm(const void* A, int64_t lda, const void* B, int64_t ldb, int64_t K, Fp8Args& a, cudaStream_t stream) {
@@ -758,8 +732,7 @@ extern "C" int nq_fp8_gemm(const void* A, int64_t lda, const float* SA, int64_t 
     const cudaStream_t s = (cudaStream_t)stream;
     if (K == 0) {
         if ((M * N + 255) / 256 > 0x7fffffffll) return NQ_ERR_UNSUPPORTED;
-        nq::fp8_empty_kernel<<<(unsigned)((M * N + 255) / 256), 256, 0, s>>>(a);
-        return cudaGetLastError() == cudaSuccess ? NQ_OK : NQ_ERR_CUDA;
+        return nq::launch_chained(nq::fp8_empty_kernel, (unsigned)((M * N + 255) / 256), 256, 0, 1, s, a);
     }
     if (!A || !B || !SA || !SB || lda < K || ldb < K || ldsa < M || ldsb < (b_block_rows == 128 ? (N + 127) / 128 : N)) return NQ_ERR_INVALID_ARG;
     if ((at(A) & 15) || (at(B) & 15) || (lda & 15) || (ldb & 15) || (at(SA) & 3) || (at(SB) & 3)) return NQ_ERR_ALIGNMENT;

@@ -91,6 +91,8 @@ __global__ void __launch_bounds__(kThreads) fp8_quantize_kernel(const QuantArgs 
 
     if (tid < kTile) s_colmax[tid] = 0;
     if (tid == 0) s_blockmax = 0;
+    start_next();
+    wait_previous();
 
     Row16<T> v[4];
     if (ALIGNED) {
@@ -228,8 +230,7 @@ int launch(const QuantArgs& a, long long tiles, cudaStream_t stream) {
             return NQ_ERR_CUDA;
         }
     }
-    fp8_quantize_kernel<T, BLOCK, ALIGNED><<<(unsigned)tiles, kThreads, smem, stream>>>(a);
-    return cudaGetLastError() == cudaSuccess ? NQ_OK : NQ_ERR_CUDA;
+    return launch_chained(fp8_quantize_kernel<T, BLOCK, ALIGNED>, (unsigned)tiles, kThreads, smem, 1, stream, a);
 }
 
 template <typename T>
