@@ -6,6 +6,7 @@
 #include "../../include/nq.h"
 #include "nq_fp8.cuh"
 #include "nq_internal.cuh"
+#include "nq_sm100.cuh"
 
 namespace nq {
 namespace {
@@ -27,96 +28,135 @@ struct Cols {
     __device__ __forceinline__ bool has(int k, int j) const { return col(k, VEC ? 0 : j) < cols; }
 };
 
+// A thread's values of a row, in pairs.
+template <int NV>
+using Row = uint64_t[NV][4];
+
 __device__ __forceinline__ uint4 ld16(const void* p) {
     uint4 v;
     asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
-
+__device__ __forceinline__ void spread(const uint4& w, uint64_t (&v)[4]) {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = pack2(u[j] << 16, u[j] & 0xffff0000u);
+}
+__device__ __forceinline__ void spread(const uint4& a, const uint4& b, uint64_t (&v)[4]) {
+    v[0] = pack2(a.x, a.y); v[1] = pack2(a.z, a.w); v[2] = pack2(b.x, b.y); v[3] = pack2(b.z, b.w);
+}
+// a row from global memory; absent columns read as zero
 template <int NV, bool VEC>
-__device__ __forceinline__ void load_row(const Cols<NV, VEC>& c, const bf16* row, float (&v)[NV][8]) {
+__device__ __forceinline__ void load_row(const Cols<NV, VEC>& c, const bf16* row, Row<NV>& v) {
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         if (VEC) {
             uint4 w = make_uint4(0u, 0u, 0u, 0u);
             if (c.has(k, 0)) w = ld16(row + c.col(k, 0));
-            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                v[k][2 * j] = __uint_as_float(u[j] << 16);
-                v[k][2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u);
-            }
+            spread(w, v[k]);
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[k][j] = c.has(k, j) ? __bfloat162float(row[c.col(k, j)]) : 0.0f;
+            for (int j = 0; j < 4; ++j)
+                v[k][j] = pack2f(c.has(k, 2 * j) ? __bfloat162float(row[c.col(k, 2 * j)]) : 0.0f,
+                                 c.has(k, 2 * j + 1) ? __bfloat162float(row[c.col(k, 2 * j + 1)]) : 0.0f);
         }
     }
 }
 template <int NV, bool VEC>
-__device__ __forceinline__ void load_row(const Cols<NV, VEC>& c, const float* row, float (&v)[NV][8]) {
+__device__ __forceinline__ void load_row(const Cols<NV, VEC>& c, const float* row, Row<NV>& v) {
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         if (VEC) {
             uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
             if (c.has(k, 0)) { a = ld16(row + c.col(k, 0)); b = ld16(row + c.col(k, 0) + 4); }
-            const uint32_t u[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[k][j] = __uint_as_float(u[j]);
+            spread(a, b, v[k]);
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[k][j] = c.has(k, j) ? row[c.col(k, j)] : 0.0f;
+            for (int j = 0; j < 4; ++j)
+                v[k][j] = pack2f(c.has(k, 2 * j) ? row[c.col(k, 2 * j)] : 0.0f, c.has(k, 2 * j + 1) ? row[c.col(k, 2 * j + 1)] : 0.0f);
         }
     }
 }
-// one piece of a parameter vector (cached: every row reads the same one); `none` where it is absent
+// the same from a row in shared memory (VEC only)
+template <int NV>
+__device__ __forceinline__ void take_row(const Cols<NV, true>& c, const bf16* row, Row<NV>& v) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        uint4 w = make_uint4(0u, 0u, 0u, 0u);
+        if (c.has(k, 0)) w = *reinterpret_cast<const uint4*>(row + c.col(k, 0));
+        spread(w, v[k]);
+    }
+}
+template <int NV>
+__device__ __forceinline__ void take_row(const Cols<NV, true>& c, const float* row, Row<NV>& v) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
+        if (c.has(k, 0)) {
+            a = *reinterpret_cast<const uint4*>(row + c.col(k, 0));
+            b = *reinterpret_cast<const uint4*>(row + c.col(k, 0) + 4);
+        }
+        spread(a, b, v[k]);
+    }
+}
+// one piece of a parameter vector; `none` where the vector is absent, zero in absent columns of one that is there
 template <int NV, bool VEC>
-__device__ __forceinline__ void load_param(const Cols<NV, VEC>& c, const float* vec, float none, int k, float (&v)[8]) {
+__device__ __forceinline__ void load_param(const Cols<NV, VEC>& c, const float* vec, float none, int k, uint64_t (&v)[4]) {
     if (!vec) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = none;
+        for (int j = 0; j < 4; ++j) v[j] = both(none);
     } else if (VEC) {
-        float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+        uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
         if (c.has(k, 0)) {
-            a = __ldg(reinterpret_cast<const float4*>(vec + c.col(k, 0)));
-            b = __ldg(reinterpret_cast<const float4*>(vec + c.col(k, 0) + 4));
+            a = __ldg(reinterpret_cast<const uint4*>(vec + c.col(k, 0)));
+            b = __ldg(reinterpret_cast<const uint4*>(vec + c.col(k, 0) + 4));
         }
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        spread(a, b, v);
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = c.has(k, j) ? __ldg(vec + c.col(k, j)) : 0.0f;
+        for (int j = 0; j < 4; ++j)
+            v[j] = pack2f(c.has(k, 2 * j) ? __ldg(vec + c.col(k, 2 * j)) : 0.0f, c.has(k, 2 * j + 1) ? __ldg(vec + c.col(k, 2 * j + 1)) : 0.0f);
     }
 }
 
-__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
+__device__ __forceinline__ uint32_t bf16x2(uint64_t v) {
+    float lo, hi;
+    unpack2(v, lo, hi);
     const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&t);
 }
 template <int NV, bool VEC>
-__device__ __forceinline__ void store_piece(const Cols<NV, VEC>& c, bf16* row, int k, const float (&v)[8]) {
+__device__ __forceinline__ void store_piece(const Cols<NV, VEC>& c, bf16* row, int k, const uint64_t (&v)[4]) {
     if (VEC) {
-        if (c.has(k, 0))
-            *reinterpret_cast<uint4*>(row + c.col(k, 0)) =
-                make_uint4(bf16x2(v[0], v[1]), bf16x2(v[2], v[3]), bf16x2(v[4], v[5]), bf16x2(v[6], v[7]));
+        if (c.has(k, 0)) *reinterpret_cast<uint4*>(row + c.col(k, 0)) = make_uint4(bf16x2(v[0]), bf16x2(v[1]), bf16x2(v[2]), bf16x2(v[3]));
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (c.has(k, j)) row[c.col(k, j)] = __float2bfloat16_rn(v[j]);
+        for (int j = 0; j < 4; ++j) {
+            float lo, hi;
+            unpack2(v[j], lo, hi);
+            if (c.has(k, 2 * j)) row[c.col(k, 2 * j)] = __float2bfloat16_rn(lo);
+            if (c.has(k, 2 * j + 1)) row[c.col(k, 2 * j + 1)] = __float2bfloat16_rn(hi);
+        }
     }
 }
 template <int NV, bool VEC>
-__device__ __forceinline__ void store_piece(const Cols<NV, VEC>& c, float* row, int k, const float (&v)[8]) {
+__device__ __forceinline__ void store_piece(const Cols<NV, VEC>& c, float* row, int k, const uint64_t (&v)[4]) {
     if (VEC) {
         if (c.has(k, 0)) {
-            *reinterpret_cast<float4*>(row + c.col(k, 0)) = make_float4(v[0], v[1], v[2], v[3]);
-            *reinterpret_cast<float4*>(row + c.col(k, 0) + 4) = make_float4(v[4], v[5], v[6], v[7]);
+            *reinterpret_cast<ulonglong2*>(row + c.col(k, 0)) = make_ulonglong2(v[0], v[1]);
+            *reinterpret_cast<ulonglong2*>(row + c.col(k, 0) + 4) = make_ulonglong2(v[2], v[3]);
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (c.has(k, j)) row[c.col(k, j)] = v[j];
+        for (int j = 0; j < 4; ++j) {
+            float lo, hi;
+            unpack2(v[j], lo, hi);
+            if (c.has(k, 2 * j)) row[c.col(k, 2 * j)] = lo;
+            if (c.has(k, 2 * j + 1)) row[c.col(k, 2 * j + 1)] = hi;
+        }
     }
 }
-// the low bytes of q, four to a word
+// eight bytes of a piece, four to a word
 template <int NV, bool VEC>
 __device__ __forceinline__ void store_bytes8(const Cols<NV, VEC>& c, uint8_t* row, int k, uint32_t lo, uint32_t hi) {
     if (VEC) {
@@ -126,6 +166,52 @@ __device__ __forceinline__ void store_bytes8(const Cols<NV, VEC>& c, uint8_t* ro
         for (int j = 0; j < 8; ++j)
             if (c.has(k, j)) row[c.col(k, j)] = (uint8_t)((j < 4 ? lo : hi) >> (8 * (j & 3)));
     }
+}
+
+// A ring of rows in shared memory, filled by bulk copies that one thread starts several rows ahead, so that the bytes in
+// flight do not depend on how many threads wait for a row's sums.  Rows of up to four tensors lie side by side in a
+// stage.  A wait that gives up (see mbar_wait) lets its thread go on with what is there: every later wait then returns
+// at once, all threads reach all barriers, and the host finds the record.
+struct RowRing {
+    uint8_t* stages;
+    uint64_t* full;
+    volatile int* abort_flag;
+    unsigned int* status;
+    int count;                             // stages
+    int stage_bytes;
+    __device__ __forceinline__ void init(uint8_t* smem, int n, int bytes, unsigned int* st) {
+        full = reinterpret_cast<uint64_t*>(smem);
+        abort_flag = reinterpret_cast<volatile int*>(smem + 120);
+        stages = smem + 128;
+        count = n;
+        stage_bytes = bytes;
+        status = st;
+        if (threadIdx.x == 0) {
+            for (int i = 0; i < n; ++i) sm100::mbar_init(sm100::smem_u32(&full[i]), 1);
+            *abort_flag = 0;
+            sm100::fence_barrier_init();
+        }
+        __syncthreads();
+    }
+    __device__ __forceinline__ uint8_t* stage(int s) const { return stages + s * stage_bytes; }
+    __device__ __forceinline__ void expect(int s) const { sm100::mbar_arrive_expect_tx(sm100::smem_u32(&full[s]), stage_bytes); }
+    __device__ __forceinline__ void copy(int s, int offset, const void* src, int bytes) const {
+        sm100::bulk_load(sm100::smem_u32(stage(s) + offset), src, bytes, sm100::smem_u32(&full[s]));
+    }
+    __device__ __forceinline__ void wait(int s, int parity) const {
+        (void)sm100::mbar_wait(sm100::smem_u32(&full[s]), parity, abort_flag, status, 0x400u);
+    }
+    __device__ __forceinline__ void leave() const {
+        if (threadIdx.x == 0 && *abort_flag) {                 // let copies in flight land before shared memory is released
+            const long long t0 = clock64();
+            while (clock64() - t0 < (1ll << 22)) { }
+        }
+    }
+};
+// stages for a block of which `blocks` share an SM: about 200 KB in all, at least two rows
+int ring_stages(int stage_bytes, int blocks) {
+    int n = (200 * 1024 / blocks - 128) / stage_bytes;
+    return n > 8 ? 8 : n;
 }
 
 // Sums of N values over the threads of a row.  Up to one warp: shuffles alone.  More: the warps' sums through shared
@@ -156,6 +242,39 @@ struct TeamSum {
     }
 };
 
+// adds `what` to the row's columns; absent ones stay as they are (zero, which sums over the row rely on)
+template <int NV, bool VEC>
+__device__ __forceinline__ void shift_row(const Cols<NV, VEC>& c, Row<NV>& v, float what) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (VEC) {
+                if (c.has(k, 0)) v[k][j] = add2(v[k][j], both(what));
+            } else {
+                v[k][j] = add2(v[k][j], pack2f(c.has(k, 2 * j) ? what : 0.0f, c.has(k, 2 * j + 1) ? what : 0.0f));
+            }
+        }
+}
+template <int NV>
+__device__ __forceinline__ float total(const Row<NV>& v) {
+    uint64_t s = 0ull;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s = add2(s, v[k][j]);
+    return sum2(s);
+}
+template <int NV>
+__device__ __forceinline__ float dot(const Row<NV>& a, const Row<NV>& b) {
+    uint64_t s = 0ull;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s = fma2(a[k][j], b[k][j], s);
+    return sum2(s);
+}
+
 struct NormArgs {
     long long rows;
     int cols;
@@ -166,125 +285,196 @@ struct NormArgs {
     long long ldx, ldy, ldr, ldh, ldhs, rows_per_gate;
     int h_dtype, post, pre;
     float skip, branch, eps, inv_cols, inv_h_scale;
+    int ring, stage_bytes;                 // RING: stages and their size
+    unsigned int* status;
 };
 
-// v -> v^ in place
+// Centres v for a layer norm and returns 1 / sqrt(mean of squares + eps); 1 for no norm.  The variance is that of the
+// centred values, from registers: no cancellation however large the mean.
 template <int NV, bool VEC, typename Sum>
-__device__ __forceinline__ void standardise(const Cols<NV, VEC>& c, float (&v)[NV][8], int kind, float inv_cols, float eps, Sum& sum) {
+__device__ __forceinline__ float norm_factor(const Cols<NV, VEC>& c, Row<NV>& v, int kind, float inv_cols, float eps, Sum& sum) {
+    if (kind == NQ_NORM_NONE) return 1.0f;
     if (kind == NQ_NORM_LAYER) {
-        float m[1] = {0.0f};
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) m[0] += v[k][j];
+        float m[1] = {total<NV>(v)};
         sum(m);
-        const float mean = m[0] * inv_cols;
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[k][j] = c.has(k, j) ? v[k][j] - mean : 0.0f;
+        shift_row(c, v, -m[0] * inv_cols);
     }
-    float q[1] = {0.0f};
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) q[0] = fmaf(v[k][j], v[k][j], q[0]);
+    float q[1] = {dot<NV>(v, v)};
     sum(q);
-    const float inv = rsqrtf(fmaf(q[0], inv_cols, eps));
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[k][j] *= inv;
+    return rsqrtf(fmaf(q[0], inv_cols, eps));
 }
 
-// One row at a time to a team of threads (a warp, or the whole block when a row needs more), the row in registers
-// throughout: each tensor is touched once, so the pass is bound by memory.
-template <typename TX, typename TY, int NV, bool VEC>
+// A team of threads (a warp, or the whole block when a row needs more) walks its share of the rows, neighbours one after
+// the other, with the row in registers throughout: each tensor is touched once, so the pass should be bound by memory.
+// What it competes with is the instruction issue -- at HBM speed an SM has 38 issue slots for 32 columns of bf16 in,
+// bf16 and e4m3 out -- so arithmetic is on pairs, the parameters stay in registers (HOLD: rows of up to 8192; the post
+// norm's weight, the gate and the branch scale as one factor, which changes only with the gate's row), and the rows
+// come through a ring in shared memory (RING: blocks that work through many rows).  16384 x 8192, bf16 to e4m3: 475 us with
+// scalar arithmetic, parameters read for each row and each row loaded when its turn came, 398 with the ring alone.
+// BIAS: one of the norms has a bias.
+template <typename TX, typename TY, int NV, bool VEC, bool RING, bool BIAS>
 __global__ void __launch_bounds__(512) block_norm_kernel(const NormArgs p, int threads) {
+    constexpr bool HOLD = NV <= 2;
     __shared__ float box[2][32][1];
+    extern __shared__ __align__(16) uint8_t ring_smem[];
     const int team = threadIdx.x / threads, teams = blockDim.x / threads;
     const Cols<NV, VEC> c{(int)threadIdx.x - team * threads, threads, p.cols};
     TeamSum<1> sum{box, 0, threads >> 5};
+    RowRing ring;
+    const int x_bytes = p.cols * (int)sizeof(TX), y_bytes = p.cols * (int)sizeof(TY);
+    const auto start = [&](int s, long long row) {             // one thread
+        ring.expect(s);
+        ring.copy(s, 0, static_cast<const TX*>(p.x) + row * p.ldx, x_bytes);
+        if (p.y) ring.copy(s, x_bytes, static_cast<const TY*>(p.y) + row * p.ldy, y_bytes);
+    };
+    if (RING) ring.init(ring_smem, p.ring, p.stage_bytes, p.status);
     start_next();
     wait_previous();
-    for (long long row = (long long)blockIdx.x * teams + team; row < p.rows; row += (long long)gridDim.x * teams) {
-        float r[NV][8];
-        load_row(c, static_cast<const TX*>(p.x) + row * p.ldx, r);
+    const long long share = (long long)blockIdx.x * teams + team, shares = (long long)gridDim.x * teams;
+    const long long row0 = p.rows * share / shares, row1 = p.rows * (share + 1) / shares;
+    if (RING && threadIdx.x == 0)
+        for (int s = 0; s < p.ring && row0 + s < row1; ++s) start(s, row0 + s);
+
+    // u enters r as fma(v, factor * inv, offset), h is fma(r^, weight, shift)
+    Row<HOLD ? NV : 1> factor, offset, weight, shift;
+    const auto load_post = [&](const float* gate, int k, uint64_t (&f)[4], uint64_t (&o)[4]) {
+        uint64_t w[4], g[4];
+        load_param(c, p.post_weight, 1.0f, k, w);
+        load_param(c, gate, 1.0f, k, g);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            g[j] = mul2(g[j], both(p.branch));
+            f[j] = mul2(g[j], w[j]);
+        }
+        if (BIAS) {
+            load_param(c, p.post_bias, 0.0f, k, o);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = mul2(o[j], g[j]);
+        }
+    };
+    const auto load_pre = [&](int k, uint64_t (&w)[4], uint64_t (&b)[4]) {
+        load_param(c, p.pre_weight, 1.0f, k, w);
+        if (BIAS) load_param(c, p.pre_bias, 0.0f, k, b);
+    };
+    if (HOLD && p.pre != NQ_NORM_NONE) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) load_pre(k, weight[HOLD ? k : 0], shift[HOLD ? k : 0]);
+    }
+    long long gate_until = row0;                               // first row that needs another gate row
+    const float* gate = p.gate;
+    int stage = 0, parity = 0;
+    for (long long row = row0; row < row1; ++row) {
+        if (p.y && row == gate_until) {
+            gate_until = row1;
+            if (p.gate && p.rows_per_gate) {
+                const long long g = row / p.rows_per_gate;
+                gate = p.gate + g * p.cols;
+                gate_until = (g + 1) * p.rows_per_gate;
+            }
+            if (HOLD) {
+#pragma unroll
+                for (int k = 0; k < NV; ++k) load_post(gate, k, factor[HOLD ? k : 0], offset[HOLD ? k : 0]);
+            }
+        }
+        const auto refill = [&]() {                            // after a barrier: every thread has taken its part
+            if (RING && threadIdx.x == 0 && row + p.ring < row1) start(stage, row + p.ring);
+        };
+        Row<NV> r;
+        if constexpr (RING) {
+            ring.wait(stage, parity);
+            take_row(c, reinterpret_cast<const TX*>(ring.stage(stage)), r);
+        } else {
+            load_row(c, static_cast<const TX*>(p.x) + row * p.ldx, r);
+        }
         if (p.y) {
-            float u[NV][8];
-            load_row(c, static_cast<const TY*>(p.y) + row * p.ldy, u);
-            if (p.post != NQ_NORM_NONE) standardise(c, u, p.post, p.inv_cols, p.eps, sum);
-            const float* gate = p.gate ? p.gate + (p.rows_per_gate ? row / p.rows_per_gate : 0) * p.cols : nullptr;
+            Row<NV> u;
+            if constexpr (RING) take_row(c, reinterpret_cast<const TY*>(ring.stage(stage) + x_bytes), u);
+            else load_row(c, static_cast<const TY*>(p.y) + row * p.ldy, u);
+            const float inv = norm_factor(c, u, p.post, p.inv_cols, p.eps, sum);
+            if (p.post != NQ_NORM_NONE) refill();
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                float w[8], b[8], g[8];
-                load_param(c, p.post_weight, 1.0f, k, w);
-                load_param(c, p.post_bias, 0.0f, k, b);
-                load_param(c, gate, 1.0f, k, g);
+                uint64_t f[4], o[4];
+                if (!HOLD) load_post(gate, k, f, o);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) r[k][j] = fmaf(p.skip, r[k][j], p.branch * g[j] * fmaf(u[k][j], w[j], b[j]));
+                for (int j = 0; j < 4; ++j) {
+                    const uint64_t fj = HOLD ? factor[HOLD ? k : 0][j] : f[j];
+                    r[k][j] = BIAS ? fma2(r[k][j], both(p.skip), HOLD ? offset[HOLD ? k : 0][j] : o[j]) : mul2(r[k][j], both(p.skip));
+                    r[k][j] = fma2(u[k][j], mul2(fj, both(inv)), r[k][j]);
+                }
             }
         } else {
 #pragma unroll
             for (int k = 0; k < NV; ++k)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) r[k][j] *= p.skip;
+                for (int j = 0; j < 4; ++j) r[k][j] = mul2(r[k][j], both(p.skip));
         }
         if (p.r) {
 #pragma unroll
             for (int k = 0; k < NV; ++k) store_piece(c, static_cast<TX*>(p.r) + row * p.ldr, k, r[k]);
         }
+        const float inv = norm_factor(c, r, p.pre, p.inv_cols, p.eps, sum);
+        if (RING) {
+            if (p.post == NQ_NORM_NONE) {
+                if (p.pre == NQ_NORM_NONE) __syncthreads();
+                refill();
+            }
+            if (++stage == p.ring) { stage = 0; parity ^= 1; }
+        }
         if (p.pre == NQ_NORM_NONE) continue;
-        standardise(c, r, p.pre, p.inv_cols, p.eps, sum);
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            float w[8], b[8];
-            load_param(c, p.pre_weight, 1.0f, k, w);
-            load_param(c, p.pre_bias, 0.0f, k, b);
-            float h[8];
+            uint64_t w[4], b[4], h[4];
+            if (!HOLD) load_pre(k, w, b);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) h[j] = c.has(k, j) ? fmaf(r[k][j], w[j], b[j]) : 0.0f;
+            for (int j = 0; j < 4; ++j) {
+                const uint64_t t = mul2(r[k][j], both(inv)), wj = HOLD ? weight[HOLD ? k : 0][j] : w[j];
+                h[j] = BIAS ? fma2(t, wj, HOLD ? shift[HOLD ? k : 0][j] : b[j]) : mul2(t, wj);
+            }
             if (p.h_dtype == NQ_BF16) {
                 store_piece(c, static_cast<bf16*>(p.h) + row * p.ldh, k, h);
             } else if (p.h_dtype == NQ_F32) {
                 store_piece(c, static_cast<float*>(p.h) + row * p.ldh, k, h);
-            } else if (p.h_dtype == NQ_I8) {
-                uint32_t q[2] = {0u, 0u};
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int i = max(-128, min(127, __float2int_rn(__fmul_rn(h[j], p.inv_h_scale))));
-                    q[j / 4] |= (uint32_t)(i & 255) << (8 * (j & 3));
-                }
-                store_bytes8(c, static_cast<uint8_t*>(p.h) + row * p.ldh, k, q[0], q[1]);
             } else {
-                // groups of 128 columns: 16 lanes of 8 neighbours each, or all lanes of four elements each
-                uint32_t m[2] = {0u, 0u};
+                float e[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) m[j / 4] = max(m[j / 4], __float_as_uint(h[j]) & 0x7fffffffu);
-                if (VEC) {
-                    m[0] = max(m[0], m[1]);
+                for (int j = 0; j < 4; ++j) unpack2(h[j], e[2 * j], e[2 * j + 1]);
+                if (p.h_dtype == NQ_I8) {
+                    uint32_t q[2] = {0u, 0u};
 #pragma unroll
-                    for (int d = 8; d > 0; d >>= 1) m[0] = max(m[0], __shfl_xor_sync(0xffffffffu, m[0], d));
-                    m[1] = m[0];
+                    for (int j = 0; j < 8; ++j) {
+                        const int i = max(-128, min(127, __float2int_rn(__fmul_rn(e[j], p.inv_h_scale))));
+                        q[j / 4] |= (uint32_t)(i & 255) << (8 * (j & 3));
+                    }
+                    store_bytes8(c, static_cast<uint8_t*>(p.h) + row * p.ldh, k, q[0], q[1]);
                 } else {
-                    m[0] = __reduce_max_sync(0xffffffffu, m[0]);
-                    m[1] = __reduce_max_sync(0xffffffffu, m[1]);
-                }
-                float s[2], inv[2];
-                group_scale(m[0], s[0], inv[0]);
-                s[1] = s[0]; inv[1] = inv[0];
-                if (!VEC) group_scale(m[1], s[1], inv[1]);
-                if ((c.t & (VEC ? 15 : 31)) == 0) {
+                    // groups of 128 columns: 16 lanes of 8 neighbours each, or all lanes of four elements each
+                    float m[2], s[2], i[2];
+                    m[0] = max_abs(max_abs(e[0], e[1]), max_abs(e[2], e[3]));
+                    m[1] = max_abs(max_abs(e[4], e[5]), max_abs(e[6], e[7]));
+                    if (VEC) {
+                        m[0] = max_abs(m[0], m[1]);
 #pragma unroll
-                    for (int i = 0; i < (VEC ? 1 : 2); ++i)
-                        if (c.has(k, 4 * i)) p.hs[(long long)(c.col(k, 4 * i) >> 7) * p.ldhs + row] = s[i];
+                        for (int d = 8; d > 0; d >>= 1) m[0] = max_abs(m[0], __shfl_xor_sync(0xffffffffu, m[0], d));
+                        group_scale(__float_as_uint(m[0]), s[0], i[0]);
+                        s[1] = s[0]; i[1] = i[0];
+                    } else {
+#pragma unroll
+                        for (int n = 0; n < 2; ++n)
+                            group_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(m[n]) & 0x7fffffffu), s[n], i[n]);
+                    }
+                    if ((c.t & (VEC ? 15 : 31)) == 0) {
+#pragma unroll
+                        for (int n = 0; n < (VEC ? 1 : 2); ++n)
+                            if (c.has(k, 4 * n)) p.hs[(long long)(c.col(k, 4 * n) >> 7) * p.ldhs + row] = s[n];
+                    }
+                    store_bytes8(c, static_cast<uint8_t*>(p.h) + row * p.ldh, k, e4m3x4(e[0] * i[0], e[1] * i[0], e[2] * i[0], e[3] * i[0]),
+                                 e4m3x4(e[4] * i[1], e[5] * i[1], e[6] * i[1], e[7] * i[1]));
                 }
-                store_bytes8(c, static_cast<uint8_t*>(p.h) + row * p.ldh, k,
-                             e4m3x4(h[0] * inv[0], h[1] * inv[0], h[2] * inv[0], h[3] * inv[0]),
-                             e4m3x4(h[4] * inv[1], h[5] * inv[1], h[6] * inv[1], h[7] * inv[1]));
             }
         }
     }
+    if (RING) ring.leave();
 }
 
 // ------------------------------------------------------------------------------------------------------- backward
@@ -302,33 +492,61 @@ struct BackArgs {
     float skip, branch, eps, inv_cols;
     float* gate_part;                      // [items, cols] sums for dgate (dgate itself when chunks == 1), or null
     float* part;                           // [4][blocks][cols]: dpre_weight, dpre_bias, dpost_weight, dpost_bias of each block
+    int ring, stage_bytes;
+    unsigned int* status;
 };
 
-// Row statistics are computed again from r and y (a row is in registers anyway).  With xh, yh the standardised rows:
-//   g  = dr + inv_r * (w dh - mean(w dh) - xh * mean(w dh xh))        (mean(w dh) for NQ_NORM_LAYER only)
-//   dx = skip * g;  du = branch * gate * g
-//   dy = inv_y * (w du - mean(w du) - yh * mean(w du yh))
-// Column sums kept in registers: P = sum dh xh, sum dh (for the pre norm's weight and bias) over all rows of the thread
-// block, A = sum g yh, sum g over the rows of one work item, which lie under one gate row: from A follow both
+// Row statistics are computed again from r and y.  With v, t the rows r and y (centred for a layer norm), e = w_pre dh,
+// f = branch * gate * w_post * g, and means over the row:
+//   g  = dr + inv_r * (e - mean(e) - v inv_r * mean(e v) inv_r);   dx = skip * g       (mean(e), mean(f) for a layer norm only)
+//   dy = inv_y * (f - mean(f) - t inv_y * mean(f t inv_y))
+// Sums over a row are joined across the block together: [r, y, e] if a norm needs means, [v^2, e v, t^2], then [f t, f]
+// -- two or three joins a row, not one for each sum.  Tensors are read again from the ring instead of being held.
+// Column sums stay in registers: P = sum dh v inv_r, sum dh (for the pre norm's weight and bias) over all rows of the thread
+// block, A = sum g t inv_y, sum g over the rows of one work item, which lie under one gate row: from A follow both
 // dgate = branch * (w A0 + b A1) and the item's share branch * gate * A of the post norm's weight and bias.
-template <typename TX, typename TY, int NV, bool VEC>
+template <typename TX, typename TY, int NV, bool VEC, bool RING, bool BIAS>
 __global__ void __launch_bounds__(512) block_norm_backward_kernel(const BackArgs p) {
-    __shared__ float box1[2][32][1];
+    constexpr bool HOLD = NV <= 2;
+    __shared__ float box3[2][32][3];
     __shared__ float box2[2][32][2];
+    extern __shared__ __align__(16) uint8_t ring_smem[];
     const int threads = blockDim.x;
     const Cols<NV, VEC> c{(int)threadIdx.x, threads, p.cols};
-    TeamSum<1> sum1{box1, 0, threads >> 5};
-    TeamSum<2> sum2{box2, 0, threads >> 5};
+    TeamSum<3> sum3{box3, 0, threads >> 5};
+    TeamSum<2> sum2v{box2, 0, threads >> 5};
     const long long plane = (long long)gridDim.x * p.cols, mine = (long long)blockIdx.x * p.cols;
+    const bool has_pre = p.pre != NQ_NORM_NONE;
 
-    float P0[NV][8], P1[NV][8];
+    // a stage: r, dh (pre norm), dr, y, as far as they are there
+    RowRing ring;
+    const int x_bytes = p.cols * (int)sizeof(TX), y_bytes = p.cols * (int)sizeof(TY);
+    const int at_dh = has_pre ? x_bytes : 0, at_dr = at_dh + (has_pre ? y_bytes : 0), at_y = at_dr + (p.dr ? x_bytes : 0);
+    const auto start = [&](int s, long long row) {
+        ring.expect(s);
+        if (has_pre) {
+            ring.copy(s, 0, static_cast<const TX*>(p.r) + row * p.ldr, x_bytes);
+            ring.copy(s, at_dh, static_cast<const TY*>(p.dh) + row * p.lddh, y_bytes);
+        }
+        if (p.dr) ring.copy(s, at_dr, static_cast<const TX*>(p.dr) + row * p.lddr, x_bytes);
+        if (p.y) ring.copy(s, at_y, static_cast<const TY*>(p.y) + row * p.ldy, y_bytes);
+    };
+    if (RING) ring.init(ring_smem, p.ring, p.stage_bytes, p.status);
+    start_next();
+    wait_previous();
+
+    Row<NV> P0, P1;
+    Row<HOLD ? NV : 1> weight, factor;
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) P0[k][j] = P1[k][j] = 0.0f;
+        for (int j = 0; j < 4; ++j) P0[k][j] = P1[k][j] = 0ull;
+    if (HOLD && has_pre) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) load_param(c, p.pre_weight, 1.0f, k, weight[HOLD ? k : 0]);
+    }
     bool first = true;
-    start_next();
-    wait_previous();
+    int stage = 0, parity = 0;
 
     for (long long item = blockIdx.x; item < p.items; item += gridDim.x) {
         const long long group = item / p.chunks;
@@ -336,138 +554,168 @@ __global__ void __launch_bounds__(512) block_norm_backward_kernel(const BackArgs
         long long row1 = min(row0 + p.chunk_rows, (group + 1) * p.group_rows);
         row1 = min(row1, p.rows);
         const float* gate = p.gate ? p.gate + group * p.cols : nullptr;
-        float A0[NV][8], A1[NV][8];
+        const auto load_factor = [&](int k, uint64_t (&f)[4]) {
+            uint64_t g[4];
+            load_param(c, p.post_weight, 1.0f, k, f);
+            load_param(c, gate, 1.0f, k, g);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f[j] = mul2(f[j], mul2(g[j], both(p.branch)));
+        };
+        if (HOLD && p.y) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) load_factor(k, factor[HOLD ? k : 0]);
+        }
+        Row<NV> A0, A1;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) A0[k][j] = A1[k][j] = 0.0f;
+            for (int j = 0; j < 4; ++j) A0[k][j] = A1[k][j] = 0ull;
+        if (RING && threadIdx.x == 0)                          // the ring is empty between items
+            for (int i = 0, s = stage; i < p.ring && row0 + i < row1; ++i, s = s + 1 == p.ring ? 0 : s + 1) start(s, row0 + i);
 
         for (long long row = row0; row < row1; ++row) {
-            float g[NV][8], v[NV][8];
+            const uint8_t* here = RING ? ring.stage(stage) : nullptr;
+            const auto get_x = [&](const void* base, long long ld, int offset, Row<NV>& v) {
+                if constexpr (RING) take_row(c, reinterpret_cast<const TX*>(here + offset), v);
+                else load_row(c, static_cast<const TX*>(base) + row * ld, v);
+            };
+            const auto get_y = [&](const void* base, long long ld, int offset, Row<NV>& v) {
+                if constexpr (RING) take_row(c, reinterpret_cast<const TY*>(here + offset), v);
+                else load_row(c, static_cast<const TY*>(base) + row * ld, v);
+            };
+            if (RING) ring.wait(stage, parity);
+            Row<NV> v, e, t;
+            float s[3] = {0.0f, 0.0f, 0.0f};
+            if (has_pre) {
+                get_x(p.r, p.ldr, 0, v);
+                get_y(p.dh, p.lddh, at_dh, e);
+            }
+            if (p.y) get_y(p.y, p.ldy, at_y, t);
+            const auto weigh = [&](int k, int j, uint64_t d) {
+                if (HOLD) return mul2(d, weight[HOLD ? k : 0][j]);
+                uint64_t w[4];
+                load_param(c, p.pre_weight, 1.0f, k, w);
+                return mul2(d, w[j]);
+            };
+            float mean_e = 0.0f;
+            if (p.pre == NQ_NORM_LAYER || p.post == NQ_NORM_LAYER) {
+                if (has_pre) {
+                    uint64_t a = 0ull;
+#pragma unroll
+                    for (int k = 0; k < NV; ++k)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) a = add2(a, weigh(k, j, e[k][j]));
+                    s[0] = total<NV>(v);
+                    s[1] = sum2(a);
+                }
+                if (p.y) s[2] = total<NV>(t);
+                sum3(s);
+                if (p.pre == NQ_NORM_LAYER) {
+                    shift_row(c, v, -s[0] * p.inv_cols);
+                    mean_e = s[1] * p.inv_cols;
+                }
+                if (p.post == NQ_NORM_LAYER) shift_row(c, t, -s[2] * p.inv_cols);
+            }
+            const float y_total = s[2];
+            if (has_pre || p.post != NQ_NORM_NONE) {
+                s[0] = s[1] = s[2] = 0.0f;
+                if (has_pre) {
+                    uint64_t a = 0ull;
+#pragma unroll
+                    for (int k = 0; k < NV; ++k)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) a = fma2(v[k][j], weigh(k, j, e[k][j]), a);
+                    s[0] = dot<NV>(v, v);
+                    s[1] = sum2(a);
+                }
+                if (p.post != NQ_NORM_NONE) s[2] = dot<NV>(t, t);
+                sum3(s);
+            }
+            const float inv_y = p.post != NQ_NORM_NONE ? rsqrtf(fmaf(s[2], p.inv_cols, p.eps)) : 1.0f;
+            Row<NV> g;
             if (p.dr) {
-                load_row(c, static_cast<const TX*>(p.dr) + row * p.lddr, g);
+                get_x(p.dr, p.lddr, at_dr, g);
             } else {
 #pragma unroll
                 for (int k = 0; k < NV; ++k)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) g[k][j] = 0.0f;
+                    for (int j = 0; j < 4; ++j) g[k][j] = 0ull;
             }
-            if (p.pre != NQ_NORM_NONE) {
-                float e[NV][8];
-                load_row(c, static_cast<const TX*>(p.r) + row * p.ldr, v);
-                load_row(c, static_cast<const TY*>(p.dh) + row * p.lddh, e);
-                if (p.pre == NQ_NORM_LAYER) {
-                    float m[1] = {0.0f};
-#pragma unroll
-                    for (int k = 0; k < NV; ++k)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) m[0] += v[k][j];
-                    sum1(m);
-                    const float mean = m[0] * p.inv_cols;
-#pragma unroll
-                    for (int k = 0; k < NV; ++k)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) v[k][j] = c.has(k, j) ? v[k][j] - mean : 0.0f;
-                }
-                float q[1] = {0.0f};
+            if (has_pre) {
+                const float inv = rsqrtf(fmaf(s[0], p.inv_cols, p.eps));
+                const uint64_t inv2 = both(inv), back = both(-(s[1] * p.inv_cols * inv) * inv);
 #pragma unroll
                 for (int k = 0; k < NV; ++k)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) q[0] = fmaf(v[k][j], v[k][j], q[0]);
-                sum1(q);
-                const float inv = rsqrtf(fmaf(q[0], p.inv_cols, p.eps));
-                float d[2] = {0.0f, 0.0f};
-#pragma unroll
-                for (int k = 0; k < NV; ++k) {
-                    float w[8];
-                    load_param(c, p.pre_weight, 1.0f, k, w);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        v[k][j] *= inv;
-                        P0[k][j] = fmaf(e[k][j], v[k][j], P0[k][j]);
-                        P1[k][j] += e[k][j];
-                        e[k][j] *= w[j];
-                        d[0] = fmaf(e[k][j], v[k][j], d[0]);
-                        d[1] += e[k][j];
+                    for (int j = 0; j < 4; ++j) {
+                        const uint64_t xh = mul2(v[k][j], inv2);
+                        P0[k][j] = fma2(e[k][j], xh, P0[k][j]);
+                        if (BIAS) P1[k][j] = add2(P1[k][j], e[k][j]);
+                        g[k][j] = fma2(weigh(k, j, e[k][j]), inv2, g[k][j]);
+                        g[k][j] = fma2(xh, back, g[k][j]);
                     }
-                }
-                sum2(d);
-                const float dot = d[0] * p.inv_cols, mean = p.pre == NQ_NORM_LAYER ? d[1] * p.inv_cols : 0.0f;
-#pragma unroll
-                for (int k = 0; k < NV; ++k)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) g[k][j] = fmaf(inv, e[k][j] - mean - v[k][j] * dot, g[k][j]);
+                if (p.pre == NQ_NORM_LAYER) shift_row(c, g, -inv * mean_e);
             }
             if (p.dx) {
 #pragma unroll
                 for (int k = 0; k < NV; ++k) {
-                    float o[8];
+                    uint64_t o[4];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) o[j] = p.skip * g[k][j];
+                    for (int j = 0; j < 4; ++j) o[j] = mul2(g[k][j], both(p.skip));
                     store_piece(c, static_cast<TX*>(p.dx) + row * p.lddx, k, o);
                 }
             }
-            if (!p.y) continue;
-            load_row(c, static_cast<const TY*>(p.y) + row * p.ldy, v);
-            float inv = 1.0f;
-            if (p.post == NQ_NORM_LAYER) {
-                float m[1] = {0.0f};
+            if (p.y) {
+                get_y(p.y, p.ldy, at_y, t);                    // again: cheaper than holding it
+                if (p.post == NQ_NORM_LAYER) shift_row(c, t, -y_total * p.inv_cols);
+                const uint64_t inv2 = both(inv_y);
+                uint64_t ft = 0ull, fs = 0ull;
 #pragma unroll
-                for (int k = 0; k < NV; ++k)
+                for (int k = 0; k < NV; ++k) {
+                    uint64_t f[4];
+                    if (!HOLD) load_factor(k, f);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) m[0] += v[k][j];
-                sum1(m);
-                const float mean = m[0] * p.inv_cols;
+                    for (int j = 0; j < 4; ++j) {
+                        const uint64_t fj = HOLD ? factor[HOLD ? k : 0][j] : f[j];
+                        t[k][j] = mul2(t[k][j], inv2);
+                        A0[k][j] = fma2(g[k][j], t[k][j], A0[k][j]);
+                        if (BIAS) A1[k][j] = add2(A1[k][j], g[k][j]);
+                        g[k][j] = mul2(g[k][j], fj);
+                        ft = fma2(g[k][j], t[k][j], ft);
+                        fs = add2(fs, g[k][j]);
+                    }
+                }
+                float d[2] = {0.0f, 0.0f};
+                if (p.post != NQ_NORM_NONE) {
+                    d[0] = sum2(ft);
+                    d[1] = p.post == NQ_NORM_LAYER ? sum2(fs) : 0.0f;
+                    sum2v(d);
+                }
+                if (p.dy) {
+                    const uint64_t back = both(-(d[0] * p.inv_cols) * inv_y), less = both(-inv_y * (d[1] * p.inv_cols));
 #pragma unroll
-                for (int k = 0; k < NV; ++k)
+                    for (int k = 0; k < NV; ++k) {
+                        uint64_t o[4];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[k][j] = c.has(k, j) ? v[k][j] - mean : 0.0f;
-            }
-            if (p.post != NQ_NORM_NONE) {
-                float q[1] = {0.0f};
-#pragma unroll
-                for (int k = 0; k < NV; ++k)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) q[0] = fmaf(v[k][j], v[k][j], q[0]);
-                sum1(q);
-                inv = rsqrtf(fmaf(q[0], p.inv_cols, p.eps));
-            }
-            float d[2] = {0.0f, 0.0f};
-#pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                float w[8], gt[8];
-                load_param(c, p.post_weight, 1.0f, k, w);
-                load_param(c, gate, 1.0f, k, gt);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    if (!c.has(k, j)) g[k][j] = 0.0f;
-                    v[k][j] *= inv;
-                    A0[k][j] = fmaf(g[k][j], v[k][j], A0[k][j]);
-                    A1[k][j] += g[k][j];
-                    g[k][j] *= p.branch * gt[j] * w[j];
-                    d[0] = fmaf(g[k][j], v[k][j], d[0]);
-                    d[1] += g[k][j];
+                        for (int j = 0; j < 4; ++j) {
+                            o[j] = fma2(g[k][j], inv2, less);
+                            if (p.post != NQ_NORM_NONE) o[j] = fma2(t[k][j], back, o[j]);
+                        }
+                        store_piece(c, static_cast<TY*>(p.dy) + row * p.lddy, k, o);
+                    }
                 }
             }
-            if (!p.dy) continue;
-            float dot = 0.0f, mean = 0.0f;
-            if (p.post != NQ_NORM_NONE) {
-                sum2(d);
-                dot = d[0] * p.inv_cols;
-                if (p.post == NQ_NORM_LAYER) mean = d[1] * p.inv_cols;
-            }
-#pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                float o[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = inv * (g[k][j] - mean - v[k][j] * dot);
-                store_piece(c, static_cast<TY*>(p.dy) + row * p.lddy, k, o);
+            if (RING) {
+                // the last reads of the stage lie before the last join; without a post norm there is none after them
+                if (p.post == NQ_NORM_NONE) __syncthreads();
+                if (threadIdx.x == 0 && row + p.ring < row1) start(stage, row + p.ring);
+                if (++stage == p.ring) { stage = 0; parity ^= 1; }
             }
         }
         if (p.y) {
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                float w[8], b[8], gt[8];
+                uint64_t w[4], b[4], gt[4];
                 load_param(c, p.post_weight, 1.0f, k, w);
                 load_param(c, p.post_bias, 0.0f, k, b);
                 load_param(c, gate, 1.0f, k, gt);
@@ -475,28 +723,40 @@ __global__ void __launch_bounds__(512) block_norm_backward_kernel(const BackArgs
                 for (int j = 0; j < 8; ++j) {
                     if (!c.has(k, j)) continue;
                     const int col = c.col(k, j);
-                    if (p.gate_part) p.gate_part[item * p.cols + col] = p.branch * fmaf(w[j], A0[k][j], b[j] * A1[k][j]);
+                    const auto pick = [&](uint64_t v) {
+                        float lo, hi;
+                        unpack2(v, lo, hi);
+                        return j & 1 ? hi : lo;
+                    };
+                    const float a0 = pick(A0[k][j / 2]), a1 = pick(A1[k][j / 2]);
+                    if (p.gate_part) p.gate_part[item * p.cols + col] = p.branch * fmaf(pick(w[j / 2]), a0, pick(b[j / 2]) * a1);
                     if (p.post != NQ_NORM_NONE) {
                         float* at = p.part + 2 * plane + mine + col;
-                        const float s = p.branch * gt[j];
-                        at[0] = fmaf(s, A0[k][j], first ? 0.0f : at[0]);
-                        at[plane] = fmaf(s, A1[k][j], first ? 0.0f : at[plane]);
+                        const float s = p.branch * pick(gt[j / 2]);
+                        at[0] = fmaf(s, a0, first ? 0.0f : at[0]);
+                        if (BIAS) at[plane] = fmaf(s, a1, first ? 0.0f : at[plane]);
                     }
                 }
             }
             first = false;
         }
     }
-    if (p.pre != NQ_NORM_NONE) {
+    if (has_pre) {
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (c.has(k, j)) {
-                    p.part[mine + c.col(k, j)] = P0[k][j];
-                    p.part[plane + mine + c.col(k, j)] = P1[k][j];
+                    float lo, hi;
+                    unpack2(P0[k][j / 2], lo, hi);
+                    p.part[mine + c.col(k, j)] = j & 1 ? hi : lo;
+                    if (BIAS) {
+                        unpack2(P1[k][j / 2], lo, hi);
+                        p.part[plane + mine + c.col(k, j)] = j & 1 ? hi : lo;
+                    }
                 }
     }
+    if (RING) ring.leave();
 }
 
 // Joins the partial sums: plane z < 4 is one of the four vectors over all blocks, the others are the gate's groups.
@@ -570,24 +830,71 @@ int check_vector(const float* p, bool* vec) {
     return NQ_OK;
 }
 
-template <typename TX, typename TY>
-int launch_norm(const NormArgs& a, bool vec, cudaStream_t stream) {
-    const Shape sh = shape_for(a.cols);
-    const int teams = sh.threads == 32 ? 4 : 1, block = sh.threads * teams;
-    long long grid = (a.rows + teams - 1) / teams;
-    const long long most = (long long)sm_count() * (2048 / block);
-    if (grid > most) grid = most;
-    const auto run = [&](auto kernel) {
-        return launch_chained(kernel, (unsigned)grid, block, 0, 1, stream, a, sh.threads);
-    };
-    if (vec) {
-        if (sh.nv == 1) return run(block_norm_kernel<TX, TY, 1, true>);
-        if (sh.nv == 2) return run(block_norm_kernel<TX, TY, 2, true>);
-        return run(block_norm_kernel<TX, TY, 4, true>);
+// Blocks of `kernel` that fit on an SM, as far as registers and threads go.
+template <typename K>
+int blocks_per_sm(K kernel, int threads, int smem) {
+    int n = 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return 1;
     }
-    if (sh.nv == 1) return run(block_norm_kernel<TX, TY, 1, false>);
-    if (sh.nv == 2) return run(block_norm_kernel<TX, TY, 2, false>);
-    return run(block_norm_kernel<TX, TY, 4, false>);
+    return n < 1 ? 1 : n;
+}
+
+// The ring kernel's blocks per SM (as many as registers allow and still leave a stage count of three), its stages and
+// shared memory; false where a ring does not fit.
+struct RingPlan {
+    int blocks, stages;
+    size_t smem;
+};
+template <typename K>
+bool plan_ring(K kernel, int (&cache)[17][64], int threads, int stage_bytes, RingPlan& r) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
+    int& fit = cache[threads >> 5][dev];
+    if (fit == 0) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return false;
+        }
+        fit = blocks_per_sm(kernel, threads, 0);
+    }
+    r.blocks = fit;
+    while (r.blocks > 1 && ring_stages(stage_bytes, r.blocks) < 3) --r.blocks;
+    r.stages = ring_stages(stage_bytes, r.blocks);
+    r.smem = 128 + (size_t)r.stages * stage_bytes;
+    return r.stages >= 2;
+}
+
+template <typename TX, typename TY, int NV, bool BIAS>
+int launch_norm_nv(NormArgs& a, const Shape& sh, bool vec, cudaStream_t stream) {
+    const int teams = sh.threads == 32 ? 4 : 1, block = sh.threads * teams;
+    const int sms = sm_count();
+    long long grid = (a.rows + teams - 1) / teams;
+    // Many rows to a block, rows of whole 16-byte pieces: through the ring.  A warp to a row (short rows) has enough loads
+    // in flight by itself.
+    if (vec && sh.threads > 32) {
+        const auto kernel = block_norm_kernel<TX, TY, NV, true, true, BIAS>;
+        static int cache[17][64] = {{0}};
+        a.stage_bytes = a.cols * (int)(sizeof(TX) + (a.y ? sizeof(TY) : 0));
+        RingPlan r;
+        if (plan_ring(kernel, cache, block, a.stage_bytes, r) && a.rows >= 3ll * r.blocks * sms) {
+            a.ring = r.stages;
+            return launch_chained(kernel, (unsigned)(r.blocks * sms), block, r.smem, 1, stream, a, sh.threads);
+        }
+    }
+    const long long most = (long long)sms * (2048 / block);
+    if (grid > most) grid = most;
+    return vec ? launch_chained(block_norm_kernel<TX, TY, NV, true, false, BIAS>, (unsigned)grid, block, 0, 1, stream, a, sh.threads)
+               : launch_chained(block_norm_kernel<TX, TY, NV, false, false, BIAS>, (unsigned)grid, block, 0, 1, stream, a, sh.threads);
+}
+template <typename TX, typename TY>
+int launch_norm(NormArgs& a, bool vec, cudaStream_t stream) {
+    const Shape sh = shape_for(a.cols);
+    const bool bias = a.post_bias || a.pre_bias;
+    if (sh.nv == 1) return bias ? launch_norm_nv<TX, TY, 1, true>(a, sh, vec, stream) : launch_norm_nv<TX, TY, 1, false>(a, sh, vec, stream);
+    if (sh.nv == 2) return bias ? launch_norm_nv<TX, TY, 2, true>(a, sh, vec, stream) : launch_norm_nv<TX, TY, 2, false>(a, sh, vec, stream);
+    return launch_norm_nv<TX, TY, 4, true>(a, sh, vec, stream);
 }
 
 // Work items of the backward pass: each gate row's rows in equal chunks, about as many items as blocks are wanted.
@@ -614,19 +921,27 @@ BackPlan plan_backward(const nq_block_norm_desc* d, bool has_gate) {
     return p;
 }
 
-template <typename TX, typename TY>
-int launch_back(const BackArgs& a, const BackPlan& pl, bool vec, cudaStream_t stream) {
-    const auto run = [&](auto kernel) {
-        return launch_chained(kernel, (unsigned)pl.blocks, pl.shape.threads, 0, 1, stream, a);
-    };
-    if (vec) {
-        if (pl.shape.nv == 1) return run(block_norm_backward_kernel<TX, TY, 1, true>);
-        if (pl.shape.nv == 2) return run(block_norm_backward_kernel<TX, TY, 2, true>);
-        return run(block_norm_backward_kernel<TX, TY, 4, true>);
+template <typename TX, typename TY, int NV, bool BIAS>
+int launch_back_nv(BackArgs& a, const BackPlan& pl, bool vec, cudaStream_t stream) {
+    const int threads = pl.shape.threads;
+    if (vec && threads > 32 && a.rows >= 3ll * pl.blocks) {
+        const auto kernel = block_norm_backward_kernel<TX, TY, NV, true, true, BIAS>;
+        static int cache[17][64] = {{0}};
+        a.stage_bytes = a.cols * (int)((a.pre != NQ_NORM_NONE ? sizeof(TX) + sizeof(TY) : 0) + (a.dr ? sizeof(TX) : 0) + (a.y ? sizeof(TY) : 0));
+        RingPlan r;
+        if (plan_ring(kernel, cache, threads, a.stage_bytes, r)) {
+            a.ring = r.stages;
+            return launch_chained(kernel, (unsigned)pl.blocks, threads, r.smem, 1, stream, a);
+        }
     }
-    if (pl.shape.nv == 1) return run(block_norm_backward_kernel<TX, TY, 1, false>);
-    if (pl.shape.nv == 2) return run(block_norm_backward_kernel<TX, TY, 2, false>);
-    return run(block_norm_backward_kernel<TX, TY, 4, false>);
+    return vec ? launch_chained(block_norm_backward_kernel<TX, TY, NV, true, false, BIAS>, (unsigned)pl.blocks, threads, 0, 1, stream, a)
+               : launch_chained(block_norm_backward_kernel<TX, TY, NV, false, false, BIAS>, (unsigned)pl.blocks, threads, 0, 1, stream, a);
+}
+template <typename TX, typename TY>
+int launch_back(BackArgs& a, const BackPlan& pl, bool bias, bool vec, cudaStream_t stream) {
+    if (pl.shape.nv == 1) return bias ? launch_back_nv<TX, TY, 1, true>(a, pl, vec, stream) : launch_back_nv<TX, TY, 1, false>(a, pl, vec, stream);
+    if (pl.shape.nv == 2) return bias ? launch_back_nv<TX, TY, 2, true>(a, pl, vec, stream) : launch_back_nv<TX, TY, 2, false>(a, pl, vec, stream);
+    return launch_back_nv<TX, TY, 4, true>(a, pl, vec, stream);
 }
 
 }  // namespace
@@ -665,6 +980,9 @@ int nq_block_norm(const nq_block_norm_desc* d, const void* X, const void* Y, con
     a.skip = d->skip_scale; a.branch = d->branch_scale; a.eps = d->eps;
     a.inv_cols = 1.0f / (float)d->cols;
     a.inv_h_scale = d->h_dtype == NQ_I8 ? 1.0f / d->h_scale : 0.0f;
+    a.ring = 0; a.stage_bytes = 0;
+    a.status = status_word();
+    if (!a.status) return NQ_ERR_CUDA;
     const cudaStream_t s = (cudaStream_t)stream;
     if (d->x_dtype == NQ_BF16) return launch_norm<bf16, bf16>(a, vec, s);
     return d->y_dtype == NQ_BF16 ? launch_norm<float, bf16>(a, vec, s) : launch_norm<float, float>(a, vec, s);
@@ -719,9 +1037,13 @@ int nq_block_norm_backward(const nq_block_norm_desc* d, const void* R, const voi
     a.part = static_cast<float*>(workspace);
     float* gate_part = a.part + 4ll * pl.blocks * d->cols;
     a.gate_part = !dgate ? nullptr : pl.chunks == 1 ? dgate : gate_part;
+    a.ring = 0; a.stage_bytes = 0;
+    a.status = status_word();
+    if (!a.status) return NQ_ERR_CUDA;
+    const bool bias = post_bias || dpost_bias || dpre_bias;    // the sums of g and dh are wanted
     int st;
-    if (d->x_dtype == NQ_BF16) st = launch_back<bf16, bf16>(a, pl, vec, s);
-    else st = d->y_dtype == NQ_BF16 ? launch_back<float, bf16>(a, pl, vec, s) : launch_back<float, float>(a, pl, vec, s);
+    if (d->x_dtype == NQ_BF16) st = launch_back<bf16, bf16>(a, pl, bias, vec, s);
+    else st = d->y_dtype == NQ_BF16 ? launch_back<float, bf16>(a, pl, bias, vec, s) : launch_back<float, float>(a, pl, bias, vec, s);
     if (st != NQ_OK) return st;
     const bool join_gate = dgate && pl.chunks > 1;
     if (!join_gate && !dpost_weight && !dpost_bias && !dpre_weight && !dpre_bias) return NQ_OK;

@@ -18,6 +18,7 @@
 #include <type_traits>
 
 #include "../../include/nq.h"
+#include "nq_fp8.cuh"
 #include "nq_internal.cuh"
 #include "nq_sm100.cuh"
 
@@ -264,28 +265,6 @@ struct PairShape {
     static constexpr int kSmem = kPairStages * (kPairStageBytes + kScales * 4) + kPairWarps * kPieces * kOutPiece + 512 + 1024;
 };
 
-// Pairs of fp32 values in one 64-bit register, for the packed FMA (half the issue slots of scalar ones: 536 -> 518 us).
-__device__ __forceinline__ uint64_t pack2(uint32_t lo, uint32_t hi) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
-    return r;
-}
-__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 // one scale to shared memory, asynchronously; zero where there is none (`any`: some readable address)
 __device__ __forceinline__ void copy_scale(uint32_t dst, const float* src, bool present, const float* any) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(present ? src : any), "r"(present ? 4 : 0) : "memory");
