@@ -313,7 +313,7 @@ __device__ __forceinline__ float norm_factor(const Cols<NV, VEC>& c, Row<NV>& v,
 // scalar arithmetic, parameters read for each row and each row loaded when its turn came, 398 with the ring alone.
 // BIAS: one of the norms has a bias.
 template <typename TX, typename TY, int NV, bool VEC, bool RING, bool BIAS>
-__global__ void __launch_bounds__(512) block_norm_kernel(const NormArgs p, int threads) {
+__global__ void __launch_bounds__(NV == 1 ? 1024 : 512) block_norm_kernel(const NormArgs p, int threads) {
     constexpr bool HOLD = NV <= 2;
     __shared__ float box[2][32][1];
     extern __shared__ __align__(16) uint8_t ring_smem[];
@@ -800,10 +800,11 @@ inline uintptr_t at(const void* p) { return reinterpret_cast<uintptr_t>(p); }
 struct Shape {
     int threads, nv;
 };
-// Threads of a row: 8 * nv columns each.
-Shape shape_for(int64_t cols) {
+// Threads of a row: 8 * nv columns each.  One piece a thread as far as the block goes (1024 threads forward, 512 with the
+// backward pass's registers): more warps hide more of each other's joins.
+Shape shape_for(int64_t cols, int most) {
     Shape s;
-    s.nv = cols <= 512 * 8 ? 1 : cols <= 512 * 16 ? 2 : 4;
+    s.nv = cols <= most * 8 ? 1 : cols <= 512 * 16 ? 2 : 4;
     s.threads = (int)((cols + 8 * s.nv - 1) / (8 * s.nv));
     s.threads = (s.threads + 31) / 32 * 32;
     return s;
@@ -848,7 +849,7 @@ struct RingPlan {
     size_t smem;
 };
 template <typename K>
-bool plan_ring(K kernel, int (&cache)[17][64], int threads, int stage_bytes, RingPlan& r) {
+bool plan_ring(K kernel, int (&cache)[33][64], int threads, int stage_bytes, RingPlan& r) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
     int& fit = cache[threads >> 5][dev];
@@ -875,7 +876,7 @@ int launch_norm_nv(NormArgs& a, const Shape& sh, bool vec, cudaStream_t stream) 
     // in flight by itself.
     if (vec && sh.threads > 32) {
         const auto kernel = block_norm_kernel<TX, TY, NV, true, true, BIAS>;
-        static int cache[17][64] = {{0}};
+        static int cache[33][64] = {{0}};
         a.stage_bytes = a.cols * (int)(sizeof(TX) + (a.y ? sizeof(TY) : 0));
         RingPlan r;
         if (plan_ring(kernel, cache, block, a.stage_bytes, r) && a.rows >= 3ll * r.blocks * sms) {
@@ -890,7 +891,7 @@ int launch_norm_nv(NormArgs& a, const Shape& sh, bool vec, cudaStream_t stream) 
 }
 template <typename TX, typename TY>
 int launch_norm(NormArgs& a, bool vec, cudaStream_t stream) {
-    const Shape sh = shape_for(a.cols);
+    const Shape sh = shape_for(a.cols, 1024);
     const bool bias = a.post_bias || a.pre_bias;
     if (sh.nv == 1) return bias ? launch_norm_nv<TX, TY, 1, true>(a, sh, vec, stream) : launch_norm_nv<TX, TY, 1, false>(a, sh, vec, stream);
     if (sh.nv == 2) return bias ? launch_norm_nv<TX, TY, 2, true>(a, sh, vec, stream) : launch_norm_nv<TX, TY, 2, false>(a, sh, vec, stream);
@@ -905,7 +906,7 @@ struct BackPlan {
 };
 BackPlan plan_backward(const nq_block_norm_desc* d, bool has_gate) {
     BackPlan p;
-    p.shape = shape_for(d->cols);
+    p.shape = shape_for(d->cols, 512);
     p.group_rows = has_gate && d->rows_per_gate > 0 ? d->rows_per_gate : (d->rows > 0 ? d->rows : 1);
     if (p.group_rows > d->rows && d->rows > 0) p.group_rows = d->rows;
     p.groups = (d->rows + p.group_rows - 1) / p.group_rows;
@@ -926,7 +927,7 @@ int launch_back_nv(BackArgs& a, const BackPlan& pl, bool vec, cudaStream_t strea
     const int threads = pl.shape.threads;
     if (vec && threads > 32 && a.rows >= 3ll * pl.blocks) {
         const auto kernel = block_norm_backward_kernel<TX, TY, NV, true, true, BIAS>;
-        static int cache[17][64] = {{0}};
+        static int cache[33][64] = {{0}};
         a.stage_bytes = a.cols * (int)((a.pre != NQ_NORM_NONE ? sizeof(TX) + sizeof(TY) : 0) + (a.dr ? sizeof(TX) : 0) + (a.y ? sizeof(TY) : 0));
         RingPlan r;
         if (plan_ring(kernel, cache, threads, a.stage_bytes, r)) {

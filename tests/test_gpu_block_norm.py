@@ -354,3 +354,34 @@ def test_refusals():
               dict(r=x, dh=x, workspace=torch.zeros(16, dtype=torch.uint8, device="cuda"))]:
         with pytest.raises(nq.NqError):
             nq.nq_block_norm_backward(**k)
+
+
+# ------------------------------------------------------------------------------------- many rows to a thread block
+def test_many_rows_layouts():
+    """Enough rows that blocks work through many of them (rows ahead of the one in work are then in flight), of few, of
+    whole and of uneven numbers of pieces a thread; against the definition in 64 bits on the device."""
+    for rows, cols, tx, ty, kind, group in ((9001, 512, torch.bfloat16, torch.bfloat16, RMS, 0), (9001, 768, torch.float32, torch.bfloat16, LAYER, 197),
+                                            (5003, 1032, torch.float32, torch.float32, LAYER, 0), (3001, 4096, torch.bfloat16, torch.bfloat16, RMS, 1),
+                                            (2003, 4104, torch.float32, torch.bfloat16, LAYER, 500), (1501, 8192, torch.bfloat16, torch.bfloat16, RMS, 0),
+                                            (901, 12000, torch.bfloat16, torch.bfloat16, LAYER, 0), (5001, 264, torch.bfloat16, torch.bfloat16, LAYER, 3)):
+        st = make(rows, cols, tx, ty, gate=True, group=group, post=kind, pre=kind)
+        check(st)
+        if rows * cols <= 9001 * 768:
+            st["post"], st["post_weight"], st["post_bias"] = NONE, None, None
+            check(st, h_dtype=torch.float32)
+            check(make(rows, cols, tx, tx, post=NONE, pre=kind, block=False))
+
+
+@pytest.mark.parametrize("rows,cols,tx,ty,kind,group", [
+    (9001, 512, torch.bfloat16, torch.bfloat16, RMS, 0), (9001, 768, torch.float32, torch.bfloat16, LAYER, 197),
+    (4003, 1032, torch.float32, torch.float32, LAYER, 0), (3001, 4096, torch.bfloat16, torch.bfloat16, RMS, 1),
+    (1003, 4104, torch.float32, torch.bfloat16, LAYER, 500), (1501, 8192, torch.bfloat16, torch.bfloat16, RMS, 0),
+    (901, 12000, torch.bfloat16, torch.bfloat16, LAYER, 0)])
+def test_many_rows_backward(rows, cols, tx, ty, kind, group):
+    check_backward(*backward_case(rows, cols, tx, ty, post=kind, pre=kind, gate=True, group=group))
+
+
+def test_many_rows_backward_without_post_norm():
+    check_backward(*backward_case(6001, 768, torch.float32, torch.bfloat16, post=NONE, pre=LAYER, gate=True, group=100))
+    st, dr, dh = backward_case(6001, 768, torch.bfloat16, torch.bfloat16, post=NONE, pre=RMS, block=False)
+    check_backward(st, dr, dh)
