@@ -450,8 +450,8 @@ __global__ void __launch_bounds__(NV == 1 ? 1024 : 512) block_norm_kernel(const 
                 } else {
                     // groups of 128 columns: 16 lanes of 8 neighbours each, or all lanes of four elements each
                     float m[2], s[2], i[2];
-                    m[0] = max_abs(max_abs(e[0], e[1]), max_abs(e[2], e[3]));
-                    m[1] = max_abs(max_abs(e[4], e[5]), max_abs(e[6], e[7]));
+                    m[0] = max_abs(max_abs(e[0], e[1], e[2]), e[3]);
+                    m[1] = max_abs(max_abs(e[4], e[5], e[6]), e[7]);
                     if (VEC) {
                         m[0] = max_abs(m[0], m[1]);
 #pragma unroll
@@ -468,8 +468,8 @@ __global__ void __launch_bounds__(NV == 1 ? 1024 : 512) block_norm_kernel(const 
                         for (int n = 0; n < (VEC ? 1 : 2); ++n)
                             if (c.has(k, 4 * n)) p.hs[(long long)(c.col(k, 4 * n) >> 7) * p.ldhs + row] = s[n];
                     }
-                    store_bytes8(c, static_cast<uint8_t*>(p.h) + row * p.ldh, k, e4m3x4(e[0] * i[0], e[1] * i[0], e[2] * i[0], e[3] * i[0]),
-                                 e4m3x4(e[4] * i[1], e[5] * i[1], e[6] * i[1], e[7] * i[1]));
+                    store_bytes8(c, static_cast<uint8_t*>(p.h) + row * p.ldh, k, e4m3x4(mul2(h[0], both(i[0])), mul2(h[1], both(i[0]))),
+                                 e4m3x4(mul2(h[2], both(i[1])), mul2(h[3], both(i[1]))));
                 }
             }
         }

@@ -17,15 +17,16 @@ __device__ __forceinline__ void group_scale(uint32_t amax_bits, float& s, float&
     inv = __frcp_rn(s);
 }
 
-// Two values to e4m3, `lo` in the low byte: nearest even, larger magnitudes clamped to 448 (fl(x * inv) can pass 448
+// Four values to e4m3, `a` in the lowest byte: nearest even, larger magnitudes clamped to 448 (fl(x * inv) can pass 448
 // by a rounding), NaN kept.
-__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
-    uint16_t r;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-    return r;
-}
 __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
-    return e4m3x2(a, b) | (e4m3x2(c, d) << 16);
+    uint32_t r;
+    asm("{\n\t.reg .b16 lo, hi;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n\t"
+        "mov.b32 %0, {lo, hi};\n\t}"
+        : "=r"(r) : "f"(a), "f"(b), "f"(c), "f"(d));
+    return r;
 }
 
 // Pairs of fp32 values in one 64-bit register: one instruction works on both (half the issue slots of scalar ones; in the
@@ -58,10 +59,21 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-// the larger magnitude; a NaN wins
+__device__ __forceinline__ uint32_t e4m3x4(uint64_t ab, uint64_t cd) {
+    float a, b, c, d;
+    unpack2(ab, a, b);
+    unpack2(cd, c, d);
+    return e4m3x4(a, b, c, d);
+}
+// the largest magnitude; a NaN wins
 __device__ __forceinline__ float max_abs(float a, float b) {
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)));
+    return r;
+}
+__device__ __forceinline__ float max_abs(float a, float b, float c) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)), "f"(fabsf(c)));
     return r;
 }
 
