@@ -168,30 +168,32 @@ __device__ __forceinline__ void store_bytes8(const Cols<NV, VEC>& c, uint8_t* ro
     }
 }
 
-// A ring of rows in shared memory, filled by bulk copies that one thread starts several rows ahead, so that the bytes in
-// flight do not depend on how many threads wait for a row's sums.  Rows of up to four tensors lie side by side in a
-// stage.  A wait that gives up (see mbar_wait) lets its thread go on with what is there: every later wait then returns
-// at once, all threads reach all barriers, and the host finds the record.
+// A ring of rows in shared memory, filled by bulk copies that one thread of the block starts several rows ahead, so that the bytes in flight do not depend on how many threads wait for a row's
+// sums.  Rows of up to four tensors lie side by side in a stage.  A wait that gives up (see mbar_wait) lets its thread go
+// on with what is there: every later wait then returns at once, all threads reach all barriers, and the host finds the
+// record.
+constexpr int kRingHead = 128;             // barriers and the abort flag, before the stages
+constexpr int kMaxStages = 8;
 struct RowRing {
     uint8_t* stages;
     uint64_t* full;
     volatile int* abort_flag;
     unsigned int* status;
-    int count;                             // stages
     int stage_bytes;
+    bool first;                            // this thread starts the copies
+    // a __syncthreads has to follow
     __device__ __forceinline__ void init(uint8_t* smem, int n, int bytes, unsigned int* st) {
         full = reinterpret_cast<uint64_t*>(smem);
-        abort_flag = reinterpret_cast<volatile int*>(smem + 120);
-        stages = smem + 128;
-        count = n;
+        abort_flag = reinterpret_cast<volatile int*>(smem + kRingHead - 8);
+        stages = smem + kRingHead;
         stage_bytes = bytes;
         status = st;
-        if (threadIdx.x == 0) {
+        first = threadIdx.x == 0;
+        if (first) {
             for (int i = 0; i < n; ++i) sm100::mbar_init(sm100::smem_u32(&full[i]), 1);
             *abort_flag = 0;
             sm100::fence_barrier_init();
         }
-        __syncthreads();
     }
     __device__ __forceinline__ uint8_t* stage(int s) const { return stages + s * stage_bytes; }
     __device__ __forceinline__ void expect(int s) const { sm100::mbar_arrive_expect_tx(sm100::smem_u32(&full[s]), stage_bytes); }
@@ -202,32 +204,27 @@ struct RowRing {
         (void)sm100::mbar_wait(sm100::smem_u32(&full[s]), parity, abort_flag, status, 0x400u);
     }
     __device__ __forceinline__ void leave() const {
-        if (threadIdx.x == 0 && *abort_flag) {                 // let copies in flight land before shared memory is released
+        if (first && *abort_flag) {                            // let copies in flight land before shared memory is released
             const long long t0 = clock64();
             while (clock64() - t0 < (1ll << 22)) { }
         }
     }
 };
-// stages for a block of which `blocks` share an SM: about 200 KB in all, at least two rows
-int ring_stages(int stage_bytes, int blocks) {
-    int n = (200 * 1024 / blocks - 128) / stage_bytes;
-    return n > 8 ? 8 : n;
-}
 
-// Sums of N values over the threads of a row.  Up to one warp: shuffles alone.  More: the warps' sums through shared
-// memory; the two halves of `box` alternate, so that one barrier a call is enough.  Every thread adds in the same
-// order, so all hold the same bits.
+// Sums of N values over the threads of a row: a warp (shuffles alone) or the whole block (the warps' sums through shared
+// memory; the two halves of `box` alternate, so that one barrier a call is enough).  Every thread adds in the same order,
+// so all hold the same bits.
 template <int N>
 struct TeamSum {
     float (*box)[32][N];
-    int half, warps;
+    int threads, half;
     __device__ __forceinline__ void operator()(float (&v)[N]) {
 #pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
             for (int d = 16; d > 0; d >>= 1) v[n] += __shfl_xor_sync(0xffffffffu, v[n], d);
-        if (warps == 1) return;
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        if (threads == 32) return;
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = threads >> 5;
         if (lane == 0)
 #pragma unroll
             for (int n = 0; n < N; ++n) box[half][warp][n] = v[n];
@@ -304,22 +301,24 @@ __device__ __forceinline__ float norm_factor(const Cols<NV, VEC>& c, Row<NV>& v,
     return rsqrtf(fmaf(q[0], inv_cols, eps));
 }
 
-// A team of threads (a warp, or the whole block when a row needs more) walks its share of the rows, neighbours one after
-// the other, with the row in registers throughout: each tensor is touched once, so the pass should be bound by memory.
-// What it competes with is the instruction issue -- at HBM speed an SM has 38 issue slots for 32 columns of bf16 in,
-// bf16 and e4m3 out -- so arithmetic is on pairs, the parameters stay in registers (HOLD: rows of up to 8192; the post
-// norm's weight, the gate and the branch scale as one factor, which changes only with the gate's row), and the rows
-// come through a ring in shared memory (RING: blocks that work through many rows).  16384 x 8192, bf16 to e4m3: 475 us with
-// scalar arithmetic, parameters read for each row and each row loaded when its turn came, 398 with the ring alone.
+// A team of threads (a warp, or as many warps as a row needs) walks its share of the rows, neighbours one after the other,
+// with the row in registers throughout: each tensor is touched once, so the pass should be bound by memory.  What it
+// competes with is the instruction issue -- at HBM speed an SM has 38 issue slots for 32 columns of bf16 in, bf16 and e4m3
+// out -- and the latency of a row's two to four joins.  So arithmetic is on pairs, and where blocks work through many
+// rows (RING) they come through a ring in shared memory; the parameters stay in registers, the post norm's weight, the gate
+// and the branch scale as one factor that changes only with the gate's row.  Otherwise rows are loaded when their turn
+// comes.  16384 x 8192, bf16 to e4m3: 475 us without all that, 398 with a ring, 229 with all (4.1 TB/s).  Tried: parameters in
+// shared memory and several teams of 16 columns a thread in a block: no room for rows enough (514 us).
 // BIAS: one of the norms has a bias.
 template <typename TX, typename TY, int NV, bool VEC, bool RING, bool BIAS>
 __global__ void __launch_bounds__(NV == 1 ? 1024 : 512) block_norm_kernel(const NormArgs p, int threads) {
     constexpr bool HOLD = NV <= 2;
     __shared__ float box[2][32][1];
     extern __shared__ __align__(16) uint8_t ring_smem[];
-    const int team = threadIdx.x / threads, teams = blockDim.x / threads;
+    // several teams in a block only without RING, each a warp
+    const int team = RING ? 0 : threadIdx.x / threads, teams = RING ? 1 : blockDim.x / threads;
     const Cols<NV, VEC> c{(int)threadIdx.x - team * threads, threads, p.cols};
-    TeamSum<1> sum{box, 0, threads >> 5};
+    TeamSum<1> sum{box, threads, 0};
     RowRing ring;
     const int x_bytes = p.cols * (int)sizeof(TX), y_bytes = p.cols * (int)sizeof(TY);
     const auto start = [&](int s, long long row) {             // one thread
@@ -327,29 +326,29 @@ __global__ void __launch_bounds__(NV == 1 ? 1024 : 512) block_norm_kernel(const 
         ring.copy(s, 0, static_cast<const TX*>(p.x) + row * p.ldx, x_bytes);
         if (p.y) ring.copy(s, x_bytes, static_cast<const TY*>(p.y) + row * p.ldy, y_bytes);
     };
-    if (RING) ring.init(ring_smem, p.ring, p.stage_bytes, p.status);
+    if (RING) {
+        ring.init(ring_smem, p.ring, p.stage_bytes, p.status);
+        __syncthreads();
+    }
     start_next();
     wait_previous();
     const long long share = (long long)blockIdx.x * teams + team, shares = (long long)gridDim.x * teams;
     const long long row0 = p.rows * share / shares, row1 = p.rows * (share + 1) / shares;
-    if (RING && threadIdx.x == 0)
+    if (RING && ring.first)
         for (int s = 0; s < p.ring && row0 + s < row1; ++s) start(s, row0 + s);
 
-    // u enters r as fma(v, factor * inv, offset), h is fma(r^, weight, shift)
+    // u enters r as fma(u, factor * inv, offset), h is fma(r^, weight, shift)
     Row<HOLD ? NV : 1> factor, offset, weight, shift;
     const auto load_post = [&](const float* gate, int k, uint64_t (&f)[4], uint64_t (&o)[4]) {
-        uint64_t w[4], g[4];
-        load_param(c, p.post_weight, 1.0f, k, w);
+        uint64_t g[4];
+        load_param(c, p.post_weight, 1.0f, k, f);
         load_param(c, gate, 1.0f, k, g);
+        if (BIAS) load_param(c, p.post_bias, 0.0f, k, o);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             g[j] = mul2(g[j], both(p.branch));
-            f[j] = mul2(g[j], w[j]);
-        }
-        if (BIAS) {
-            load_param(c, p.post_bias, 0.0f, k, o);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) o[j] = mul2(o[j], g[j]);
+            f[j] = mul2(f[j], g[j]);
+            if (BIAS) o[j] = mul2(o[j], g[j]);
         }
     };
     const auto load_pre = [&](int k, uint64_t (&w)[4], uint64_t (&b)[4]) {
@@ -377,7 +376,7 @@ __global__ void __launch_bounds__(NV == 1 ? 1024 : 512) block_norm_kernel(const 
             }
         }
         const auto refill = [&]() {                            // after a barrier: every thread has taken its part
-            if (RING && threadIdx.x == 0 && row + p.ring < row1) start(stage, row + p.ring);
+            if (RING && ring.first && row + p.ring < row1) start(stage, row + p.ring);
         };
         Row<NV> r;
         if constexpr (RING) {
@@ -506,15 +505,14 @@ struct BackArgs {
 // block, A = sum g t inv_y, sum g over the rows of one work item, which lie under one gate row: from A follow both
 // dgate = branch * (w A0 + b A1) and the item's share branch * gate * A of the post norm's weight and bias.
 template <typename TX, typename TY, int NV, bool VEC, bool RING, bool BIAS>
-__global__ void __launch_bounds__(512) block_norm_backward_kernel(const BackArgs p) {
+__global__ void __launch_bounds__(512) block_norm_backward_kernel(const BackArgs p, int threads) {
     constexpr bool HOLD = NV <= 2;
     __shared__ float box3[2][32][3];
     __shared__ float box2[2][32][2];
     extern __shared__ __align__(16) uint8_t ring_smem[];
-    const int threads = blockDim.x;
     const Cols<NV, VEC> c{(int)threadIdx.x, threads, p.cols};
-    TeamSum<3> sum3{box3, 0, threads >> 5};
-    TeamSum<2> sum2v{box2, 0, threads >> 5};
+    TeamSum<3> sum3{box3, threads, 0};
+    TeamSum<2> sum2v{box2, threads, 0};
     const long long plane = (long long)gridDim.x * p.cols, mine = (long long)blockIdx.x * p.cols;
     const bool has_pre = p.pre != NQ_NORM_NONE;
 
@@ -531,7 +529,10 @@ __global__ void __launch_bounds__(512) block_norm_backward_kernel(const BackArgs
         if (p.dr) ring.copy(s, at_dr, static_cast<const TX*>(p.dr) + row * p.lddr, x_bytes);
         if (p.y) ring.copy(s, at_y, static_cast<const TY*>(p.y) + row * p.ldy, y_bytes);
     };
-    if (RING) ring.init(ring_smem, p.ring, p.stage_bytes, p.status);
+    if (RING) {
+        ring.init(ring_smem, p.ring, p.stage_bytes, p.status);
+        __syncthreads();
+    }
     start_next();
     wait_previous();
 
@@ -570,7 +571,7 @@ __global__ void __launch_bounds__(512) block_norm_backward_kernel(const BackArgs
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int j = 0; j < 4; ++j) A0[k][j] = A1[k][j] = 0ull;
-        if (RING && threadIdx.x == 0)                          // the ring is empty between items
+        if (RING && ring.first)                                // the ring is empty between items
             for (int i = 0, s = stage; i < p.ring && row0 + i < row1; ++i, s = s + 1 == p.ring ? 0 : s + 1) start(s, row0 + i);
 
         for (long long row = row0; row < row1; ++row) {
@@ -708,7 +709,7 @@ __global__ void __launch_bounds__(512) block_norm_backward_kernel(const BackArgs
             if (RING) {
                 // the last reads of the stage lie before the last join; without a post norm there is none after them
                 if (p.post == NQ_NORM_NONE) __syncthreads();
-                if (threadIdx.x == 0 && row + p.ring < row1) start(stage, row + p.ring);
+                if (ring.first && row + p.ring < row1) start(stage, row + p.ring);
                 if (++stage == p.ring) { stage = 0; parity ^= 1; }
             }
         }
@@ -797,17 +798,47 @@ __global__ void __launch_bounds__(kJoinCols* kJoinSlices) block_norm_join_kernel
 // ------------------------------------------------------------------------------------------------------------ host
 inline uintptr_t at(const void* p) { return reinterpret_cast<uintptr_t>(p); }
 
+// Threads of a row: 8 * nv columns each.
 struct Shape {
     int threads, nv;
 };
-// Threads of a row: 8 * nv columns each.  One piece a thread as far as the block goes (1024 threads forward, 512 with the
-// backward pass's registers): more warps hide more of each other's joins.
-Shape shape_for(int64_t cols, int most) {
-    Shape s;
-    s.nv = cols <= most * 8 ? 1 : cols <= 512 * 16 ? 2 : 4;
-    s.threads = (int)((cols + 8 * s.nv - 1) / (8 * s.nv));
-    s.threads = (s.threads + 31) / 32 * 32;
-    return s;
+Shape shape_of(int64_t cols, int nv) {
+    return Shape{(int)((cols + 256 * nv - 1) / (256 * nv)) * 32, nv};
+}
+// One piece a thread as far as the block goes: more warps hide more of a row's latencies.
+Shape wide_shape(int64_t cols, int most_threads) {
+    return shape_of(cols, cols <= (int64_t)most_threads * 8 ? 1 : cols <= 512 * 16 ? 2 : 4);
+}
+
+// Rows through shared memory: the blocks of an SM, the stages of each and its shared memory.
+struct RingPlan {
+    int stages, blocks;
+    size_t smem;
+};
+constexpr size_t kRingSmem = 216 * 1024;   // of an SM, for all its blocks
+// `fit`: blocks of an SM as far as registers go; fewer where they would leave less than three stages each
+bool plan_ring(int fit, int64_t stage_bytes, RingPlan& r) {
+    const auto stages = [&](int blocks) { return (int)((kRingSmem / blocks - 1024 - kRingHead) / stage_bytes); };
+    r.blocks = fit < 1 ? 1 : fit;
+    while (r.blocks > 1 && stages(r.blocks) < 3) --r.blocks;
+    r.stages = stages(r.blocks);
+    if (r.stages > kMaxStages) r.stages = kMaxStages;
+    r.smem = kRingHead + (size_t)r.stages * stage_bytes;
+    return r.stages >= 2;
+}
+// the opt-in to large shared memory, once per kernel and device
+template <typename K>
+bool allow_smem(K kernel, bool (&done)[64]) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
+    if (!done[dev]) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingSmem) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return false;
+        }
+        done[dev] = true;
+    }
+    return true;
 }
 
 bool desc_ok(const nq_block_norm_desc* d) {
@@ -831,86 +862,63 @@ int check_vector(const float* p, bool* vec) {
     return NQ_OK;
 }
 
-// Blocks of `kernel` that fit on an SM, as far as registers and threads go.
-template <typename K>
-int blocks_per_sm(K kernel, int threads, int smem) {
-    int n = 0;
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return 1;
-    }
-    return n < 1 ? 1 : n;
-}
-
-// The ring kernel's blocks per SM (as many as registers allow and still leave a stage count of three), its stages and
-// shared memory; false where a ring does not fit.
-struct RingPlan {
-    int blocks, stages;
-    size_t smem;
-};
-template <typename K>
-bool plan_ring(K kernel, int (&cache)[33][64], int threads, int stage_bytes, RingPlan& r) {
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
-    int& fit = cache[threads >> 5][dev];
-    if (fit == 0) {
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024) != cudaSuccess) {
-            (void)cudaGetLastError();
-            return false;
-        }
-        fit = blocks_per_sm(kernel, threads, 0);
-    }
-    r.blocks = fit;
-    while (r.blocks > 1 && ring_stages(stage_bytes, r.blocks) < 3) --r.blocks;
-    r.stages = ring_stages(stage_bytes, r.blocks);
-    r.smem = 128 + (size_t)r.stages * stage_bytes;
-    return r.stages >= 2;
-}
-
 template <typename TX, typename TY, int NV, bool BIAS>
-int launch_norm_nv(NormArgs& a, const Shape& sh, bool vec, cudaStream_t stream) {
+int launch_norm_ring(NormArgs& a, const Shape& sh, const RingPlan& r, cudaStream_t stream) {
+    const auto kernel = block_norm_kernel<TX, TY, NV, true, true, BIAS>;
+    static bool done[64] = {false};
+    if (!allow_smem(kernel, done)) return NQ_ERR_CUDA;
+    a.ring = r.stages;
+    return launch_chained(kernel, (unsigned)(r.blocks * sm_count()), (unsigned)sh.threads, r.smem, 1, stream, a, sh.threads);
+}
+template <typename TX, typename TY, int NV, bool BIAS>
+int launch_norm_plain(const NormArgs& a, const Shape& sh, bool vec, cudaStream_t stream) {
     const int teams = sh.threads == 32 ? 4 : 1, block = sh.threads * teams;
-    const int sms = sm_count();
     long long grid = (a.rows + teams - 1) / teams;
-    // Many rows to a block, rows of whole 16-byte pieces: through the ring.  A warp to a row (short rows) has enough loads
-    // in flight by itself.
-    if (vec && sh.threads > 32) {
-        const auto kernel = block_norm_kernel<TX, TY, NV, true, true, BIAS>;
-        static int cache[33][64] = {{0}};
-        a.stage_bytes = a.cols * (int)(sizeof(TX) + (a.y ? sizeof(TY) : 0));
-        RingPlan r;
-        if (plan_ring(kernel, cache, block, a.stage_bytes, r) && a.rows >= 3ll * r.blocks * sms) {
-            a.ring = r.stages;
-            return launch_chained(kernel, (unsigned)(r.blocks * sms), block, r.smem, 1, stream, a, sh.threads);
-        }
-    }
-    const long long most = (long long)sms * (2048 / block);
+    const long long most = (long long)sm_count() * (2048 / block);
     if (grid > most) grid = most;
     return vec ? launch_chained(block_norm_kernel<TX, TY, NV, true, false, BIAS>, (unsigned)grid, block, 0, 1, stream, a, sh.threads)
                : launch_chained(block_norm_kernel<TX, TY, NV, false, false, BIAS>, (unsigned)grid, block, 0, 1, stream, a, sh.threads);
 }
+template <typename TX, typename TY, bool BIAS>
+int launch_norm_bias(NormArgs& a, bool vec, cudaStream_t stream) {
+    const Shape wide = wide_shape(a.cols, 1024);
+    // The ring is worth filling from two rows a block on; a warp to a row (up to 256) has enough loads in flight by itself
+    // (50000 x 200: 27 us).
+    if (vec && wide.threads > 32) {
+        a.stage_bytes = a.cols * (int)(sizeof(TX) + (a.y ? sizeof(TY) : 0));
+        // both instantiations are bound to the registers that fill an SM: 64 at 1024 threads, 128 at 512
+        RingPlan r;
+        if (plan_ring((wide.nv == 1 ? 1024 : 512) / wide.threads, a.stage_bytes, r) && a.rows >= 2ll * r.blocks * sm_count())
+            return wide.nv == 1 ? launch_norm_ring<TX, TY, 1, BIAS>(a, wide, r, stream) : launch_norm_ring<TX, TY, 4, BIAS>(a, wide, r, stream);
+    }
+    return wide.nv == 1 ? launch_norm_plain<TX, TY, 1, BIAS>(a, wide, vec, stream) : launch_norm_plain<TX, TY, 4, BIAS>(a, wide, vec, stream);
+}
 template <typename TX, typename TY>
 int launch_norm(NormArgs& a, bool vec, cudaStream_t stream) {
-    const Shape sh = shape_for(a.cols, 1024);
-    const bool bias = a.post_bias || a.pre_bias;
-    if (sh.nv == 1) return bias ? launch_norm_nv<TX, TY, 1, true>(a, sh, vec, stream) : launch_norm_nv<TX, TY, 1, false>(a, sh, vec, stream);
-    if (sh.nv == 2) return bias ? launch_norm_nv<TX, TY, 2, true>(a, sh, vec, stream) : launch_norm_nv<TX, TY, 2, false>(a, sh, vec, stream);
-    return launch_norm_nv<TX, TY, 4, true>(a, sh, vec, stream);
+    return a.post_bias || a.pre_bias ? launch_norm_bias<TX, TY, true>(a, vec, stream) : launch_norm_bias<TX, TY, false>(a, vec, stream);
 }
 
 // Work items of the backward pass: each gate row's rows in equal chunks, about as many items as blocks are wanted.
 struct BackPlan {
     Shape shape;
+    RingPlan ring;
+    bool use_ring;
     long long group_rows, groups, chunk_rows, items;
-    int chunks, blocks;
+    int chunks, blocks, stage_bytes;
 };
+// The workspace is sized before the pointers are known, so the plan goes by the shape and types alone; rows that turn
+// out not to be aligned take the plain kernel with the same items and blocks.
 BackPlan plan_backward(const nq_block_norm_desc* d, bool has_gate) {
     BackPlan p;
-    p.shape = shape_for(d->cols, 512);
     p.group_rows = has_gate && d->rows_per_gate > 0 ? d->rows_per_gate : (d->rows > 0 ? d->rows : 1);
     if (p.group_rows > d->rows && d->rows > 0) p.group_rows = d->rows;
     p.groups = (d->rows + p.group_rows - 1) / p.group_rows;
-    const int per_sm = 1024 / p.shape.threads < 1 ? 1 : 1024 / p.shape.threads;
+    p.shape = wide_shape(d->cols, 512);
+    const int xs = d->x_dtype == NQ_BF16 ? 2 : 4, ys = d->y_dtype == NQ_BF16 ? 2 : 4;
+    p.stage_bytes = (int)d->cols * 2 * (xs + ys);              // at most: r, dr and y, dh
+    p.use_ring = d->cols % 8 == 0 && p.shape.threads > 32 && plan_ring(512 / p.shape.threads, p.stage_bytes, p.ring) &&
+                 d->rows >= 4ll * p.ring.blocks * sm_count();
+    const int per_sm = p.use_ring ? p.ring.blocks : 1024 / p.shape.threads;
     const long long want = (long long)sm_count() * per_sm;
     long long chunks = p.groups ? want / p.groups : 1;
     if (chunks < 1) chunks = 1;
@@ -923,26 +931,33 @@ BackPlan plan_backward(const nq_block_norm_desc* d, bool has_gate) {
 }
 
 template <typename TX, typename TY, int NV, bool BIAS>
-int launch_back_nv(BackArgs& a, const BackPlan& pl, bool vec, cudaStream_t stream) {
-    const int threads = pl.shape.threads;
-    if (vec && threads > 32 && a.rows >= 3ll * pl.blocks) {
-        const auto kernel = block_norm_backward_kernel<TX, TY, NV, true, true, BIAS>;
-        static int cache[33][64] = {{0}};
-        a.stage_bytes = a.cols * (int)((a.pre != NQ_NORM_NONE ? sizeof(TX) + sizeof(TY) : 0) + (a.dr ? sizeof(TX) : 0) + (a.y ? sizeof(TY) : 0));
-        RingPlan r;
-        if (plan_ring(kernel, cache, threads, a.stage_bytes, r)) {
-            a.ring = r.stages;
-            return launch_chained(kernel, (unsigned)pl.blocks, threads, r.smem, 1, stream, a);
-        }
+int launch_back_ring(BackArgs& a, const BackPlan& pl, cudaStream_t stream) {
+    const auto kernel = block_norm_backward_kernel<TX, TY, NV, true, true, BIAS>;
+    static bool done[64] = {false};
+    if (!allow_smem(kernel, done)) return NQ_ERR_CUDA;
+    a.ring = pl.ring.stages;
+    a.stage_bytes = a.cols * (int)((a.pre != NQ_NORM_NONE ? sizeof(TX) + sizeof(TY) : 0) + (a.dr ? sizeof(TX) : 0) + (a.y ? sizeof(TY) : 0));
+    return launch_chained(kernel, (unsigned)pl.blocks, (unsigned)pl.shape.threads, pl.ring.smem, 1, stream, a, pl.shape.threads);
+}
+template <typename TX, typename TY, int NV, bool BIAS>
+int launch_back_plain(const BackArgs& a, const BackPlan& pl, bool vec, cudaStream_t stream) {
+    return vec ? launch_chained(block_norm_backward_kernel<TX, TY, NV, true, false, BIAS>, (unsigned)pl.blocks, pl.shape.threads, 0, 1, stream, a, pl.shape.threads)
+               : launch_chained(block_norm_backward_kernel<TX, TY, NV, false, false, BIAS>, (unsigned)pl.blocks, pl.shape.threads, 0, 1, stream, a, pl.shape.threads);
+}
+template <typename TX, typename TY, bool BIAS>
+int launch_back_bias(BackArgs& a, const BackPlan& pl, bool vec, cudaStream_t stream) {
+    if (vec && pl.use_ring) {
+        if (pl.shape.nv == 1) return launch_back_ring<TX, TY, 1, BIAS>(a, pl, stream);
+        if (pl.shape.nv == 2) return launch_back_ring<TX, TY, 2, BIAS>(a, pl, stream);
+        return launch_back_ring<TX, TY, 4, BIAS>(a, pl, stream);
     }
-    return vec ? launch_chained(block_norm_backward_kernel<TX, TY, NV, true, false, BIAS>, (unsigned)pl.blocks, threads, 0, 1, stream, a)
-               : launch_chained(block_norm_backward_kernel<TX, TY, NV, false, false, BIAS>, (unsigned)pl.blocks, threads, 0, 1, stream, a);
+    if (pl.shape.nv == 1) return launch_back_plain<TX, TY, 1, BIAS>(a, pl, vec, stream);
+    if (pl.shape.nv == 2) return launch_back_plain<TX, TY, 2, BIAS>(a, pl, vec, stream);
+    return launch_back_plain<TX, TY, 4, BIAS>(a, pl, vec, stream);
 }
 template <typename TX, typename TY>
 int launch_back(BackArgs& a, const BackPlan& pl, bool bias, bool vec, cudaStream_t stream) {
-    if (pl.shape.nv == 1) return bias ? launch_back_nv<TX, TY, 1, true>(a, pl, vec, stream) : launch_back_nv<TX, TY, 1, false>(a, pl, vec, stream);
-    if (pl.shape.nv == 2) return bias ? launch_back_nv<TX, TY, 2, true>(a, pl, vec, stream) : launch_back_nv<TX, TY, 2, false>(a, pl, vec, stream);
-    return launch_back_nv<TX, TY, 4, true>(a, pl, vec, stream);
+    return bias ? launch_back_bias<TX, TY, true>(a, pl, vec, stream) : launch_back_bias<TX, TY, false>(a, pl, vec, stream);
 }
 
 }  // namespace
