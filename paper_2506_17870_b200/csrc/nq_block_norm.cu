@@ -108,14 +108,14 @@ __device__ __forceinline__ void load_param(const Cols<NV, VEC>& c, const float* 
     } else if (VEC) {
         uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
         if (c.has(k, 0)) {
-            a = __ldg(reinterpret_cast<const uint4*>(vec + c.col(k, 0)));
-            b = __ldg(reinterpret_cast<const uint4*>(vec + c.col(k, 0) + 4));
+            a = *reinterpret_cast<const uint4*>(vec + c.col(k, 0));
+            b = *reinterpret_cast<const uint4*>(vec + c.col(k, 0) + 4);
         }
         spread(a, b, v);
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            v[j] = pack2f(c.has(k, 2 * j) ? __ldg(vec + c.col(k, 2 * j)) : 0.0f, c.has(k, 2 * j + 1) ? __ldg(vec + c.col(k, 2 * j + 1)) : 0.0f);
+            v[j] = pack2f(c.has(k, 2 * j) ? vec[c.col(k, 2 * j)] : 0.0f, c.has(k, 2 * j + 1) ? vec[c.col(k, 2 * j + 1)] : 0.0f);
     }
 }
 
@@ -769,7 +769,7 @@ struct JoinArgs {
     int cols, col_blocks, blocks, chunks;
     long long groups;
 };
-constexpr int kJoinCols = 32, kJoinSlices = 8;
+constexpr int kJoinCols = 32, kJoinSlices = 16;
 __global__ void __launch_bounds__(kJoinCols* kJoinSlices) block_norm_join_kernel(const JoinArgs p) {
     __shared__ float box[kJoinSlices][kJoinCols];
     const int lane = threadIdx.x % kJoinCols, slice = threadIdx.x / kJoinCols;
@@ -783,6 +783,7 @@ __global__ void __launch_bounds__(kJoinCols* kJoinSlices) block_norm_join_kernel
         const float* in = z < 4 ? p.part + z * p.blocks * (long long)p.cols : p.gate_part + (z - 4) * p.chunks * (long long)p.cols;
         float s = 0.0f;
         if (col < p.cols)
+#pragma unroll 8
             for (int i = slice; i < n; i += kJoinSlices) s += in[(long long)i * p.cols + col];
         box[slice][lane] = s;
         __syncthreads();

@@ -47,7 +47,7 @@ struct Fp8Args {
 };
 
 __device__ __forceinline__ void store_out(const Fp8Args& p, long long m, int n, float v) {
-    if (p.bias) v += __ldg(p.bias + n);
+    if (p.bias) v += p.bias[n];
     const long long at = m * p.ldy + n;
     if (p.y_is_bf16) {
         static_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(v);
@@ -159,11 +159,11 @@ fp8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         const long long sb_row = (n0 + nl < p.N) ? (long long)((n0 + nl) >> p.b_shift) : -1;
         float next_b = 0.0f, next_a[PER];
         const auto fetch = [&](int kb) {
-            next_b = sb_row >= 0 ? __ldg(p.sb + (long long)kb * p.ldsb + sb_row) : 0.0f;
+            next_b = sb_row >= 0 ? p.sb[(long long)kb * p.ldsb + sb_row] : 0.0f;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
                 const int c = i * 32 + lane;
-                next_a[i] = (c < NT && m0 + c < p.M) ? __ldg(p.sa + (long long)kb * p.ldsa + m0 + c) : 0.0f;
+                next_a[i] = (c < NT && m0 + c < p.M) ? p.sa[(long long)kb * p.ldsa + m0 + c] : 0.0f;
             }
         };
         if (kb0 < kb1) fetch(kb0);
@@ -459,10 +459,10 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         const float *from_a = nullptr, *from_b = nullptr;
         float next_a = 0.0f, next_b = 1.0f;
         const auto fetch = [&]() {
-            next_a = __ldg(from_a);
+            next_a = *from_a;
             from_a += p.ldsa;
             if (!ROW_SCALES) {
-                next_b = __ldg(from_b);
+                next_b = *from_b;
                 from_b += p.ldsb;
             }
         };
@@ -548,12 +548,12 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 for (int i = 0; i < 128; i += 4) {
                     float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                     if (whole) {
-                        v = __ldg(reinterpret_cast<const float4*>(p.bias + col + i));
+                        v = *reinterpret_cast<const float4*>(p.bias + col + i);
                     } else {
-                        if (col + i < p.N) v.x = __ldg(p.bias + col + i);
-                        if (col + i + 1 < p.N) v.y = __ldg(p.bias + col + i + 1);
-                        if (col + i + 2 < p.N) v.z = __ldg(p.bias + col + i + 2);
-                        if (col + i + 3 < p.N) v.w = __ldg(p.bias + col + i + 3);
+                        if (col + i < p.N) v.x = p.bias[col + i];
+                        if (col + i + 1 < p.N) v.y = p.bias[col + i + 1];
+                        if (col + i + 2 < p.N) v.z = p.bias[col + i + 2];
+                        if (col + i + 3 < p.N) v.w = p.bias[col + i + 3];
                     }
                     acc[i / 2] = add2(acc[i / 2], pack2(__float_as_uint(v.x), __float_as_uint(v.y)));
                     acc[i / 2 + 1] = add2(acc[i / 2 + 1], pack2(__float_as_uint(v.z), __float_as_uint(v.w)));

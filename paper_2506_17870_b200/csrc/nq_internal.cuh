@@ -10,7 +10,8 @@ namespace nq {
 // Programmatic dependent launch: a kernel started with launch_chained() may begin while the one before it in the stream
 // still runs, provided that one called start_next(); it must call wait_previous() before it touches global memory
 // (which waits until everything before it in the stream is complete and visible).  What overlaps is the launch itself and a
-// block's set-up: for a call of a few microseconds that is most of its time.
+// block's set-up: for a call of a few microseconds that is most of its time.  Such kernels read global memory by ordinary
+// loads, not through __ldg: the compiler may move a load of memory that never changes across the wait.
 __device__ __forceinline__ void wait_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void start_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
