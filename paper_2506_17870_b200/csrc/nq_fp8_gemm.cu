@@ -262,7 +262,7 @@ template <bool ROW_SCALES>
 struct PairShape {
     static constexpr int kPieces = 4;                                                    // output pieces a warp fills before it hands them over
     static constexpr int kScales = ROW_SCALES ? 256 : 0;                                 // of a group: rows of B
-    static constexpr int kSmem = kPairStages * (kPairStageBytes + kScales * 4) + kPairWarps * kPieces * kOutPiece + 512 + 1024;
+    static constexpr int kSmem = kPairStages * (kPairStageBytes + kScales * 4) + kPairWarps * (kPieces * kOutPiece + 128 * 4) + 512 + 1024;
 };
 
 // one scale to shared memory, asynchronously; zero where there is none (`any`: some readable address)
@@ -342,7 +342,8 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     uint8_t* sB = sA + STAGES * 128 * kGroup;
     uint8_t* sOut = sB + STAGES * 128 * kGroup;
     float* sScale = reinterpret_cast<float*>(sOut + kPairWarps * S::kPieces * kOutPiece);
-    uint64_t* full = reinterpret_cast<uint64_t*>(sScale + STAGES * S::kScales);
+    float* sBias = sScale + STAGES * S::kScales;              // [8 warps][128]
+    uint64_t* full = reinterpret_cast<uint64_t*>(sBias + kPairWarps * 128);
     uint64_t* done = full + STAGES;
     uint64_t* sfull = done + 2 * STAGES;
     uint64_t* sempty = sfull + STAGES;
@@ -455,6 +456,7 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         const int quarter = warp & 3, h = (warp - 4) >> 2;     // 32 rows of one half
         const uint32_t tmem_mine = tmem_base + h * 128 + ((uint32_t)(quarter * 32) << 16);
         uint8_t* pieces = sOut + (warp - 4) * S::kPieces * kOutPiece;
+        float* my_bias = sBias + (warp - 4) * 128;
         // this row's scales and (blocks) the column block's, one group ahead
         const float *from_a = nullptr, *from_b = nullptr;
         float next_a = 0.0f, next_b = 1.0f;
@@ -481,6 +483,12 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             fetch_first(mt, nt);
         }
         for (int tile = pair; ok && tile < num_tiles; tile += num_pairs) {
+            float bias[4];                                     // four of the tile's 128 columns; they are needed at its end
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int c = nt * 256 + h * 128 + 4 * lane + i;
+                bias[i] = p.bias && c < p.N ? p.bias[c] : 0.0f;
+            }
             uint64_t acc[64];                                  // pairs of neighbouring columns
 #pragma unroll
             for (int i = 0; i < 64; ++i) acc[i] = 0ull;
@@ -543,20 +551,14 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             }
             if (row0 >= p.M || col >= p.N) continue;
             if (p.bias) {
-                const bool whole = (reinterpret_cast<uintptr_t>(p.bias) & 15) == 0 && col + 128 <= p.N;
+                __syncwarp();                                  // the last tile's have been read
+                *reinterpret_cast<float4*>(my_bias + 4 * lane) = make_float4(bias[0], bias[1], bias[2], bias[3]);
+                __syncwarp();
 #pragma unroll
-                for (int i = 0; i < 128; i += 4) {
-                    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    if (whole) {
-                        v = *reinterpret_cast<const float4*>(p.bias + col + i);
-                    } else {
-                        if (col + i < p.N) v.x = p.bias[col + i];
-                        if (col + i + 1 < p.N) v.y = p.bias[col + i + 1];
-                        if (col + i + 2 < p.N) v.z = p.bias[col + i + 2];
-                        if (col + i + 3 < p.N) v.w = p.bias[col + i + 3];
-                    }
-                    acc[i / 2] = add2(acc[i / 2], pack2(__float_as_uint(v.x), __float_as_uint(v.y)));
-                    acc[i / 2 + 1] = add2(acc[i / 2 + 1], pack2(__float_as_uint(v.z), __float_as_uint(v.w)));
+                for (int i = 0; i < 64; i += 2) {
+                    const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(my_bias + 2 * i);
+                    acc[i] = add2(acc[i], v.x);
+                    acc[i + 1] = add2(acc[i + 1], v.y);
                 }
             }
             if (p.y_tma) {                                     // the pieces' last stores have read them
