@@ -57,13 +57,19 @@ __device__ __forceinline__ void store_out(const Fp8Args& p, long long m, int n, 
     }
 }
 
+__device__ __forceinline__ float half_of(uint64_t v, int which) {
+    float lo, hi;
+    unpack2(v, lo, hi);
+    return which ? hi : lo;
+}
+
 // ------------------------------------------------------------------------------------------------------ tile kernel
 constexpr int kTileThreads = 192;        // warp 0 TMA, warp 1 MMA and TMEM, warps 2-5 promotion (a 32-lane quarter each)
 template <int NT>
 struct TileShape {
     static constexpr int kStageBytes = (128 + NT) * kGroup;
-    static constexpr int kStages = NT <= 16 ? 6 : NT <= 32 ? 5 : NT <= 64 ? 4 : 3;      // two CTAs an SM: about 100 KB each
-    static constexpr int kBufs = NT <= 64 ? 4 : 2;                                      // D buffers: 64 .. 256 TMEM columns
+    static constexpr int kStages = NT == 16 ? 6 : NT == 32 ? 5 : 4;                     // two CTAs an SM: about 100 KB each
+    static constexpr int kBufs = 4;                                                     // D buffers: 64 .. 256 TMEM columns
     static constexpr int kSmem = kStages * kStageBytes + 4 * 2 * NT * 4 + 512 + 1024;
     static_assert(NT * 128 * 4 <= kStages * kStageBytes, "the joined tile lies where the stages were");
 };
@@ -112,9 +118,9 @@ fp8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     start_next();
     wait_previous();
 
-    float acc[NT];
+    uint64_t acc[NT / 2];                                      // pairs of neighbouring rows of A
 #pragma unroll
-    for (int c = 0; c < NT; ++c) acc[c] = 0.0f;
+    for (int c = 0; c < NT / 2; ++c) acc[c] = 0ull;
     const int quarter = warp & 3;
     const int nl = quarter * 32 + lane;                        // this lane's row of the B tile (promotion warps)
 
@@ -171,7 +177,7 @@ fp8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         for (int kb = kb0; kb < kb1; ++kb, ++it) {
             const uint32_t b = it % BUFS, buse = it / BUFS;
             float* sc = mine + (it & 1) * NT;
-            const float scale_b = next_b;
+            const uint64_t scale_b = both(next_b);
 #pragma unroll
             for (int i = 0; i < PER; ++i)
                 if (i * 32 + lane < NT) sc[i * 32 + lane] = next_a[i];
@@ -181,30 +187,40 @@ fp8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc_fence_after_sync();
+            const uint32_t from = tmem_base + b * NT + ((uint32_t)(quarter * 32) << 16);
+            constexpr int PIECES = NT / 16;
+            uint32_t d[2][16];
+            tmem_ld_32x16(from, d[0]);
+            if (PIECES > 1) tmem_ld_32x16(from + 16, d[1]);
 #pragma unroll
-            for (int c0 = 0; c0 < NT; c0 += 16) {
-                uint32_t d[16];
-                tmem_ld_32x16(tmem_base + b * NT + c0 + ((uint32_t)(quarter * 32) << 16), d);
-                tmem_ld_wait();
-                if (c0 + 16 == NT) {
-                    tc_fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_u32(&tempty[b]));
+            for (int c = 0; c < PIECES; ++c) {                 // two loads in flight, waited for in pairs
+                if ((c & 1) == 0) {
+                    tmem_ld_wait();
+                    if (c + 2 >= PIECES) {                     // all have arrived
+                        tc_fence_before_sync();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&tempty[b]));
+                    }
                 }
 #pragma unroll
-                for (int j = 0; j < 16; ++j) acc[c0 + j] = fmaf(__uint_as_float(d[j]) * scale_b, sc[c0 + j], acc[c0 + j]);
+                for (int j = 0; j < 8; j += 2) {
+                    const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(sc + c * 16 + 2 * j);
+                    acc[c * 8 + j] = fma2(mul2(pack2(d[c & 1][2 * j], d[c & 1][2 * j + 1]), w.x), scale_b, acc[c * 8 + j]);
+                    acc[c * 8 + j + 1] = fma2(mul2(pack2(d[c & 1][2 * j + 2], d[c & 1][2 * j + 3]), w.y), scale_b, acc[c * 8 + j + 1]);
+                }
+                if (c + 2 < PIECES) tmem_ld_32x16(from + (c + 2) * 16, d[c & 1]);
             }
         }
         if (p.split == 1) {
             if (n0 + nl < p.N)
 #pragma unroll
                 for (int c = 0; c < NT; ++c)
-                    if (m0 + c < p.M) store_out(p, m0 + c, n0 + nl, acc[c]);
+                    if (m0 + c < p.M) store_out(p, m0 + c, n0 + nl, half_of(acc[c / 2], c & 1));
         } else {
             // every stage has been read by then: the last group's MMAs are complete, and so are all before them
             float* red = reinterpret_cast<float*>(smem);
 #pragma unroll
-            for (int c = 0; c < NT; ++c) red[c * 128 + nl] = acc[c];
+            for (int c = 0; c < NT; ++c) red[c * 128 + nl] = half_of(acc[c / 2], c & 1);
         }
     }
 
@@ -212,18 +228,51 @@ fp8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     if (p.split > 1) {
         cluster_sync_all();
         if (warp >= 2) {
-            // CTA `rank` joins its share of the tile's rows of A, adding the ranks in order
-            const int c0 = NT * rank / p.split, c1 = NT * (rank + 1) / p.split;
-            const uint32_t red = smem_u32(smem) + nl * 4;
-            for (int c = c0; c < c1; ++c) {
-                if (m0 + c >= p.M) break;
-                float v = 0.0f;
+            // CTA `rank` joins its share of the tile's rows of A, adding the ranks in order; a lane takes four neighbouring
+            // columns, and four rows' loads from all ranks are on their way at once (a load from another CTA takes about a
+            // microsecond: joined value by value, 37 tokens took 15.9 us)
+            const int c0 = NT * rank / p.split, c1 = min(NT * (rank + 1) / p.split, p.M - m0);
+            const uint32_t red = smem_u32(smem) + lane * 16;
+            const int n = n0 + lane * 4;
+            const bool vec = (p.ldy & 3) == 0 && (reinterpret_cast<uintptr_t>(p.y) & 15) == 0 && n + 4 <= p.N && !p.accumulate;
+            float4 bias = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (p.bias && vec) bias = make_float4(p.bias[n], p.bias[n + 1], p.bias[n + 2], p.bias[n + 3]);
+            for (int first = c0 + warp - 2; first < c1; first += 16) {
+                float4 v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                 for (int r = 0; r < p.split; ++r) {
-                    float t;
-                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(t) : "r"(map_to_cta(red + c * 512, r)) : "memory");
-                    v += t;
+                    const uint32_t from = map_to_cta(red, r);
+                    float4 t[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (first + 4 * i < c1)
+                            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(t[i].x), "=f"(t[i].y), "=f"(t[i].z), "=f"(t[i].w)
+                                         : "r"(from + (first + 4 * i) * 512));
+                        else
+                            t[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) { v[i].x += t[i].x; v[i].y += t[i].y; v[i].z += t[i].z; v[i].w += t[i].w; }
                 }
-                if (n0 + nl < p.N) store_out(p, m0 + c, n0 + nl, v);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int c = first + 4 * i;
+                    if (c >= c1) break;
+                    const long long m = m0 + c;
+                    if (vec && p.y_is_bf16) {
+                        const __nv_bfloat162 lo = __floats2bfloat162_rn(v[i].x + bias.x, v[i].y + bias.y), hi = __floats2bfloat162_rn(v[i].z + bias.z, v[i].w + bias.w);
+                        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.y) + m * p.ldy + n) =
+                            make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+                    } else if (vec) {
+                        *reinterpret_cast<float4*>(static_cast<float*>(p.y) + m * p.ldy + n) =
+                            make_float4(v[i].x + bias.x, v[i].y + bias.y, v[i].z + bias.z, v[i].w + bias.w);
+                    } else {
+                        if (n < p.N) store_out(p, m, n, v[i].x);
+                        if (n + 1 < p.N) store_out(p, m, n + 1, v[i].y);
+                        if (n + 2 < p.N) store_out(p, m, n + 2, v[i].z);
+                        if (n + 3 < p.N) store_out(p, m, n + 3, v[i].w);
+                    }
+                }
             }
         }
         __syncwarp();
@@ -619,14 +668,19 @@ __global__ void fp8_empty_kernel(const Fp8Args p) {
 }
 
 // ------------------------------------------------------------------------------------------------------------ host
+// How K is split: while that still adds CTAs that run at once (two fit on an SM), a CTA keeping two groups at least.
+int tile_split(long long tiles, int k_blocks) {
+    int split = 1;
+    while (split < 8 && tiles * split * 2 <= 2 * sm_count() && k_blocks >= 4 * split) split *= 2;
+    return split;
+}
+
 template <int NT>
 int launch_tile(const CUtensorMap& tmB, const void* A, int64_t lda, int64_t K, Fp8Args& a, cudaStream_t stream) {
     a.m_tiles = (a.M + NT - 1) / NT;
     a.n_tiles = (a.N + 127) / 128;
     const long long tiles = (long long)a.m_tiles * a.n_tiles;
-    // Split K while that still adds CTAs that run at once (two fit on an SM); a CTA keeps two groups at least.
-    int split = 1;
-    while (split < 8 && tiles * split * 2 <= 2 * sm_count() && a.k_blocks >= 4 * split) split *= 2;
+    const int split = tile_split(tiles, a.k_blocks);
     a.split = split;
     if (tiles * split > 0x7fffffffll) return NQ_ERR_UNSUPPORTED;
     CUtensorMap tmA;
@@ -666,7 +720,22 @@ int launch_pair(const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensorMa
 int run_fp8_gemm(const void* A, int64_t lda, const void* B, int64_t ldb, int64_t K, Fp8Args& a, cudaStream_t stream) {
     CUtensorMap tmB;
     const long long pair_tiles = (long long)((a.M + 255) / 256) * ((a.N + 255) / 256);
-    if (a.M > 128 && a.N > 128 && pair_tiles * 2 > sm_count() / 2) {
+    // Which kernel: by the time each would take in microseconds, (rounds of tiles over the machine) x (groups of K a tile and
+    // round x t + c), with t and c fitted to measurements from 128 x 128 to 8192 x 8192 outputs and K of 768 to 16384 that they
+    // meet within a sixth:
+    //   pair      t 0.55 (1.0 with row scales), c 1.5, and 5 once     512 x 4096 x 4096: 22.3,  4096^3: 78,  300 x 300 x 16384: 137
+    //   64 rows   t 0.55, c 7.4                                                         26.6          177                     15.9
+    //   32 rows   t 0.465, c 4.8                                                        39.7          274                     12.3
+    // (128 rows a tile spill their sums: 33 us for 128 x 8192 x 4096 against 16.5 with 64.)
+    const auto tile_cost = [&](int nt, double t, double c) {
+        const long long tiles = (long long)((a.M + nt - 1) / nt) * ((a.N + 127) / 128);
+        const int split = tile_split(tiles, a.k_blocks);
+        return (double)((tiles * split + 2 * sm_count() - 1) / (2 * sm_count())) * (((a.k_blocks + split - 1) / split) * t + c);
+    };
+    const double cost32 = tile_cost(32, 0.465, 4.8), cost64 = tile_cost(64, 0.55, 7.4);
+    const long long pairs = sm_count() / 2;
+    const double cost_pair = 5.0 + (double)((pair_tiles + pairs - 1) / pairs) * (a.k_blocks * (a.b_shift ? 0.55 : 1.0) + 1.5);
+    if (a.M > 64 && cost_pair <= cost32 && cost_pair <= cost64) {
         if (pair_tiles > 0x3fffffffll) return NQ_ERR_UNSUPPORTED;
         CUtensorMap tmA, tmY;
         int st = encode_tensor_map_2d(&tmA, A, (uint64_t)K, (uint64_t)a.M, (uint64_t)lda, kGroup, 128, 128);
@@ -687,9 +756,7 @@ int run_fp8_gemm(const void* A, int64_t lda, const void* B, int64_t ldb, int64_t
     const int st = encode_tensor_map_2d(&tmB, B, (uint64_t)K, (uint64_t)a.N, (uint64_t)ldb, kGroup, 128, 128);
     if (st != NQ_OK) return st;
     if (a.M <= 16) return launch_tile<16>(tmB, A, lda, K, a, stream);
-    if (a.M <= 32) return launch_tile<32>(tmB, A, lda, K, a, stream);
-    if (a.M <= 64) return launch_tile<64>(tmB, A, lda, K, a, stream);
-    return launch_tile<128>(tmB, A, lda, K, a, stream);
+    return a.M <= 32 || cost32 < cost64 ? launch_tile<32>(tmB, A, lda, K, a, stream) : launch_tile<64>(tmB, A, lda, K, a, stream);
 }
 
 }  // namespace
