@@ -1,0 +1,200 @@
+"""The linear half of a transformer in e4m3, trained and served: the block-scaled product, its quantiser and the block
+norm, strung together as a user would.  Every step of their arithmetic runs in the kernels behind ``include/nq.h``; torch
+supplies the memory, the autograd graph, the activation between the two linears and the optimiser.
+
+  training   block norm (bf16 out) -> quantised both ways -> product; backward: gradient quantised both ways -> input
+             gradient (blocks of W^T), weight gradient (both transposes, fp32), block norm backward
+  serving    block norm straight to e4m3 -> product -> activation -> quantised -> product, for one token or many
+  INT8       block norm straight to INT8 (static scale) -> nq_gemm_nested on the two stored parts of a nested weight
+
+``python -m paper_2506_17870_b200.fp8_block`` trains a small stack on synthetic data and serves it.
+"""
+from __future__ import annotations
+
+from typing import List, NamedTuple, Optional, Tuple
+
+import torch
+
+from . import binding as nq
+
+
+class Fp8Weight(NamedTuple):
+    """A weight [out, in] in blocks of 128 x 128, as it is and transposed; laid out once, kept while it does not change."""
+    q: torch.Tensor
+    s: torch.Tensor
+    qt: torch.Tensor
+    st: torch.Tensor
+
+
+def quantize_weight(w: torch.Tensor) -> Fp8Weight:
+    return Fp8Weight(*nq.nq_fp8_quantize(w, block_rows=128, transposed=True))
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias):
+        q, s, qt, st = nq.nq_fp8_quantize(x, transposed=True)
+        w = quantize_weight(weight)
+        ctx.save_for_backward(qt, st, w.qt, w.st)
+        ctx.has_bias = bias is not None
+        return nq.nq_fp8_gemm(q, s, w.q, w.s, bias=bias, y_dtype=x.dtype)
+
+    @staticmethod
+    def backward(ctx, dy):
+        xt, sxt, wt, swt = ctx.saved_tensors
+        d, sd, dt, sdt = nq.nq_fp8_quantize(dy.contiguous(), transposed=True)
+        dx = nq.nq_fp8_gemm(d, sd, wt, swt, y_dtype=dy.dtype)
+        dw = nq.nq_fp8_gemm(dt, sdt, xt, sxt, b_block_rows=1, y_dtype=torch.float32)
+        return dx, dw, dy.float().sum(0) if ctx.has_bias else None
+
+
+def fp8_linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """x [tokens, in] fp32 or bf16, weight [out, in] fp32 -> x W^T + bias in x's type, with gradients."""
+    return _Linear.apply(x, weight, bias)
+
+
+class _BlockNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, y, post_weight, gate, pre_weight, how):
+        r, h, _ = nq.nq_block_norm(x, y, post_weight=post_weight, gate=gate, pre_weight=pre_weight, want_r=True, **how)
+        ctx.how = how
+        ctx.save_for_backward(r, y, post_weight, gate, pre_weight)
+        return r, h
+
+    @staticmethod
+    def backward(ctx, dr, dh):
+        r, y, post_weight, gate, pre_weight = ctx.saved_tensors
+        how = {k: v for k, v in ctx.how.items() if k != "h_dtype"}
+        dx, dy, dgate, dpost, _, dpre, _ = nq.nq_block_norm_backward(
+            r, y, dr=dr.contiguous(), dh=dh.contiguous(), post_weight=post_weight, gate=gate, pre_weight=pre_weight, **how)
+        return dx, dy, dpost, dgate, dpre, None
+
+
+def block_norm(x: torch.Tensor, y: Optional[torch.Tensor], post_weight: Optional[torch.Tensor], gate: Optional[torch.Tensor],
+               pre_weight: torch.Tensor, **how) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(r, h) of nq_block_norm, with gradients; without y, r = skip_scale * x and there is no post norm."""
+    how.setdefault("pre", nq.NQ_NORM_RMS)
+    how.setdefault("post", nq.NQ_NORM_NONE if y is None else nq.NQ_NORM_RMS)
+    return _BlockNorm.apply(x, y, post_weight, gate, pre_weight, how)
+
+
+class MlpBlock(torch.nn.Module):
+    """norm -> up -> activation -> down; its output meets the stream in the next block's (or the final) norm, which
+    applies this block's post norm, gate and residual scale."""
+
+    def __init__(self, width: int, hidden: int, device="cuda"):
+        super().__init__()
+        new = lambda *shape: torch.nn.Parameter(torch.empty(*shape, device=device))
+        self.pre_weight, self.post_weight, self.gate = new(width), new(width), new(1, width)
+        self.up, self.down, self.up_bias = new(hidden, width), new(width, hidden), new(hidden)
+        with torch.no_grad():
+            self.pre_weight.fill_(1.0)
+            self.post_weight.fill_(1.0)
+            self.gate.fill_(0.5)
+            self.up_bias.zero_()
+            self.up.normal_(std=width ** -0.5)
+            self.down.normal_(std=hidden ** -0.5)
+        self.served: Optional[Tuple[Fp8Weight, Fp8Weight]] = None
+
+    def forward(self, h: torch.Tensor) -> torch.Tensor:
+        return fp8_linear(torch.nn.functional.gelu(fp8_linear(h, self.up, self.up_bias)), self.down)
+
+    @torch.no_grad()
+    def freeze(self) -> None:
+        """Lays the weights out for serving."""
+        self.served = (quantize_weight(self.up), quantize_weight(self.down))
+
+    @torch.no_grad()
+    def serve(self, h: torch.Tensor, hs: torch.Tensor) -> torch.Tensor:
+        up, down = self.served
+        a = torch.nn.functional.gelu(nq.nq_fp8_gemm(h, hs, up.q, up.s, bias=self.up_bias))
+        q, s, _, _ = nq.nq_fp8_quantize(a)
+        return nq.nq_fp8_gemm(q, s, down.q, down.s)
+
+
+class MlpStack(torch.nn.Module):
+    def __init__(self, blocks: int, width: int, hidden: int, skip_scale: float = 1.0, branch_scale: float = 1.0, device="cuda"):
+        super().__init__()
+        self.blocks = torch.nn.ModuleList(MlpBlock(width, hidden, device) for _ in range(blocks))
+        self.final_weight = torch.nn.Parameter(torch.ones(width, device=device))
+        self.how = dict(skip_scale=skip_scale, branch_scale=branch_scale)
+
+    def _between(self, i: int):
+        """What stands before block i: the post norm and gate of the block before it, and the pre norm of this one."""
+        last = self.blocks[i - 1] if i else None
+        pre = self.blocks[i].pre_weight if i < len(self.blocks) else self.final_weight
+        return (last.post_weight, last.gate, pre, self.how) if i else (None, None, pre, {})
+
+    def forward(self, x: torch.Tensor) -> torch.Tensor:
+        y = None
+        for i in range(len(self.blocks) + 1):
+            post, gate, pre, how = self._between(i)
+            x, h = block_norm(x, y, post, gate, pre, **how)
+            if i < len(self.blocks):
+                y = self.blocks[i](h)
+        return h
+
+    def freeze(self) -> None:
+        for b in self.blocks:
+            b.freeze()
+
+    @torch.no_grad()
+    def serve(self, x: torch.Tensor) -> torch.Tensor:
+        """The same for one token or many, with the norms' outputs as e4m3 operands."""
+        y = None
+        for i in range(len(self.blocks) + 1):
+            post, gate, pre, how = self._between(i)
+            kind = nq.NQ_NORM_NONE if y is None else nq.NQ_NORM_RMS
+            final = i == len(self.blocks)
+            r, h, hs = nq.nq_block_norm(x, y, post=kind, post_weight=post, gate=gate, pre_weight=pre,
+                                        h_dtype=torch.bfloat16 if final else torch.float8_e4m3fn, **how)
+            x = x if r is None else r
+            if not final:
+                y = self.blocks[i].serve(h, hs)
+        return h
+
+
+class NestedLinear:
+    """A linear on a nested INT8 weight behind a block norm whose output is INT8: what the norm hands over is the
+    activation operand of nq_gemm_nested (full-bit) or nq_gemm_part (part-bit, w_high alone)."""
+
+    def __init__(self, w_int: torch.Tensor, w_scale: torch.Tensor, h_bits: int, act_scale: float, mask: torch.Tensor):
+        self.rows, self.h_bits, self.w_scale, self.act_scale = w_int.shape[0], h_bits, w_scale, act_scale
+        self.high, self.low = nq.nq_decompose(w_int, mask, 8, h_bits, True)
+
+    def __call__(self, x: torch.Tensor, pre_weight: torch.Tensor, pre_bias: Optional[torch.Tensor], part_bit: bool = False) -> torch.Tensor:
+        _, h, _ = nq.nq_block_norm(x, None, pre=nq.NQ_NORM_LAYER, pre_weight=pre_weight, pre_bias=pre_bias, h_dtype=torch.int8,
+                                   h_scale=self.act_scale)
+        if part_bit:
+            return nq.nq_gemm_part(h, self.high, self.rows, 8, self.h_bits, self.w_scale, self.act_scale)[1]
+        return nq.nq_gemm_nested(h, self.high, self.low, self.rows, 8, self.h_bits, self.w_scale, self.act_scale)[1]
+
+
+def main(steps: int = 60, tokens: int = 2048, width: int = 512, hidden: int = 2048, blocks: int = 3) -> List[float]:
+    """Fits a stack to a fixed random stack's outputs; prints the loss, then serves one token and the batch."""
+    torch.manual_seed(0)
+    teacher, student = MlpStack(blocks, width, hidden), MlpStack(blocks, width, hidden)
+    optimiser = torch.optim.AdamW(student.parameters(), lr=2e-3)
+    losses = []
+    for step in range(steps):
+        x = torch.randn(tokens, width, device="cuda", dtype=torch.bfloat16)
+        with torch.no_grad():
+            want = teacher(x)
+        loss = (student(x).float() - want.float()).square().mean()
+        optimiser.zero_grad(set_to_none=True)
+        loss.backward()
+        optimiser.step()
+        losses.append(float(loss.detach()))
+        if step % 10 == 0 or step == steps - 1:
+            print(f"step {step:3d}  loss {losses[-1]:.5f}")
+    student.freeze()
+    with torch.no_grad():
+        trained = student(x).float()
+    many, one = student.serve(x).float(), student.serve(x[:1]).float()
+    print(f"served against trained forward: {float((many - trained).norm() / trained.norm()):.4f} of the norm; "
+          f"one token against the batch: {float((one - many[:1]).norm() / one.norm()):.4f}")
+    return losses
+
+
+if __name__ == "__main__":
+    main()
