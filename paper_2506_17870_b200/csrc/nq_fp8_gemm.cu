@@ -314,7 +314,7 @@ struct PairShape {
     static constexpr int kSmem = kPairStages * (kPairStageBytes + kScales * 4) + kPairWarps * (kPieces * kOutPiece + 128 * 4) + 512 + 1024;
 };
 
-// one scale to shared memory, asynchronously; zero where there is none (`any`: some readable address)
+// one scale (or bias) to shared memory, asynchronously; zero where there is none (`any`: some readable address)
 __device__ __forceinline__ void copy_scale(uint32_t dst, const float* src, bool present, const float* any) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(present ? src : any), "r"(present ? 4 : 0) : "memory");
 }
@@ -430,9 +430,9 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     const uint32_t tmem_base = *tmem_slot;
     start_next();
     wait_previous();
-    // 384 threads are launched with 168 registers each (64512); the promotion warps take 224 (256 x 224 = 57344), the
-    // other four 56 (128 x 56 = 7168): together what was launched.
-    if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    // 384 threads are launched with 168 registers each (64512); the promotion warps take 232 (256 x 232 = 59392), the
+    // other four 40 (128 x 40 = 5120): together what was launched.
+    if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
 
     if (warp == 0) {
         if (lane == 0) {
@@ -501,7 +501,7 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
     } else if (warp >= 4) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
         const int quarter = warp & 3, h = (warp - 4) >> 2;     // 32 rows of one half
         const uint32_t tmem_mine = tmem_base + h * 128 + ((uint32_t)(quarter * 32) << 16);
         uint8_t* pieces = sOut + (warp - 4) * S::kPieces * kOutPiece;
@@ -532,11 +532,13 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             fetch_first(mt, nt);
         }
         for (int tile = pair; ok && tile < num_tiles; tile += num_pairs) {
-            float bias[4];                                     // four of the tile's 128 columns; they are needed at its end
+            if (p.bias) {                                      // needed at the tile's end; asynchronous, so it costs no registers
+                __syncwarp();                                  // the last tile's have been read
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int c = nt * 256 + h * 128 + 4 * lane + i;
-                bias[i] = p.bias && c < p.N ? p.bias[c] : 0.0f;
+                for (int i = 0; i < 4; ++i) {
+                    const int c = nt * 256 + h * 128 + 32 * i + lane;
+                    copy_scale(smem_u32(my_bias + 32 * i + lane), p.bias + c, c < p.N, p.bias);
+                }
             }
             uint64_t acc[64];                                  // pairs of neighbouring columns
 #pragma unroll
@@ -600,8 +602,7 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             }
             if (row0 >= p.M || col >= p.N) continue;
             if (p.bias) {
-                __syncwarp();                                  // the last tile's have been read
-                *reinterpret_cast<float4*>(my_bias + 4 * lane) = make_float4(bias[0], bias[1], bias[2], bias[3]);
+                asm volatile("cp.async.wait_all;" ::: "memory");
                 __syncwarp();
 #pragma unroll
                 for (int i = 0; i < 64; i += 2) {
