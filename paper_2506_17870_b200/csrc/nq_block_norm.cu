@@ -77,7 +77,7 @@ __device__ __forceinline__ void load_row(const Cols<NV, VEC>& c, const float* ro
         }
     }
 }
-// the same from a row in shared memory (VEC only)
+// the same from a row in shared memory
 template <int NV>
 __device__ __forceinline__ void take_row(const Cols<NV, true>& c, const bf16* row, Row<NV>& v) {
 #pragma unroll
@@ -98,6 +98,15 @@ __device__ __forceinline__ void take_row(const Cols<NV, true>& c, const float* r
         }
         spread(a, b, v[k]);
     }
+}
+// ... and, element by element, from one that starts anywhere
+template <int NV, typename T>
+__device__ __forceinline__ void take_row(const Cols<NV, false>& c, const T* row, Row<NV>& v) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            v[k][j] = pack2f(c.has(k, 2 * j) ? (float)row[c.col(k, 2 * j)] : 0.0f, c.has(k, 2 * j + 1) ? (float)row[c.col(k, 2 * j + 1)] : 0.0f);
 }
 // one piece of a parameter vector; `none` where the vector is absent, zero in absent columns of one that is there
 template <int NV, bool VEC>
@@ -174,6 +183,8 @@ __device__ __forceinline__ void store_bytes8(const Cols<NV, VEC>& c, uint8_t* ro
 // record.
 constexpr int kRingHead = 128;             // barriers and the abort flag, before the stages
 constexpr int kMaxStages = 8;
+// room for a row in a stage
+__host__ __device__ inline int row_slot(int bytes, bool vec) { return vec ? bytes : (bytes + 30) & ~15; }
 struct RowRing {
     uint8_t* stages;
     uint64_t* full;
@@ -196,10 +207,18 @@ struct RowRing {
         }
     }
     __device__ __forceinline__ uint8_t* stage(int s) const { return stages + s * stage_bytes; }
-    __device__ __forceinline__ void expect(int s) const { sm100::mbar_arrive_expect_tx(sm100::smem_u32(&full[s]), stage_bytes); }
-    __device__ __forceinline__ void copy(int s, int offset, const void* src, int bytes) const {
-        sm100::bulk_load(sm100::smem_u32(stage(s) + offset), src, bytes, sm100::smem_u32(&full[s]));
+    __device__ __forceinline__ void expect(int s, int bytes) const { sm100::mbar_arrive_expect_tx(sm100::smem_u32(&full[s]), bytes); }
+    // Rows that start anywhere are copied as the 16-byte granules that hold them (the granules lie in the same
+    // allocation: no allocation starts or ends inside one); the row then starts at its address modulo 16.
+    static __device__ __forceinline__ int granules(const void* src, int bytes) {
+        const uint64_t a = reinterpret_cast<uint64_t>(src);
+        return (int)(((a + bytes + 15) & ~15ull) - (a & ~15ull));
     }
+    __device__ __forceinline__ void copy(int s, int offset, const void* src, int bytes) const {
+        sm100::bulk_load(sm100::smem_u32(stage(s) + offset), reinterpret_cast<const void*>(reinterpret_cast<uint64_t>(src) & ~15ull), granules(src, bytes),
+                         sm100::smem_u32(&full[s]));
+    }
+    static __device__ __forceinline__ int shift(const void* src) { return (int)(reinterpret_cast<uint64_t>(src) & 15); }
     __device__ __forceinline__ void wait(int s, int parity) const {
         (void)sm100::mbar_wait(sm100::smem_u32(&full[s]), parity, abort_flag, status, 0x400u);
     }
@@ -320,11 +339,13 @@ __global__ void __launch_bounds__(NV == 1 ? 1024 : 512) block_norm_kernel(const 
     const Cols<NV, VEC> c{(int)threadIdx.x - team * threads, threads, p.cols};
     TeamSum<1> sum{box, threads, 0};
     RowRing ring;
-    const int x_bytes = p.cols * (int)sizeof(TX), y_bytes = p.cols * (int)sizeof(TY);
+    const int x_bytes = p.cols * (int)sizeof(TX), y_bytes = p.cols * (int)sizeof(TY), at_y = row_slot(x_bytes, VEC);
     const auto start = [&](int s, long long row) {             // one thread
-        ring.expect(s);
-        ring.copy(s, 0, static_cast<const TX*>(p.x) + row * p.ldx, x_bytes);
-        if (p.y) ring.copy(s, x_bytes, static_cast<const TY*>(p.y) + row * p.ldy, y_bytes);
+        const TX* x = static_cast<const TX*>(p.x) + row * p.ldx;
+        const TY* y = static_cast<const TY*>(p.y) + row * p.ldy;
+        ring.expect(s, RowRing::granules(x, x_bytes) + (p.y ? RowRing::granules(y, y_bytes) : 0));
+        ring.copy(s, 0, x, x_bytes);
+        if (p.y) ring.copy(s, at_y, y, y_bytes);
     };
     if (RING) {
         ring.init(ring_smem, p.ring, p.stage_bytes, p.status);
@@ -381,13 +402,14 @@ __global__ void __launch_bounds__(NV == 1 ? 1024 : 512) block_norm_kernel(const 
         Row<NV> r;
         if constexpr (RING) {
             ring.wait(stage, parity);
-            take_row(c, reinterpret_cast<const TX*>(ring.stage(stage)), r);
+            take_row(c, reinterpret_cast<const TX*>(ring.stage(stage) + (VEC ? 0 : RowRing::shift(static_cast<const TX*>(p.x) + row * p.ldx))), r);
         } else {
             load_row(c, static_cast<const TX*>(p.x) + row * p.ldx, r);
         }
         if (p.y) {
             Row<NV> u;
-            if constexpr (RING) take_row(c, reinterpret_cast<const TY*>(ring.stage(stage) + x_bytes), u);
+            if constexpr (RING)
+                take_row(c, reinterpret_cast<const TY*>(ring.stage(stage) + at_y + (VEC ? 0 : RowRing::shift(static_cast<const TY*>(p.y) + row * p.ldy))), u);
             else load_row(c, static_cast<const TY*>(p.y) + row * p.ldy, u);
             const float inv = norm_factor(c, u, p.post, p.inv_cols, p.eps, sum);
             if (p.post != NQ_NORM_NONE) refill();
@@ -519,15 +541,19 @@ __global__ void __launch_bounds__(512) block_norm_backward_kernel(const BackArgs
     // a stage: r, dh (pre norm), dr, y, as far as they are there
     RowRing ring;
     const int x_bytes = p.cols * (int)sizeof(TX), y_bytes = p.cols * (int)sizeof(TY);
-    const int at_dh = has_pre ? x_bytes : 0, at_dr = at_dh + (has_pre ? y_bytes : 0), at_y = at_dr + (p.dr ? x_bytes : 0);
+    const int x_slot = row_slot(x_bytes, VEC), y_slot = row_slot(y_bytes, VEC);
+    const int at_dh = has_pre ? x_slot : 0, at_dr = at_dh + (has_pre ? y_slot : 0), at_y = at_dr + (p.dr ? x_slot : 0);
     const auto start = [&](int s, long long row) {
-        ring.expect(s);
+        const TX *r = static_cast<const TX*>(p.r) + row * p.ldr, *dr = static_cast<const TX*>(p.dr) + row * p.lddr;
+        const TY *dh = static_cast<const TY*>(p.dh) + row * p.lddh, *y = static_cast<const TY*>(p.y) + row * p.ldy;
+        ring.expect(s, (has_pre ? RowRing::granules(r, x_bytes) + RowRing::granules(dh, y_bytes) : 0) + (p.dr ? RowRing::granules(dr, x_bytes) : 0) +
+                           (p.y ? RowRing::granules(y, y_bytes) : 0));
         if (has_pre) {
-            ring.copy(s, 0, static_cast<const TX*>(p.r) + row * p.ldr, x_bytes);
-            ring.copy(s, at_dh, static_cast<const TY*>(p.dh) + row * p.lddh, y_bytes);
+            ring.copy(s, 0, r, x_bytes);
+            ring.copy(s, at_dh, dh, y_bytes);
         }
-        if (p.dr) ring.copy(s, at_dr, static_cast<const TX*>(p.dr) + row * p.lddr, x_bytes);
-        if (p.y) ring.copy(s, at_y, static_cast<const TY*>(p.y) + row * p.ldy, y_bytes);
+        if (p.dr) ring.copy(s, at_dr, dr, x_bytes);
+        if (p.y) ring.copy(s, at_y, y, y_bytes);
     };
     if (RING) {
         ring.init(ring_smem, p.ring, p.stage_bytes, p.status);
@@ -577,11 +603,11 @@ __global__ void __launch_bounds__(512) block_norm_backward_kernel(const BackArgs
         for (long long row = row0; row < row1; ++row) {
             const uint8_t* here = RING ? ring.stage(stage) : nullptr;
             const auto get_x = [&](const void* base, long long ld, int offset, Row<NV>& v) {
-                if constexpr (RING) take_row(c, reinterpret_cast<const TX*>(here + offset), v);
+                if constexpr (RING) take_row(c, reinterpret_cast<const TX*>(here + offset + (VEC ? 0 : RowRing::shift(static_cast<const TX*>(base) + row * ld))), v);
                 else load_row(c, static_cast<const TX*>(base) + row * ld, v);
             };
             const auto get_y = [&](const void* base, long long ld, int offset, Row<NV>& v) {
-                if constexpr (RING) take_row(c, reinterpret_cast<const TY*>(here + offset), v);
+                if constexpr (RING) take_row(c, reinterpret_cast<const TY*>(here + offset + (VEC ? 0 : RowRing::shift(static_cast<const TY*>(base) + row * ld))), v);
                 else load_row(c, static_cast<const TY*>(base) + row * ld, v);
             };
             if (RING) ring.wait(stage, parity);
@@ -863,9 +889,9 @@ int check_vector(const float* p, bool* vec) {
     return NQ_OK;
 }
 
-template <typename TX, typename TY, int NV, bool BIAS>
+template <typename TX, typename TY, int NV, bool VEC, bool BIAS>
 int launch_norm_ring(NormArgs& a, const Shape& sh, const RingPlan& r, cudaStream_t stream) {
-    const auto kernel = block_norm_kernel<TX, TY, NV, true, true, BIAS>;
+    const auto kernel = block_norm_kernel<TX, TY, NV, VEC, true, BIAS>;
     static bool done[64] = {false};
     if (!allow_smem(kernel, done)) return NQ_ERR_CUDA;
     a.ring = r.stages;
@@ -885,12 +911,13 @@ int launch_norm_bias(NormArgs& a, bool vec, cudaStream_t stream) {
     const Shape wide = wide_shape(a.cols, 1024);
     // The ring is worth filling from two rows a block on; a warp to a row (up to 256) has enough loads in flight by itself
     // (50000 x 200: 27 us).
-    if (vec && wide.threads > 32) {
-        a.stage_bytes = a.cols * (int)(sizeof(TX) + (a.y ? sizeof(TY) : 0));
+    if (wide.threads > 32) {
+        a.stage_bytes = row_slot(a.cols * (int)sizeof(TX), vec) + (a.y ? row_slot(a.cols * (int)sizeof(TY), vec) : 0);
         // both instantiations are bound to the registers that fill an SM: 64 at 1024 threads, 128 at 512
         RingPlan r;
         if (plan_ring((wide.nv == 1 ? 1024 : 512) / wide.threads, a.stage_bytes, r) && a.rows >= 2ll * r.blocks * sm_count())
-            return wide.nv == 1 ? launch_norm_ring<TX, TY, 1, BIAS>(a, wide, r, stream) : launch_norm_ring<TX, TY, 4, BIAS>(a, wide, r, stream);
+            return wide.nv == 1 ? (vec ? launch_norm_ring<TX, TY, 1, true, BIAS>(a, wide, r, stream) : launch_norm_ring<TX, TY, 1, false, BIAS>(a, wide, r, stream))
+                                : (vec ? launch_norm_ring<TX, TY, 4, true, BIAS>(a, wide, r, stream) : launch_norm_ring<TX, TY, 4, false, BIAS>(a, wide, r, stream));
     }
     return wide.nv == 1 ? launch_norm_plain<TX, TY, 1, BIAS>(a, wide, vec, stream) : launch_norm_plain<TX, TY, 4, BIAS>(a, wide, vec, stream);
 }
@@ -907,8 +934,8 @@ struct BackPlan {
     long long group_rows, groups, chunk_rows, items;
     int chunks, blocks, stage_bytes;
 };
-// The workspace is sized before the pointers are known, so the plan goes by the shape and types alone; rows that turn
-// out not to be aligned take the plain kernel with the same items and blocks.
+// The workspace is sized before the pointers are known, so the plan goes by the shape and types alone (stages have room
+// for rows that start anywhere).
 BackPlan plan_backward(const nq_block_norm_desc* d, bool has_gate) {
     BackPlan p;
     p.group_rows = has_gate && d->rows_per_gate > 0 ? d->rows_per_gate : (d->rows > 0 ? d->rows : 1);
@@ -916,8 +943,8 @@ BackPlan plan_backward(const nq_block_norm_desc* d, bool has_gate) {
     p.groups = (d->rows + p.group_rows - 1) / p.group_rows;
     p.shape = wide_shape(d->cols, 512);
     const int xs = d->x_dtype == NQ_BF16 ? 2 : 4, ys = d->y_dtype == NQ_BF16 ? 2 : 4;
-    p.stage_bytes = (int)d->cols * 2 * (xs + ys);              // at most: r, dr and y, dh
-    p.use_ring = d->cols % 8 == 0 && p.shape.threads > 32 && plan_ring(512 / p.shape.threads, p.stage_bytes, p.ring) &&
+    p.stage_bytes = 2 * (row_slot((int)d->cols * xs, false) + row_slot((int)d->cols * ys, false));     // at most: r, dr and y, dh
+    p.use_ring = p.shape.threads > 32 && plan_ring(512 / p.shape.threads, p.stage_bytes, p.ring) &&
                  d->rows >= 4ll * p.ring.blocks * sm_count();
     const int per_sm = p.use_ring ? p.ring.blocks : 1024 / p.shape.threads;
     const long long want = (long long)sm_count() * per_sm;
@@ -931,13 +958,14 @@ BackPlan plan_backward(const nq_block_norm_desc* d, bool has_gate) {
     return p;
 }
 
-template <typename TX, typename TY, int NV, bool BIAS>
+template <typename TX, typename TY, int NV, bool VEC, bool BIAS>
 int launch_back_ring(BackArgs& a, const BackPlan& pl, cudaStream_t stream) {
-    const auto kernel = block_norm_backward_kernel<TX, TY, NV, true, true, BIAS>;
+    const auto kernel = block_norm_backward_kernel<TX, TY, NV, VEC, true, BIAS>;
     static bool done[64] = {false};
     if (!allow_smem(kernel, done)) return NQ_ERR_CUDA;
     a.ring = pl.ring.stages;
-    a.stage_bytes = a.cols * (int)((a.pre != NQ_NORM_NONE ? sizeof(TX) + sizeof(TY) : 0) + (a.dr ? sizeof(TX) : 0) + (a.y ? sizeof(TY) : 0));
+    const int x = row_slot(a.cols * (int)sizeof(TX), VEC), y = row_slot(a.cols * (int)sizeof(TY), VEC);
+    a.stage_bytes = (a.pre != NQ_NORM_NONE ? x + y : 0) + (a.dr ? x : 0) + (a.y ? y : 0);
     return launch_chained(kernel, (unsigned)pl.blocks, (unsigned)pl.shape.threads, pl.ring.smem, 1, stream, a, pl.shape.threads);
 }
 template <typename TX, typename TY, int NV, bool BIAS>
@@ -947,10 +975,10 @@ int launch_back_plain(const BackArgs& a, const BackPlan& pl, bool vec, cudaStrea
 }
 template <typename TX, typename TY, bool BIAS>
 int launch_back_bias(BackArgs& a, const BackPlan& pl, bool vec, cudaStream_t stream) {
-    if (vec && pl.use_ring) {
-        if (pl.shape.nv == 1) return launch_back_ring<TX, TY, 1, BIAS>(a, pl, stream);
-        if (pl.shape.nv == 2) return launch_back_ring<TX, TY, 2, BIAS>(a, pl, stream);
-        return launch_back_ring<TX, TY, 4, BIAS>(a, pl, stream);
+    if (pl.use_ring) {
+        if (pl.shape.nv == 1) return vec ? launch_back_ring<TX, TY, 1, true, BIAS>(a, pl, stream) : launch_back_ring<TX, TY, 1, false, BIAS>(a, pl, stream);
+        if (pl.shape.nv == 2) return vec ? launch_back_ring<TX, TY, 2, true, BIAS>(a, pl, stream) : launch_back_ring<TX, TY, 2, false, BIAS>(a, pl, stream);
+        return vec ? launch_back_ring<TX, TY, 4, true, BIAS>(a, pl, stream) : launch_back_ring<TX, TY, 4, false, BIAS>(a, pl, stream);
     }
     if (pl.shape.nv == 1) return launch_back_plain<TX, TY, 1, BIAS>(a, pl, vec, stream);
     if (pl.shape.nv == 2) return launch_back_plain<TX, TY, 2, BIAS>(a, pl, vec, stream);

@@ -381,6 +381,24 @@ def test_many_rows_backward(rows, cols, tx, ty, kind, group):
     check_backward(*backward_case(rows, cols, tx, ty, post=kind, pre=kind, gate=True, group=group))
 
 
+@pytest.mark.parametrize("cols,pitch,offset", [(768, 771, 1), (1001, 1001, 0), (1138, 1140, 3), (4097, 4097, 0)])
+@pytest.mark.parametrize("tx,ty", TYPES)
+def test_many_rows_that_start_anywhere(cols, pitch, offset, tx, ty):
+    rows = 4500 if cols < 2000 else 1500
+
+    def put(t):
+        buf = torch.full((rows * pitch + offset,), 1e3, dtype=t.dtype, device="cuda")
+        v = buf[offset:].view(rows, pitch)[:, :cols]
+        v.copy_(t)
+        return v
+    st, dr, dh = backward_case(rows, cols, tx, ty, gate=True, post=LAYER, group=700)
+    for name in ("x", "y", "r"):
+        st[name] = put(st[name])
+    forward = {k: v for k, v in st.items() if k != "r"}
+    check(forward)
+    check_backward(st, put(dr), put(dh))
+
+
 def test_many_rows_backward_without_post_norm():
     check_backward(*backward_case(6001, 768, torch.float32, torch.bfloat16, post=NONE, pre=LAYER, gate=True, group=100))
     st, dr, dh = backward_case(6001, 768, torch.bfloat16, torch.bfloat16, post=NONE, pre=RMS, block=False)
