@@ -39,7 +39,7 @@ __device__ __forceinline__ float norm_factor(const Cols<NV, VEC>& c, Row<NV>& v,
 // out -- and the latency of a row's two to four joins.  So arithmetic is on pairs, and where blocks work through many
 // rows (RING) they come through a ring in shared memory; the parameters stay in registers, the post norm's weight, the gate
 // and the branch scale as one factor that changes only with the gate's row.  Otherwise rows are loaded when their turn
-// comes.  16384 x 8192, bf16 to e4m3: 475 us without all that, 398 with a ring, 229 with all (4.1 TB/s).  Tried: parameters in
+// comes.  16384 x 8192, bf16 to e4m3: 475 us without all that, 398 with a ring, 224 with all (4.2 TB/s).  Tried: parameters in
 // shared memory and several teams of 16 columns a thread in a block: no room for rows enough (514 us).
 // BIAS: one of the norms has a bias.
 template <typename TX, typename TY, int NV, bool VEC, bool RING, bool BIAS>
