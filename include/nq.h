@@ -357,7 +357,7 @@ NQ_API int nq_fp8_quantize(const void *X, int64_t ldx, int x_dtype, int64_t rows
  *     pitch is fastest).  accumulate != 0 (NQ_F32 only) adds to what Y holds: gradients over several passes.
  *   A linear layer y = x W^T with W quantised in 128 x 128 blocks: forward A = x, B = W; input gradient A = dy,
  *     B = W^T (nq_fp8_quantize's Qt, St); weight gradient A = dy^T, B = x^T, both transposes with block_rows 1.
- *   M, N, K < 2^30.  Allocates nothing and needs no workspace; results repeat bit for bit.
+ *   M, N, K < 2^29.  Allocates nothing and needs no workspace; results repeat bit for bit.
  */
 NQ_API int nq_fp8_gemm(const void *A, int64_t lda, const float *SA, int64_t ldsa, const void *B, int64_t ldb, const float *SB,
                 int64_t ldsb, int b_block_rows, const float *bias, int64_t M, int64_t N, int64_t K,
@@ -473,7 +473,7 @@ NQ_API int nq_debug_set(int which, int enabled);
 NQ_API int nq_i8_mma_ceiling(int64_t stage_iters, double *ops_out, void *stream);
 
 /*
- * Every on-device wait in the GEMM / convolution kernels is bounded.  If one expires the kernel
+ * Every on-device wait in the GEMM / convolution, e4m3 and block-norm kernels is bounded.  If one expires the kernel
  * records it and returns instead of hanging.  This call synchronises `stream`, reads and clears
  * the record of the current device: returns NQ_OK, NQ_ERR_TIMEOUT (with *where_out = an internal
  * code of the wait that gave up) or NQ_ERR_CUDA.

@@ -775,7 +775,7 @@ extern "C" int nq_fp8_gemm(const void* A, int64_t lda, const float* SA, int64_t 
     if (M < 0 || N < 0 || K < 0 || (y_dtype != NQ_F32 && y_dtype != NQ_BF16) || (b_block_rows != 1 && b_block_rows != 128))
         return NQ_ERR_INVALID_ARG;
     if (accumulate && y_dtype != NQ_F32) return NQ_ERR_UNSUPPORTED;
-    if (M >= (1ll << 30) || N >= (1ll << 30) || K >= (1ll << 30)) return NQ_ERR_UNSUPPORTED;
+    if (M >= (1ll << 29) || N >= (1ll << 29) || K >= (1ll << 29)) return NQ_ERR_UNSUPPORTED;     // byte coordinates fit 32 bits
     if (M == 0 || N == 0) return NQ_OK;
     if (!Y || ldy < N) return NQ_ERR_INVALID_ARG;
     const auto at = [](const void* p) { return reinterpret_cast<uintptr_t>(p); };
