@@ -198,6 +198,8 @@ fp8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             for (int c = 0; c < PIECES; ++c) {                 // two loads in flight, waited for in pairs
                 if ((c & 1) == 0) {
                     tmem_ld_wait();
+                    tmem_arrived(d[0]);
+                    if (PIECES > 1) tmem_arrived(d[1]);
                     if (c + 2 >= PIECES) {                     // all have arrived
                         tc_fence_before_sync();
                         __syncwarp();
@@ -578,11 +580,15 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 tmem_ld_32x32(from + 32, d[1]);
                 if (ROW_SCALES) ok = mbar_wait(smem_u32(&sfull[s]), parity, abort_flag, p.status, 0x331u);
                 tmem_ld_wait();
+                tmem_arrived(d[0]);
+                tmem_arrived(d[1]);
                 add(0);
                 tmem_ld_32x32(from + 64, d[0]);
                 add(1);
                 tmem_ld_32x32(from + 96, d[1]);
                 tmem_ld_wait();
+                tmem_arrived(d[0]);
+                tmem_arrived(d[1]);
                 tc_fence_before_sync();
                 __syncwarp();
                 if (lane == 0) {                               // the buffer goes back before its last sums are added

@@ -233,6 +233,14 @@ __device__ __forceinline__ void tmem_ld_wait() {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
+// Ties registers that a tcgen05.ld fills to this point, which follows its wait: the compiler may not move their use
+// before it (the wait itself names no registers).  No instruction.
+template <int N>
+__device__ __forceinline__ void tmem_arrived(uint32_t (&r)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+r"(r[i]));
+}
+
 // ------------------------------------------------------------------------------------ CTA pairs
 // Two CTAs of a cluster share one tcgen05.mma (cta_group::2): each holds half of the operands in its own
 // shared memory and half of the accumulator rows in its own TMEM; the even ("leader") CTA issues the MMAs.
