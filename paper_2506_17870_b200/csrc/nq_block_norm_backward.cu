@@ -31,7 +31,7 @@ struct BackArgs {
 // Column sums stay in registers: P = sum dh v inv_r, sum dh (for the pre norm's weight and bias) over all rows of the thread
 // block, A = sum g t inv_y, sum g over the rows of one work item, which lie under one gate row: from A follow both
 // dgate = branch * (w A0 + b A1) and the item's share branch * gate * A of the post norm's weight and bias.
-// Measured: 16384 x 4096 bf16 213 us (3.8 TB/s; 524 with one join for each sum and no ring), 12608 x 768 fp32 stream 74 us,
+// Measured: 16384 x 4096 bf16 218 us (3.7 TB/s; 524 with one join for each sum and no ring), 12608 x 768 fp32 stream 74 us,
 // 10 of them joining the blocks' sums.  Bound by issue and by the joins: half of the issue slots are used at four warps a
 // scheduler, which the accumulators' registers allow.  (Parameters read for each row instead of held: 330 - 380 us.)
 template <typename TX, typename TY, int NV, bool VEC, bool RING, bool BIAS>
