@@ -532,6 +532,10 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             from_b = p.sb + (col < p.N ? col >> 7 : 0);
             fetch();
         };
+        // whether this warp's part of a tile holds anything of Y
+        const auto inside = [&](int m, int n) {
+            return (long long)m * 256 + rank * 128 + quarter * 32 < p.M && n * 256 + h * 128 < p.N;
+        };
         uint32_t it = 0;
         bool ok = true;
         int mt = 0, nt = 0;
@@ -540,7 +544,9 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             fetch_first(mt, nt);
         }
         for (int tile = pair; ok && tile < num_tiles; tile += num_pairs) {
-            if (p.bias) {                                      // needed at the tile's end; asynchronous, so it costs no registers
+            // Needed at the tile's end; asynchronous, so it costs no registers.  A warp without anything to store starts no
+            // copies: it would not wait for them, and copies of two tiles to one place are not ordered.
+            if (p.bias && inside(mt, nt)) {
                 __syncwarp();                                  // the last tile's have been read
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -608,11 +614,12 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             if (!ok) break;
             const long long row0 = (long long)mt * 256 + rank * 128 + quarter * 32;
             const int col = nt * 256 + h * 128;
+            const bool empty = !inside(mt, nt);
             if (tile + num_pairs < num_tiles) {
                 pair_tile(tile + num_pairs, p, mt, nt);
                 fetch_first(mt, nt);
             }
-            if (row0 >= p.M || col >= p.N) continue;
+            if (empty) continue;
             if (p.bias) {
                 asm volatile("cp.async.wait_all;" ::: "memory");
                 __syncwarp();
@@ -660,6 +667,7 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 }
             }
         }
+        asm volatile("cp.async.wait_all;" ::: "memory");       // nothing to wait for, unless a wait above gave up
         if (lane == 0) bulk_wait_all();                        // this lane's tile stores are done before the block leaves
     }
 
