@@ -584,7 +584,10 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 tc_fence_after_sync();
                 tmem_ld_32x32(from, d[0]);
                 tmem_ld_32x32(from + 32, d[1]);
-                if (ROW_SCALES) ok = mbar_wait(smem_u32(&sfull[s]), parity, abort_flag, p.status, 0x331u);
+                if (ROW_SCALES) {
+                    ok = mbar_wait(smem_u32(&sfull[s]), parity, abort_flag, p.status, 0x331u);
+                    ok = __all_sync(0xffffffffu, ok);          // together again: what follows is for the whole warp
+                }
                 tmem_ld_wait();
                 tmem_arrived(d[0]);
                 tmem_arrived(d[1]);
@@ -607,7 +610,6 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 if (ROW_SCALES) {
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_u32(&sempty[s]));
-                    ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
                 }
             }
