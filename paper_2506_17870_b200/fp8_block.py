@@ -55,27 +55,30 @@ def fp8_linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tenso
 
 class _BlockNorm(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, y, post_weight, gate, pre_weight, how):
-        r, h, _ = nq.nq_block_norm(x, y, post_weight=post_weight, gate=gate, pre_weight=pre_weight, want_r=True, **how)
+    def forward(ctx, x, y, post_weight, post_bias, gate, pre_weight, pre_bias, how):
+        r, h, _ = nq.nq_block_norm(x, y, post_weight=post_weight, post_bias=post_bias, gate=gate, pre_weight=pre_weight, pre_bias=pre_bias,
+                                   want_r=True, **how)
         ctx.how = how
-        ctx.save_for_backward(r, y, post_weight, gate, pre_weight)
+        ctx.save_for_backward(r, y, post_weight, post_bias, gate, pre_weight, pre_bias)
         return r, h
 
     @staticmethod
     def backward(ctx, dr, dh):
-        r, y, post_weight, gate, pre_weight = ctx.saved_tensors
+        r, y, post_weight, post_bias, gate, pre_weight, pre_bias = ctx.saved_tensors
         how = {k: v for k, v in ctx.how.items() if k != "h_dtype"}
-        dx, dy, dgate, dpost, _, dpre, _ = nq.nq_block_norm_backward(
-            r, y, dr=dr.contiguous(), dh=dh.contiguous(), post_weight=post_weight, gate=gate, pre_weight=pre_weight, **how)
-        return dx, dy, dpost, dgate, dpre, None
+        dx, dy, dgate, dpost_weight, dpost_bias, dpre_weight, dpre_bias = nq.nq_block_norm_backward(
+            r, y, dr=dr.contiguous(), dh=dh.contiguous(), post_weight=post_weight, post_bias=post_bias, gate=gate, pre_weight=pre_weight,
+            pre_bias=pre_bias, **how)
+        return dx, dy, dpost_weight, dpost_bias, dgate, dpre_weight, dpre_bias, None
 
 
 def block_norm(x: torch.Tensor, y: Optional[torch.Tensor], post_weight: Optional[torch.Tensor], gate: Optional[torch.Tensor],
-               pre_weight: torch.Tensor, **how) -> Tuple[torch.Tensor, torch.Tensor]:
+               pre_weight: torch.Tensor, *, post_bias: Optional[torch.Tensor] = None, pre_bias: Optional[torch.Tensor] = None,
+               **how) -> Tuple[torch.Tensor, torch.Tensor]:
     """(r, h) of nq_block_norm, with gradients; without y, r = skip_scale * x and there is no post norm."""
     how.setdefault("pre", nq.NQ_NORM_RMS)
     how.setdefault("post", nq.NQ_NORM_NONE if y is None else nq.NQ_NORM_RMS)
-    return _BlockNorm.apply(x, y, post_weight, gate, pre_weight, how)
+    return _BlockNorm.apply(x, y, post_weight, post_bias, gate, pre_weight, pre_bias, how)
 
 
 class MlpBlock(torch.nn.Module):

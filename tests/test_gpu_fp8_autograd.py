@@ -1,0 +1,75 @@
+"""Autograd over the e4m3 entry points where a stack of RMS norms does not go: layer norms with biases, no pre norm, outputs of
+another type than the branch, 8-bit outputs, second derivatives, weights that change after they were laid out.
+
+Gradients have to be bit for bit those of nq_block_norm_backward on the r that the forward pass returned, and within the
+bounds of test_gpu_block_norm.py (derived there) of 64-bit autograd of the definition."""
+import pytest
+import torch
+
+import paper_2506_17870_b200 as nq
+from paper_2506_17870_b200 import fp8_block as fb
+from test_gpu_block_norm import F, LAYER, NONE, RMS, gradients, make, near
+
+pytestmark = pytest.mark.gpu
+PARAMS = ("post_weight", "post_bias", "gate", "pre_weight", "pre_bias")
+
+
+def leaf(t):
+    return None if t is None else t.detach().clone().requires_grad_(True)
+
+
+def run(st, dr, dh, **more):
+    """block_norm of the leaves and its backward pass -> (leaves, r, h)"""
+    v = {k: leaf(st[k]) for k in ("x", "y") + PARAMS}
+    how = {k: st[k] for k in ("post", "pre", "rows_per_gate", "skip_scale", "branch_scale", "eps")}
+    r, h = fb.block_norm(v["x"], v["y"], v["post_weight"], v["gate"], v["pre_weight"], post_bias=v["post_bias"], pre_bias=v["pre_bias"], **how, **more)
+    outs = [(r, dr)] + ([(h, dh)] if h is not None else [])
+    torch.autograd.backward([o for o, _ in outs], [g for _, g in outs])
+    return v, r, h
+
+
+def check(st, v, r, dr, dh):
+    """dh: as the entry point takes it"""
+    how = {k: st[k] for k in ("post", "pre", "rows_per_gate", "skip_scale", "branch_scale", "eps") + PARAMS}
+    got = nq.nq_block_norm_backward(r.detach(), st["y"], dr=dr, dh=dh, **how)
+    names = ("x", "y", "gate", "post_weight", "post_bias", "pre_weight", "pre_bias")
+    for name, g in zip(names, got):
+        if st[name] is None:
+            assert g is None and v[name] is None
+        else:
+            assert v[name].grad is not None, f"{name} got no gradient"
+            assert torch.equal(v[name].grad, g), name
+    want = gradients({**st, "r": r.detach()}, dr, dh)
+    rows = r.shape[0]
+    top = lambda t: t.abs().max(1, keepdim=True).values + 8.0
+    near(v["x"].grad, want["x"], top(want["x"]) * 8)
+    for name, key in (("y", "y"), ("gate", "gate"), ("post_weight", "pw"), ("post_bias", "pb"), ("pre_weight", "qw"), ("pre_bias", "qb")):
+        if st[name] is not None:
+            near(v[name].grad, want[key], top(want["y"]) * 8 if key == "y" else torch.full_like(want[key], 8.0 * rows ** 0.5 + 8 * float(want[key].abs().max())))
+
+
+def incoming(rows, cols, tr, th, seed=5):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randn(rows, cols, generator=g).to(tr).cuda(), torch.randn(rows, cols, generator=g).to(th).cuda()
+
+
+@pytest.mark.parametrize("rows,cols,group", [(37, 264, 0), (394, 768, 197), (5, 31, 2)])
+@pytest.mark.parametrize("tx,ty", [(torch.float32, torch.bfloat16), (torch.bfloat16, torch.bfloat16), (torch.float32, torch.float32)])
+def test_layer_norm_biases(rows, cols, group, tx, ty):
+    st = make(rows, cols, tx, ty, gate=True, group=group, post=LAYER, pre=LAYER)
+    dr, dh = incoming(rows, cols, tx, ty)
+    v, r, _ = run(st, dr, dh)
+    check(st, v, r, dr, dh)
+
+
+def test_bias_of_one_norm():
+    for drop in ("post_bias", "pre_bias"):
+        st = make(20, 264, torch.float32, torch.float32, gate=True, post=LAYER, pre=LAYER)
+        st[drop] = None
+        dr, dh = incoming(20, 264, torch.float32, torch.float32)
+        v, r, _ = run(st, dr, dh)
+        check(st, v, r, dr, dh)
+    st = make(20, 264, torch.float32, torch.float32, pre=LAYER, block=False)              # the norm of the stream alone
+    dr, dh = incoming(20, 264, torch.float32, torch.float32)
+    v, r, _ = run(st, dr, dh)
+    check(st, v, r, dr, dh)
