@@ -66,16 +66,18 @@ class _BlockNorm(torch.autograd.Function):
     def backward(ctx, dr, dh):
         r, y, post_weight, post_bias, gate, pre_weight, pre_bias = ctx.saved_tensors
         how = {k: v for k, v in ctx.how.items() if k != "h_dtype"}
+        dh = None if dh is None else dh.contiguous()           # no pre norm, no h
         dx, dy, dgate, dpost_weight, dpost_bias, dpre_weight, dpre_bias = nq.nq_block_norm_backward(
-            r, y, dr=dr.contiguous(), dh=dh.contiguous(), post_weight=post_weight, post_bias=post_bias, gate=gate, pre_weight=pre_weight,
+            r, y, dr=dr.contiguous(), dh=dh, post_weight=post_weight, post_bias=post_bias, gate=gate, pre_weight=pre_weight,
             pre_bias=pre_bias, **how)
         return dx, dy, dpost_weight, dpost_bias, dgate, dpre_weight, dpre_bias, None
 
 
 def block_norm(x: torch.Tensor, y: Optional[torch.Tensor], post_weight: Optional[torch.Tensor], gate: Optional[torch.Tensor],
-               pre_weight: torch.Tensor, *, post_bias: Optional[torch.Tensor] = None, pre_bias: Optional[torch.Tensor] = None,
-               **how) -> Tuple[torch.Tensor, torch.Tensor]:
-    """(r, h) of nq_block_norm, with gradients; without y, r = skip_scale * x and there is no post norm."""
+               pre_weight: Optional[torch.Tensor], *, post_bias: Optional[torch.Tensor] = None, pre_bias: Optional[torch.Tensor] = None,
+               **how) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """(r, h) of nq_block_norm, with gradients; without y, r = skip_scale * x and there is no post norm; without a pre norm
+    (pre=NQ_NORM_NONE) h is None."""
     how.setdefault("pre", nq.NQ_NORM_RMS)
     how.setdefault("post", nq.NQ_NORM_NONE if y is None else nq.NQ_NORM_RMS)
     return _BlockNorm.apply(x, y, post_weight, post_bias, gate, pre_weight, pre_bias, how)

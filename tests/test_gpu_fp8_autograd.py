@@ -73,3 +73,13 @@ def test_bias_of_one_norm():
     dr, dh = incoming(20, 264, torch.float32, torch.float32)
     v, r, _ = run(st, dr, dh)
     check(st, v, r, dr, dh)
+
+
+@pytest.mark.parametrize("post,gate", [(NONE, True), (RMS, None), (LAYER, True)])
+def test_without_pre_norm(post, gate):
+    """No pre norm: h is None and r's gradient is the only one that arrives."""
+    st = make(33, 264, torch.float32, torch.bfloat16, gate=gate, post=post, pre=NONE)
+    dr, _ = incoming(33, 264, torch.float32, torch.float32)
+    v, r, h = run(st, dr, None)
+    assert h is None
+    check(st, v, r, dr, None)
