@@ -66,7 +66,10 @@ class _BlockNorm(torch.autograd.Function):
     def backward(ctx, dr, dh):
         r, y, post_weight, post_bias, gate, pre_weight, pre_bias = ctx.saved_tensors
         how = {k: v for k, v in ctx.how.items() if k != "h_dtype"}
-        dh = None if dh is None else dh.contiguous()           # no pre norm, no h
+        if dh is not None:                                     # (no pre norm, no h)
+            # it comes in h's type, the kernel takes it in the branch's; alone, a bf16 stream goes with bf16 only
+            kind = y.dtype if y is not None else r.dtype if r.dtype == torch.bfloat16 else dh.dtype
+            dh = dh.contiguous().to(kind)
         dx, dy, dgate, dpost_weight, dpost_bias, dpre_weight, dpre_bias = nq.nq_block_norm_backward(
             r, y, dr=dr.contiguous(), dh=dh, post_weight=post_weight, post_bias=post_bias, gate=gate, pre_weight=pre_weight,
             pre_bias=pre_bias, **how)
@@ -77,7 +80,7 @@ def block_norm(x: torch.Tensor, y: Optional[torch.Tensor], post_weight: Optional
                pre_weight: Optional[torch.Tensor], *, post_bias: Optional[torch.Tensor] = None, pre_bias: Optional[torch.Tensor] = None,
                **how) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
     """(r, h) of nq_block_norm, with gradients; without y, r = skip_scale * x and there is no post norm; without a pre norm
-    (pre=NQ_NORM_NONE) h is None."""
+    (pre=NQ_NORM_NONE) h is None.  The gradient of an h whose type is not y's (h_dtype) is rounded to y's."""
     how.setdefault("pre", nq.NQ_NORM_RMS)
     how.setdefault("post", nq.NQ_NORM_NONE if y is None else nq.NQ_NORM_RMS)
     return _BlockNorm.apply(x, y, post_weight, post_bias, gate, pre_weight, pre_bias, how)

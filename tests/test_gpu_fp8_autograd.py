@@ -83,3 +83,15 @@ def test_without_pre_norm(post, gate):
     v, r, h = run(st, dr, None)
     assert h is None
     check(st, v, r, dr, None)
+
+
+@pytest.mark.parametrize("tx,ty,th", [(torch.float32, torch.bfloat16, torch.float32), (torch.bfloat16, torch.bfloat16, torch.float32),
+                                      (torch.float32, torch.float32, torch.bfloat16), (torch.float32, None, torch.bfloat16),
+                                      (torch.bfloat16, None, torch.float32)])
+def test_output_of_another_type(tx, ty, th):
+    """h's gradient comes in h's type; the kernel takes it in the branch's (without one in its own, or bf16 beside a bf16 stream)."""
+    st = make(21, 264, tx, ty or tx, gate=True, post=LAYER, pre=LAYER, block=ty is not None)
+    dr, dh = incoming(21, 264, tx, th)
+    v, r, h = run(st, dr, dh, h_dtype=th)
+    assert h.dtype == th
+    check(st, v, r, dr, dh.to(ty or (tx if tx == torch.bfloat16 else th)))
