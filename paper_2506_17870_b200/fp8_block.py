@@ -55,9 +55,9 @@ def fp8_linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tenso
 
 class _BlockNorm(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, y, post_weight, post_bias, gate, pre_weight, pre_bias, how):
+    def forward(ctx, x, y, post_weight, post_bias, gate, pre_weight, pre_bias, how, output):
         r, h, _ = nq.nq_block_norm(x, y, post_weight=post_weight, post_bias=post_bias, gate=gate, pre_weight=pre_weight, pre_bias=pre_bias,
-                                   want_r=True, **how)
+                                   want_r=True, **how, **output)
         ctx.how = how
         ctx.save_for_backward(r, y, post_weight, post_bias, gate, pre_weight, pre_bias)
         return r, h
@@ -65,25 +65,32 @@ class _BlockNorm(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dr, dh):
         r, y, post_weight, post_bias, gate, pre_weight, pre_bias = ctx.saved_tensors
-        how = {k: v for k, v in ctx.how.items() if k != "h_dtype"}
         if dh is not None:                                     # (no pre norm, no h)
             # it comes in h's type, the kernel takes it in the branch's; alone, a bf16 stream goes with bf16 only
             kind = y.dtype if y is not None else r.dtype if r.dtype == torch.bfloat16 else dh.dtype
             dh = dh.contiguous().to(kind)
         dx, dy, dgate, dpost_weight, dpost_bias, dpre_weight, dpre_bias = nq.nq_block_norm_backward(
             r, y, dr=dr.contiguous(), dh=dh, post_weight=post_weight, post_bias=post_bias, gate=gate, pre_weight=pre_weight,
-            pre_bias=pre_bias, **how)
-        return dx, dy, dpost_weight, dpost_bias, dgate, dpre_weight, dpre_bias, None
+            pre_bias=pre_bias, **ctx.how)
+        return dx, dy, dpost_weight, dpost_bias, dgate, dpre_weight, dpre_bias, None, None
 
 
 def block_norm(x: torch.Tensor, y: Optional[torch.Tensor], post_weight: Optional[torch.Tensor], gate: Optional[torch.Tensor],
                pre_weight: Optional[torch.Tensor], *, post_bias: Optional[torch.Tensor] = None, pre_bias: Optional[torch.Tensor] = None,
-               **how) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+               post: Optional[int] = None, pre: int = nq.NQ_NORM_RMS, rows_per_gate: int = 0, skip_scale: float = 1.0,
+               branch_scale: float = 1.0, eps: float = 1e-6, h_dtype: Optional[torch.dtype] = None,
+               h_scale: float = 1.0) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
     """(r, h) of nq_block_norm, with gradients; without y, r = skip_scale * x and there is no post norm; without a pre norm
-    (pre=NQ_NORM_NONE) h is None.  The gradient of an h whose type is not y's (h_dtype) is rounded to y's."""
-    how.setdefault("pre", nq.NQ_NORM_RMS)
-    how.setdefault("post", nq.NQ_NORM_NONE if y is None else nq.NQ_NORM_RMS)
-    return _BlockNorm.apply(x, y, post_weight, post_bias, gate, pre_weight, pre_bias, how)
+    (pre=NQ_NORM_NONE) h is None.  The gradient of an h whose type is not y's (h_dtype) is rounded to y's.  An INT8 h (with its
+    h_scale) has none and comes only where no gradient is wanted; e4m3 codes come with their scales, from nq_block_norm."""
+    how = dict(post=(nq.NQ_NORM_NONE if y is None else nq.NQ_NORM_RMS) if post is None else post, pre=pre, rows_per_gate=rows_per_gate,
+               skip_scale=skip_scale, branch_scale=branch_scale, eps=eps)
+    tensors = (x, y, post_weight, post_bias, gate, pre_weight, pre_bias)
+    if h_dtype is torch.float8_e4m3fn:
+        raise ValueError("e4m3 output has scales: call nq_block_norm")
+    if h_dtype is torch.int8 and torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise ValueError("INT8 output has no gradient: call block_norm under no_grad, or nq_block_norm")
+    return _BlockNorm.apply(*tensors, how, dict(h_dtype=h_dtype, h_scale=h_scale))
 
 
 class MlpBlock(torch.nn.Module):

@@ -95,3 +95,24 @@ def test_output_of_another_type(tx, ty, th):
     v, r, h = run(st, dr, dh, h_dtype=th)
     assert h.dtype == th
     check(st, v, r, dr, dh.to(ty or (tx if tx == torch.bfloat16 else th)))
+
+
+def test_eight_bit_outputs():
+    """An 8-bit h has no gradient, and e4m3 codes are worth nothing without their scales: both belong to nq_block_norm."""
+    st = make(9, 256, torch.float32, torch.float32, gate=True)
+    for dtype in (torch.int8, torch.float8_e4m3fn):
+        with pytest.raises(ValueError):
+            fb.block_norm(leaf(st["x"]), st["y"], st["post_weight"], st["gate"], st["pre_weight"], h_dtype=dtype, h_scale=0.02)
+    with pytest.raises(ValueError):
+        fb.block_norm(st["x"], st["y"], st["post_weight"], st["gate"], st["pre_weight"], h_dtype=torch.float8_e4m3fn)
+    r, h = fb.block_norm(st["x"], st["y"], st["post_weight"], st["gate"], st["pre_weight"], h_dtype=torch.int8, h_scale=0.02)     # no gradient wanted
+    want_r, want_h, _ = nq.nq_block_norm(st["x"], st["y"], post=RMS, post_weight=st["post_weight"], gate=st["gate"], pre_weight=st["pre_weight"],
+                                         h_dtype=torch.int8, h_scale=0.02)
+    assert torch.equal(r, want_r) and torch.equal(h, want_h)
+    x = st["x"].clone()
+    with pytest.raises(TypeError):
+        fb.block_norm(x, st["y"], st["post_weight"], st["gate"], st["pre_weight"], r_out=x)      # autograd would not see the write
+    assert torch.equal(x, st["x"])
+    dr, dh = incoming(9, 256, torch.float32, torch.float32)
+    v, r, _ = run(st, dr, dh, h_scale=0.02)                        # of no meaning for an fp32 h, as in nq_block_norm
+    check(st, v, r, dr, dh)
