@@ -30,6 +30,25 @@ def quantize_weight(w: torch.Tensor) -> Fp8Weight:
     return Fp8Weight(*nq.nq_fp8_quantize(w, block_rows=128, transposed=True))
 
 
+class _Refusal(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, anchor, grad):
+        return grad.view_as(grad)
+
+    @staticmethod
+    def backward(ctx, _):
+        raise RuntimeError("the gradients of fp8_linear and block_norm cannot be differentiated again")
+
+
+def _first_order(*grads):
+    """Gradients out of kernels, of which autograd knows no more than their values.  Where they become part of a graph
+    (create_graph) it would take them for constants: they are tied to a node that refuses to be differentiated."""
+    if not torch.is_grad_enabled():
+        return grads
+    anchor = torch.zeros((), requires_grad=True)
+    return tuple(None if g is None else _Refusal.apply(anchor, g) for g in grads)
+
+
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias):
@@ -45,7 +64,7 @@ class _Linear(torch.autograd.Function):
         d, sd, dt, sdt = nq.nq_fp8_quantize(dy.contiguous(), transposed=True)
         dx = nq.nq_fp8_gemm(d, sd, wt, swt, y_dtype=dy.dtype)
         dw = nq.nq_fp8_gemm(dt, sdt, xt, sxt, b_block_rows=1, y_dtype=torch.float32)
-        return dx, dw, dy.float().sum(0) if ctx.has_bias else None
+        return *_first_order(dx, dw), dy.float().sum(0) if ctx.has_bias else None
 
 
 def fp8_linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -72,7 +91,7 @@ class _BlockNorm(torch.autograd.Function):
         dx, dy, dgate, dpost_weight, dpost_bias, dpre_weight, dpre_bias = nq.nq_block_norm_backward(
             r, y, dr=dr.contiguous(), dh=dh, post_weight=post_weight, post_bias=post_bias, gate=gate, pre_weight=pre_weight,
             pre_bias=pre_bias, **ctx.how)
-        return dx, dy, dpost_weight, dpost_bias, dgate, dpre_weight, dpre_bias, None, None
+        return *_first_order(dx, dy, dpost_weight, dpost_bias, dgate, dpre_weight, dpre_bias), None, None
 
 
 def block_norm(x: torch.Tensor, y: Optional[torch.Tensor], post_weight: Optional[torch.Tensor], gate: Optional[torch.Tensor],

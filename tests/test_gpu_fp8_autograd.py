@@ -116,3 +116,34 @@ def test_eight_bit_outputs():
     dr, dh = incoming(9, 256, torch.float32, torch.float32)
     v, r, _ = run(st, dr, dh, h_scale=0.02)                        # of no meaning for an fp32 h, as in nq_block_norm
     check(st, v, r, dr, dh)
+
+
+def test_second_derivatives_are_refused():
+    """Gradients out of kernels are no constants: a loss that contains them must not be differentiated as if they were, whether
+    or not the gradients that arrived themselves depend on the leaves."""
+    x, w = torch.randn(40, 128, device="cuda").requires_grad_(True), torch.randn(64, 128, device="cuda").requires_grad_(True)
+    p = torch.ones(128, device="cuda").requires_grad_(True)
+    for through in (lambda y: y.square().sum(), lambda y: y.sum()):
+        for wrt in (x, w):
+            y = fb.fp8_linear(x, w)
+            d, = torch.autograd.grad(through(y), wrt, create_graph=True)
+            with pytest.raises(RuntimeError, match="differentiated again"):
+                (y.sum() + d.square().sum()).backward()
+        for wrt in (x, p):
+            r, h = fb.block_norm(x, None, None, None, p)
+            d, = torch.autograd.grad(through(h), wrt, create_graph=True)
+            with pytest.raises(RuntimeError, match="differentiated again"):
+                (h.sum() + d.square().sum()).backward()
+    x.grad = w.grad = None
+    # a graph of the gradients that is not used does no harm, and the bias's gradient is a sum that autograd knows
+    b = torch.zeros(64, device="cuda").requires_grad_(True)
+    fb.fp8_linear(x, w, b).square().sum().backward(create_graph=True)
+    once = [t.grad.detach().clone() for t in (x, w, b)]
+    x.grad = w.grad = b.grad = None
+    fb.fp8_linear(x, w, b).square().sum().backward()
+    assert all(torch.equal(a, t.grad) for a, t in zip(once, (x, w, b)))
+    x.grad = w.grad = b.grad = None
+    y = fb.fp8_linear(x, w, b)
+    db, = torch.autograd.grad(y.square().sum(), b, create_graph=True)
+    again, = torch.autograd.grad(db.sum(), b)
+    assert torch.equal(again, torch.full_like(b, 2.0 * 40))        # d/db of sum over rows of 2 y
