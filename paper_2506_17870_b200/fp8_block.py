@@ -129,17 +129,46 @@ class MlpBlock(torch.nn.Module):
             self.up.normal_(std=width ** -0.5)
             self.down.normal_(std=hidden ** -0.5)
         self.served: Optional[Tuple[Fp8Weight, Fp8Weight]] = None
+        self._served_from = None                               # what up and down were when they were laid out
 
     def forward(self, h: torch.Tensor) -> torch.Tensor:
-        return fp8_linear(torch.nn.functional.gelu(fp8_linear(h, self.up, self.up_bias)), self.down)
+        y = fp8_linear(torch.nn.functional.gelu(fp8_linear(h, self.up, self.up_bias)), self.down)
+        if y.requires_grad and (self.up.requires_grad or self.down.requires_grad):
+            y.register_hook(self._backward_came)
+        return y
+
+    def _backward_came(self, _) -> None:
+        self._served_from = None                               # a fused optimiser's step is not counted as a write
+
+    def _weights(self):
+        """The two weights, where they lie and how often they were written (not counting writes through .data)."""
+        return [(w, w.data_ptr(), 0 if w.is_inference() else w._version) for w in (self.up, self.down)]
+
+    def _served_as_they_are(self) -> bool:
+        return self._served_from is not None and all(a is b and rest == now for (a, *rest), (b, *now) in zip(self._served_from, self._weights()))
+
+    # a copy of a block has weights of its own
+    def __getstate__(self):
+        return {**self.__dict__, "_served_from": self._served_as_they_are()}
+
+    def __setstate__(self, state):
+        super().__setstate__(state)
+        current, self._served_from = self._served_from, None
+        if current:
+            self._served_from = self._weights()
+        else:
+            self.served = None
 
     @torch.no_grad()
     def freeze(self) -> None:
-        """Lays the weights out for serving."""
-        self.served = (quantize_weight(self.up), quantize_weight(self.down))
+        """Lays the weights out for serving; to be called again after a backward pass or a change of the weights.  (Not noticed
+        by serve(): writes through .data, and a fused optimiser's step on gradients from before this call.)"""
+        self.served, self._served_from = (quantize_weight(self.up), quantize_weight(self.down)), self._weights()
 
     @torch.no_grad()
     def serve(self, h: torch.Tensor, hs: torch.Tensor) -> torch.Tensor:
+        if not self._served_as_they_are():
+            raise RuntimeError("the weights were not laid out for serving, or were trained or changed since: call freeze()")
         up, down = self.served
         a = torch.nn.functional.gelu(nq.nq_fp8_gemm(h, hs, up.q, up.s, bias=self.up_bias))
         q, s, _, _ = nq.nq_fp8_quantize(a)

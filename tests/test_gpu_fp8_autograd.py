@@ -3,6 +3,8 @@ another type than the branch, 8-bit outputs, second derivatives, weights that ch
 
 Gradients have to be bit for bit those of nq_block_norm_backward on the r that the forward pass returned, and within the
 bounds of test_gpu_block_norm.py (derived there) of 64-bit autograd of the definition."""
+import copy
+
 import pytest
 import torch
 
@@ -147,3 +149,59 @@ def test_second_derivatives_are_refused():
     db, = torch.autograd.grad(y.square().sum(), b, create_graph=True)
     again, = torch.autograd.grad(db.sum(), b)
     assert torch.equal(again, torch.full_like(b, 2.0 * 40))        # d/db of sum over rows of 2 y
+
+
+@pytest.mark.parametrize("options", [dict(), dict(foreach=False), dict(fused=True)], ids=["default", "each", "fused"])
+def test_weights_laid_out_before_a_step_are_not_served(options):
+    torch.manual_seed(6)
+    stack = fb.MlpStack(2, 128, 256)
+    x = torch.randn(65, 128, device="cuda", dtype=torch.bfloat16)
+    with pytest.raises(RuntimeError):
+        stack.serve(x)                                             # never laid out
+    stack.freeze()
+    before = stack.serve(x)
+    assert torch.equal(before, stack.serve(x))
+    optimiser = torch.optim.AdamW(stack.parameters(), lr=0.1, **options)
+    loss = stack(x).float().square().mean()
+    assert torch.equal(before, stack.serve(x))                     # a forward pass alone changes nothing
+    loss.backward()
+    optimiser.step()
+    with pytest.raises(RuntimeError):
+        stack.serve(x)
+    stack.freeze()
+    fresh = fb.MlpStack(2, 128, 256)
+    fresh.load_state_dict(stack.state_dict())
+    fresh.freeze()
+    assert torch.equal(stack.serve(x), fresh.serve(x)) and not torch.equal(before, stack.serve(x))
+    fresh.load_state_dict(fb.MlpStack(2, 128, 256).state_dict())
+    with pytest.raises(RuntimeError):
+        fresh.serve(x)
+    fresh.freeze()
+    for p in fresh.parameters():
+        p.requires_grad_(False)
+    v = x.clone().requires_grad_(True)
+    fresh(v).float().sum().backward()                              # through weights that are not trained
+    fresh.serve(x)
+    fresh.blocks[1].down = torch.nn.Parameter(fresh.blocks[1].down.detach().clone())
+    with pytest.raises(RuntimeError):
+        fresh.serve(x)
+
+
+def test_copies_of_a_laid_out_stack(tmp_path):
+    torch.manual_seed(7)
+    stack = fb.MlpStack(1, 128, 256)
+    x = torch.randn(9, 128, device="cuda", dtype=torch.bfloat16)
+    stack.freeze()
+    want = stack.serve(x)
+    torch.save(stack, tmp_path / "stack")
+    for twin in (copy.deepcopy(stack), torch.load(tmp_path / "stack", weights_only=False)):
+        assert torch.equal(twin.serve(x), want)
+        with torch.no_grad():
+            twin.blocks[0].up.mul_(2.0)
+        with pytest.raises(RuntimeError):
+            twin.serve(x)
+        with pytest.raises(RuntimeError):
+            copy.deepcopy(twin).serve(x)
+    assert torch.equal(stack.serve(x), want)
+    with torch.inference_mode():
+        assert torch.equal(stack.serve(x), want)
