@@ -636,14 +636,22 @@ def _new(rows: int, cols: int, dtype, device, pitch: Optional[int] = None) -> to
     return torch.empty_strided((rows, cols), (cols if pitch is None else pitch, 1), dtype=dtype, device=device)
 
 
-def _matrix(t: torch.Tensor, name: str, dtype=None, shape=None) -> int:
-    """Checks a [rows, cols] CUDA tensor with neighbouring columns; -> its row pitch."""
+def _on(t: torch.Tensor, name: str, index: int) -> None:
+    """Refuses a tensor that is not on the GPU of this index, the first operand's."""
+    here = t.get_device()
+    if here < 0:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if here != index:
+        raise ValueError(f"{name} is on cuda:{here}, the first operand on {'the host' if index < 0 else f'cuda:{index}'}")
+
+
+def _matrix(t: torch.Tensor, name: str, index: int, dtype=None, shape=None) -> int:
+    """Checks a [rows, cols] tensor on the GPU of this index, with neighbouring columns; -> its row pitch."""
     if t.dim() != 2 or (shape is not None and t.shape != shape):
         raise ValueError(f"{name} must be a {'[rows, cols]' if shape is None else list(shape)} tensor, got {list(t.shape)}")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor")
+    _on(t, name, index)
     ld, step = t.stride()
     rows, cols = t.shape
     if step != 1 and cols > 1 and rows > 0:
@@ -659,21 +667,21 @@ def _fp8_pitch(cols: int) -> int:
     return (cols + 15) & ~15
 
 
-def _fp8_ld(t: torch.Tensor, name: str, shape=None) -> int:
+def _fp8_ld(t: torch.Tensor, name: str, index: int, shape=None) -> int:
     """The row pitch of an e4m3 (or INT8) matrix: of a single row, the one that its columns need."""
-    ld = _matrix(t, name, t.dtype, shape)
+    ld = _matrix(t, name, index, t.dtype, shape)
     return ld if t.shape[0] > 1 else _fp8_pitch(t.shape[1])
 
 
-def _scales(t: torch.Tensor, name: str, groups: int, count: int) -> int:
-    return _matrix(t, name, torch.float32, (groups, count))
+def _scales(t: torch.Tensor, name: str, index: int, groups: int, count: int) -> int:
+    return _matrix(t, name, index, torch.float32, (groups, count))
 
 
 def nq_fp8_quantize(x: torch.Tensor, block_rows: int = 1, rowwise: bool = True, transposed: bool = False):
     """[rows, cols] fp32 / bf16 -> (q, s, qt, st): e4m3 [rows, cols] and its scales, groups first
     ([ceil(cols / 128), rows], or [ceil(cols / 128), ceil(rows / 128)] for block_rows == 128); the same of the transpose
     x^T (groups along the rows of x).  A pair that is not asked for is (None, None)."""
-    ld = _matrix(x, "x")
+    ld = _matrix(x, "x", x.get_device())
     if x.dtype not in _FLOATS:
         raise ValueError(f"x must be float32 or bfloat16, got {x.dtype}")
     if block_rows not in (1, 128):
@@ -711,17 +719,19 @@ def nq_fp8_gemm(a: torch.Tensor, sa: torch.Tensor, b: torch.Tensor, sb: torch.Te
     M, K = a.shape
     N = b.shape[0]
     groups, sb_cols = (K + 127) // 128, -(-N // b_block_rows)
+    index = a.get_device()
     if (K & 15 == 0 and a.is_contiguous() and b.is_contiguous() and sa.is_contiguous() and sb.is_contiguous() and sa.dtype is f32
-            and sb.dtype is f32 and sa.shape == (groups, M) and sb.shape == (groups, sb_cols) and a.is_cuda and b.is_cuda and sa.is_cuda and sb.is_cuda):
+            and sb.dtype is f32 and sa.shape == (groups, M) and sb.shape == (groups, sb_cols)
+            and b.get_device() == sa.get_device() == sb.get_device() == index >= 0):
         lda = ldb = K                                    # dense throughout: a call of few microseconds checks no further
         ldsa, ldsb = M, sb_cols
     else:
-        lda, ldb = _fp8_ld(a, "a"), _fp8_ld(b, "b")
-        ldsa, ldsb = _scales(sa, "sa", groups, M), _scales(sb, "sb", groups, sb_cols)
+        lda, ldb = _fp8_ld(a, "a", index), _fp8_ld(b, "b", index)
+        ldsa, ldsb = _scales(sa, "sa", index, groups, M), _scales(sb, "sb", index, groups, sb_cols)
     device = a.device
     if y_out is not None:
         y = y_out
-        ldy = _matrix(y, "y_out", None, (M, N))
+        ldy = _matrix(y, "y_out", index, None, (M, N))
     else:
         if accumulate:
             raise ValueError("accumulate needs y_out")
@@ -730,29 +740,31 @@ def nq_fp8_gemm(a: torch.Tensor, sa: torch.Tensor, b: torch.Tensor, sb: torch.Te
     if y.dtype not in _FLOATS:
         raise ValueError(f"the output must be float32 or bfloat16, got {y.dtype}")
     _check(lib().nq_fp8_gemm(a.data_ptr(), lda, sa.data_ptr(), ldsa, b.data_ptr(), ldb, sb.data_ptr(), ldsb, b_block_rows,
-                             _vector(bias, "bias", N), M, N, K, y.data_ptr(), ldy, _FLOATS[y.dtype], accumulate,
+                             _vector(bias, "bias", N, index), M, N, K, y.data_ptr(), ldy, _FLOATS[y.dtype], accumulate,
                              _raw_stream(a)), "nq_fp8_gemm")
     return y
 
 
 # --------------------------------------------------------------------------- block norm
-def _vector(t: Optional[torch.Tensor], name: str, cols: int):
+def _vector(t: Optional[torch.Tensor], name: str, cols: int, index: int):
     if t is None:
         return None
-    if t.dtype is not torch.float32 or t.dim() != 1 or t.numel() != cols or not t.is_cuda or not t.is_contiguous():
+    if t.dtype is not torch.float32 or t.dim() != 1 or t.numel() != cols or not t.is_contiguous():
         raise ValueError(f"{name} must be a dense float32 CUDA vector of {cols}")
+    _on(t, name, index)
     return t.data_ptr()
 
 
-def _norm_check(rows, cols, gate, rows_per_gate, post, pre):
+def _norm_check(rows, cols, gate, rows_per_gate, post, pre, index):
     if not (0 <= post <= 2 and 0 <= pre <= 2):
         raise ValueError("post and pre are NQ_NORM_NONE, NQ_NORM_RMS or NQ_NORM_LAYER")
     if rows_per_gate < 0:
         raise ValueError("rows_per_gate must not be negative")
     if gate is not None:
         need = -(-rows // rows_per_gate) if rows_per_gate else 1
-        if gate.dtype != torch.float32 or not gate.is_cuda or not gate.is_contiguous() or gate.shape != (need, cols):
+        if gate.dtype != torch.float32 or not gate.is_contiguous() or gate.shape != (need, cols):
             raise ValueError(f"gate must be a dense float32 CUDA tensor [{need}, {cols}]")
+        _on(gate, "gate", index)
 
 
 def _norm_types(x: torch.Tensor, y: Optional[torch.Tensor], names) -> None:
@@ -774,18 +786,19 @@ def nq_block_norm(x: torch.Tensor, y: Optional[torch.Tensor] = None, *, post: in
     x, r: the residual stream [rows, cols]; y: the block's output, None for the plain norm of x (then r is returned only
     when want_r).  gate: [1, cols], or one row for each rows_per_gate rows.  h_dtype: float32, bfloat16 (default: y's
     type, without y x's), float8_e4m3fn (hs: its scales, groups first) or int8 (static scale h_scale).  r_out may be x."""
-    ldx = _matrix(x, "x")
+    index = x.get_device()
+    ldx = _matrix(x, "x", index)
     _norm_types(x, y, ("x", "y"))
     rows, cols = x.shape
     device = x.device
-    _norm_check(rows, cols, gate, rows_per_gate, post, pre)
+    _norm_check(rows, cols, gate, rows_per_gate, post, pre, index)
     y_type = x.dtype if y is None else y.dtype
-    ldy = 0 if y is None else _matrix(y, "y", shape=x.shape)
+    ldy = 0 if y is None else _matrix(y, "y", index, shape=x.shape)
     r = h = hs = r_ptr = h_ptr = hs_ptr = None
     ldr = ldh = h_code = 0
     if r_out is not None:
         r = r_out
-        ldr = _matrix(r, "r_out", x.dtype, x.shape)
+        ldr = _matrix(r, "r_out", index, x.dtype, x.shape)
         r_ptr = r.data_ptr()
     elif want_r or (want_r is None and y is not None):
         r, ldr = _new(rows, cols, x.dtype, device), cols
@@ -805,9 +818,9 @@ def nq_block_norm(x: torch.Tensor, y: Optional[torch.Tensor] = None, *, post: in
     d = nq_block_norm_desc(rows, cols, ldx, ldy, ldr, ldh, 0, 0, 0, 0, rows_per_gate, _FLOATS[x.dtype], _FLOATS[y_type], h_code,
                            post, pre, skip_scale, branch_scale, eps, h_scale)
     _check(lib().nq_block_norm(ctypes.addressof(d), x.data_ptr(), None if y is None else y.data_ptr(),
-                               _vector(post_weight, "post_weight", cols), _vector(post_bias, "post_bias", cols),
-                               None if gate is None else gate.data_ptr(), _vector(pre_weight, "pre_weight", cols),
-                               _vector(pre_bias, "pre_bias", cols), r_ptr, h_ptr, hs_ptr, rows, _raw_stream(x)), "nq_block_norm")
+                               _vector(post_weight, "post_weight", cols, index), _vector(post_bias, "post_bias", cols, index),
+                               None if gate is None else gate.data_ptr(), _vector(pre_weight, "pre_weight", cols, index),
+                               _vector(pre_bias, "pre_bias", cols, index), r_ptr, h_ptr, hs_ptr, rows, _raw_stream(x)), "nq_block_norm")
     return r, h, hs
 
 
@@ -825,7 +838,8 @@ def nq_block_norm_backward(r: torch.Tensor, y: Optional[torch.Tensor] = None, *,
     """Gradients of nq_block_norm from the r and y of the forward pass and the gradients dr, dh of its outputs (dh in
     y's type, without y in any that goes with x; one of the two may be None).
     -> (dx, dy, dgate, dpost_weight, dpost_bias, dpre_weight, dpre_bias), None for each input that was absent."""
-    ldr = _matrix(r, "r")
+    index = r.get_device()
+    ldr = _matrix(r, "r", index)
     rows, cols = r.shape
     device = r.device
     like = y if y is not None else dh if dh is not None else r
@@ -834,11 +848,11 @@ def nq_block_norm_backward(r: torch.Tensor, y: Optional[torch.Tensor] = None, *,
         raise ValueError("dh goes with the pre norm: give both or neither")
     if dr is None and dh is None:
         raise ValueError("give dr, dh or both")
-    _norm_check(rows, cols, gate, rows_per_gate, post, pre)
+    _norm_check(rows, cols, gate, rows_per_gate, post, pre, index)
     y_type = like.dtype
-    ldy = 0 if y is None else _matrix(y, "y", shape=r.shape)
-    lddr = 0 if dr is None else _matrix(dr, "dr", r.dtype, r.shape)
-    lddh = 0 if dh is None else _matrix(dh, "dh", y_type, r.shape)
+    ldy = 0 if y is None else _matrix(y, "y", index, shape=r.shape)
+    lddr = 0 if dr is None else _matrix(dr, "dr", index, r.dtype, r.shape)
+    lddh = 0 if dh is None else _matrix(dh, "dh", index, y_type, r.shape)
     d = nq_block_norm_desc(rows, cols, 0, ldy, ldr, 0, cols, cols, lddr, lddh, rows_per_gate, _FLOATS[r.dtype], _FLOATS[y_type], 0,
                            post, pre, skip_scale, branch_scale, eps, 0.0)
     dx = _new(rows, cols, r.dtype, device)
@@ -848,12 +862,17 @@ def nq_block_norm_backward(r: torch.Tensor, y: Optional[torch.Tensor] = None, *,
     if workspace is None:
         need = nq_block_norm_backward_workspace_bytes(d, gate is not None)
         workspace = torch.empty_strided((max(need, 16),), (1,), dtype=torch.uint8, device=device)
+    else:
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        _on(workspace, "workspace", index)
     ptr = lambda t: None if t is None else t.data_ptr()
-    _vector(pre_bias, "pre_bias", cols)
+    _vector(pre_bias, "pre_bias", cols, index)
     _check(lib().nq_block_norm_backward(
-        ctypes.addressof(d), r.data_ptr(), ptr(y), ptr(dr), ptr(dh), _vector(post_weight, "post_weight", cols),
-        _vector(post_bias, "post_bias", cols), ptr(gate), _vector(pre_weight, "pre_weight", cols), dx.data_ptr(), ptr(dy),
-        ptr(dgate), *map(ptr, vec), workspace.data_ptr(), workspace.numel(), _raw_stream(r)), "nq_block_norm_backward")
+        ctypes.addressof(d), r.data_ptr(), ptr(y), ptr(dr), ptr(dh), _vector(post_weight, "post_weight", cols, index),
+        _vector(post_bias, "post_bias", cols, index), ptr(gate), _vector(pre_weight, "pre_weight", cols, index), dx.data_ptr(), ptr(dy),
+        ptr(dgate), *map(ptr, vec), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+        _raw_stream(r)), "nq_block_norm_backward")
     return dx, dy, dgate, vec[0], vec[1], vec[2], vec[3]
 
 
