@@ -27,3 +27,28 @@ def test_bias_of_each_tile(M, N, K, block):
     y = nq.nq_fp8_gemm(a, sa, b, sb, b_block_rows=block, bias=bias)
     assert torch.equal(y, want.float().to(torch.bfloat16))
     nq.nq_device_status()
+
+
+@pytest.mark.parametrize("block", [1, 128])
+@pytest.mark.parametrize("bias", [False, True])
+def test_scales_that_are_no_numbers(block, bias):
+    """A NaN or infinite scale shows in its row, or in the columns of its block, and nowhere else."""
+    M, N, K = 2000, 2304, 640
+    a, sa, b, sb = operands(M, N, K, block)
+    want, _ = definition(a, sa, b, sb, block)
+    add = (torch.arange(N, device="cuda") % 17).float() if bias else None
+    want = want if add is None else want + add.double()
+    sa[2, 1500], sa[0, 127], sa[4, 1999] = float("nan"), float("inf"), float("nan")
+    at = 2 if block == 128 else 300
+    sb[1, at], sb[3, -1] = float("inf"), float("nan")
+    columns = torch.zeros(N, dtype=torch.bool, device="cuda")
+    columns[at * block:(at + 1) * block] = True
+    columns[(sb.shape[1] - 1) * block:] = True
+    rows = torch.zeros(M, dtype=torch.bool, device="cuda")
+    rows[[127, 1500, 1999]] = True
+    for dtype in (torch.float32, torch.bfloat16):
+        y = nq.nq_fp8_gemm(a, sa, b, sb, b_block_rows=block, bias=add, y_dtype=dtype)
+        assert torch.equal(~torch.isfinite(y), rows[:, None] | columns[None, :])
+        good = (~rows[:, None] & ~columns[None, :])
+        assert torch.equal(y[good], want.float().to(dtype)[good])
+    nq.nq_device_status()
