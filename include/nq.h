@@ -385,7 +385,9 @@ NQ_API int nq_fp8_gemm(const void *A, int64_t lda, const float *SA, int64_t ldsa
  *     NQ_I8             the activations of the INT8 layers: clip(round_half_even(fl(h * fl(1 / h_scale))), -128, 127), a
  *                       NaN as 0; ldh a multiple of 16, H 16-byte aligned
  *   Any other tensor may have any element alignment and pitch (16-byte aligned rows with cols a multiple of 8 are
- *   fastest).  cols in [1, 16384].
+ *   fastest).  cols in [1, 16384].  Rows of X and Y that do not start or end on 16 bytes may be read as the aligned
+ *   16-byte granules that hold them: up to 14 bytes on either side of a row are fetched and ignored.  They must be
+ *   readable, which the granules of any device allocation are.  The backward pass reads R, Y, dR and dH likewise.
  */
 enum { NQ_NORM_NONE = 0, NQ_NORM_RMS = 1, NQ_NORM_LAYER = 2 };
 typedef struct {

@@ -39,8 +39,9 @@ __device__ __forceinline__ float norm_factor(const Cols<NV, VEC>& c, Row<NV>& v,
 // out -- and the latency of a row's two to four joins.  So arithmetic is on pairs, and where blocks work through many
 // rows (RING) they come through a ring in shared memory; the parameters stay in registers, the post norm's weight, the gate
 // and the branch scale as one factor that changes only with the gate's row.  Otherwise rows are loaded when their turn
-// comes.  16384 x 8192, bf16 to e4m3: 475 us without all that, 398 with a ring, 224 with all (4.2 TB/s).  Tried: parameters in
-// shared memory and several teams of 16 columns a thread in a block: no room for rows enough (514 us).
+// comes.  16384 x 8192, bf16 to e4m3: 475 us without all that, 398 with a ring, 223 with all (4.2 TB/s).  16384 x 4096, bf16 to
+// e4m3 114 us, to INT8 110, to bf16 97, to fp32 124; 12608 x 768, fp32 stream, layer norms, a gate row for 197 rows, to INT8 32.
+// Tried: parameters in shared memory and several teams of 16 columns a thread in a block: no room for rows enough (514 us).
 // BIAS: one of the norms has a bias.
 template <typename TX, typename TY, int NV, bool VEC, bool RING, bool BIAS>
 __global__ void __launch_bounds__(NV == 1 ? 1024 : 512) block_norm_kernel(const NormArgs p, int threads) {
@@ -232,8 +233,10 @@ int launch_norm_plain(const NormArgs& a, const Shape& sh, bool vec, cudaStream_t
 template <typename TX, typename TY, bool BIAS>
 int launch_norm_bias(NormArgs& a, bool vec, cudaStream_t stream) {
     const Shape wide = wide_shape(a.cols, 1024);
-    // The ring is worth filling from two rows a block on; a warp to a row (up to 256) has enough loads in flight by itself
-    // (50000 x 200: 27 us).
+    // The ring is worth filling from two rows a block on (us with / without, bf16 to e4m3, in a graph: 768 columns, 740 rows
+    // 4.1 / 3.7, 1480 4.7 / 5.0, 2960 -- two rows a block -- 7.2 / 8.8, 5920 12.2 / 15.3; 4096 columns, 148 rows 4.3 / 4.1,
+    // 296 4.5 / 5.1, 592 -- two a block -- 6.8 / 9.5, 2368 20.7 / 24.5); a warp to a row (up to 256) has enough loads in flight
+    // by itself (50000 x 200: 27 us).
     if (wide.threads > 32) {
         a.stage_bytes = row_slot(a.cols * (int)sizeof(TX), vec) + (a.y ? row_slot(a.cols * (int)sizeof(TY), vec) : 0);
         // both instantiations are bound to the registers that fill an SM: 64 at 1024 threads, 128 at 512

@@ -34,6 +34,11 @@ struct BackArgs {
 // Measured: 16384 x 4096 bf16 218 us (3.7 TB/s; 524 with one join for each sum and no ring), 12608 x 768 fp32 stream 74 us,
 // 10 of them joining the blocks' sums.  Bound by issue and by the joins: half of the issue slots are used at four warps a
 // scheduler, which the accumulators' registers allow.  (Parameters read for each row instead of held: 330 - 380 us.)
+// Short groups: 12608 x 768 with a gate row for each row 262 us, for 8 rows 104, for 64 92 (the ring starts anew with each item,
+// and an item's share of the post norm's sums goes to memory).
+// Wide rows do not fit the registers, of which a thread has 128: at 2 pieces a thread (4097 to 8192 columns) a frame of 112 - 320
+// bytes is spilled, at 4 pieces, whose four accumulators alone take 128, 0.7 KB (rows that start anywhere: 1.4).  bf16, RMS /
+// layer norm: 16384 x 5000 401 / 657 us (150 at HBM rate), 16384 x 8192 474 / 759 (246), 8192 x 16384 1495 / 1718 (246).
 template <typename TX, typename TY, int NV, bool VEC, bool RING, bool BIAS>
 __global__ void __launch_bounds__(512) block_norm_backward_kernel(const BackArgs p, int threads) {
     constexpr bool HOLD = NV <= 2;
@@ -341,6 +346,15 @@ struct BackPlan {
 };
 // The workspace is sized before the pointers are known, so the plan goes by the shape and types alone (stages have room
 // for rows that start anywhere).
+// The ring from four rows a block on, and four rows an item at least, measured in a graph with one gate row (us):
+//   768 columns, layer norms, fp32 stream
+//     with / without the ring: 1024 rows 26.2 / 29.2, 2048 31.7 / 34.4, 2960 (four a block) 43.6 / 38.6, 4096 39.7 / 57.9, 8192 54 / 82
+//     items of 1 / 2 / 4 / 8 rows: 64 rows 12.9 / 13.5 / 15.9 / 22.9, 256 19.3 / 17.5 / 20.6 / 29.3, 1024 39.8 / 28.3 / 29.2 / 36.9
+//   4096 columns, RMS, bf16
+//     with / without the ring: 32 rows 19.8 / 22.6, 296 23.4 / 29.3, 592 (four a block) 25.3 / 30.5, 1184 32.4 / 55.3
+//     items of 1 / 2 / 4 / 8 rows: 32 rows 15.7 / 17.5 / 22.5 / 32.1, 128 19.0 / 21.7 / 26.9 / 39.8, 296 33.2 / 23.4 / 29.1 / 41.9
+// The ring gains below that too with wide rows, and two rows an item are up to a quarter faster up to some hundred rows: the
+// bounds are on the safe side of that, not at the best place for each width.
 BackPlan plan_backward(const nq_block_norm_desc* d, bool has_gate) {
     BackPlan p;
     p.group_rows = has_gate && d->rows_per_gate > 0 ? d->rows_per_gate : (d->rows > 0 ? d->rows : 1);

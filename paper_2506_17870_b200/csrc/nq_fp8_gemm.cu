@@ -65,8 +65,9 @@ __device__ __forceinline__ float half_of(uint64_t v, int which) {
 
 // ------------------------------------------------------------------------------------------------------ tile kernel
 constexpr int kTileThreads = 192;        // warp 0 TMA, warp 1 MMA and TMEM, warps 2-5 promotion (a 32-lane quarter each)
-// Bound by latencies: 1 x 4096 x 4096 takes 7 us of which the weights' 17 MB are 2.6 at HBM rate, 37 x 8192 x 4096 11.6 us
-// (5.2): launch, tensor memory, the first loads, and the two cluster barriers of the join.
+// Bound by latencies: 1 x 4096 x 4096 takes 7.2 us of which the weights' 17 MB are 2.6 at HBM rate (6.1 with the weights in L2),
+// 37 x 8192 x 4096 11.7 us (5.2; 11.0 from L2), in a graph: launch, tensor memory, the first loads, and the two cluster barriers
+// of the join.
 template <int NT>
 struct TileShape {
     static constexpr int kStageBytes = (128 + NT) * kGroup;
@@ -295,16 +296,19 @@ fp8_tile_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
 // half of B (32 KB a group of K) and gets 128 x 128 sums a half; four such buffers fill its tensor memory.  What bounds the
 // rate is the hand-over of a buffer -- commit, promotion warps in BOTH CTAs read it, their signal travels to the
 // leader's MMA thread: about a thousand cycles, against 512 in which the tensor core computes a group of 256 x 256.  With
-// two buffers of 256 columns the tensor core waited for it every group; with four of 128 it has three others to fill
-// meanwhile, at the price of reading A from shared memory twice.
+// two buffers of 256 columns the tensor core waited for it every group (735 us for 8192^3, in a kernel that had neither the
+// promotion warps of a half, nor two issuing threads, nor packed arithmetic yet; not tried again with them); with four of 128
+// it has three others to fill meanwhile, at the price of reading A from shared memory twice.
 // Eight promotion warps, two to a scheduler, one for each half: a warp reads 32 rows x 128 columns in four loads of 32, two in
 // flight, and adds them to 128 accumulators a thread.  The two warps of a scheduler work half a group apart, so that the
 // FMAs of one fall into the waits of the other (both on the same half, 64 columns each, they waited together: 8192^3 took
 // 656 us; sixteen warps of 64 accumulators have no registers to take in what they add: 637 us).
-// Measured: 8192^3 520 us as a burst (2.1 PFLOP/s), 600 us back to back, where the power limit holds the clock near 1.5 GHz;
-// 4096 x 4096 x 12608 with row scales 370 us.  Without the FMAs the same kernel takes 430 us, without reading tensor memory
-// either 430: what is left is the promotion's own time, 256 FMA cycles a scheduler and group (512 with row scales, which
-// multiply twice) plus the waits that two warps cannot cover.
+// Measured: 8192^3 545 - 590 us one call at a time (1.9 - 2.0 PFLOP/s), 612 - 622 us back to back, where the power limit holds the
+// clock near 1.5 GHz; 4096 x 4096 x 12608 with row scales 378 us in a graph, 400 - 405 by calls.  When 8192^3 took 520 - 536 us as
+// a burst, the kernel without the FMAs took 430, and 430 without reading tensor memory either, where the products alone should
+// take 339: that part is the tensor side's own, probably A read twice, and the rest the promotion's, 256 FMA cycles a
+// scheduler and group (512 with row scales, which multiply twice) plus the waits that two warps cannot cover.  Adding to what Y
+// holds (accumulate) goes by ordinary loads and stores: 4096 x 4096 x 12608 606 us, 768 x 768 x 2048 12.3 against 9.2.
 // Barriers (at the same offsets in both CTAs): full[s] in the leader counts the bytes of both CTAs' loads; done[s][h], in
 // each CTA, is arrived on by the commit of half h of the group in stage s: it hands the sums to the promotion warps, and
 // both halves together free the stage for the producer (a waiter is never more than one phase behind: the next use of the

@@ -78,8 +78,10 @@ __device__ __forceinline__ void store_bytes(uint8_t* dst, uint4 v, int n) {
 // One thread block per 128 x 128 tile: a tile holds whole groups in both directions, so the matrix is read once
 // however many outputs are wanted.  Thread t holds rows 4 * (t / 8) + {0..3}, columns 16 * (t % 8) + {0..15}: 32 (fp32:
 // 64) contiguous bytes a row to load, 16 to store, and for the transpose four rows of a column make one 32-bit word.
-// 16384 x 8192 bf16 both ways: 88 us, 6.1 TB/s (0.93 of the measured copy rate; 117 us with scalar products and column maxima by
-// shared-memory atomics); one way 61 us.  Bound by HBM.
+// 16384 x 8192 bf16 both ways: 87 us replayed from a graph, 6.3 TB/s (0.96 of the measured copy rate), 97 - 98 us by calls that
+// each take fresh outputs (0.85); 117 us at first, with scalar products and column maxima by shared-memory atomics; one way
+// 61 us.  Bound by HBM.  Rows that start off 32 bytes (!ALIGNED) come element by element: 16384 x 5001 both ways 184 us in fp32
+// and 97 us in bf16, against 75 and 50 at HBM rate.
 // The transposed tile is put together in shared memory, its 16-byte pieces rotated by column / 16 so that neither
 // the word writes (8 column groups x 4 row groups a warp) nor the 16-byte reads meet bank conflicts.
 template <typename T, bool BLOCK, bool ALIGNED>
