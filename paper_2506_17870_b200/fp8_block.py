@@ -153,10 +153,8 @@ class MlpBlock(torch.nn.Module):
 
     def __setstate__(self, state):
         super().__setstate__(state)
-        current, self._served_from = self._served_from, None
-        if current:
-            self._served_from = self._weights()
-        else:
+        self._served_from = self._weights() if state.get("_served_from") else None
+        if self._served_from is None:
             self.served = None
 
     @torch.no_grad()

@@ -202,6 +202,12 @@ def test_copies_of_a_laid_out_stack(tmp_path):
             twin.serve(x)
         with pytest.raises(RuntimeError):
             copy.deepcopy(twin).serve(x)
+    state = stack.blocks[0].__getstate__()
+    del state["_served_from"]                                      # a block that was stored without it
+    stored = fb.MlpBlock.__new__(fb.MlpBlock)
+    stored.__setstate__(state)
+    with pytest.raises(RuntimeError):
+        stored.serve(torch.zeros(1, 128, device="cuda").to(torch.float8_e4m3fn), torch.ones(1, 1, device="cuda"))
     assert torch.equal(stack.serve(x), want)
     with torch.inference_mode():
         assert torch.equal(stack.serve(x), want)
