@@ -423,6 +423,87 @@ NQ_API int nq_block_norm_backward(const nq_block_norm_desc *desc, const void *R,
                            float *dpre_weight, float *dpre_bias, void *workspace, int64_t workspace_bytes, void *stream);
 
 /*
+ * Attention of a served transformer: heads normed and rotated, their keys and values in a paged cache, one new token or whole
+ * prompts attending to them.  (The paper has no counterpart; definitions are the library's own.)  Heads have 64 or 128 values;
+ * kv_heads key and value heads serve q_heads query heads, a multiple: query head h reads key head h / (q_heads / kv_heads).
+ *
+ * The cache.  A page holds page_size tokens (a multiple of 16, at most 32768); k and v are [pages, kv_heads, page_size, head_dim],
+ * dense, 16-byte aligned, of dtype NQ_BF16, NQ_E4M3 or NQ_I8.  The latter two have fp32 scales ks, vs [pages, kv_heads, page_size]
+ * (NULL for NQ_BF16), one for each token and head:
+ *   a = max |x|;  s = max(fl(a / most), 2^-126), most = 448 or 127;  i = fl(1 / s)
+ *   code = e4m3_nearest_even(clip(fl(x * i), -448, 448))  or  clip(round_half_even(fl(x * i)), -127, 127);  it is worth code * s
+ *   A head that holds a NaN gets scale NaN, one that holds an infinity gets +inf: its values read as NaN.
+ * A token's SLOT is page * page_size + its place in the page.  pages * page_size < 2^31.  Sequences are told apart by a TABLE
+ * [sequences, columns] (pitch ld_table) of page numbers: token t of sequence s is in page table[s, t / page_size], at place
+ * t % page_size.  Page numbers, slots, lengths and starts are int32 in device memory and read when the kernels run: nothing on
+ * the host depends on them, a captured call follows their values.  A page number or slot outside the cache is never accessed:
+ * what was to be written there is dropped, and what was to be read there counts as hidden (nq_paged_attention) or as zeros
+ * (nq_kv_cache_read).
+ */
+typedef struct {
+    void *k, *v;
+    float *ks, *vs;
+    int64_t pages;
+    int32_t page_size, kv_heads, head_dim, dtype;
+} nq_kv_pages;
+
+/*
+ * Norm of queries and keys for each head, and the rotation by position, in one pass; keys and values may go straight to the cache.
+ *   X (device) [tokens, (q_heads + kv_heads) * head_dim], with a cache [tokens, (q_heads + 2 kv_heads) * head_dim], of x_dtype
+ *     (NQ_F32, NQ_BF16), pitch ldx: a fused projection's rows, queries | keys | values
+ *   norm: NQ_NORM_RMS  u = x / sqrt(mean(x^2) + eps) * weight, with weights (device) fp32 [head_dim] or NULL (1); NQ_NORM_NONE  u = x
+ *   The first rotary_dim values (a multiple of 16, at most head_dim, may be 0) are turned in pairs by the angles of the token's
+ *     position:  (a, b) -> (a cos - b sin, b cos + a sin).  Pair i is values i and i + rotary_dim / 2, or with `neighbours` != 0
+ *     values 2 i and 2 i + 1.  angles (device) fp32 [angle_rows, rotary_dim], dense: a position's cosines, then its sines;
+ *     positions (device) int32 [tokens].  A position outside the table turns those values into NaN.
+ *   Arithmetic is fp32, with one rounding to the output's type (or the cache's).  Values are neither normed nor turned.
+ *   Q (device, out) [tokens, q_heads * head_dim] of y_dtype (NQ_F32, NQ_BF16), pitch ldq; with X's type and pitch it may be X's own
+ *     queries (in place).  K (device, out) likewise, pitch ldk, may be NULL where there is a cache.
+ *   cache (host struct of device pointers) and slots (device) int32 [tokens], or both NULL.  A slot outside the cache: the token is
+ *     not stored.  A slot that is named twice holds one of its tokens or a mixture.
+ *   X, Q, K, weights, angles 16-byte aligned, pitches multiples of 16 bytes.
+ */
+typedef struct {
+    int64_t tokens, ldx, ldq, ldk, angle_rows;
+    int32_t x_dtype, y_dtype, q_heads, kv_heads, head_dim, rotary_dim, norm, neighbours;
+    float eps;
+} nq_qk_desc;
+NQ_API int nq_qk_norm_rotate(const nq_qk_desc *desc, const void *X, const float *q_weight, const float *k_weight, const float *angles,
+                             const int32_t *positions, void *Q, void *K, const nq_kv_pages *cache, const int32_t *slots, void *stream);
+
+/*
+ * Keys and values into the cache, quantised as it holds them: K, V (device) [tokens, kv_heads * head_dim] of x_dtype (NQ_F32,
+ * NQ_BF16), pitches ldk, ldv (multiples of 16 bytes, 16-byte aligned); slots as above.
+ */
+NQ_API int nq_kv_cache_write(const nq_kv_pages *cache, const void *K, int64_t ldk, const void *V, int64_t ldv, int x_dtype,
+                             const int32_t *slots, int64_t tokens, void *stream);
+
+/*
+ * ... and back, as packed rows: token t of sequence s to row starts[s] + t of K, V (device, out) [rows, kv_heads * head_dim] of
+ * y_dtype (NQ_F32, NQ_BF16).  starts (device) int32 [seqs + 1], not decreasing: sequence s has starts[s + 1] - starts[s] tokens.
+ * Rows before starts[0] and from starts[seqs] on are left as they were; starts past `rows` are not followed.
+ */
+NQ_API int nq_kv_cache_read(const nq_kv_pages *cache, const int32_t *table, int64_t ld_table, int64_t table_cols, const int32_t *starts,
+                            int64_t seqs, void *K, int64_t ldk, void *V, int64_t ldv, int y_dtype, int64_t rows, void *stream);
+
+/*
+ * Attention of one new token a sequence over the cache (which holds the token itself, if it is to see itself):
+ *   y_h = sum_t w_t v_t,  w = softmax over t of (scale * q_h . k_t),  t in [max(0, n - window), n), n = min(lengths[s], what the
+ *   table's columns hold); window == 0: all of them.
+ *   A sequence that sees nothing (n <= 0, or no page in the cache), or whose scores are all -infinity, gets zeros.
+ *   Q (device) bf16 [seqs, q_heads * head_dim], pitch ldq; Y (device, out) likewise, pitch ldy (multiples of 8, 16-byte aligned)
+ *   table (device) int32 [seqs, table_cols], lengths (device) int32 [seqs]
+ *   Sums, maxima and weights are fp32.  A weight is rounded to bf16 (bf16 cache) or f16 (8-bit caches, times the value's scale)
+ *   for its product with the values, which is exact in both; queries meet 8-bit keys as f16, scaled by a power of two.
+ *   workspace (device) nq_paged_attention_workspace_bytes() bytes, 16-byte aligned: parts of sequences that several thread blocks
+ *   share.  Two calls that may run at the same time need two.  No atomics: results repeat bit for bit.
+ */
+NQ_API int64_t nq_paged_attention_workspace_bytes(const nq_kv_pages *cache, int64_t q_heads, int64_t seqs, int64_t table_cols);
+NQ_API int nq_paged_attention(const nq_kv_pages *cache, const void *Q, int64_t ldq, int64_t q_heads, const int32_t *table, int64_t ld_table,
+                              int64_t table_cols, const int32_t *lengths, int64_t seqs, int window, float scale, void *Y, int64_t ldy,
+                              void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
  * The convolution again, for callers that must not allocate.  (The paper has no counterpart; this is a
  * convenience of the library.)  nq_conv_implicit_gemm needs a workspace whenever it re-lays the input
  * (NCHW activations, or a channel count it cannot gather in place), and somebody has to allocate that.

@@ -34,6 +34,7 @@ EXPORTS = (
     "nq_i8_mma_ceiling", "nq_debug_set",
     "nq_conv_implicit_gemm_q8_res", "nq_conv_implicit_gemm_nested_q8_res", "nq_maxpool_nhwc_i8", "nq_avgpool_requant_nhwc_i8",
     "nq_fp8_quantize", "nq_fp8_gemm", "nq_block_norm", "nq_block_norm_backward", "nq_block_norm_backward_workspace_bytes",
+    "nq_qk_norm_rotate", "nq_kv_cache_write", "nq_kv_cache_read", "nq_paged_attention", "nq_paged_attention_workspace_bytes",
     "nq_device_status",
 )
 
@@ -65,6 +66,12 @@ class nq_block_norm_desc(ctypes.Structure):
                 [(k, ctypes.c_float) for k in ("skip_scale", "branch_scale", "eps", "h_scale")])
 
 
+class nq_qk_desc(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_int64) for k in ("tokens", "ldx", "ldq", "ldk", "angle_rows")] +
+                [(k, ctypes.c_int32) for k in ("x_dtype", "y_dtype", "q_heads", "kv_heads", "head_dim", "rotary_dim", "norm", "neighbours")] +
+                [("eps", ctypes.c_float)])
+
+
 # Argument types of the entry points whose calls pass plain numbers: a call of a few microseconds is not spent on
 # wrapping each of them.
 _P, _L, _I, _F = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_float
@@ -74,6 +81,11 @@ _ARGTYPES = {
     "nq_block_norm": (_P,) * 11 + (_L, _P),
     "nq_block_norm_backward": (_P,) * 17 + (_L, _P),
     "nq_block_norm_backward_workspace_bytes": (_P, _I),
+    "nq_qk_norm_rotate": (_P,) * 11,
+    "nq_kv_cache_write": (_P, _P, _L, _P, _L, _I, _P, _L, _P),
+    "nq_kv_cache_read": (_P, _P, _L, _L, _P, _L, _P, _L, _P, _L, _I, _L, _P),
+    "nq_paged_attention": (_P, _P, _L, _L, _P, _L, _L, _P, _L, _I, _F, _P, _L, _P, _L, _P),
+    "nq_paged_attention_workspace_bytes": (_P, _L, _L, _L),
 }
 
 
@@ -91,7 +103,7 @@ def lib() -> ctypes.CDLL:
             raise NqLibraryError(f"cannot load {_LIB_PATH}: {e}") from e
         L.nq_status_str.restype = ctypes.c_char_p
         for name in ("nq_packed_row_bytes", "nq_packed_bytes", "nq_batch_table_bytes", "nq_conv_workspace_bytes",
-                     "nq_word64_row_words", "nq_block_norm_backward_workspace_bytes"):
+                     "nq_word64_row_words", "nq_block_norm_backward_workspace_bytes", "nq_paged_attention_workspace_bytes"):
             getattr(L, name).restype = ctypes.c_int64
         for name, types in _ARGTYPES.items():
             getattr(L, name).argtypes = types
@@ -874,6 +886,187 @@ def nq_block_norm_backward(r: torch.Tensor, y: Optional[torch.Tensor] = None, *,
         ptr(dgate), *map(ptr, vec), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
         _raw_stream(r)), "nq_block_norm_backward")
     return dx, dy, dgate, vec[0], vec[1], vec[2], vec[3]
+
+
+# --------------------------------------------------------------------------- attention of a served transformer
+_CACHE_TYPES = {torch.bfloat16: NQ_BF16, torch.float8_e4m3fn: NQ_E4M3, torch.int8: NQ_I8}
+
+
+class nq_kv_pages(ctypes.Structure):
+    """A paged key-value cache: k, v [pages, kv_heads, page_size, head_dim] bf16, float8_e4m3fn or int8, dense; the latter two with
+    fp32 scales ks, vs [pages, kv_heads, page_size].  Holds on to the tensors; made once for a cache, it costs its calls nothing."""
+    _fields_ = ([(k, ctypes.c_void_p) for k in ("k", "v", "ks", "vs")] + [("pages", ctypes.c_int64)] +
+                [(k, ctypes.c_int32) for k in ("page_size", "kv_heads", "head_dim", "dtype")])
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, ks: Optional[torch.Tensor] = None, vs: Optional[torch.Tensor] = None):
+        code = _CACHE_TYPES.get(k.dtype)
+        if code is None:
+            raise ValueError(f"a cache is bfloat16, float8_e4m3fn or int8, got {k.dtype}")
+        if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype:
+            raise ValueError(f"k and v must be [pages, kv_heads, page_size, head_dim] of one type, got {list(k.shape)} {k.dtype} and {list(v.shape)} {v.dtype}")
+        if (code == NQ_BF16) != (ks is None) or (code == NQ_BF16) != (vs is None):
+            raise ValueError("ks and vs go with a float8_e4m3fn or int8 cache")
+        index = k.get_device()
+        shape = k.shape
+        for name, t in (("k", k), ("v", v), ("ks", ks), ("vs", vs)):
+            if t is None:
+                continue
+            _on(t, name, index)
+            if name in ("ks", "vs") and (t.dtype is not torch.float32 or t.shape != shape[:3]):
+                raise ValueError(f"{name} must be float32 {list(shape[:3])}, got {t.dtype} {list(t.shape)}")
+            if not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous")
+        super().__init__(k.data_ptr(), v.data_ptr(), None if ks is None else ks.data_ptr(), None if vs is None else vs.data_ptr(),
+                         shape[0], shape[2], shape[1], shape[3], code)
+        self.tensors, self.index = (k, v, ks, vs), index
+
+
+def _pages_on(cache: nq_kv_pages, index: int) -> int:
+    if cache.index != index:
+        raise ValueError(f"the cache is on cuda:{cache.index}, the first operand on {'the host' if index < 0 else f'cuda:{index}'}")
+    return ctypes.addressof(cache)
+
+
+def _ints(t: torch.Tensor, name: str, count: int, index: int) -> int:
+    if t.dtype is not torch.int32 or t.dim() != 1 or t.shape[0] != count or not t.is_contiguous():
+        raise ValueError(f"{name} must be a dense int32 CUDA vector of {count}")
+    _on(t, name, index)
+    return t.data_ptr()
+
+
+def _heads(t: torch.Tensor, name: str, index: int, heads: int, dim: int) -> int:
+    """Checks [tokens, heads, dim] on the GPU of this index, a token's heads dense; -> its pitch of tokens."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
+        raise ValueError(f"{name} must be [tokens, {heads}, {dim}], got {list(t.shape)}")
+    _on(t, name, index)
+    ld, between, step = t.stride()
+    if t.numel() > 0 and ((step != 1 and dim > 1) or (between != dim and heads > 1)):
+        raise ValueError(f"{name} must have dense heads in a token (strides {list(t.stride())})")
+    if t.shape[0] > 1:
+        if ld < heads * dim:
+            raise ValueError(f"{name} must have tokens that do not overlap (pitch {ld})")
+        return ld
+    return heads * dim
+
+
+def _table(t: torch.Tensor, seqs: int, index: int) -> int:
+    return _matrix(t, "table", index, torch.int32, (seqs, t.shape[-1]))
+
+
+def nq_qk_norm_rotate(x: torch.Tensor, angles: Optional[torch.Tensor], positions: Optional[torch.Tensor], *, q_heads: int, kv_heads: int,
+                      head_dim: Optional[int] = None, norm: int = NQ_NORM_RMS, q_weight: Optional[torch.Tensor] = None,
+                      k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, neighbours: bool = False,
+                      cache: Optional[nq_kv_pages] = None, slots: Optional[torch.Tensor] = None, want_k: Optional[bool] = None,
+                      y_dtype: torch.dtype = torch.bfloat16):
+    """Rows x [tokens, (q_heads + 2 kv_heads) * head_dim] of a fused projection (queries | keys | values) -> (q [tokens, q_heads,
+    head_dim], k [tokens, kv_heads, head_dim] or None): normed for each head, turned by the angles [positions, rotary_dim] (cosines |
+    sines) of each token's position.  With a cache and its slots int32 [tokens], keys and values are stored there in the same pass, and
+    a dense k comes only when asked for (want_k).  Without one, the values' columns may be missing.  angles None: no rotation."""
+    index = x.get_device()
+    ldx = _matrix(x, "x", index)
+    if x.dtype not in _FLOATS or y_dtype not in _FLOATS:
+        raise ValueError(f"x and the output must be float32 or bfloat16, got {x.dtype} and {y_dtype}")
+    if q_heads < 0 or kv_heads < 0 or q_heads + kv_heads == 0:
+        raise ValueError(f"no heads: q_heads {q_heads}, kv_heads {kv_heads}")
+    tokens, width = x.shape
+    dim = width // (q_heads + 2 * kv_heads) if head_dim is None else head_dim
+    if width != (q_heads + 2 * kv_heads) * dim and (cache is not None or width != (q_heads + kv_heads) * dim):
+        raise ValueError(f"x has {width} columns: {q_heads} + 2 * {kv_heads} heads of {dim} are {(q_heads + 2 * kv_heads) * dim}")
+    if (cache is None) != (slots is None):
+        raise ValueError("cache and slots go together")
+    if (angles is None) != (positions is None):
+        raise ValueError("angles and positions go together")
+    if want_k is None:
+        want_k = cache is None
+    rows = rotary = 0
+    if angles is not None:
+        if angles.dtype is not torch.float32 or angles.dim() != 2 or not angles.is_contiguous():
+            raise ValueError("angles must be a dense float32 CUDA tensor [positions, rotary_dim]")
+        _on(angles, "angles", index)
+        rows, rotary = angles.shape
+    q = torch.empty_strided((tokens, q_heads, dim), (q_heads * dim, dim, 1), dtype=y_dtype, device=x.device)
+    k = torch.empty_strided((tokens, kv_heads, dim), (kv_heads * dim, dim, 1), dtype=y_dtype, device=x.device) if want_k else None
+    d = nq_qk_desc(tokens, ldx, q_heads * dim, kv_heads * dim, rows, _FLOATS[x.dtype], _FLOATS[y_dtype], q_heads, kv_heads, dim, rotary, norm, neighbours, eps)
+    _check(lib().nq_qk_norm_rotate(ctypes.addressof(d), x.data_ptr(), _vector(q_weight, "q_weight", dim, index), _vector(k_weight, "k_weight", dim, index),
+                                   None if angles is None else angles.data_ptr(), None if positions is None else _ints(positions, "positions", tokens, index),
+                                   q.data_ptr(), None if k is None else k.data_ptr(), None if cache is None else _pages_on(cache, index),
+                                   None if slots is None else _ints(slots, "slots", tokens, index), _raw_stream(x)), "nq_qk_norm_rotate")
+    return q, k
+
+
+def nq_kv_cache_write(cache: nq_kv_pages, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
+    """Stores k, v [tokens, kv_heads, head_dim] (fp32 or bf16) in the slots int32 [tokens], quantised as the cache holds them; a slot
+    outside the cache (-1, say) is passed over."""
+    index = k.get_device()
+    heads, dim = cache.kv_heads, cache.head_dim
+    if k.dtype not in _FLOATS or v.dtype is not k.dtype or v.shape != k.shape:
+        raise ValueError(f"k and v must be float32 or bfloat16 of one type and shape, got {k.dtype} {list(k.shape)} and {v.dtype} {list(v.shape)}")
+    ldk, ldv = _heads(k, "k", index, heads, dim), _heads(v, "v", index, heads, dim)
+    tokens = k.shape[0]
+    _check(lib().nq_kv_cache_write(_pages_on(cache, index), k.data_ptr(), ldk, v.data_ptr(), ldv, _FLOATS[k.dtype], _ints(slots, "slots", tokens, index),
+                                   tokens, _raw_stream(k)), "nq_kv_cache_write")
+
+
+def nq_kv_cache_read(cache: nq_kv_pages, table: torch.Tensor, starts: torch.Tensor, rows: int, *, y_dtype: torch.dtype = torch.bfloat16,
+                     k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None):
+    """The cache's tokens as packed rows -> (k, v) [rows, kv_heads, head_dim]: sequence s, whose pages are table[s] (int32 [sequences,
+    columns]), fills rows starts[s] to starts[s + 1] (int32 [sequences + 1]).  Rows of no sequence stay as they were in k_out, v_out."""
+    index = table.get_device()
+    heads, dim = cache.kv_heads, cache.head_dim
+    if (k_out is None) != (v_out is None):
+        raise ValueError("give k_out and v_out, or neither")
+    if rows < 0:
+        raise ValueError("rows must not be negative")
+    if k_out is None:
+        make = lambda: torch.empty_strided((rows, heads, dim), (heads * dim, dim, 1), dtype=y_dtype, device=table.device)
+        k_out, v_out = make(), make()
+    if k_out.dtype not in _FLOATS or v_out.dtype is not k_out.dtype or k_out.shape[0] != rows or v_out.shape[0] != rows:
+        raise ValueError(f"k and v must be float32 or bfloat16 with {rows} rows, got {k_out.dtype} {list(k_out.shape)} and {v_out.dtype} {list(v_out.shape)}")
+    ldk, ldv = _heads(k_out, "k_out", index, heads, dim), _heads(v_out, "v_out", index, heads, dim)
+    seqs = table.shape[0]
+    _check(lib().nq_kv_cache_read(_pages_on(cache, index), table.data_ptr(), _table(table, seqs, index), table.shape[-1], _ints(starts, "starts", seqs + 1, index),
+                                  seqs, k_out.data_ptr(), ldk, v_out.data_ptr(), ldv, _FLOATS[k_out.dtype], rows, _raw_stream(table)), "nq_kv_cache_read")
+    return k_out, v_out
+
+
+def nq_paged_attention_workspace_bytes(cache: nq_kv_pages, q_heads: int, seqs: int, table_cols: int) -> int:
+    return int(lib().nq_paged_attention_workspace_bytes(ctypes.addressof(cache), q_heads, seqs, table_cols))
+
+
+def nq_paged_attention(q: torch.Tensor, cache: nq_kv_pages, table: torch.Tensor, lengths: torch.Tensor, *, window: int = 0,
+                       scale: Optional[float] = None, y_out: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """One new token a sequence, q bf16 [sequences, q_heads, head_dim], over the first lengths[s] tokens (int32 [sequences]) of the pages
+    table[s] (int32 [sequences, columns]), or the last `window` of them -> y like q.  scale: head_dim ** -0.5 where not given.
+    A sequence that sees nothing gets zeros."""
+    index = q.get_device()
+    dim = cache.head_dim
+    if q.dtype is not torch.bfloat16:
+        raise ValueError(f"q must be bfloat16, got {q.dtype}")
+    if q.dim() != 3:
+        raise ValueError(f"q must be [sequences, q_heads, {dim}], got {list(q.shape)}")
+    seqs, heads = q.shape[:2]
+    ldq = _heads(q, "q", index, heads, dim)
+    if y_out is None:
+        y_out = torch.empty_strided((seqs, heads, dim), (heads * dim, dim, 1), dtype=torch.bfloat16, device=q.device)
+        ldy = heads * dim
+    else:
+        if y_out.dtype is not torch.bfloat16 or y_out.shape != q.shape:
+            raise ValueError(f"y_out must be bfloat16 {list(q.shape)}, got {y_out.dtype} {list(y_out.shape)}")
+        ldy = _heads(y_out, "y_out", index, heads, dim)
+    ld_table, cols = _table(table, seqs, index), table.shape[1]
+    pages = _pages_on(cache, index)
+    if workspace is None:
+        need = lib().nq_paged_attention_workspace_bytes(pages, heads, seqs, cols)
+        workspace = torch.empty_strided((max(need, 16),), (1,), dtype=torch.uint8, device=q.device)
+    else:
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        _on(workspace, "workspace", index)
+    _check(lib().nq_paged_attention(pages, q.data_ptr(), ldq, heads, table.data_ptr(), ld_table, cols, _ints(lengths, "lengths", seqs, index), seqs,
+                                    window, dim ** -0.5 if scale is None else scale, y_out.data_ptr(), ldy, workspace.data_ptr(),
+                                    workspace.numel() * workspace.element_size(), _raw_stream(q)), "nq_paged_attention")
+    return y_out
 
 
 def nq_i8_mma_ceiling(stage_iters: int) -> float:

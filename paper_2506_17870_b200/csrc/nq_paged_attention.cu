@@ -1,0 +1,698 @@
+// Attention of one new token a sequence over the paged key-value cache.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "../../include/nq.h"
+#include "nq_kv_cache.cuh"
+
+namespace nq {
+namespace {
+
+// The cache is read once, 16 tokens of one kv head (a "step") at a time by one warp, straight into the registers of the matrix
+// instruction: no shared memory, no barrier, nothing between warps until they have their sums.  Both products have the tokens or
+// the head's channels as their 16 rows and the query heads of the kv head as their 8 columns:
+//   S^T [16 tokens, 8 heads] = K Q^T       a lane's 16-byte pieces of two tokens are the operand as they come: the channels are
+//                                          summed over, so any order of them will do as long as Q has the same
+//   O^T [16 channels, 8 heads] += V^T P^T  a lane holds a piece of four tokens; a byte permutation puts two tokens' values of a
+//                                          channel side by side; P^T is S^T's fragment, transposed in 8 x 8 blocks
+// Heads as columns need half of the instructions and accumulators that heads as 16 rows would (a group has 1 to 8 heads, or 16).
+// The sequences' steps (of all kv heads) lie in one long row that is cut evenly over the warps of a full GPU, however the
+// lengths fall.  What a warp has of a sequence and head, if not all of it, is joined in its thread block, and over thread blocks by
+// a second kernel, in a fixed order.
+constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr float kRescale = 8.0f;         // the running maximum moves when a score passes it by 2^8 (fp32 sums have room)
+constexpr float kShift = 7.0f;           // f16 weights are held times 2^7: at most 2^15, and exact down to 2^-21 of the largest
+constexpr float kTiny = 1.17549435e-38f;
+
+struct TokenArgs {
+    Pages c;
+    const __nv_bfloat16* q;
+    long long ldq;
+    int q_heads, group, head_blocks;     // query heads of a kv head, and how many blocks of columns they make
+    const int* table;
+    long long ld_table;
+    int table_tokens;                    // what the table's columns can hold
+    const int* lengths;
+    int seqs, window;
+    float scale2;                        // score scale * log2(e)
+    __nv_bfloat16* y;
+    long long ldy;
+    int4* records;                       // [blocks]: a sequence and head that begins in this block and goes on: its number, head, last block
+    float* slots;                        // [blocks][2]: what the block has of the one it goes on with (0) and of that one (1)
+};
+
+template <int D, int NT>
+constexpr int kSlotFloats = 8 * NT * (D + 2);      // sums [heads][D], maxima [heads], weights' sums [heads]
+
+__device__ __forceinline__ float exp2a(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t s) {
+    uint32_t r;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(s));
+    return r;
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+template <bool HALF>
+__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if (HALF)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// Two codes (in the low 16 bits) to f16 exactly.
+template <int CACHE>
+__device__ __forceinline__ uint32_t codes2(uint32_t two) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((unsigned short)two));
+    return h;
+}
+// Four codes to two words of f16, in their order.  INT8: code + 128 as the low bits of 1024 + (code + 128), less 1152.
+template <int CACHE>
+__device__ __forceinline__ void codes4(uint32_t w, uint32_t& lo, uint32_t& hi) {
+    if (CACHE == NQ_E4M3) {
+        lo = codes2<CACHE>(w);
+        hi = codes2<CACHE>(w >> 16);
+    } else {
+        const uint32_t u = w ^ 0x80808080u;
+        const __half2 off = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));
+        const uint32_t a = prmt(u, 0x64646464u, 0x4140), b = prmt(u, 0x64646464u, 0x4342);
+        const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&a), off), y = __hsub2(*reinterpret_cast<const __half2*>(&b), off);
+        lo = *reinterpret_cast<const uint32_t*>(&x);
+        hi = *reinterpret_cast<const uint32_t*>(&y);
+    }
+}
+
+// Steps of a sequence, its tokens and the number of its first step (behind a window it is not 0).
+__device__ __forceinline__ int steps_of(const TokenArgs& a, int seq, int& length, int& first) {
+    length = min(a.lengths[seq], a.table_tokens);
+    first = a.window > 0 && length > a.window ? (length - a.window) >> 4 : 0;
+    return length <= 0 ? 0 : ((length + 15) >> 4) - first;
+}
+
+// Where a warp is in the long row.
+struct Place {
+    int seq, head, block, step;              // sequence, kv head, block of columns, step among the sequence's
+    int steps, length, first;                // of the sequence
+    __device__ __forceinline__ void next(const TokenArgs& a) {
+        if (++step < steps) return;
+        step = 0;
+        if (++block < a.head_blocks) return;
+        block = 0;
+        if (++head < a.c.kv_heads) return;
+        head = 0;
+        do {
+            if (++seq >= a.seqs) return;
+            steps = steps_of(a, seq, length, first);
+        } while (steps == 0);
+    }
+};
+
+__device__ __forceinline__ void zero_row(const TokenArgs& a, int seq, int columns) {
+    uint4* to = reinterpret_cast<uint4*>(a.y + seq * a.ldy);
+    for (int i = threadIdx.x; i < columns / 8; i += kThreads) to[i] = make_uint4(0, 0, 0, 0);
+}
+
+template <int D, int CACHE, int NT>
+__global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) token_kernel(const TokenArgs a) {
+    constexpr bool kCodes = CACHE != NQ_BF16;
+    constexpr int kRow = D * (kCodes ? 1 : 2);                       // bytes of a token's head
+    constexpr int kKPieces = kRow / 64;                              // 16-byte pieces of a K row in a lane (4 lanes a row)
+    constexpr int kVBytes = kRow / 8 > 16 ? 16 : kRow / 8;           // piece of a V row in a lane (8 lanes a row)
+    constexpr int kVPieces = kRow / 8 / kVBytes, kVWords = kVBytes / 4;
+    constexpr int kSteps = D / 16;                                   // matrix instructions of 16 channels
+    constexpr int kSlot = kSlotFloats<D, NT>;
+    extern __shared__ __align__(16) float s_parts[];                 // [2 * kWarps][kSlot]
+    __shared__ long long s_before[kThreads + 1];
+    __shared__ long long s_warp[kWarps];
+    __shared__ int4 s_meta[2 * kWarps];                              // of each part: sequence (-1: none), unit, whether it holds the first (1) and the last (2) step
+
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = lane >> 2, j = lane & 3;
+    const int units = a.c.kv_heads * a.head_blocks;
+    start_next();
+    wait_previous();
+
+    // ---- the long row: steps before each chunk of sequences
+    const int chunk = (a.seqs + kThreads - 1) / kThreads;
+    long long mine = 0;
+    for (int s = threadIdx.x * chunk; s < min(a.seqs, (int)(threadIdx.x + 1) * chunk); ++s) {
+        int length, first;
+        mine += steps_of(a, s, length, first);
+    }
+    long long sum = mine;
+#pragma unroll
+    for (int m = 1; m < 32; m *= 2) {
+        const long long o = __shfl_up_sync(0xffffffffu, sum, m);
+        if (lane >= m) sum += o;
+    }
+    if (lane == 31) s_warp[warp] = sum;
+    if (threadIdx.x < 2 * kWarps) s_meta[threadIdx.x] = make_int4(-1, 0, 0, 0);
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) sum += s_warp[w];
+    s_before[threadIdx.x + 1] = sum;
+    if (threadIdx.x == 0) s_before[0] = 0;
+    __syncthreads();
+    const long long total = s_before[kThreads] * units;
+    for (int s = blockIdx.x; s < a.seqs; s += gridDim.x)
+        if (a.lengths[s] <= 0 || a.table_tokens == 0) zero_row(a, s, a.q_heads * D);
+
+    // ---- this block's and this warp's part of it
+    const long long blocks = min((long long)gridDim.x, (total + kWarps - 1) / kWarps);
+    const long long begin = blockIdx.x < blocks ? total * blockIdx.x / blocks : 0, end = blockIdx.x < blocks ? total * (blockIdx.x + 1) / blocks : 0;
+    const long long from = begin + (end - begin) * warp / kWarps;
+    int left = (int)(begin + (end - begin) * (warp + 1) / kWarps - from);
+    int part = 2 * warp;                                             // next part to fill
+    if (left > 0) {
+        Place at;
+        {
+            const long long step = from / units;                     // sequences' steps before `at` are no more than this
+            int lo = 0, hi = kThreads;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (s_before[mid] <= step) lo = mid; else hi = mid;
+            }
+            long long rest = from - s_before[lo] * units;
+            at.seq = lo * chunk;
+            at.steps = steps_of(a, at.seq, at.length, at.first);
+            while (rest >= (long long)at.steps * units) {
+                rest -= (long long)at.steps * units;
+                at.steps = steps_of(a, ++at.seq, at.length, at.first);
+            }
+            const int unit = (int)(rest / at.steps);
+            at.step = (int)(rest - (long long)unit * at.steps);
+            at.head = unit / a.head_blocks;
+            at.block = unit - at.head * a.head_blocks;
+        }
+        const int per_page = a.c.page_size >> 4;
+        const long long page_rows = (long long)a.c.kv_heads * a.c.page_size;
+
+        uint4 kw[2][kKPieces];                                       // K of tokens i, i + 8
+        uint32_t vw[4][kVPieces][kVWords];                           // V of tokens 2 j, 2 j + 1, 2 j + 8, 2 j + 9
+        float ks[2] = {1.0f, 1.0f}, vs[2] = {1.0f, 1.0f};            // scales of tokens i, i + 8
+        long long my_row = -1;                                       // lane's page of step pages_from + lane: its first row for head 0, -1: none
+        int pages_seq = -1, pages_from = 0;
+
+        auto row_of = [&](const Place& p) -> long long {             // row of the step's first token in the cache, -1: none
+            const int number = p.first + p.step;
+            if (p.seq != pages_seq || number < pages_from || number >= pages_from + 32) {
+                pages_seq = p.seq;
+                pages_from = number;
+                const int n = number + lane;
+                my_row = -1;
+                if (n < p.first + p.steps) {
+                    const int nth = n / per_page, page = a.table[p.seq * a.ld_table + nth];
+                    if (page >= 0 && page < a.c.pages) my_row = page * page_rows + (n - nth * per_page) * 16;
+                }
+            }
+            const long long row = __shfl_sync(0xffffffffu, my_row, number - pages_from);
+            return row < 0 ? -1 : row + (long long)p.head * a.c.page_size;
+        };
+        auto load_k = [&](long long row) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                for (int p = 0; p < kKPieces; ++p)
+                    kw[t][p] = row < 0 ? make_uint4(0, 0, 0, 0) : load16(a.c.k + (row + i + 8 * t) * kRow + 16 * (j + 4 * p));
+                if (kCodes && row >= 0) ks[t] = a.c.ks[row + i + 8 * t];
+            }
+        };
+        auto load_v = [&](long long row) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const int token = 2 * j + (t & 1) + 8 * (t >> 1);
+#pragma unroll
+                for (int p = 0; p < kVPieces; ++p) {
+                    const uint8_t* src = a.c.v + (row + token) * kRow + kVBytes * (i + 8 * p);
+                    if (row < 0) {
+#pragma unroll
+                        for (int w = 0; w < kVWords; ++w) vw[t][p][w] = 0;
+                    } else if (kVWords == 4) {
+                        const uint4 v = load16(src);
+                        vw[t][p][0] = v.x; vw[t][p][1] = v.y; vw[t][p][2 % kVWords] = v.z; vw[t][p][3 % kVWords] = v.w;
+                    } else {
+                        asm volatile("ld.global.L1::no_allocate.v2.b32 {%0, %1}, [%2];" : "=r"(vw[t][p][0]), "=r"(vw[t][p][1]) : "l"(src) : "memory");
+                    }
+                }
+            }
+            if (kCodes && row >= 0) {
+                vs[0] = a.c.vs[row + i];
+                vs[1] = a.c.vs[row + i + 8];
+            }
+        };
+
+        uint32_t qf[NT][kSteps][2];
+        float q_scale[NT][2];                                        // of heads 2 j, 2 j + 1: what a product of codes is multiplied by
+        float o[NT][kSteps][4], top[NT][2], weight[NT][2], largest = kTiny;
+        int begun = 0;
+
+        long long row = row_of(at);
+        load_k(row);
+        load_v(row);
+        bool fresh = true;
+        while (left > 0) {
+            const Place cur = at;
+            const bool there = row >= 0;
+            const int block = cur.block, kv_head = cur.head;
+            if (fresh) {                                             // another sequence or head
+                fresh = false;
+                begun = cur.step == 0;
+                largest = kTiny;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const int h = (block * NT + n) * 8 + i;
+                    const bool live = h < a.group;
+                    const __nv_bfloat16* src = a.q + cur.seq * a.ldq + (long long)(kv_head * a.group + (live ? h : 0)) * D;
+                    top[n][0] = top[n][1] = -INFINITY;
+                    weight[n][0] = weight[n][1] = 0.0f;
+#pragma unroll
+                    for (int s = 0; s < kSteps; ++s) o[n][s][0] = o[n][s][1] = o[n][s][2] = o[n][s][3] = 0.0f;
+                    if (!kCodes) {
+#pragma unroll
+                        for (int p = 0; p < kKPieces; ++p) {
+                            const uint4 v = live ? load16(src + 8 * (j + 4 * p)) : make_uint4(0, 0, 0, 0);
+                            qf[n][2 * p][0] = v.x; qf[n][2 * p][1] = v.y; qf[n][2 * p + 1][0] = v.z; qf[n][2 * p + 1][1] = v.w;
+                        }
+                        q_scale[n][0] = q_scale[n][1] = a.scale2;
+                    } else {
+                        // bf16 to f16, times a power of two that puts the head's largest into [1, 2): exact but for values below
+                        // 2^-13 of it, which lose bits under 2^-24 of it
+                        uint4 v[2 * kKPieces];
+                        uint32_t m = 0;
+#pragma unroll
+                        for (int p = 0; p < kKPieces; ++p) {
+#pragma unroll
+                            for (int half = 0; half < 2; ++half) {
+                                const uint4 x = live ? load16(src + 16 * (j + 4 * p) + 8 * half) : make_uint4(0, 0, 0, 0);
+                                v[2 * p + half] = x;
+                                m = __vmaxu2(m, __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
+                            }
+                        }
+                        m = max(m >> 16, m & 0xffffu);
+                        m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+                        m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+                        const int e = min(max((int)(m >> 7), 1), 253);               // 254, 255 (infinity, NaN): infinite in f16, as they should be
+                        const float up = __int_as_float((254 - e) << 23), down = __int_as_float(e << 23);
+#pragma unroll
+                        for (int w = 0; w < 8 * kKPieces; ++w) {
+                            const uint4 x = v[w / 4];
+                            const uint32_t u = w % 4 == 0 ? x.x : w % 4 == 1 ? x.y : w % 4 == 2 ? x.z : x.w;
+                            const __half2 h2 = __floats2half2_rn(__uint_as_float(u << 16) * up, __uint_as_float(u & 0xffff0000u) * up);
+                            qf[n][w / 2][w & 1] = *reinterpret_cast<const uint32_t*>(&h2);
+                        }
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) q_scale[n][c] = __shfl_sync(0xffffffffu, down, 4 * (2 * j + c)) * a.scale2;
+                    }
+                }
+            }
+
+            // ---- scores
+            float sc[NT][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.0f;
+#pragma unroll
+            for (int p = 0; p < kKPieces; ++p) {
+                const uint32_t w0[4] = {kw[0][p].x, kw[0][p].y, kw[0][p].z, kw[0][p].w}, w1[4] = {kw[1][p].x, kw[1][p].y, kw[1][p].z, kw[1][p].w};
+                if (!kCodes) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) mma<false>(sc[n], w0[2 * h], w1[2 * h], w0[2 * h + 1], w1[2 * h + 1], qf[n][2 * p + h][0], qf[n][2 * p + h][1]);
+                } else {
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        uint32_t a0, a1, a2, a3;
+                        codes4<CACHE>(w0[h], a0, a2);
+                        codes4<CACHE>(w1[h], a1, a3);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) mma<true>(sc[n], a0, a1, a2, a3, qf[n][4 * p + h][0], qf[n][4 * p + h][1]);
+                    }
+                }
+            }
+            const float kscale[2] = {ks[0], ks[1]}, vscale[2] = {vs[0], vs[1]};
+            --left;
+            at.next(a);
+            const bool closes = left == 0 || at.step == 0;           // the warp's last step of this sequence and head
+            if (left > 0) {
+                row = row_of(at);
+                load_k(row);
+            }
+            // ---- masks: only a sequence's first and last steps have any
+            const int length = cur.length, token0 = (cur.first + cur.step) * 16;
+            const int lo = a.window > 0 ? length - a.window : 0;
+            const bool edge = token0 + 16 > length || token0 < lo || !there;
+            bool seen[2] = {true, true};
+            float vscale_used[2] = {vscale[0], vscale[1]};
+            if (edge) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const int token = token0 + i + 8 * t;
+                    seen[t] = there && token < length && token >= lo;
+                    if (!seen[t]) vscale_used[t] = 0.0f;
+                }
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const int token = token0 + 2 * j + (t & 1) + 8 * (t >> 1);
+                    if (there && token < length && token >= lo) continue;
+#pragma unroll
+                    for (int p = 0; p < kVPieces; ++p)
+#pragma unroll
+                        for (int w = 0; w < kVWords; ++w) vw[t][p][w] = 0;
+                }
+            }
+            // ---- weights
+            bool move = false;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float s = sc[n][e] * q_scale[n][e & 1];
+                    if (kCodes) s *= kscale[e >> 1];
+                    s = seen[e >> 1] ? s : -INFINITY;
+                    sc[n][e] = s;
+                    move |= s > top[n][e & 1] + kRescale;
+                }
+            if (kCodes) move |= fabsf(vscale_used[0]) > largest || fabsf(vscale_used[1]) > largest;
+            if (__any_sync(0xffffffffu, move)) {
+                float shrink = 1.0f;
+                if (kCodes) {
+                    float m = fmaxf(largest, fmaxf(fabsf(vscale_used[0]), fabsf(vscale_used[1])));
+#pragma unroll
+                    for (int x = 4; x < 32; x *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+                    shrink = largest / m;
+                    largest = m;
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    float by[2];
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        float m = fmaxf(top[n][c], fmaxf(sc[n][c], sc[n][2 + c]));
+#pragma unroll
+                        for (int x = 4; x < 32; x *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+                        by[c] = top[n][c] == -INFINITY ? 0.0f : exp2a(top[n][c] - m);
+                        top[n][c] = m;
+                        weight[n][c] *= by[c];
+                        by[c] *= shrink;
+                    }
+#pragma unroll
+                    for (int s = 0; s < kSteps; ++s) {
+                        o[n][s][0] *= by[0]; o[n][s][1] *= by[1]; o[n][s][2] *= by[0]; o[n][s][3] *= by[1];
+                    }
+                }
+            }
+            uint32_t pf[NT][2];
+            float value[2] = {1.0f, 1.0f};
+            if (kCodes) {
+                const float inv = 1.0f / largest;
+                value[0] = vscale_used[0] * inv * 128.0f;            // 2^kShift
+                value[1] = vscale_used[1] * inv * 128.0f;
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float p[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float m = top[n][e & 1];
+                    p[e] = exp2a(sc[n][e] - (m == -INFINITY ? 0.0f : m));
+                    weight[n][e & 1] += p[e];
+                    if (kCodes) p[e] *= value[e >> 1];
+                }
+                if (kCodes) {
+                    const __half2 x = __floats2half2_rn(p[0], p[1]), y = __floats2half2_rn(p[2], p[3]);
+                    pf[n][0] = transpose8x8(*reinterpret_cast<const uint32_t*>(&x));
+                    pf[n][1] = transpose8x8(*reinterpret_cast<const uint32_t*>(&y));
+                } else {
+                    // bf16 has fp32's range: a weight is off by at most 2^-9 of itself
+                    const __nv_bfloat162 x = __floats2bfloat162_rn(p[0], p[1]), y = __floats2bfloat162_rn(p[2], p[3]);
+                    pf[n][0] = transpose8x8(*reinterpret_cast<const uint32_t*>(&x));
+                    pf[n][1] = transpose8x8(*reinterpret_cast<const uint32_t*>(&y));
+                }
+            }
+            // ---- values
+            if (!kCodes) {
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s) {
+                    // two pieces of 8 channels: rows 0-7 of tile s are channel s of piece i, rows 8-15 of piece i + 8; one piece: channels 2 s, 2 s + 1
+                    const int w = kVPieces == 2 ? s / 2 : s;
+                    const uint32_t lo0 = kVPieces == 2 ? ((s & 1) ? 0x7632u : 0x5410u) : 0x5410u, hi0 = kVPieces == 2 ? lo0 : 0x7632u;
+                    const uint32_t a0 = prmt(vw[0][0][w], vw[1][0][w], lo0), a1 = prmt(vw[0][kVPieces - 1][w], vw[1][kVPieces - 1][w], hi0);
+                    const uint32_t a2 = prmt(vw[2][0][w], vw[3][0][w], lo0), a3 = prmt(vw[2][kVPieces - 1][w], vw[3][kVPieces - 1][w], hi0);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) mma<false>(o[n][s], a0, a1, a2, a3, pf[n][0], pf[n][1]);
+                }
+            } else {
+#pragma unroll
+                for (int w = 0; w < kVWords; ++w) {                  // four channels: two tiles, channels 2 s, 2 s + 1 of the lane's piece
+                    uint32_t x[4], y[4];
+                    codes4<CACHE>(prmt(vw[0][0][w], vw[1][0][w], 0x5140), x[0], x[1]);
+                    codes4<CACHE>(prmt(vw[0][0][w], vw[1][0][w], 0x7362), x[2], x[3]);
+                    codes4<CACHE>(prmt(vw[2][0][w], vw[3][0][w], 0x5140), y[0], y[1]);
+                    codes4<CACHE>(prmt(vw[2][0][w], vw[3][0][w], 0x7362), y[2], y[3]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        mma<true>(o[n][2 * w], x[0], x[1], y[0], y[1], pf[n][0], pf[n][1]);
+                        mma<true>(o[n][2 * w + 1], x[2], x[3], y[2], y[3], pf[n][0], pf[n][1]);
+                    }
+                }
+            }
+            if (left > 0) load_v(row);
+
+            if (closes) {
+                fresh = true;
+                const int ended = cur.step + 1 == cur.steps;
+                const float unit = kCodes ? largest * (1.0f / 128.0f) : 1.0f;
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int x = 4; x < 32; x *= 2) weight[n][c] += __shfl_xor_sync(0xffffffffu, weight[n][c], x);
+                // a lane's channels of a head: kVPieces runs of 8 (bf16), or one run of 2 * kSteps
+                float* slot = s_parts + part * kSlot;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const int column = n * 8 + 2 * j + c, h = block * NT * 8 + column;
+                        const float by = begun && ended ? (weight[n][c] > 0.0f || weight[n][c] != weight[n][c] ? unit / weight[n][c] : 0.0f) : unit;
+                        constexpr int kRuns = !kCodes && kVPieces == 2 ? 2 : 1, kRun = D / 8 / kRuns;
+#pragma unroll
+                        for (int r = 0; r < kRuns; ++r) {
+                            const int channel = kRun * (i + 8 * r);
+                            float v[kRun];
+#pragma unroll
+                            for (int x = 0; x < kRun; ++x) v[x] = by * (kRuns == 2 ? o[n][x % kSteps][2 * r + c] : o[n][x / 2][2 * (x & 1) + c]);
+                            if (begun && ended) {
+                                if (h < a.group) {
+                                    __nv_bfloat16* to = a.y + cur.seq * a.ldy + (long long)(kv_head * a.group + h) * D + channel;
+#pragma unroll
+                                    for (int x = 0; x < kRun; x += 8) {
+                                        uint32_t w4[4];
+#pragma unroll
+                                        for (int y = 0; y < 4; ++y) {
+                                            const __nv_bfloat162 b2 = __floats2bfloat162_rn(v[x + 2 * y], v[x + 2 * y + 1]);
+                                            w4[y] = *reinterpret_cast<const uint32_t*>(&b2);
+                                        }
+                                        *reinterpret_cast<uint4*>(to + x) = make_uint4(w4[0], w4[1], w4[2], w4[3]);
+                                    }
+                                }
+                            } else {
+#pragma unroll
+                                for (int x = 0; x < kRun; x += 4) *reinterpret_cast<float4*>(slot + column * D + channel + x) = make_float4(v[x], v[x + 1], v[x + 2], v[x + 3]);
+                            }
+                        }
+                        if (!(begun && ended) && i == 0) {
+                            slot[8 * NT * D + column] = top[n][c];
+                            slot[8 * NT * (D + 1) + column] = weight[n][c];
+                        }
+                    }
+                }
+                if (!(begun && ended)) {
+                    if (lane == 0) s_meta[part] = make_int4(cur.seq, cur.head * a.head_blocks + cur.block, begun + 2 * ended, cur.steps - 1 - cur.step);
+                    ++part;
+                }
+            }
+        }
+    }
+    __syncthreads();
+
+    // ---- the block's parts: neighbours of one sequence and head are joined; all of it: out; otherwise to the block's slots
+    int4 record = make_int4(-1, 0, 0, 0);
+    for (int p = 0; p < 2 * kWarps;) {
+        const int4 first = s_meta[p];
+        if (first.x < 0) {
+            ++p;
+            continue;
+        }
+        int last = p, ends = first.z & 2, rest = first.w;
+        for (int x = p + 1; x < 2 * kWarps; ++x) {
+            const int4 m = s_meta[x];
+            if (m.x < 0) continue;
+            if (m.x != first.x || m.y != first.y) break;
+            last = x;
+            ends |= m.z & 2;
+            rest = m.w;
+        }
+        const bool begins = first.z & 1;
+        const int block = first.y % a.head_blocks, kv_head = first.y / a.head_blocks;
+        float* slot = a.slots + (2ll * blockIdx.x + (begins ? 1 : 0)) * kSlot;
+        for (int e = threadIdx.x; e < 8 * NT * D; e += kThreads) {
+            const int column = e / D, h = block * NT * 8 + column;
+            float m = -INFINITY;
+            for (int x = p; x <= last; ++x)
+                if (s_meta[x].x >= 0) m = fmaxf(m, s_parts[x * kSlot + 8 * NT * D + column]);
+            float sum_o = 0.0f, sum_w = 0.0f;
+            for (int x = p; x <= last; ++x) {
+                if (s_meta[x].x < 0) continue;
+                const float t = s_parts[x * kSlot + 8 * NT * D + column], by = t == -INFINITY && m == -INFINITY ? 1.0f : exp2a(t - m);
+                sum_o += by * s_parts[x * kSlot + e];
+                sum_w += by * s_parts[x * kSlot + 8 * NT * (D + 1) + column];
+            }
+            if (begins && ends) {
+                if (h < a.group)
+                    a.y[first.x * a.ldy + (long long)(kv_head * a.group + h) * D + e % D] = __float2bfloat16_rn(sum_w == 0.0f ? 0.0f : sum_o / sum_w);
+            } else {
+                slot[e] = sum_o;
+                if (e % D == 0) {
+                    slot[8 * NT * D + column] = m;
+                    slot[8 * NT * (D + 1) + column] = sum_w;
+                }
+            }
+        }
+        if (begins && !ends) {
+            // the last step of it is `rest` steps behind this block's end
+            const long long x = end - 1 + rest;
+            record = make_int4(first.x, first.y, (int)(((x + 1) * blocks - 1) / total), 0);
+        }
+        p = last + 1;
+    }
+    if (threadIdx.x == 0) a.records[blockIdx.x] = record;
+}
+
+// A sequence and head that begins in block blockIdx.x and goes on in others: their parts joined.  blockIdx.y: the column.
+template <int D, int NT>
+__global__ void __launch_bounds__(D) join_kernel(const TokenArgs a) {
+    constexpr int kSlot = kSlotFloats<D, NT>;
+    const int column = blockIdx.y;
+    start_next();
+    wait_previous();
+    const int4 rec = a.records[blockIdx.x];
+    if (rec.x < 0) return;
+    const int block = rec.y % a.head_blocks, kv_head = rec.y / a.head_blocks, h = block * NT * 8 + column;
+    if (h >= a.group) return;
+    const int n = rec.z - (int)blockIdx.x + 1;                       // parts: slot 1 of this block, slot 0 of the others
+    const auto part = [&](int x) { return a.slots + (2ll * (blockIdx.x + x) + (x == 0)) * kSlot; };
+    float m = -INFINITY;
+    for (int x = threadIdx.x & 31; x < n; x += 32) m = fmaxf(m, part(x)[8 * NT * D + column]);
+#pragma unroll
+    for (int s = 1; s < 32; s *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
+    float sum_o = 0.0f, sum_w = 0.0f;
+#pragma unroll 8
+    for (int x = 0; x < n; ++x) {
+        const float* f = part(x);
+        const float t = f[8 * NT * D + column], by = t == -INFINITY && m == -INFINITY ? 1.0f : exp2a(t - m);
+        sum_o += by * f[column * D + threadIdx.x];
+        sum_w += by * f[8 * NT * (D + 1) + column];
+    }
+    a.y[rec.x * a.ldy + (long long)(kv_head * a.group + h) * D + threadIdx.x] = __float2bfloat16_rn(sum_w == 0.0f ? 0.0f : sum_o / sum_w);
+}
+
+int tiles(int group) { return group <= 8 ? 1 : 2; }
+
+// Thread blocks: as many as the GPU holds at once, no more than there can be work for.
+int64_t block_count(const nq_kv_pages* c, int64_t q_heads, int64_t seqs, int64_t table_cols) {
+    const int group = (int)(q_heads / c->kv_heads), nt = tiles(group);
+    const int64_t per = (group + 8 * nt - 1) / (8 * nt) * c->kv_heads * table_cols * (c->page_size / 16);     // steps of the longest sequence
+    const int64_t most = (nt == 1 ? 3 : 2) * (int64_t)sm_count();
+    if (per >= most * kWarps || seqs >= most * kWarps) return most;
+    const int64_t need = (per * seqs + kWarps - 1) / kWarps;
+    return need < 1 ? 1 : need < most ? need : most;
+}
+int64_t slot_floats(const nq_kv_pages* c, int64_t q_heads) { return 8ll * tiles((int)(q_heads / c->kv_heads)) * (c->head_dim + 2); }
+
+int check_call(const nq_kv_pages* c, int64_t q_heads, int64_t seqs, int64_t table_cols) {
+    const int bad = check_pages(c);
+    if (bad != NQ_OK) return bad;
+    if (q_heads <= 0 || q_heads % c->kv_heads || seqs < 0 || table_cols < 0) return NQ_ERR_INVALID_ARG;
+    if (q_heads > 65536 || seqs >= 1 << 30 || table_cols > 0x7fffffffll / c->page_size) return NQ_ERR_UNSUPPORTED;
+    return NQ_OK;
+}
+
+template <int D, int CACHE, int NT>
+int launch_token(const TokenArgs& a, unsigned blocks, cudaStream_t s) {
+    const int smem = 2 * kWarps * kSlotFloats<D, NT> * (int)sizeof(float);
+    if (smem > 48 * 1024 - 2048 && cudaFuncSetAttribute(token_kernel<D, CACHE, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return NQ_ERR_CUDA;
+    }
+    const int st = launch_chained(token_kernel<D, CACHE, NT>, blocks, kThreads, smem, 1, s, a);
+    if (st != NQ_OK || blocks == 1) return st;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks, 8 * NT, 1);
+    cfg.blockDim = dim3(D, 1, 1);
+    cfg.stream = s;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, join_kernel<D, NT>, a) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return NQ_ERR_CUDA;
+    }
+    return NQ_OK;
+}
+template <int D, int CACHE>
+int launch_tiles(const TokenArgs& a, unsigned blocks, cudaStream_t s) {
+    return tiles(a.group) == 1 ? launch_token<D, CACHE, 1>(a, blocks, s) : launch_token<D, CACHE, 2>(a, blocks, s);
+}
+template <int D>
+int launch_cache(const TokenArgs& a, int cache, unsigned blocks, cudaStream_t s) {
+    return cache == NQ_BF16 ? launch_tiles<D, NQ_BF16>(a, blocks, s) : cache == NQ_E4M3 ? launch_tiles<D, NQ_E4M3>(a, blocks, s) : launch_tiles<D, NQ_I8>(a, blocks, s);
+}
+
+}  // namespace
+}  // namespace nq
+
+extern "C" int64_t nq_paged_attention_workspace_bytes(const nq_kv_pages* cache, int64_t q_heads, int64_t seqs, int64_t table_cols) {
+    if (nq::check_call(cache, q_heads, seqs, table_cols) != NQ_OK) return -1;
+    return nq::block_count(cache, q_heads, seqs, table_cols) * (int64_t)(sizeof(int4) + 2 * sizeof(float) * nq::slot_floats(cache, q_heads));
+}
+
+extern "C" int nq_paged_attention(const nq_kv_pages* cache, const void* Q, int64_t ldq, int64_t q_heads, const int32_t* table, int64_t ld_table,
+                                  int64_t table_cols, const int32_t* lengths, int64_t seqs, int window, float scale, void* Y, int64_t ldy,
+                                  void* workspace, int64_t workspace_bytes, void* stream) {
+    using nq::misaligned;
+    const int bad = nq::check_call(cache, q_heads, seqs, table_cols);
+    if (bad != NQ_OK) return bad;
+    if (window < 0 || !(scale - scale == 0.0f)) return NQ_ERR_INVALID_ARG;
+    if (seqs == 0) return NQ_OK;
+    const int64_t width = q_heads * cache->head_dim;
+    if (!Q || !Y || !lengths || (table_cols > 0 && (!table || ld_table < table_cols)) || ldq < width || ldy < width) return NQ_ERR_INVALID_ARG;
+    if (misaligned(Q, 16) || misaligned(Y, 16) || (ldq & 7) || (ldy & 7) || misaligned(table, 4) || misaligned(lengths, 4) || misaligned(workspace, 16)) return NQ_ERR_ALIGNMENT;
+    const int64_t blocks = nq::block_count(cache, q_heads, seqs, table_cols);
+    if (!workspace || workspace_bytes < nq_paged_attention_workspace_bytes(cache, q_heads, seqs, table_cols)) return NQ_ERR_WORKSPACE;
+    nq::TokenArgs a = {};
+    a.c = nq::pages_of(cache);
+    a.q = static_cast<const __nv_bfloat16*>(Q); a.ldq = ldq; a.q_heads = (int)q_heads; a.group = (int)(q_heads / cache->kv_heads);
+    a.head_blocks = (a.group + 8 * nq::tiles(a.group) - 1) / (8 * nq::tiles(a.group));
+    a.table = table; a.ld_table = ld_table; a.table_tokens = (int)(table_cols * cache->page_size);
+    a.lengths = lengths; a.seqs = (int)seqs; a.window = window; a.scale2 = scale * 1.44269504088896341f;
+    a.y = static_cast<__nv_bfloat16*>(Y); a.ldy = ldy;
+    a.records = static_cast<int4*>(workspace);
+    a.slots = reinterpret_cast<float*>(a.records + blocks);
+    const cudaStream_t s = (cudaStream_t)stream;
+    return cache->head_dim == 64 ? nq::launch_cache<64>(a, cache->dtype, (unsigned)blocks, s) : nq::launch_cache<128>(a, cache->dtype, (unsigned)blocks, s);
+}
