@@ -490,7 +490,7 @@ NQ_API int nq_kv_cache_read(const nq_kv_pages *cache, const int32_t *table, int6
  * Attention of one new token a sequence over the cache (which holds the token itself, if it is to see itself):
  *   y_h = sum_t w_t v_t,  w = softmax over t of (scale * q_h . k_t),  t in [max(0, n - window), n), n = min(lengths[s], what the
  *   table's columns hold); window == 0: all of them.
- *   A sequence that sees nothing (n <= 0, or no page in the cache), or whose scores are all -infinity, gets zeros.
+ *   scale > 0.  A sequence that sees nothing (n <= 0, or no page in the cache), or whose scores are all -infinity, gets zeros.
  *   Q (device) bf16 [seqs, q_heads * head_dim], pitch ldq; Y (device, out) likewise, pitch ldy (multiples of 8, 16-byte aligned)
  *   table (device) int32 [seqs, table_cols], lengths (device) int32 [seqs]
  *   Sums, maxima and weights are fp32.  A weight is rounded to bf16 (bf16 cache) or f16 (8-bit caches, times the value's scale)
@@ -502,6 +502,25 @@ NQ_API int64_t nq_paged_attention_workspace_bytes(const nq_kv_pages *cache, int6
 NQ_API int nq_paged_attention(const nq_kv_pages *cache, const void *Q, int64_t ldq, int64_t q_heads, const int32_t *table, int64_t ld_table,
                               int64_t table_cols, const int32_t *lengths, int64_t seqs, int window, float scale, void *Y, int64_t ldy,
                               void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * Attention over whole prompts, packed: the queries of sequence s are rows starts_q[s] .. starts_q[s + 1] of Q, its keys and values rows
+ * starts_k[s] .. starts_k[s + 1] of K and V.  With n queries and m keys, query i sees key j
+ *   causal != 0: j <= i + m - n (the last query sees all keys: they may have a prefix before the queries);  window > 0: j > i + m - n - window
+ *   y_i = sum_j w_j v_j,  w = softmax over the seen j of (scale * q_i . k_j);  a row that sees nothing, or whose scores are all -infinity, is zero.
+ *   What a row does not see has no part in it, infinities and NaN in its keys or values included.
+ *   Q, Y bf16 [rows_q, q_heads * head_dim], K, V bf16 [rows_k, kv_heads * head_dim] (device), pitches multiples of 8, 16-byte aligned
+ *   starts (device) int32 [seqs + 1], not decreasing, in [0, rows]: read when the kernel runs.  Rows of Y outside the sequences are left as they were.
+ *   Products on the tensor core (exact products, fp32 sums); maxima, sums and weights are fp32; a weight is rounded to bf16 for its product with
+ *   the values.  scale > 0.  Needs no workspace; results repeat bit for bit.
+ */
+typedef struct {
+    int64_t seqs, rows_q, rows_k, ldq, ldk, ldv, ldy;
+    int32_t q_heads, kv_heads, head_dim, causal, window;
+    float scale;
+} nq_prompt_desc;
+NQ_API int nq_prompt_attention(const nq_prompt_desc *desc, const void *Q, const void *K, const void *V, const int32_t *starts_q, const int32_t *starts_k,
+                               void *Y, void *stream);
 
 /*
  * The convolution again, for callers that must not allocate.  (The paper has no counterpart; this is a
@@ -556,7 +575,7 @@ NQ_API int nq_debug_set(int which, int enabled);
 NQ_API int nq_i8_mma_ceiling(int64_t stage_iters, double *ops_out, void *stream);
 
 /*
- * Every on-device wait in the GEMM / convolution, e4m3 and block-norm kernels is bounded.  If one expires the kernel
+ * Every on-device wait in the GEMM / convolution, e4m3, block-norm and attention kernels is bounded.  If one expires the kernel
  * records it and returns instead of hanging.  This call synchronises `stream`, reads and clears
  * the record of the current device: returns NQ_OK, NQ_ERR_TIMEOUT (with *where_out = an internal
  * code of the wait that gave up) or NQ_ERR_CUDA.

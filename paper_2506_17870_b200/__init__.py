@@ -17,5 +17,6 @@ from .binding import (  # noqa: F401
     NQ_E4M3, NQ_I8, NQ_NORM_NONE, NQ_NORM_RMS, NQ_NORM_LAYER, nq_fp8_quantize, nq_fp8_gemm, nq_block_norm_desc, nq_block_norm,
     nq_block_norm_backward, nq_block_norm_backward_workspace_bytes,
     nq_kv_pages, nq_qk_desc, nq_qk_norm_rotate, nq_kv_cache_write, nq_kv_cache_read, nq_paged_attention, nq_paged_attention_workspace_bytes,
+    nq_prompt_desc, nq_prompt_attention,
     nq_rounding_mask, NQ_ROUND_DOWN, NQ_ROUND_UP, NQ_ROUND_NEAREST,
 )

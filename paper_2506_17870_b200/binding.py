@@ -35,6 +35,7 @@ EXPORTS = (
     "nq_conv_implicit_gemm_q8_res", "nq_conv_implicit_gemm_nested_q8_res", "nq_maxpool_nhwc_i8", "nq_avgpool_requant_nhwc_i8",
     "nq_fp8_quantize", "nq_fp8_gemm", "nq_block_norm", "nq_block_norm_backward", "nq_block_norm_backward_workspace_bytes",
     "nq_qk_norm_rotate", "nq_kv_cache_write", "nq_kv_cache_read", "nq_paged_attention", "nq_paged_attention_workspace_bytes",
+    "nq_prompt_attention",
     "nq_device_status",
 )
 
@@ -72,6 +73,11 @@ class nq_qk_desc(ctypes.Structure):
                 [("eps", ctypes.c_float)])
 
 
+class nq_prompt_desc(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_int64) for k in ("seqs", "rows_q", "rows_k", "ldq", "ldk", "ldv", "ldy")] +
+                [(k, ctypes.c_int32) for k in ("q_heads", "kv_heads", "head_dim", "causal", "window")] + [("scale", ctypes.c_float)])
+
+
 # Argument types of the entry points whose calls pass plain numbers: a call of a few microseconds is not spent on
 # wrapping each of them.
 _P, _L, _I, _F = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_float
@@ -86,6 +92,7 @@ _ARGTYPES = {
     "nq_kv_cache_read": (_P, _P, _L, _L, _P, _L, _P, _L, _P, _L, _I, _L, _P),
     "nq_paged_attention": (_P, _P, _L, _L, _P, _L, _L, _P, _L, _I, _F, _P, _L, _P, _L, _P),
     "nq_paged_attention_workspace_bytes": (_P, _L, _L, _L),
+    "nq_prompt_attention": (_P,) * 8,
 }
 
 
@@ -1066,6 +1073,38 @@ def nq_paged_attention(q: torch.Tensor, cache: nq_kv_pages, table: torch.Tensor,
     _check(lib().nq_paged_attention(pages, q.data_ptr(), ldq, heads, table.data_ptr(), ld_table, cols, _ints(lengths, "lengths", seqs, index), seqs,
                                     window, dim ** -0.5 if scale is None else scale, y_out.data_ptr(), ldy, workspace.data_ptr(),
                                     workspace.numel() * workspace.element_size(), _raw_stream(q)), "nq_paged_attention")
+    return y_out
+
+
+def nq_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts_q: torch.Tensor, starts_k: Optional[torch.Tensor] = None, *,
+                        causal: bool = True, window: int = 0, scale: Optional[float] = None, y_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Packed sequences: q bf16 [rows, q_heads, head_dim], k, v bf16 [key rows, kv_heads, head_dim]; sequence s has queries starts_q[s] to
+    starts_q[s + 1] and keys starts_k[s] to starts_k[s + 1] (int32 [sequences + 1]; starts_k None: the same) -> y like q.  A causal
+    sequence's last query sees all its keys; window: only that many keys up to its own place.  scale: head_dim ** -0.5 where not given.  Rows
+    that see nothing are zero; rows of no sequence stay as they were in y_out."""
+    index = q.get_device()
+    if q.dtype is not torch.bfloat16 or k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16:
+        raise ValueError(f"q, k and v must be bfloat16, got {q.dtype}, {k.dtype} and {v.dtype}")
+    if q.dim() != 3 or k.dim() != 3 or v.shape != k.shape or k.shape[2] != q.shape[2]:
+        raise ValueError(f"q, k and v must be [rows, heads, head_dim], k and v alike, got {list(q.shape)}, {list(k.shape)} and {list(v.shape)}")
+    rows, heads, dim = q.shape
+    kv_heads = k.shape[1]
+    ldq, ldk, ldv = _heads(q, "q", index, heads, dim), _heads(k, "k", index, kv_heads, dim), _heads(v, "v", index, kv_heads, dim)
+    seqs = starts_q.shape[0] - 1 if starts_q.dim() == 1 else -1
+    if seqs < 0:
+        raise ValueError("starts_q must be int32 [sequences + 1]")
+    if starts_k is None:
+        starts_k = starts_q
+    if y_out is None:
+        y_out = torch.empty_strided((rows, heads, dim), (heads * dim, dim, 1), dtype=torch.bfloat16, device=q.device)
+        ldy = heads * dim
+    else:
+        if y_out.dtype is not torch.bfloat16 or y_out.shape != q.shape:
+            raise ValueError(f"y_out must be bfloat16 {list(q.shape)}, got {y_out.dtype} {list(y_out.shape)}")
+        ldy = _heads(y_out, "y_out", index, heads, dim)
+    d = nq_prompt_desc(seqs, rows, k.shape[0], ldq, ldk, ldv, ldy, heads, kv_heads, dim, causal, window, dim ** -0.5 if scale is None else scale)
+    _check(lib().nq_prompt_attention(ctypes.addressof(d), q.data_ptr(), k.data_ptr(), v.data_ptr(), _ints(starts_q, "starts_q", seqs + 1, index),
+                                     _ints(starts_k, "starts_k", seqs + 1, index), y_out.data_ptr(), _raw_stream(q)), "nq_prompt_attention")
     return y_out
 
 

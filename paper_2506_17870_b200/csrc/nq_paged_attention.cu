@@ -677,7 +677,7 @@ extern "C" int nq_paged_attention(const nq_kv_pages* cache, const void* Q, int64
     using nq::misaligned;
     const int bad = nq::check_call(cache, q_heads, seqs, table_cols);
     if (bad != NQ_OK) return bad;
-    if (window < 0 || !(scale - scale == 0.0f)) return NQ_ERR_INVALID_ARG;
+    if (window < 0 || !(scale > 0.0f) || !(scale - scale == 0.0f)) return NQ_ERR_INVALID_ARG;
     if (seqs == 0) return NQ_OK;
     const int64_t width = q_heads * cache->head_dim;
     if (!Q || !Y || !lengths || (table_cols > 0 && (!table || ld_table < table_cols)) || ldq < width || ldy < width) return NQ_ERR_INVALID_ARG;

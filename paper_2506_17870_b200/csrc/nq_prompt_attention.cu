@@ -1,0 +1,569 @@
+// Attention over whole prompts of different lengths, packed behind one another.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/nq.h"
+#include "nq_fp8.cuh"
+#include "nq_internal.cuh"
+#include "nq_sm100.cuh"
+#include "nq_sm100_bf16.cuh"
+
+namespace nq {
+namespace {
+
+using namespace sm100;
+
+// A unit of work is 256 rows of queries of one head, as two tiles of 128; a thread block works through units, one block an SM.
+// For each 128 keys ("step") and tile:  S = Q K^T into tensor memory (128 columns), the tile's four softmax warps read a row a
+// thread, keep its maximum and sum, write the weights back as bf16 over S, and O += P V takes them from there (P as the operand in
+// tensor memory, V as it lies, N-major).  While one tile's weights are being computed the tensor core works for the other:
+//   PV(0, j - 1)  QK(0, j)  PV(1, j - 1)  QK(1, j)  ...
+// The running maximum moves only when a score passes it by 2^8, so the sums in tensor memory are seldom rescaled (by the softmax warps:
+// S(j) being there says that PV(j - 1) is complete, for the tensor core works in order).
+// Two warps look after V where a step has hidden keys (the last of a sequence, the diagonal, a window's edge): rows of V behind the
+// sequence are zeroed, since 0 x NaN is NaN in the product, and where the sequence's own rows hold infinities or NaN, the tiles that
+// hide some of the step take their weights times V by themselves, only what each row sees.
+constexpr int kThreads = 384;            // warp 0 TMA, warp 1 MMA and TMEM, warps 2, 3 look after V, warps 4-7 and 8-11 softmax of the tiles
+constexpr int kTile = 128;
+constexpr float kRescale = 8.0f;
+
+template <int D>
+struct Shape {
+    static constexpr int kTileBytes = kTile * D * 2;
+    static constexpr int kStages = D == 128 ? 2 : 4;          // of K, and of V
+    static constexpr int kSmem = (2 + 2 * kStages) * kTileBytes + 1024 + 1024;
+    static constexpr int kSlab = kTile * 128;                 // 64 values of all rows of a tile
+};
+
+struct PromptArgs {
+    const int *starts_q, *starts_k;
+    int seqs, rows_q, rows_k, q_heads, group, causal, window;
+    float scale2;                        // score scale * log2(e)
+    __nv_bfloat16* y;
+    long long ldy;
+    unsigned int* status;
+};
+
+struct Unit {
+    int q0, k0;                          // rows of the tensors: the sequence's first query and key
+    int lq, lk, row;                     // its lengths, and the unit's first row in it
+    int head;
+    int lo[2], hi[2];                    // steps of each tile (hi <= lo: none)
+    int all_lo[2], all_hi[2];            // keys that all rows of the tile see
+    __device__ __forceinline__ int first() const { return hi[0] > lo[0] ? (hi[1] > lo[1] ? min(lo[0], lo[1]) : lo[0]) : lo[1]; }
+    __device__ __forceinline__ int last() const { return hi[0] > lo[0] ? (hi[1] > lo[1] ? max(hi[0], hi[1]) : hi[0]) : hi[1]; }
+    __device__ __forceinline__ bool takes(int t, int j) const { return j >= lo[t] && j < hi[t]; }
+    __device__ __forceinline__ bool hides(int t, int j) const { return takes(t, j) && (j * kTile < all_lo[t] || (j + 1) * kTile > all_hi[t]); }
+};
+
+__device__ __forceinline__ int clamp_start(int v, int low, int high) { return min(max(v, low), high); }
+
+// `before`: units (of one head) before each chunk of sequences
+__device__ __forceinline__ Unit unit_of(const PromptArgs& a, const int* before, int chunk, int index) {
+    Unit u;
+    const int pair = before[kThreads] - 1 - index / a.q_heads;     // the longest rows of a causal prompt first
+    u.head = index % a.q_heads;
+    int lo = 0, hi = kThreads;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (before[mid] <= pair) lo = mid; else hi = mid;
+    }
+    int rest = pair - before[lo], s = lo * chunk;
+    for (;; ++s) {
+        u.q0 = clamp_start(a.starts_q[s], 0, a.rows_q);
+        u.lq = clamp_start(a.starts_q[s + 1], u.q0, a.rows_q) - u.q0;
+        const int n = (u.lq + 2 * kTile - 1) / (2 * kTile);
+        if (rest < n) break;
+        rest -= n;
+    }
+    u.k0 = clamp_start(a.starts_k[s], 0, a.rows_k);
+    u.lk = clamp_start(a.starts_k[s + 1], u.k0, a.rows_k) - u.k0;
+    u.row = rest * 2 * kTile;
+    const int off = u.lk - u.lq;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const int a0 = u.row + t * kTile, b0 = min(a0 + kTile, u.lq);              // rows [a0, b0)
+        u.lo[t] = u.hi[t] = u.all_lo[t] = u.all_hi[t] = 0;
+        if (a0 >= b0) continue;
+        const int seen_hi = a.causal ? min(u.lk, b0 + off) : u.lk, seen_lo = a.window ? max(0, a0 + off + 1 - a.window) : 0;
+        u.all_hi[t] = a.causal ? min(u.lk, a0 + off + 1) : u.lk;
+        u.all_lo[t] = a.window ? max(0, b0 + off - a.window) : 0;
+        if (seen_hi > seen_lo) {
+            u.lo[t] = seen_lo / kTile;
+            u.hi[t] = (seen_hi + kTile - 1) / kTile;
+        }
+    }
+    return u;
+}
+
+__device__ __forceinline__ float exp2a(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const PromptArgs a) {
+    using P = Shape<D>;
+    constexpr int ST = P::kStages;
+    constexpr uint32_t kS = 0, kO = 256;                       // tensor memory columns: S of tile t at kS + 128 t, O at kO + D t
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t* sQ = smem;                                        // [2 tiles]
+    uint8_t* sK = sQ + 2 * P::kTileBytes;                      // [ST]
+    uint8_t* sV = sK + ST * P::kTileBytes;                     // [ST]
+    uint64_t* bars = reinterpret_cast<uint64_t*>(sV + ST * P::kTileBytes);
+    uint64_t *q_full = bars, *q_empty = q_full + 1, *s_full = q_empty + 1, *p_full = s_full + 2, *o_full = p_full + 2;
+    uint64_t *k_full = o_full + 2, *k_empty = k_full + ST, *v_full = k_empty + ST, *v_empty = v_full + ST, *v_ok = v_empty + ST;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(v_ok + ST);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    volatile int* v_odd = abort_flag + 1;                      // [ST][2]: whether the step's V holds what is no number, by the two warps
+    __shared__ int s_before[kThreads + 1];
+    __shared__ int s_warp[kThreads / 32];
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        mbar_init(smem_u32(q_full), 1);
+        mbar_init(smem_u32(q_empty), 1);
+        for (int t = 0; t < 2; ++t) { mbar_init(smem_u32(&s_full[t]), 1); mbar_init(smem_u32(&p_full[t]), 4); mbar_init(smem_u32(&o_full[t]), 1); }
+        for (int s = 0; s < ST; ++s) {
+            mbar_init(smem_u32(&k_full[s]), 1); mbar_init(smem_u32(&k_empty[s]), 1);
+            mbar_init(smem_u32(&v_full[s]), 1); mbar_init(smem_u32(&v_empty[s]), 3);       // the products and warps 2, 3
+            mbar_init(smem_u32(&v_ok[s]), 2);
+        }
+        *abort_flag = 0;
+        fence_barrier_init();
+        prefetch_tensormap(&tmQ);
+        prefetch_tensormap(&tmK);
+        prefetch_tensormap(&tmV);
+    }
+    if (warp == 1) {
+        tmem_alloc(smem_u32(tmem_slot), 512);
+        tmem_relinquish();
+    }
+    start_next();
+    wait_previous();
+
+    // units of one head before each chunk of sequences
+    const int chunk = (a.seqs + kThreads - 1) / kThreads;
+    {
+        int sum = 0;
+        for (int s = threadIdx.x * chunk; s < min(a.seqs, (int)(threadIdx.x + 1) * chunk); ++s) {
+            const int from = clamp_start(a.starts_q[s], 0, a.rows_q);
+            sum += (clamp_start(a.starts_q[s + 1], from, a.rows_q) - from + 2 * kTile - 1) / (2 * kTile);
+        }
+#pragma unroll
+        for (int m = 1; m < 32; m *= 2) {
+            const int o = __shfl_up_sync(0xffffffffu, sum, m);
+            if (lane >= m) sum += o;
+        }
+        if (lane == 31) s_warp[warp] = sum;
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) sum += s_warp[w];
+        s_before[threadIdx.x + 1] = sum;
+        if (threadIdx.x == 0) s_before[0] = 0;
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = *tmem_slot;
+    const int units = s_before[kThreads] * a.q_heads;          // the host has checked that it fits
+    const auto nth = [&](int round) { return round * (int)gridDim.x + ((round & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x); };
+
+    // 128 x 80 + 256 x 208 registers of the 384 x 168 that the block was launched with
+    if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    else asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t it = 0;                                   // steps so far
+            bool ok = true;
+            uint32_t used = 0;                                 // units with any step
+            for (int r = 0; ok && r * (int)gridDim.x < units; ++r) {
+                if (nth(r) >= units) continue;
+                const Unit u = unit_of(a, s_before, chunk, nth(r));
+                if (u.last() <= u.first()) continue;
+                if (!(ok = mbar_wait(smem_u32(q_empty), (used & 1) ^ 1, abort_flag, a.status, 0x310u))) break;
+                ++used;
+                const bool two[2] = {u.hi[0] > u.lo[0], u.hi[1] > u.lo[1]};
+                mbar_arrive_expect_tx(smem_u32(q_full), (two[0] + two[1]) * P::kTileBytes);
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+                    if (two[t])
+#pragma unroll
+                        for (int h = 0; h < D / 64; ++h)
+                            tma_load_3d(smem_u32(sQ + t * P::kTileBytes + h * P::kSlab), &tmQ, 64 * h, u.head, u.q0 + u.row + t * kTile, smem_u32(q_full));
+                for (int j = u.first(); j < u.last(); ++j, ++it) {
+                    const uint32_t s = it % ST, use = it / ST;
+                    if (!(ok = mbar_wait(smem_u32(&k_empty[s]), (use & 1) ^ 1, abort_flag, a.status, 0x311u))) break;
+                    mbar_arrive_expect_tx(smem_u32(&k_full[s]), P::kTileBytes);
+#pragma unroll
+                    for (int h = 0; h < D / 64; ++h)
+                        tma_load_3d(smem_u32(sK + s * P::kTileBytes + h * P::kSlab), &tmK, 64 * h, u.head / a.group, u.k0 + j * kTile, smem_u32(&k_full[s]));
+                    if (!(ok = mbar_wait(smem_u32(&v_empty[s]), (use & 1) ^ 1, abort_flag, a.status, 0x312u))) break;
+                    mbar_arrive_expect_tx(smem_u32(&v_full[s]), P::kTileBytes);
+#pragma unroll
+                    for (int h = 0; h < D / 64; ++h)
+                        tma_load_3d(smem_u32(sV + s * P::kTileBytes + h * P::kSlab), &tmV, 64 * h, u.head / a.group, u.k0 + j * kTile, smem_u32(&v_full[s]));
+                }
+            }
+            if (!ok) {
+                const long long t0 = clock64();                // let copies in flight land before shared memory is released
+                while (clock64() - t0 < (1ll << 22)) { }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            constexpr uint32_t kQK = idesc_bf16(kTile, kTile, false), kPV = idesc_bf16(kTile, D, true);
+            uint32_t it = 0, used = 0, weights[2] = {0, 0}, checked[ST] = {};
+            bool ok = true;
+            for (int r = 0; ok && r * (int)gridDim.x < units; ++r) {
+                if (nth(r) >= units) continue;
+                const Unit u = unit_of(a, s_before, chunk, nth(r));
+                const int first = u.first(), last = u.last();
+                if (last <= first) continue;
+                if (!(ok = mbar_wait(smem_u32(q_full), used & 1, abort_flag, a.status, 0x320u))) break;
+                ++used;
+                for (int j = first; ok && j <= last; ++j) {
+                    const uint32_t i = it + (j - first), s = i % ST, use = i / ST;           // of step j
+                    const uint32_t sp = (i - 1) % ST, usep = (i - 1) / ST;                   // of step j - 1
+                    bool odd = false;
+                    if (j < last && !(ok = mbar_wait(smem_u32(&k_full[s]), use & 1, abort_flag, a.status, 0x321u))) break;
+                    if (j > first) {
+                        if (u.hides(0, j - 1) || u.hides(1, j - 1)) {
+                            uint32_t n = 0;
+#pragma unroll
+                            for (int x = 0; x < ST; ++x)
+                                if (x == (int)sp) n = checked[x]++;
+                            if (!(ok = mbar_wait(smem_u32(&v_ok[sp]), n & 1, abort_flag, a.status, 0x322u))) break;
+                            odd = v_odd[2 * sp] || v_odd[2 * sp + 1];
+                        }
+                        if (!(ok = mbar_wait(smem_u32(&v_full[sp]), usep & 1, abort_flag, a.status, 0x323u))) break;
+                    }
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        if (j > first && u.takes(t, j - 1)) {
+                            if (!(ok = mbar_wait(smem_u32(&p_full[t]), weights[t]++ & 1, abort_flag, a.status, 0x324u))) break;
+                            tc_fence_after_sync();
+                            if (!(odd && u.hides(t, j - 1))) {
+                                const uint64_t dv = smem_desc_mn_sw128(smem_u32(sV + sp * P::kTileBytes), P::kSlab);
+#pragma unroll
+                                for (int k = 0; k < kTile / 16; ++k)
+                                    mma_bf16_ts(tmem + kO + t * D, tmem + kS + t * kTile + 8 * k, dv + k * (16 * 128 / 16), kPV, j - 1 > u.lo[t] || k > 0);
+                            }
+                            if (j == u.hi[t]) mma_commit(smem_u32(&o_full[t]));
+                        }
+                        if (j < last && u.takes(t, j)) {
+                            tc_fence_after_sync();
+                            const uint64_t dq = smem_desc_sw128(smem_u32(sQ + t * P::kTileBytes)), dk = smem_desc_sw128(smem_u32(sK + s * P::kTileBytes));
+#pragma unroll
+                            for (int k = 0; k < D / 16; ++k) {
+                                const uint64_t at = (k % 4) * 2 + (k / 4) * (P::kSlab / 16);
+                                mma_bf16(tmem + kS + t * kTile, dq + at, dk + at, kQK, k > 0);
+                            }
+                            mma_commit(smem_u32(&s_full[t]));
+                        }
+                    }
+                    if (!ok) break;
+                    if (j > first) mma_commit(smem_u32(&v_empty[sp]));
+                    if (j < last) mma_commit(smem_u32(&k_empty[s]));
+                    if (j == last - 1) mma_commit(smem_u32(q_empty));
+                }
+                it += last - first;
+            }
+        }
+    } else if (warp < 4) {
+        // rows (warp - 2) * 64 .. + 64 of V where a step hides something
+        uint32_t it = 0;
+        bool ok = true;
+        for (int r = 0; ok && r * (int)gridDim.x < units; ++r) {
+            if (nth(r) >= units) continue;
+            const Unit u = unit_of(a, s_before, chunk, nth(r));
+            const int first = u.first(), last = u.last();
+            for (int j = first; j < last; ++j) {
+                // every step is waited for and let go, for a wait must not be more than one phase behind its barrier
+                const uint32_t i = it + (j - first), s = i % ST, use = i / ST;
+                ok = mbar_wait(smem_u32(&v_full[s]), use & 1, abort_flag, a.status, 0x330u);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                if (!u.hides(0, j) && !u.hides(1, j)) {
+                    if (lane == 0) mbar_arrive(smem_u32(&v_empty[s]));
+                    continue;
+                }
+                const int live = u.lk - j * kTile;             // rows of the sequence
+                uint32_t odd = 0;
+                // a lane takes a 16-byte piece of every fourth row: 8 lanes are a row of 64 values
+#pragma unroll
+                for (int h = 0; h < D / 64; ++h) {
+                    for (int x = 0; x < 64; x += 4) {
+                        const int row = (warp - 2) * 64 + x + (lane >> 3);
+                        uint4* p = reinterpret_cast<uint4*>(sV + s * P::kTileBytes + h * P::kSlab + row * 128 + (lane & 7) * 16);
+                        if (row >= live) {
+                            *p = make_uint4(0, 0, 0, 0);
+                        } else {
+                            const uint4 v = *p;
+                            odd |= ((v.x & 0x7f807f80u) + 0x00800080u) | ((v.y & 0x7f807f80u) + 0x00800080u) | ((v.z & 0x7f807f80u) + 0x00800080u) |
+                                   ((v.w & 0x7f807f80u) + 0x00800080u);
+                        }
+                    }
+                }
+                const bool any = __any_sync(0xffffffffu, (odd & 0x80008000u) != 0);
+                fence_proxy_async_smem();
+                if (lane == 0) v_odd[2 * s + warp - 2] = any;
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(smem_u32(&v_ok[s]));
+                    mbar_arrive(smem_u32(&v_empty[s]));
+                }
+            }
+            it += max(0, last - first);
+        }
+    } else {
+        const int t = (warp - 4) >> 2, quarter = warp & 3;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        const uint32_t s_at = tmem + kS + t * kTile + lanes, o_at = tmem + kO + t * D + lanes;
+        uint32_t it = 0, scores = 0, outs = 0, checked[ST] = {};
+        bool ok = true;
+        for (int r = 0; ok && r * (int)gridDim.x < units; ++r) {
+            if (nth(r) >= units) continue;
+            const Unit u = unit_of(a, s_before, chunk, nth(r));
+            const int first = u.first(), last = u.last();
+            const int row = u.row + t * kTile + quarter * 32 + lane, off = u.lk - u.lq;
+            const int mine = min(row, u.lq - 1);               // rows behind the last one only must not get in the way
+            const int see_hi = a.causal ? min(u.lk, mine + off + 1) : u.lk, see_lo = a.window ? max(0, mine + off + 1 - a.window) : 0;
+            float top = -INFINITY, total = 0.0f;
+            for (int j = first; j < last; ++j) {
+                const uint32_t sl = (it + (j - first)) % ST;
+                const bool some = u.hides(0, j) || u.hides(1, j);
+                uint32_t n_checked = 0;
+                if (some) {
+#pragma unroll
+                    for (int x = 0; x < ST; ++x)
+                        if (x == (int)sl) n_checked = checked[x]++;
+                }
+                if (!u.takes(t, j)) continue;
+                ok = mbar_wait(smem_u32(&s_full[t]), scores & 1, abort_flag, a.status, 0x340u);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                ++scores;
+                tc_fence_after_sync();
+                uint32_t s[4][32];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) tmem_ld_32x32(s_at + 32 * x, s[x]);
+                tmem_ld_wait();
+#pragma unroll
+                for (int x = 0; x < 4; ++x) tmem_arrived(s[x]);
+                const bool hides = u.hides(t, j);
+                if (hides) {
+                    const int lo = see_lo - j * kTile, hi = see_hi - j * kTile;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+#pragma unroll
+                        for (int c = 0; c < 32; ++c)
+                            if (32 * x + c < lo || 32 * x + c >= hi) s[x][c] = 0xff800000u;
+                }
+                float m = -INFINITY;
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) m = fmaxf(m, __uint_as_float(s[x][c]));
+                m *= a.scale2;
+                const bool move = m > top + kRescale;
+                if (__any_sync(0xffffffffu, move)) {
+                    const float to = fmaxf(top, m), by = top == -INFINITY ? 0.0f : exp2a(top - to);
+                    top = to;
+                    total *= by;
+                    if (j > u.lo[t]) {
+#pragma unroll
+                        for (int c0 = 0; c0 < D; c0 += 32) {
+                            uint32_t o[32];
+                            tmem_ld_32x32(o_at + c0, o);
+                            tmem_ld_wait();
+                            tmem_arrived(o);
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * by);
+                            tmem_st_32x32(o_at + c0, o);
+                        }
+                    }
+                }
+                const float minus = top == -INFINITY ? 0.0f : -top;
+                uint64_t sum = 0;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    uint32_t p[16];
+#pragma unroll
+                    for (int c = 0; c < 32; c += 2) {
+                        float e0, e1;
+                        unpack2(fma2(pack2(s[x][c], s[x][c + 1]), both(a.scale2), both(minus)), e0, e1);
+                        e0 = exp2a(e0);
+                        e1 = exp2a(e1);
+                        sum = add2(sum, pack2f(e0, e1));
+                        p[c / 2] = bf16x2(e0, e1);             // a weight is off by at most 2^-9 of itself
+                    }
+                    tmem_st_32x16(s_at + 16 * x, p);
+                }
+                total += sum2(sum);
+                tmem_st_wait();
+                if (some) {
+                    ok = mbar_wait(smem_u32(&v_ok[sl]), n_checked & 1, abort_flag, a.status, 0x341u);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    if (hides && (v_odd[2 * sl] || v_odd[2 * sl + 1])) {
+                        // some of V is no number, and this tile hides some of it: the product by hand, of what each row sees
+                        const int lo = see_lo - j * kTile, hi = see_hi - j * kTile;
+                        for (int c0 = 0; c0 < D; c0 += 32) {
+                            uint32_t o[32];
+                            if (j > u.lo[t]) {
+                                tmem_ld_32x32(o_at + c0, o);
+                                tmem_ld_wait();
+                                tmem_arrived(o);
+                            } else {
+#pragma unroll
+                                for (int c = 0; c < 32; ++c) o[c] = 0;
+                            }
+                            for (int k = 0; k < kTile; ++k) {
+                                uint32_t two = tmem_ld_32x1(s_at + k / 2);
+                                tmem_ld_wait();
+                                asm volatile("" : "+r"(two));
+                                const float w = __uint_as_float((k & 1) ? two & 0xffff0000u : two << 16);
+                                const bool seen = k >= lo && k < hi;
+                                const uint8_t* v = sV + sl * P::kTileBytes + (c0 / 64) * P::kSlab + k * 128;
+#pragma unroll
+                                for (int x = 0; x < 4; ++x) {
+                                    const uint4 q = *reinterpret_cast<const uint4*>(v + ((((c0 % 64) / 8 + x) ^ (k & 7)) << 4));
+                                    const uint32_t words[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                                    for (int y = 0; y < 4; ++y) {
+                                        float& e0 = reinterpret_cast<float&>(o[8 * x + 2 * y]);
+                                        float& e1 = reinterpret_cast<float&>(o[8 * x + 2 * y + 1]);
+                                        e0 = seen ? fmaf(w, __uint_as_float(words[y] << 16), e0) : e0;
+                                        e1 = seen ? fmaf(w, __uint_as_float(words[y] & 0xffff0000u), e1) : e1;
+                                    }
+                                }
+                            }
+                            tmem_st_32x32(o_at + c0, o);
+                        }
+                        tmem_st_wait();
+                    }
+                }
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&p_full[t]));
+            }
+            if (!ok) break;
+            it += max(0, last - first);
+            if (u.row + t * kTile >= u.lq) continue;           // the whole tile
+            const bool some = u.hi[t] > u.lo[t];
+            if (some) {
+                ok = mbar_wait(smem_u32(&o_full[t]), outs & 1, abort_flag, a.status, 0x342u);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                ++outs;
+                tc_fence_after_sync();
+            }
+            const float by = total == 0.0f ? 0.0f : 1.0f / total;
+            __nv_bfloat16* to = a.y + (long long)(u.q0 + row) * a.ldy + u.head * D;
+#pragma unroll
+            for (int c0 = 0; c0 < D; c0 += 32) {
+                uint32_t o[32];
+                if (some) {
+                    tmem_ld_32x32(o_at + c0, o);
+                    tmem_ld_wait();
+                    tmem_arrived(o);
+                }
+                if (row >= u.lq) continue;
+#pragma unroll
+                for (int x = 0; x < 32; x += 8) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) w[y] = by == 0.0f ? 0u : bf16x2(__uint_as_float(o[x + 2 * y]) * by, __uint_as_float(o[x + 2 * y + 1]) * by);
+                    *reinterpret_cast<uint4*>(to + c0 + x) = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            }
+            tc_fence_before_sync();                            // the next unit's first PV comes after this warp's next p_full
+        }
+    }
+
+    __syncwarp();
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after_sync();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                             const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// Heads of bf16 values as a 3-D tensor (values, heads, tokens), a token `pitch` elements after the other: boxes of 64 values of one head
+// x 128 tokens in the 128-byte swizzle.
+int encode_heads(CUtensorMap* map, const void* base, int64_t dim, int64_t heads, int64_t tokens, int64_t pitch) {
+    static EncodeFn fn = nullptr;
+    if (!fn) {
+        void* sym = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &q) != cudaSuccess || !sym || q != cudaDriverEntryPointSuccess) {
+            (void)cudaGetLastError();
+            return NQ_ERR_CUDA;
+        }
+        fn = reinterpret_cast<EncodeFn>(sym);
+    }
+    const cuuint64_t dims[3] = {(cuuint64_t)dim, (cuuint64_t)heads, (cuuint64_t)(tokens > 0 ? tokens : 1)}, strides[2] = {(cuuint64_t)dim * 2, (cuuint64_t)pitch * 2};
+    const cuuint32_t box[3] = {64, 1, kTile}, each[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? NQ_OK : NQ_ERR_CUDA;
+}
+
+template <int D>
+int launch_prompt(const nq_prompt_desc* d, const void* Q, const void* K, const void* V, const PromptArgs& a, int64_t most, cudaStream_t s) {
+    CUtensorMap tmQ, tmK, tmV;
+    int st = encode_heads(&tmQ, Q, D, d->q_heads, d->rows_q, d->ldq);
+    // (no keys at all: nothing is loaded, but a map needs an address)
+    if (st == NQ_OK) st = encode_heads(&tmK, d->rows_k > 0 ? K : Q, D, d->kv_heads, d->rows_k, d->rows_k > 0 ? d->ldk : d->kv_heads * (int64_t)D);
+    if (st == NQ_OK) st = encode_heads(&tmV, d->rows_k > 0 ? V : Q, D, d->kv_heads, d->rows_k, d->rows_k > 0 ? d->ldv : d->kv_heads * (int64_t)D);
+    if (st != NQ_OK) return st;
+    if (cudaFuncSetAttribute(prompt_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return NQ_ERR_CUDA;
+    }
+    const unsigned grid = (unsigned)(most < sm_count() ? most : sm_count());
+    return launch_chained(prompt_kernel<D>, grid, kThreads, Shape<D>::kSmem, 1, s, tmQ, tmK, tmV, a);
+}
+
+}  // namespace
+}  // namespace nq
+
+extern "C" int nq_prompt_attention(const nq_prompt_desc* d, const void* Q, const void* K, const void* V, const int32_t* starts_q, const int32_t* starts_k,
+                                   void* Y, void* stream) {
+    if (!d || d->seqs < 0 || d->rows_q < 0 || d->rows_k < 0 || d->q_heads <= 0 || d->kv_heads <= 0 || d->q_heads % d->kv_heads || d->window < 0) return NQ_ERR_INVALID_ARG;
+    if (!(d->scale > 0.0f) || !(d->scale - d->scale == 0.0f)) return NQ_ERR_INVALID_ARG;
+    if (d->head_dim != 64 && d->head_dim != 128) return NQ_ERR_UNSUPPORTED;
+    const int64_t most_rows = 0x7fffffffll - 4096;
+    if (d->rows_q > most_rows || d->rows_k > most_rows || d->seqs >= 1 << 30 || d->q_heads > 65536) return NQ_ERR_UNSUPPORTED;
+    if (d->seqs == 0 || d->rows_q == 0) return NQ_OK;
+    const int64_t wide = (int64_t)d->q_heads * d->head_dim, narrow = (int64_t)d->kv_heads * d->head_dim;
+    if (!Q || !Y || (d->rows_k > 0 && (!K || !V)) || !starts_q || !starts_k) return NQ_ERR_INVALID_ARG;
+    if (d->ldq < wide || d->ldy < wide || (d->rows_k > 0 && (d->ldk < narrow || d->ldv < narrow))) return NQ_ERR_INVALID_ARG;
+    const auto off = [](const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; };
+    if (off(Q, 16) || off(Y, 16) || (d->ldq & 7) || (d->ldy & 7) || off(starts_q, 4) || off(starts_k, 4)) return NQ_ERR_ALIGNMENT;
+    if (d->rows_k > 0 && (off(K, 16) || off(V, 16) || (d->ldk & 7) || (d->ldv & 7))) return NQ_ERR_ALIGNMENT;
+    const int64_t most = (d->rows_q / 256 + (d->seqs < d->rows_q ? d->seqs : d->rows_q)) * d->q_heads;      // units
+    if (most > 0x7fff0000ll || d->ldq >= 1ll << 38 || d->ldk >= 1ll << 38 || d->ldv >= 1ll << 38) return NQ_ERR_UNSUPPORTED;
+    nq::PromptArgs a = {};
+    a.starts_q = starts_q; a.starts_k = starts_k; a.seqs = (int)d->seqs; a.rows_q = (int)d->rows_q; a.rows_k = (int)d->rows_k;
+    a.q_heads = d->q_heads; a.group = d->q_heads / d->kv_heads; a.causal = d->causal != 0; a.window = d->window;
+    a.scale2 = d->scale * 1.44269504088896341f;
+    a.y = static_cast<__nv_bfloat16*>(Y); a.ldy = d->ldy;
+    a.status = nq::status_word();
+    if (!a.status) return NQ_ERR_CUDA;
+    const cudaStream_t s = (cudaStream_t)stream;
+    return d->head_dim == 64 ? nq::launch_prompt<64>(d, Q, K, V, a, most, s) : nq::launch_prompt<128>(d, Q, K, V, a, most, s);
+}

@@ -123,3 +123,20 @@ def test_python_refusals():
         nq.nq_qk_norm_rotate(bf(3, 256), None, None, q_heads=2, kv_heads=1)
     with pytest.raises(ValueError, match="\\[rows, cols\\]"):
         nq.nq_qk_norm_rotate(bf(3, 2, 128), None, None, q_heads=2, kv_heads=1)
+
+
+def test_prompt_attention(L):
+    def call(q=64, k=64, v=64, sq=64, sk=64, y=64, **change):
+        base = dict(seqs=2, rows_q=9, rows_k=11, ldq=256, ldk=128, ldv=128, ldy=256, q_heads=4, kv_heads=2, head_dim=64, causal=1, window=0, scale=0.125)
+        d = nq.nq_prompt_desc(**{**base, **change})
+        return L.nq_prompt_attention(ctypes.addressof(d), q, k, v, sq, sk, y, None)
+    for change in (dict(seqs=-1), dict(rows_q=-1), dict(rows_k=-1), dict(q_heads=0), dict(kv_heads=0), dict(q_heads=3), dict(window=-1), dict(scale=0.0), dict(scale=-1.0),
+                   dict(scale=float("nan")), dict(scale=float("inf")), dict(q=None), dict(k=None), dict(v=None), dict(sq=None), dict(sk=None), dict(y=None), dict(ldq=255),
+                   dict(ldk=127), dict(ldv=127), dict(ldy=255)):
+        assert call(**change) == 1, change
+    for change in (dict(head_dim=96), dict(head_dim=256), dict(rows_q=1 << 31), dict(rows_k=1 << 31), dict(seqs=1 << 30), dict(q_heads=65538)):
+        assert call(**change) == 2, change
+    for change in (dict(q=72), dict(k=72), dict(v=72), dict(y=72), dict(sq=66), dict(sk=66), dict(ldq=260), dict(ldk=132), dict(ldv=132), dict(ldy=260)):
+        assert call(**change) == 3, change
+    assert call(seqs=0, q=None) == 0 and call(rows_q=0, q=None) == 0
+    assert L.nq_prompt_attention(None, 64, 64, 64, 64, 64, 64, None) == 1
