@@ -109,6 +109,19 @@ __device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
     return r;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// scores of the columns outside [lo, hi) to -infinity
+__device__ __forceinline__ void hide(uint32_t (&s)[32], int lo, int hi) {
+    const uint32_t below = lo <= 0 ? 0u : lo >= 32 ? ~0u : (1u << lo) - 1u, under = hi <= 0 ? 0u : hi >= 32 ? ~0u : (1u << hi) - 1u;
+    const uint32_t keep = under & ~below;
+#pragma unroll
+    for (int c = 0; c < 32; ++c) s[c] = (keep >> c) & 1u ? s[c] : 0xff800000u;
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const PromptArgs a) {
@@ -117,13 +130,11 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     constexpr uint32_t kS = 0, kO = 256;                       // tensor memory columns: S of tile t at kS + 128 t, O at kO + D t
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    uint8_t* sQ = smem;                                        // [2 tiles]
-    uint8_t* sK = sQ + 2 * P::kTileBytes;                      // [ST]
-    uint8_t* sV = sK + ST * P::kTileBytes;                     // [ST]
-    uint64_t* bars = reinterpret_cast<uint64_t*>(sV + ST * P::kTileBytes);
-    uint64_t *q_full = bars, *q_empty = q_full + 1, *s_full = q_empty + 1, *p_full = s_full + 2, *o_full = p_full + 2;
-    uint64_t *k_full = o_full + 2, *k_empty = k_full + ST, *v_full = k_empty + ST, *v_empty = v_full + ST, *v_ok = v_empty + ST;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(v_ok + ST);
+    // shared-memory addresses: tiles of Q [2], K [ST], V [ST], then barriers
+    const uint32_t sQ = smem_u32(smem), sK = sQ + 2 * P::kTileBytes, sV = sK + ST * P::kTileBytes, bars = sV + ST * P::kTileBytes;
+    const uint32_t q_full = bars, q_empty = bars + 8, s_full = bars + 16, p_full = bars + 32, o_full = bars + 48;               // the last three [2]
+    const uint32_t k_full = bars + 64, k_empty = k_full + 8 * ST, v_full = k_empty + 8 * ST, v_empty = v_full + 8 * ST, v_ok = v_empty + 8 * ST;   // [ST]
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + (2 + 2 * ST) * P::kTileBytes + 64 + 40 * ST);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     volatile int* v_odd = abort_flag + 1;                      // [ST][2]: whether the step's V holds what is no number, by the two warps
     __shared__ int s_before[kThreads + 1];
@@ -131,13 +142,13 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        mbar_init(smem_u32(q_full), 1);
-        mbar_init(smem_u32(q_empty), 1);
-        for (int t = 0; t < 2; ++t) { mbar_init(smem_u32(&s_full[t]), 1); mbar_init(smem_u32(&p_full[t]), 4); mbar_init(smem_u32(&o_full[t]), 1); }
+        mbar_init(q_full, 1);
+        mbar_init(q_empty, 1);
+        for (int t = 0; t < 2; ++t) { mbar_init(s_full + 8 * t, 1); mbar_init(p_full + 8 * t, 4); mbar_init(o_full + 8 * t, 1); }
         for (int s = 0; s < ST; ++s) {
-            mbar_init(smem_u32(&k_full[s]), 1); mbar_init(smem_u32(&k_empty[s]), 1);
-            mbar_init(smem_u32(&v_full[s]), 1); mbar_init(smem_u32(&v_empty[s]), 3);       // the products and warps 2, 3
-            mbar_init(smem_u32(&v_ok[s]), 2);
+            mbar_init(k_full + 8 * s, 1); mbar_init(k_empty + 8 * s, 1);
+            mbar_init(v_full + 8 * s, 1); mbar_init(v_empty + 8 * s, 3);       // the products and warps 2, 3
+            mbar_init(v_ok + 8 * s, 2);
         }
         *abort_flag = 0;
         fence_barrier_init();
@@ -178,163 +189,168 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     const int units = s_before[kThreads] * a.q_heads;          // the host has checked that it fits
     const auto nth = [&](int round) { return round * (int)gridDim.x + ((round & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x); };
 
-    // 128 x 80 + 256 x 208 registers of the 384 x 168 that the block was launched with
-    if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-    else asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-    if (warp == 0) {
-        if (lane == 0) {
-            uint32_t it = 0;                                   // steps so far
-            bool ok = true;
-            uint32_t used = 0;                                 // units with any step
-            for (int r = 0; ok && r * (int)gridDim.x < units; ++r) {
-                if (nth(r) >= units) continue;
-                const Unit u = unit_of(a, s_before, chunk, nth(r));
-                if (u.last() <= u.first()) continue;
-                if (!(ok = mbar_wait(smem_u32(q_empty), (used & 1) ^ 1, abort_flag, a.status, 0x310u))) break;
-                ++used;
-                const bool two[2] = {u.hi[0] > u.lo[0], u.hi[1] > u.lo[1]};
-                mbar_arrive_expect_tx(smem_u32(q_full), (two[0] + two[1]) * P::kTileBytes);
+    // 128 x 72 + 256 x 216 registers, all of the 384 x 168 that the block was launched with
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if (warp == 0) {
+            if (lane == 0) {
+                uint32_t it = 0;                                   // steps so far
+                bool ok = true;
+                uint32_t used = 0;                                 // units with any step
+                for (int r = 0; ok && r * (int)gridDim.x < units; ++r) {
+                    if (nth(r) >= units) continue;
+                    const Unit u = unit_of(a, s_before, chunk, nth(r));
+                    if (u.last() <= u.first()) continue;
+                    if (!(ok = mbar_wait(q_empty, (used & 1) ^ 1, abort_flag, a.status, 0x310u))) break;
+                    ++used;
+                    const bool two[2] = {u.hi[0] > u.lo[0], u.hi[1] > u.lo[1]};
+                    mbar_arrive_expect_tx(q_full, (two[0] + two[1]) * P::kTileBytes);
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
-                    if (two[t])
+                    for (int t = 0; t < 2; ++t)
+                        if (two[t])
+#pragma unroll
+                            for (int h = 0; h < D / 64; ++h)
+                                tma_load_3d(sQ + t * P::kTileBytes + h * P::kSlab, &tmQ, 64 * h, u.head, u.q0 + u.row + t * kTile, q_full);
+                    for (int j = u.first(); j < u.last(); ++j, ++it) {
+                        const uint32_t s = it % ST, use = it / ST;
+                        if (!(ok = mbar_wait(k_empty + 8 * s, (use & 1) ^ 1, abort_flag, a.status, 0x311u))) break;
+                        mbar_arrive_expect_tx(k_full + 8 * s, P::kTileBytes);
 #pragma unroll
                         for (int h = 0; h < D / 64; ++h)
-                            tma_load_3d(smem_u32(sQ + t * P::kTileBytes + h * P::kSlab), &tmQ, 64 * h, u.head, u.q0 + u.row + t * kTile, smem_u32(q_full));
-                for (int j = u.first(); j < u.last(); ++j, ++it) {
-                    const uint32_t s = it % ST, use = it / ST;
-                    if (!(ok = mbar_wait(smem_u32(&k_empty[s]), (use & 1) ^ 1, abort_flag, a.status, 0x311u))) break;
-                    mbar_arrive_expect_tx(smem_u32(&k_full[s]), P::kTileBytes);
+                            tma_load_3d(sK + s * P::kTileBytes + h * P::kSlab, &tmK, 64 * h, u.head / a.group, u.k0 + j * kTile, k_full + 8 * s);
+                        if (!(ok = mbar_wait(v_empty + 8 * s, (use & 1) ^ 1, abort_flag, a.status, 0x312u))) break;
+                        mbar_arrive_expect_tx(v_full + 8 * s, P::kTileBytes);
 #pragma unroll
-                    for (int h = 0; h < D / 64; ++h)
-                        tma_load_3d(smem_u32(sK + s * P::kTileBytes + h * P::kSlab), &tmK, 64 * h, u.head / a.group, u.k0 + j * kTile, smem_u32(&k_full[s]));
-                    if (!(ok = mbar_wait(smem_u32(&v_empty[s]), (use & 1) ^ 1, abort_flag, a.status, 0x312u))) break;
-                    mbar_arrive_expect_tx(smem_u32(&v_full[s]), P::kTileBytes);
-#pragma unroll
-                    for (int h = 0; h < D / 64; ++h)
-                        tma_load_3d(smem_u32(sV + s * P::kTileBytes + h * P::kSlab), &tmV, 64 * h, u.head / a.group, u.k0 + j * kTile, smem_u32(&v_full[s]));
+                        for (int h = 0; h < D / 64; ++h)
+                            tma_load_3d(sV + s * P::kTileBytes + h * P::kSlab, &tmV, 64 * h, u.head / a.group, u.k0 + j * kTile, v_full + 8 * s);
+                    }
+                }
+                if (!ok) {
+                    const long long t0 = clock64();                // let copies in flight land before shared memory is released
+                    while (clock64() - t0 < (1ll << 22)) { }
                 }
             }
-            if (!ok) {
-                const long long t0 = clock64();                // let copies in flight land before shared memory is released
-                while (clock64() - t0 < (1ll << 22)) { }
+        } else if (warp == 1) {
+            if (lane == 0) {
+                constexpr uint32_t kQK = idesc_bf16(kTile, kTile, false), kPV = idesc_bf16(kTile, D, true);
+                uint32_t it = 0, used = 0, weights = 0, checked = 0;            // the latter two: a phase bit for each tile, for each stage
+                bool ok = true;
+                for (int r = 0; ok && r * (int)gridDim.x < units; ++r) {
+                    if (nth(r) >= units) continue;
+                    const Unit u = unit_of(a, s_before, chunk, nth(r));
+                    const int first = u.first(), last = u.last();
+                    if (last <= first) continue;
+                    if (!(ok = mbar_wait(q_full, used & 1, abort_flag, a.status, 0x320u))) break;
+                    ++used;
+                    for (int j = first; ok && j <= last; ++j) {
+                        const uint32_t i = it + (j - first), s = i % ST, use = i / ST;           // of step j
+                        const uint32_t sp = (i - 1) % ST, usep = (i - 1) / ST;                   // of step j - 1
+                        bool odd = false;
+                        if (j < last && !(ok = mbar_wait(k_full + 8 * s, use & 1, abort_flag, a.status, 0x321u))) break;
+                        if (j > first) {
+                            if (u.hides(0, j - 1) || u.hides(1, j - 1)) {
+                                if (!(ok = mbar_wait(v_ok + 8 * sp, (checked >> sp) & 1, abort_flag, a.status, 0x322u))) break;
+                                checked ^= 1u << sp;
+                                odd = v_odd[2 * sp] || v_odd[2 * sp + 1];
+                            }
+                            if (!(ok = mbar_wait(v_full + 8 * sp, usep & 1, abort_flag, a.status, 0x323u))) break;
+                        }
+#pragma unroll 1
+                        for (int t = 0; t < 2; ++t) {                                            // (unrolled it takes more registers than there are)
+                            const int lo = t ? u.lo[1] : u.lo[0], hi = t ? u.hi[1] : u.hi[0];
+                            if (j > lo && j <= hi) {
+                                if (!(ok = mbar_wait(p_full + 8 * t, (weights >> t) & 1, abort_flag, a.status, 0x324u))) break;
+                                weights ^= 1u << t;
+                                tc_fence_after_sync();
+                                if (!(odd && (t ? u.hides(1, j - 1) : u.hides(0, j - 1)))) {
+                                    const uint64_t dv = smem_desc_mn_sw128(sV + sp * P::kTileBytes, P::kSlab);
+                                    const uint32_t to = tmem + kO + t * D, from = tmem + kS + t * kTile;
+#pragma unroll
+                                    for (int k = 0; k < kTile / 16; ++k) mma_bf16_ts(to, from + 8 * k, dv + k * (16 * 128 / 16), kPV, k > 0 || j - 1 > lo);
+                                }
+                                if (j == hi) mma_commit(o_full + 8 * t);
+                            }
+                            if (j >= lo && j < hi) {
+                                tc_fence_after_sync();
+                                const uint64_t dq = smem_desc_sw128(sQ + t * P::kTileBytes), dk = smem_desc_sw128(sK + s * P::kTileBytes);
+                                const uint32_t to = tmem + kS + t * kTile;
+#pragma unroll
+                                for (int k = 0; k < D / 16; ++k) {
+                                    const uint64_t at = (k % 4) * 2 + (k / 4) * (P::kSlab / 16);
+                                    mma_bf16(to, dq + at, dk + at, kQK, k > 0);
+                                }
+                                mma_commit(s_full + 8 * t);
+                            }
+                        }
+                        if (!ok) break;
+                        if (j > first) mma_commit(v_empty + 8 * sp);
+                        if (j < last) mma_commit(k_empty + 8 * s);
+                        if (j == last - 1) mma_commit(q_empty);
+                    }
+                    it += last - first;
+                }
             }
-        }
-    } else if (warp == 1) {
-        if (lane == 0) {
-            constexpr uint32_t kQK = idesc_bf16(kTile, kTile, false), kPV = idesc_bf16(kTile, D, true);
-            uint32_t it = 0, used = 0, weights[2] = {0, 0}, checked[ST] = {};
+        } else {
+            // rows (warp - 2) * 64 .. + 64 of V where a step hides something
+            uint32_t it = 0;
             bool ok = true;
             for (int r = 0; ok && r * (int)gridDim.x < units; ++r) {
                 if (nth(r) >= units) continue;
                 const Unit u = unit_of(a, s_before, chunk, nth(r));
                 const int first = u.first(), last = u.last();
-                if (last <= first) continue;
-                if (!(ok = mbar_wait(smem_u32(q_full), used & 1, abort_flag, a.status, 0x320u))) break;
-                ++used;
-                for (int j = first; ok && j <= last; ++j) {
-                    const uint32_t i = it + (j - first), s = i % ST, use = i / ST;           // of step j
-                    const uint32_t sp = (i - 1) % ST, usep = (i - 1) / ST;                   // of step j - 1
-                    bool odd = false;
-                    if (j < last && !(ok = mbar_wait(smem_u32(&k_full[s]), use & 1, abort_flag, a.status, 0x321u))) break;
-                    if (j > first) {
-                        if (u.hides(0, j - 1) || u.hides(1, j - 1)) {
-                            uint32_t n = 0;
-#pragma unroll
-                            for (int x = 0; x < ST; ++x)
-                                if (x == (int)sp) n = checked[x]++;
-                            if (!(ok = mbar_wait(smem_u32(&v_ok[sp]), n & 1, abort_flag, a.status, 0x322u))) break;
-                            odd = v_odd[2 * sp] || v_odd[2 * sp + 1];
-                        }
-                        if (!(ok = mbar_wait(smem_u32(&v_full[sp]), usep & 1, abort_flag, a.status, 0x323u))) break;
-                    }
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        if (j > first && u.takes(t, j - 1)) {
-                            if (!(ok = mbar_wait(smem_u32(&p_full[t]), weights[t]++ & 1, abort_flag, a.status, 0x324u))) break;
-                            tc_fence_after_sync();
-                            if (!(odd && u.hides(t, j - 1))) {
-                                const uint64_t dv = smem_desc_mn_sw128(smem_u32(sV + sp * P::kTileBytes), P::kSlab);
-#pragma unroll
-                                for (int k = 0; k < kTile / 16; ++k)
-                                    mma_bf16_ts(tmem + kO + t * D, tmem + kS + t * kTile + 8 * k, dv + k * (16 * 128 / 16), kPV, j - 1 > u.lo[t] || k > 0);
-                            }
-                            if (j == u.hi[t]) mma_commit(smem_u32(&o_full[t]));
-                        }
-                        if (j < last && u.takes(t, j)) {
-                            tc_fence_after_sync();
-                            const uint64_t dq = smem_desc_sw128(smem_u32(sQ + t * P::kTileBytes)), dk = smem_desc_sw128(smem_u32(sK + s * P::kTileBytes));
-#pragma unroll
-                            for (int k = 0; k < D / 16; ++k) {
-                                const uint64_t at = (k % 4) * 2 + (k / 4) * (P::kSlab / 16);
-                                mma_bf16(tmem + kS + t * kTile, dq + at, dk + at, kQK, k > 0);
-                            }
-                            mma_commit(smem_u32(&s_full[t]));
-                        }
-                    }
+                for (int j = first; j < last; ++j) {
+                    // every step is waited for and let go, for a wait must not be more than one phase behind its barrier
+                    const uint32_t i = it + (j - first), s = i % ST, use = i / ST;
+                    ok = mbar_wait(v_full + 8 * s, use & 1, abort_flag, a.status, 0x330u);
+                    ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
-                    if (j > first) mma_commit(smem_u32(&v_empty[sp]));
-                    if (j < last) mma_commit(smem_u32(&k_empty[s]));
-                    if (j == last - 1) mma_commit(smem_u32(q_empty));
-                }
-                it += last - first;
-            }
-        }
-    } else if (warp < 4) {
-        // rows (warp - 2) * 64 .. + 64 of V where a step hides something
-        uint32_t it = 0;
-        bool ok = true;
-        for (int r = 0; ok && r * (int)gridDim.x < units; ++r) {
-            if (nth(r) >= units) continue;
-            const Unit u = unit_of(a, s_before, chunk, nth(r));
-            const int first = u.first(), last = u.last();
-            for (int j = first; j < last; ++j) {
-                // every step is waited for and let go, for a wait must not be more than one phase behind its barrier
-                const uint32_t i = it + (j - first), s = i % ST, use = i / ST;
-                ok = mbar_wait(smem_u32(&v_full[s]), use & 1, abort_flag, a.status, 0x330u);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                if (!u.hides(0, j) && !u.hides(1, j)) {
-                    if (lane == 0) mbar_arrive(smem_u32(&v_empty[s]));
-                    continue;
-                }
-                const int live = u.lk - j * kTile;             // rows of the sequence
-                uint32_t odd = 0;
-                // a lane takes a 16-byte piece of every fourth row: 8 lanes are a row of 64 values
+                    if (!u.hides(0, j) && !u.hides(1, j)) {
+                        if (lane == 0) mbar_arrive(v_empty + 8 * s);
+                        continue;
+                    }
+                    const int live = u.lk - j * kTile;             // rows of the sequence
+                    uint32_t odd = 0;
+                    // a lane takes a 16-byte piece of every fourth row: 8 lanes are a row of 64 values
 #pragma unroll
-                for (int h = 0; h < D / 64; ++h) {
-                    for (int x = 0; x < 64; x += 4) {
-                        const int row = (warp - 2) * 64 + x + (lane >> 3);
-                        uint4* p = reinterpret_cast<uint4*>(sV + s * P::kTileBytes + h * P::kSlab + row * 128 + (lane & 7) * 16);
-                        if (row >= live) {
-                            *p = make_uint4(0, 0, 0, 0);
-                        } else {
-                            const uint4 v = *p;
-                            odd |= ((v.x & 0x7f807f80u) + 0x00800080u) | ((v.y & 0x7f807f80u) + 0x00800080u) | ((v.z & 0x7f807f80u) + 0x00800080u) |
-                                   ((v.w & 0x7f807f80u) + 0x00800080u);
+                    for (int h = 0; h < D / 64; ++h) {
+                        for (int x = 0; x < 64; x += 4) {
+                            const int row = (warp - 2) * 64 + x + (lane >> 3);
+                            uint4* p = reinterpret_cast<uint4*>(smem + (2 + ST + s) * P::kTileBytes + h * P::kSlab + row * 128 + (lane & 7) * 16);
+                            if (row >= live) {
+                                *p = make_uint4(0, 0, 0, 0);
+                            } else {
+                                const uint4 v = *p;
+                                odd |= ((v.x & 0x7f807f80u) + 0x00800080u) | ((v.y & 0x7f807f80u) + 0x00800080u) | ((v.z & 0x7f807f80u) + 0x00800080u) |
+                                       ((v.w & 0x7f807f80u) + 0x00800080u);
+                            }
                         }
                     }
+                    const bool any = __any_sync(0xffffffffu, (odd & 0x80008000u) != 0);
+                    fence_proxy_async_smem();
+                    if (lane == 0) v_odd[2 * s + warp - 2] = any;
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(v_ok + 8 * s);
+                        mbar_arrive(v_empty + 8 * s);
+                    }
                 }
-                const bool any = __any_sync(0xffffffffu, (odd & 0x80008000u) != 0);
-                fence_proxy_async_smem();
-                if (lane == 0) v_odd[2 * s + warp - 2] = any;
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(smem_u32(&v_ok[s]));
-                    mbar_arrive(smem_u32(&v_empty[s]));
-                }
+                it += max(0, last - first);
             }
-            it += max(0, last - first);
         }
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         const int t = (warp - 4) >> 2, quarter = warp & 3;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         const uint32_t s_at = tmem + kS + t * kTile + lanes, o_at = tmem + kO + t * D + lanes;
-        uint32_t it = 0, scores = 0, outs = 0, checked[ST] = {};
+        uint32_t it = 0, scores = 0, outs = 0, checked = 0;
         bool ok = true;
         for (int r = 0; ok && r * (int)gridDim.x < units; ++r) {
             if (nth(r) >= units) continue;
             const Unit u = unit_of(a, s_before, chunk, nth(r));
             const int first = u.first(), last = u.last();
+            // (arrays that t picks from would live in local memory, which has next to no L1 here: 900 us for 8192 tokens of 8 heads against 165)
+            const int lo_t = t ? u.lo[1] : u.lo[0], hi_t = t ? u.hi[1] : u.hi[0];
+            const int all_lo = t ? u.all_lo[1] : u.all_lo[0], all_hi = t ? u.all_hi[1] : u.all_hi[0];
             const int row = u.row + t * kTile + quarter * 32 + lane, off = u.lk - u.lq;
             const int mine = min(row, u.lq - 1);               // rows behind the last one only must not get in the way
             const int see_hi = a.causal ? min(u.lk, mine + off + 1) : u.lk, see_lo = a.window ? max(0, mine + off + 1 - a.window) : 0;
@@ -342,45 +358,38 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             for (int j = first; j < last; ++j) {
                 const uint32_t sl = (it + (j - first)) % ST;
                 const bool some = u.hides(0, j) || u.hides(1, j);
-                uint32_t n_checked = 0;
-                if (some) {
-#pragma unroll
-                    for (int x = 0; x < ST; ++x)
-                        if (x == (int)sl) n_checked = checked[x]++;
-                }
-                if (!u.takes(t, j)) continue;
-                ok = mbar_wait(smem_u32(&s_full[t]), scores & 1, abort_flag, a.status, 0x340u);
+                const uint32_t phase = (checked >> sl) & 1;
+                if (some) checked ^= 1u << sl;
+                if (j < lo_t || j >= hi_t) continue;
+                ok = mbar_wait(s_full + 8 * t, scores & 1, abort_flag, a.status, 0x340u);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 ++scores;
                 tc_fence_after_sync();
-                uint32_t s[4][32];
-#pragma unroll
-                for (int x = 0; x < 4; ++x) tmem_ld_32x32(s_at + 32 * x, s[x]);
-                tmem_ld_wait();
-#pragma unroll
-                for (int x = 0; x < 4; ++x) tmem_arrived(s[x]);
-                const bool hides = u.hides(t, j);
-                if (hides) {
-                    const int lo = see_lo - j * kTile, hi = see_hi - j * kTile;
-#pragma unroll
-                    for (int x = 0; x < 4; ++x)
-#pragma unroll
-                        for (int c = 0; c < 32; ++c)
-                            if (32 * x + c < lo || 32 * x + c >= hi) s[x][c] = 0xff800000u;
-                }
+                const bool hides = j * kTile < all_lo || (j + 1) * kTile > all_hi;
+                const int lo = see_lo - j * kTile, hi = see_hi - j * kTile;                  // columns that this row sees
                 float m = -INFINITY;
 #pragma unroll
-                for (int x = 0; x < 4; ++x)
+                for (int x = 0; x < 4; x += 2) {
+                    uint32_t s[2][32];
+                    tmem_ld_32x32(s_at + 32 * x, s[0]);
+                    tmem_ld_32x32(s_at + 32 * x + 32, s[1]);
+                    tmem_ld_wait();
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) m = fmaxf(m, __uint_as_float(s[x][c]));
+                    for (int y = 0; y < 2; ++y) {
+                        tmem_arrived(s[y]);
+                        if (hides) hide(s[y], lo - 32 * (x + y), hi - 32 * (x + y));
+#pragma unroll
+                        for (int c = 0; c < 32; c += 2) m = max3(m, __uint_as_float(s[y][c]), __uint_as_float(s[y][c + 1]));
+                    }
+                }
                 m *= a.scale2;
                 const bool move = m > top + kRescale;
                 if (__any_sync(0xffffffffu, move)) {
                     const float to = fmaxf(top, m), by = top == -INFINITY ? 0.0f : exp2a(top - to);
                     top = to;
                     total *= by;
-                    if (j > u.lo[t]) {
+                    if (j > lo_t) {
 #pragma unroll
                         for (int c0 = 0; c0 < D; c0 += 32) {
                             uint32_t o[32];
@@ -395,32 +404,39 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 }
                 const float minus = top == -INFINITY ? 0.0f : -top;
                 uint64_t sum = 0;
+                // S is read a second time, 32 columns ahead of their use, rather than kept: all 128 with what the weights need do not
+                // fit into the registers (900 us for 8192 tokens of 8 heads, when what did not fit went to local memory)
+                uint32_t s[2][32];
+                tmem_ld_32x32(s_at, s[0]);
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
+                    tmem_ld_wait();
+                    tmem_arrived(s[x & 1]);
+                    if (x < 3) tmem_ld_32x32(s_at + 32 * (x + 1), s[(x + 1) & 1]);
+                    if (hides) hide(s[x & 1], lo - 32 * x, hi - 32 * x);
                     uint32_t p[16];
 #pragma unroll
                     for (int c = 0; c < 32; c += 2) {
                         float e0, e1;
-                        unpack2(fma2(pack2(s[x][c], s[x][c + 1]), both(a.scale2), both(minus)), e0, e1);
+                        unpack2(fma2(pack2(s[x & 1][c], s[x & 1][c + 1]), both(a.scale2), both(minus)), e0, e1);
                         e0 = exp2a(e0);
                         e1 = exp2a(e1);
                         sum = add2(sum, pack2f(e0, e1));
                         p[c / 2] = bf16x2(e0, e1);             // a weight is off by at most 2^-9 of itself
                     }
-                    tmem_st_32x16(s_at + 16 * x, p);
+                    tmem_st_32x16(s_at + 16 * x, p);           // over columns that have been read
                 }
                 total += sum2(sum);
                 tmem_st_wait();
                 if (some) {
-                    ok = mbar_wait(smem_u32(&v_ok[sl]), n_checked & 1, abort_flag, a.status, 0x341u);
+                    ok = mbar_wait(v_ok + 8 * sl, phase, abort_flag, a.status, 0x341u);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
                     if (hides && (v_odd[2 * sl] || v_odd[2 * sl + 1])) {
                         // some of V is no number, and this tile hides some of it: the product by hand, of what each row sees
-                        const int lo = see_lo - j * kTile, hi = see_hi - j * kTile;
                         for (int c0 = 0; c0 < D; c0 += 32) {
                             uint32_t o[32];
-                            if (j > u.lo[t]) {
+                            if (j > lo_t) {
                                 tmem_ld_32x32(o_at + c0, o);
                                 tmem_ld_wait();
                                 tmem_arrived(o);
@@ -434,7 +450,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                                 asm volatile("" : "+r"(two));
                                 const float w = __uint_as_float((k & 1) ? two & 0xffff0000u : two << 16);
                                 const bool seen = k >= lo && k < hi;
-                                const uint8_t* v = sV + sl * P::kTileBytes + (c0 / 64) * P::kSlab + k * 128;
+                                const uint8_t* v = smem + (2 + ST + sl) * P::kTileBytes + (c0 / 64) * P::kSlab + k * 128;
 #pragma unroll
                                 for (int x = 0; x < 4; ++x) {
                                     const uint4 q = *reinterpret_cast<const uint4*>(v + ((((c0 % 64) / 8 + x) ^ (k & 7)) << 4));
@@ -455,14 +471,14 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 }
                 tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&p_full[t]));
+                if (lane == 0) mbar_arrive(p_full + 8 * t);
             }
             if (!ok) break;
             it += max(0, last - first);
             if (u.row + t * kTile >= u.lq) continue;           // the whole tile
-            const bool some = u.hi[t] > u.lo[t];
+            const bool some = hi_t > lo_t;
             if (some) {
-                ok = mbar_wait(smem_u32(&o_full[t]), outs & 1, abort_flag, a.status, 0x342u);
+                ok = mbar_wait(o_full + 8 * t, outs & 1, abort_flag, a.status, 0x342u);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 ++outs;
