@@ -114,6 +114,23 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
+// Asks for a thread block of this grid that has not begun: its launch is cancelled, and 16 bytes that name it (or say that there is none)
+// arrive at `to` and are counted on `bar`.
+__device__ __forceinline__ void cancel_next(uint32_t to, uint32_t bar) {
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(to), "r"(bar) : "memory");
+}
+// The block's number, -1 where there was none.
+__device__ __forceinline__ int cancelled(uint32_t from) {
+    int index;
+    asm volatile(
+        "{\n\t.reg .pred P;\n\t.reg .b128 h;\n\t"
+        "ld.shared.b128 h, [%1];\n\t"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 P, h;\n\t"
+        "mov.b32 %0, -1;\n\t"
+        "@P clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, h;\n\t}"
+        : "=r"(index) : "r"(from) : "memory");
+    return index;
+}
 // scores of the columns outside [lo, hi) to -infinity
 __device__ __forceinline__ void hide(uint32_t (&s)[32], int lo, int hi) {
     const uint32_t below = lo <= 0 ? 0u : lo >= 32 ? ~0u : (1u << lo) - 1u, under = hi <= 0 ? 0u : hi >= 32 ? ~0u : (1u << hi) - 1u;
@@ -134,11 +151,14 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     const uint32_t sQ = smem_u32(smem), sK = sQ + 2 * P::kTileBytes, sV = sK + ST * P::kTileBytes, bars = sV + ST * P::kTileBytes;
     const uint32_t q_full = bars, q_empty = bars + 8, s_full = bars + 16, p_full = bars + 32, o_full = bars + 48;               // the last three [2]
     const uint32_t k_full = bars + 64, k_empty = k_full + 8 * ST, v_full = k_empty + 8 * ST, v_empty = v_full + 8 * ST, v_ok = v_empty + 8 * ST;   // [ST]
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + (2 + 2 * ST) * P::kTileBytes + 64 + 40 * ST);
+    const uint32_t u_full = v_ok + 8 * ST, u_empty = u_full + 16, c_full = u_empty + 16;                                        // the first two [2]
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + (2 + 2 * ST) * P::kTileBytes + 64 + 40 * ST + 40);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     volatile int* v_odd = abort_flag + 1;                      // [ST][2]: whether the step's V holds what is no number, by the two warps
     __shared__ int s_before[kThreads + 1];
     __shared__ int s_warp[kThreads / 32];
+    __shared__ Unit s_unit[2];
+    __shared__ __align__(16) uint4 s_cancelled;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
@@ -150,6 +170,8 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             mbar_init(v_full + 8 * s, 1); mbar_init(v_empty + 8 * s, 3);       // the products and warps 2, 3
             mbar_init(v_ok + 8 * s, 2);
         }
+        for (int s = 0; s < 2; ++s) { mbar_init(u_full + 8 * s, 1); mbar_init(u_empty + 8 * s, 11); }       // read by MMA, warps 2 and 3, softmax
+        mbar_init(c_full, 1);
         *abort_flag = 0;
         fence_barrier_init();
         prefetch_tensormap(&tmQ);
@@ -187,43 +209,75 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     tc_fence_after_sync();
     const uint32_t tmem = *tmem_slot;
     const int units = s_before[kThreads] * a.q_heads;          // the host has checked that it fits
-    const auto nth = [&](int round) { return round * (int)gridDim.x + ((round & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x); };
+
+    // The grid has a block for each unit that there can be; a block that is done with its own takes one that has not begun (it
+    // cancels that block's launch), so that all SMs end together however the units differ.  Warp 0 does this, one unit ahead of the
+    // tensor core, and hands what it has worked out to the others.
+    const auto take = [&](uint32_t n, Unit& u) {                // the n-th unit of this block, for a whole warp; false: no more, or given up
+        bool ok = mbar_wait(u_full + 8 * (n & 1), (n >> 1) & 1, abort_flag, a.status, 0x301u);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) return false;
+        u = s_unit[n & 1];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(u_empty + 8 * (n & 1));
+        return u.lq > 0;
+    };
 
     // 128 x 72 + 256 x 216 registers, all of the 384 x 168 that the block was launched with
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == 0) {
             if (lane == 0) {
-                uint32_t it = 0;                                   // steps so far
+                uint32_t it = 0, used = 0, asks = 0;               // steps, units with any step, cancellations so far
                 bool ok = true;
-                uint32_t used = 0;                                 // units with any step
-                for (int r = 0; ok && r * (int)gridDim.x < units; ++r) {
-                    if (nth(r) >= units) continue;
-                    const Unit u = unit_of(a, s_before, chunk, nth(r));
-                    if (u.last() <= u.first()) continue;
-                    if (!(ok = mbar_wait(q_empty, (used & 1) ^ 1, abort_flag, a.status, 0x310u))) break;
-                    ++used;
-                    const bool two[2] = {u.hi[0] > u.lo[0], u.hi[1] > u.lo[1]};
-                    mbar_arrive_expect_tx(q_full, (two[0] + two[1]) * P::kTileBytes);
+                int index = blockIdx.x;                            // -1: no more
+                const uint32_t answer = smem_u32(&s_cancelled);
+                const auto ask = [&] {
+                    mbar_arrive_expect_tx(c_full, 16);
+                    cancel_next(answer, c_full);
+                };
+                const auto answered = [&] {
+                    ok = mbar_wait(c_full, asks++ & 1, abort_flag, a.status, 0x313u);
+                    index = ok ? cancelled(answer) : -1;
+                    fence_proxy_async_smem();
+                    if (index >= 0) ask();
+                };
+                ask();
+                for (uint32_t n = 0;; ++n) {
+                    while (index >= units) answered();             // (the host knows no more than how many units there can be)
+                    if (!ok || !(ok = mbar_wait(u_empty + 8 * (n & 1), ((n >> 1) & 1) ^ 1, abort_flag, a.status, 0x314u))) break;
+                    Unit u = {};
+                    if (index >= 0) u = unit_of(a, s_before, chunk, index);
+                    s_unit[n & 1] = u;
+                    mbar_arrive(u_full + 8 * (n & 1));
+                    if (index < 0) break;
+                    if (u.last() > u.first()) {
+                        if (!(ok = mbar_wait(q_empty, (used & 1) ^ 1, abort_flag, a.status, 0x310u))) break;
+                        ++used;
+                        const bool two[2] = {u.hi[0] > u.lo[0], u.hi[1] > u.lo[1]};
+                        mbar_arrive_expect_tx(q_full, (two[0] + two[1]) * P::kTileBytes);
 #pragma unroll
-                    for (int t = 0; t < 2; ++t)
-                        if (two[t])
+                        for (int t = 0; t < 2; ++t)
+                            if (two[t])
+#pragma unroll
+                                for (int h = 0; h < D / 64; ++h)
+                                    tma_load_3d(sQ + t * P::kTileBytes + h * P::kSlab, &tmQ, 64 * h, u.head, u.q0 + u.row + t * kTile, q_full);
+                        for (int j = u.first(); j < u.last(); ++j, ++it) {
+                            const uint32_t s = it % ST, use = it / ST;
+                            if (!(ok = mbar_wait(k_empty + 8 * s, (use & 1) ^ 1, abort_flag, a.status, 0x311u))) break;
+                            mbar_arrive_expect_tx(k_full + 8 * s, P::kTileBytes);
 #pragma unroll
                             for (int h = 0; h < D / 64; ++h)
-                                tma_load_3d(sQ + t * P::kTileBytes + h * P::kSlab, &tmQ, 64 * h, u.head, u.q0 + u.row + t * kTile, q_full);
-                    for (int j = u.first(); j < u.last(); ++j, ++it) {
-                        const uint32_t s = it % ST, use = it / ST;
-                        if (!(ok = mbar_wait(k_empty + 8 * s, (use & 1) ^ 1, abort_flag, a.status, 0x311u))) break;
-                        mbar_arrive_expect_tx(k_full + 8 * s, P::kTileBytes);
+                                tma_load_3d(sK + s * P::kTileBytes + h * P::kSlab, &tmK, 64 * h, u.head / a.group, u.k0 + j * kTile, k_full + 8 * s);
+                            if (!(ok = mbar_wait(v_empty + 8 * s, (use & 1) ^ 1, abort_flag, a.status, 0x312u))) break;
+                            mbar_arrive_expect_tx(v_full + 8 * s, P::kTileBytes);
 #pragma unroll
-                        for (int h = 0; h < D / 64; ++h)
-                            tma_load_3d(sK + s * P::kTileBytes + h * P::kSlab, &tmK, 64 * h, u.head / a.group, u.k0 + j * kTile, k_full + 8 * s);
-                        if (!(ok = mbar_wait(v_empty + 8 * s, (use & 1) ^ 1, abort_flag, a.status, 0x312u))) break;
-                        mbar_arrive_expect_tx(v_full + 8 * s, P::kTileBytes);
-#pragma unroll
-                        for (int h = 0; h < D / 64; ++h)
-                            tma_load_3d(sV + s * P::kTileBytes + h * P::kSlab, &tmV, 64 * h, u.head / a.group, u.k0 + j * kTile, v_full + 8 * s);
+                            for (int h = 0; h < D / 64; ++h)
+                                tma_load_3d(sV + s * P::kTileBytes + h * P::kSlab, &tmV, 64 * h, u.head / a.group, u.k0 + j * kTile, v_full + 8 * s);
+                        }
                     }
+                    if (!ok) break;
+                    answered();                                    // (asked before this unit)
                 }
                 if (!ok) {
                     const long long t0 = clock64();                // let copies in flight land before shared memory is released
@@ -235,9 +289,11 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 constexpr uint32_t kQK = idesc_bf16(kTile, kTile, false), kPV = idesc_bf16(kTile, D, true);
                 uint32_t it = 0, used = 0, weights = 0, checked = 0;            // the latter two: a phase bit for each tile, for each stage
                 bool ok = true;
-                for (int r = 0; ok && r * (int)gridDim.x < units; ++r) {
-                    if (nth(r) >= units) continue;
-                    const Unit u = unit_of(a, s_before, chunk, nth(r));
+                for (uint32_t n = 0; ok; ++n) {
+                    if (!(ok = mbar_wait(u_full + 8 * (n & 1), (n >> 1) & 1, abort_flag, a.status, 0x302u))) break;
+                    const Unit u = s_unit[n & 1];
+                    mbar_arrive(u_empty + 8 * (n & 1));
+                    if (u.lq == 0) break;
                     const int first = u.first(), last = u.last();
                     if (last <= first) continue;
                     if (!(ok = mbar_wait(q_full, used & 1, abort_flag, a.status, 0x320u))) break;
@@ -294,9 +350,8 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             // rows (warp - 2) * 64 .. + 64 of V where a step hides something
             uint32_t it = 0;
             bool ok = true;
-            for (int r = 0; ok && r * (int)gridDim.x < units; ++r) {
-                if (nth(r) >= units) continue;
-                const Unit u = unit_of(a, s_before, chunk, nth(r));
+            Unit u;
+                for (uint32_t n = 0; ok && take(n, u); ++n) {
                 const int first = u.first(), last = u.last();
                 for (int j = first; j < last; ++j) {
                     // every step is waited for and let go, for a wait must not be more than one phase behind its barrier
@@ -344,9 +399,8 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         const uint32_t s_at = tmem + kS + t * kTile + lanes, o_at = tmem + kO + t * D + lanes;
         uint32_t it = 0, scores = 0, outs = 0, checked = 0;
         bool ok = true;
-        for (int r = 0; ok && r * (int)gridDim.x < units; ++r) {
-            if (nth(r) >= units) continue;
-            const Unit u = unit_of(a, s_before, chunk, nth(r));
+        Unit u;
+            for (uint32_t n = 0; ok && take(n, u); ++n) {
             const int first = u.first(), last = u.last();
             // (arrays that t picks from would live in local memory, which has next to no L1 here: 900 us for 8192 tokens of 8 heads against 165)
             const int lo_t = t ? u.lo[1] : u.lo[0], hi_t = t ? u.hi[1] : u.hi[0];
@@ -550,8 +604,7 @@ int launch_prompt(const nq_prompt_desc* d, const void* Q, const void* K, const v
         (void)cudaGetLastError();
         return NQ_ERR_CUDA;
     }
-    const unsigned grid = (unsigned)(most < sm_count() ? most : sm_count());
-    return launch_chained(prompt_kernel<D>, grid, kThreads, Shape<D>::kSmem, 1, s, tmQ, tmK, tmV, a);
+    return launch_chained(prompt_kernel<D>, (unsigned)most, kThreads, Shape<D>::kSmem, 1, s, tmQ, tmK, tmV, a);
 }
 
 }  // namespace
