@@ -240,11 +240,12 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                     ok = mbar_wait(c_full, asks++ & 1, abort_flag, a.status, 0x313u);
                     index = ok ? cancelled(answer) : -1;
                     fence_proxy_async_smem();
-                    if (index >= 0) ask();
                 };
-                ask();
                 for (uint32_t n = 0;; ++n) {
-                    while (index >= units) answered();             // (the host knows no more than how many units there can be)
+                    while (index >= units) {                       // (the host knows no more than how many units there can be)
+                        ask();
+                        answered();
+                    }
                     if (!ok || !(ok = mbar_wait(u_empty + 8 * (n & 1), ((n >> 1) & 1) ^ 1, abort_flag, a.status, 0x314u))) break;
                     Unit u = {};
                     if (index >= 0) u = unit_of(a, s_before, chunk, index);
@@ -264,6 +265,9 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                                     tma_load_3d(sQ + t * P::kTileBytes + h * P::kSlab, &tmQ, 64 * h, u.head, u.q0 + u.row + t * kTile, q_full);
                         for (int j = u.first(); j < u.last(); ++j, ++it) {
                             const uint32_t s = it % ST, use = it / ST;
+                            // the next unit is asked for as late as its answer still comes in time: asked for at this one's start, a
+                            // long unit's block takes a second one that others would begin earlier (8192 tokens of 8 heads 165 -> 208 us)
+                            if (j == u.last() - 1) ask();
                             if (!(ok = mbar_wait(k_empty + 8 * s, (use & 1) ^ 1, abort_flag, a.status, 0x311u))) break;
                             mbar_arrive_expect_tx(k_full + 8 * s, P::kTileBytes);
 #pragma unroll
@@ -277,7 +281,8 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                         }
                     }
                     if (!ok) break;
-                    answered();                                    // (asked before this unit)
+                    if (u.last() <= u.first()) ask();
+                    answered();
                 }
                 if (!ok) {
                     const long long t0 = clock64();                // let copies in flight land before shared memory is released
