@@ -25,16 +25,16 @@ using namespace sm100;
 // Two warps look after V where a step has hidden keys (the last of a sequence, the diagonal, a window's edge): rows of V behind the
 // sequence are zeroed, since 0 x NaN is NaN in the product, and where the sequence's own rows hold infinities or NaN, the tiles that
 // hide some of the step take their weights times V by themselves, only what each row sees.
-constexpr int kThreads = 384;            // warp 0 TMA, warp 1 MMA and TMEM, warps 2, 3 look after V, warps 4-7 and 8-11 softmax of the tiles
-constexpr int kTile = 128;
+constexpr int kThreads = 384;            // warp 0 TMA and units, warps 1 and 2 MMA of the tiles (1 also TMEM), warp 3 looks after V, warps 4-7 and 8-11 softmax of the tiles
+constexpr int kTile = 128, kKeys = 64;   // rows of a tile, keys of a step
 constexpr float kRescale = 8.0f;
 
 template <int D>
 struct Shape {
-    static constexpr int kTileBytes = kTile * D * 2;
-    static constexpr int kStages = D == 128 ? 2 : 4;          // of K, and of V
-    static constexpr int kSmem = (2 + 2 * kStages) * kTileBytes + 1024 + 1024;
-    static constexpr int kSlab = kTile * 128;                 // 64 values of all rows of a tile
+    static constexpr int kTileBytes = kTile * D * 2, kStageBytes = kKeys * D * 2;
+    static constexpr int kStages = D == 128 ? 4 : 8;          // of K, and of V
+    static constexpr int kSmem = 2 * kTileBytes + 2 * kStages * kStageBytes + 1024 + 1024;
+    static constexpr int kSlabQ = kTile * 128, kSlab = kKeys * 128;      // 64 values of all rows of a tile, of a stage
 };
 
 struct PromptArgs {
@@ -52,17 +52,15 @@ struct Unit {
     int head;
     int lo[2], hi[2];                    // steps of each tile (hi <= lo: none)
     int all_lo[2], all_hi[2];            // keys that all rows of the tile see
-    __device__ __forceinline__ int first() const { return hi[0] > lo[0] ? (hi[1] > lo[1] ? min(lo[0], lo[1]) : lo[0]) : lo[1]; }
-    __device__ __forceinline__ int last() const { return hi[0] > lo[0] ? (hi[1] > lo[1] ? max(hi[0], hi[1]) : hi[0]) : hi[1]; }
+    int begin, end;                      // steps of either
     __device__ __forceinline__ bool takes(int t, int j) const { return j >= lo[t] && j < hi[t]; }
-    __device__ __forceinline__ bool hides(int t, int j) const { return takes(t, j) && (j * kTile < all_lo[t] || (j + 1) * kTile > all_hi[t]); }
+    __device__ __forceinline__ bool hides(int t, int j) const { return takes(t, j) && (j * kKeys < all_lo[t] || (j + 1) * kKeys > all_hi[t]); }
 };
 
 __device__ __forceinline__ int clamp_start(int v, int low, int high) { return min(max(v, low), high); }
 
 // `before`: units (of one head) before each chunk of sequences
-__device__ __forceinline__ Unit unit_of(const PromptArgs& a, const int* before, int chunk, int index) {
-    Unit u;
+__device__ __forceinline__ void unit_of(const PromptArgs& a, const int* before, int chunk, int index, Unit& u) {
     const int pair = before[kThreads] - 1 - index / a.q_heads;     // the longest rows of a causal prompt first
     u.head = index % a.q_heads;
     int lo = 0, hi = kThreads;
@@ -91,11 +89,13 @@ __device__ __forceinline__ Unit unit_of(const PromptArgs& a, const int* before, 
         u.all_hi[t] = a.causal ? min(u.lk, a0 + off + 1) : u.lk;
         u.all_lo[t] = a.window ? max(0, b0 + off - a.window) : 0;
         if (seen_hi > seen_lo) {
-            u.lo[t] = seen_lo / kTile;
-            u.hi[t] = (seen_hi + kTile - 1) / kTile;
+            u.lo[t] = seen_lo / kKeys;
+            u.hi[t] = (seen_hi + kKeys - 1) / kKeys;
         }
     }
-    return u;
+    const bool one = u.hi[0] > u.lo[0], two = u.hi[1] > u.lo[1];
+    u.begin = one && two ? min(u.lo[0], u.lo[1]) : one ? u.lo[0] : u.lo[1];
+    u.end = one && two ? max(u.hi[0], u.hi[1]) : one ? u.hi[0] : u.hi[1];
 }
 
 __device__ __forceinline__ float exp2a(float x) {
@@ -111,7 +111,7 @@ __device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));       // a NaN shows
     return r;
 }
 // Asks for a thread block of this grid that has not begun: its launch is cancelled, and 16 bytes that name it (or say that there is none)
@@ -139,38 +139,74 @@ __device__ __forceinline__ void hide(uint32_t (&s)[32], int lo, int hi) {
     for (int c = 0; c < 32; ++c) s[c] = (keep >> c) & 1u ? s[c] : 0xff800000u;
 }
 
+// Weights 2^(s scale + minus) of 32 scores, their sum, and as pairs of bf16 (a weight is off by at most 2^-9 of itself).
+// The exponential unit takes 4 a cycle and scheduler, which alone would be as long as both products.  So (MIXED) 3 of 8 come from the
+// other pipes: 2^y = 2^n 2^f, n = y rounded (y + 1.5 * 2^23 holds it in its low bits), f in [-1/2, 1/2] by a polynomial of degree 3, fitted
+// to 2^f for the least relative error on that interval: 7.5e-5 (2^-13.7), where a weight's rounding is 2^-9.  y under -126 counts as that.
+template <bool MIXED>
+__device__ __forceinline__ void weights_of(const uint32_t (&s)[32], float scale, float minus, uint64_t& sum, uint32_t (&p)[16]) {
+    constexpr float kBig = 12582912.0f;
+#pragma unroll
+    for (int c = 0; c < 32; c += 2) {
+        uint64_t y = fma2(pack2(s[c], s[c + 1]), both(scale), both(minus));
+        float e0, e1;
+        unpack2(y, e0, e1);
+        if (MIXED && (c / 2) % 8 >= 5) {
+            y = pack2f(fmaxf(e0, -126.0f), fmaxf(e1, -126.0f));
+            const uint64_t big = add2(y, both(kBig)), f = fma2(add2(big, both(-kBig)), both(-1.0f), y);
+            const uint64_t q = fma2(fma2(fma2(both(0.0551716793f), f, both(0.2426111685f)), f, both(0.6932609878f)), f, both(0.9999280708f));
+            float n0, n1;
+            unpack2(big, n0, n1);
+            unpack2(q, e0, e1);
+            e0 = __uint_as_float(__float_as_uint(e0) + (__float_as_uint(n0) << 23));
+            e1 = __uint_as_float(__float_as_uint(e1) + (__float_as_uint(n1) << 23));
+        } else {
+            e0 = exp2a(e0);
+            e1 = exp2a(e1);
+        }
+        sum = add2(sum, pack2f(e0, e1));
+        p[c / 2] = bf16x2(e0, e1);
+    }
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const PromptArgs a) {
     using P = Shape<D>;
     constexpr int ST = P::kStages;
-    constexpr uint32_t kS = 0, kO = 256;                       // tensor memory columns: S of tile t at kS + 128 t, O at kO + D t
+    constexpr uint32_t kS = 0, kO = 256;                       // tensor memory columns: S of tile t at kS + 128 t (two buffers of 64), O at kO + D t
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    // shared-memory addresses: tiles of Q [2], K [ST], V [ST], then barriers
-    const uint32_t sQ = smem_u32(smem), sK = sQ + 2 * P::kTileBytes, sV = sK + ST * P::kTileBytes, bars = sV + ST * P::kTileBytes;
-    const uint32_t q_full = bars, q_empty = bars + 8, s_full = bars + 16, p_full = bars + 32, o_full = bars + 48;               // the last three [2]
-    const uint32_t k_full = bars + 64, k_empty = k_full + 8 * ST, v_full = k_empty + 8 * ST, v_empty = v_full + 8 * ST, v_ok = v_empty + 8 * ST;   // [ST]
-    const uint32_t u_full = v_ok + 8 * ST, u_empty = u_full + 16, c_full = u_empty + 16;                                        // the first two [2]
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + (2 + 2 * ST) * P::kTileBytes + 64 + 40 * ST + 40);
+    // shared-memory addresses: tiles of Q [2], stages of K [ST] and of V [ST], then barriers
+    const uint32_t sQ = smem_u32(smem), sK = sQ + 2 * P::kTileBytes, sV = sK + ST * P::kStageBytes, bars = sV + ST * P::kStageBytes;
+    const uint32_t q_full = bars, q_empty = bars + 8, s_full = bars + 16, p_full = bars + 48, o_full = bars + 80;       // one, one, [2 tiles][2 buffers] each
+    const uint32_t k_full = bars + 112, k_empty = k_full + 8 * ST, v_full = k_empty + 8 * ST, v_empty = v_full + 8 * ST, v_ok = v_empty + 8 * ST;   // [ST]
+    const uint32_t u_full = v_ok + 8 * ST, u_empty = u_full + 16, c_full = u_empty + 16;                                // [2], [2], one
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 2 * P::kTileBytes + 2 * ST * P::kStageBytes + 112 + 40 * ST + 40);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    volatile int* v_odd = abort_flag + 1;                      // [ST][2]: whether the step's V holds what is no number, by the two warps
+    volatile int* v_odd = abort_flag + 1;                      // [ST]: whether the step's V holds what is no number
     __shared__ int s_before[kThreads + 1];
     __shared__ int s_warp[kThreads / 32];
     __shared__ Unit s_unit[2];
     __shared__ __align__(16) uint4 s_cancelled;
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;      // (the compiler then knows that a warp shares it)
     if (threadIdx.x == 0) {
         mbar_init(q_full, 1);
-        mbar_init(q_empty, 1);
-        for (int t = 0; t < 2; ++t) { mbar_init(s_full + 8 * t, 1); mbar_init(p_full + 8 * t, 4); mbar_init(o_full + 8 * t, 1); }
-        for (int s = 0; s < ST; ++s) {
-            mbar_init(k_full + 8 * s, 1); mbar_init(k_empty + 8 * s, 1);
-            mbar_init(v_full + 8 * s, 1); mbar_init(v_empty + 8 * s, 3);       // the products and warps 2, 3
-            mbar_init(v_ok + 8 * s, 2);
+        mbar_init(q_empty, 2);
+        for (int t = 0; t < 4; ++t) {
+            mbar_init(s_full + 8 * t, 1);
+            mbar_init(p_full + 8 * t, 4);
+            mbar_init(o_full + 8 * t, 1);
         }
-        for (int s = 0; s < 2; ++s) { mbar_init(u_full + 8 * s, 1); mbar_init(u_empty + 8 * s, 11); }       // read by MMA, warps 2 and 3, softmax
+        for (int s = 0; s < ST; ++s) {
+            mbar_init(k_full + 8 * s, 1);
+            mbar_init(k_empty + 8 * s, 2);
+            mbar_init(v_full + 8 * s, 1);
+            mbar_init(v_empty + 8 * s, 3);                     // both tiles' products, and the warp that looks after V
+            mbar_init(v_ok + 8 * s, 1);
+        }
+        for (int s = 0; s < 2; ++s) { mbar_init(u_full + 8 * s, 1); mbar_init(u_empty + 8 * s, 11); }       // warps 1 to 3, softmax
         mbar_init(c_full, 1);
         *abort_flag = 0;
         fence_barrier_init();
@@ -207,20 +243,20 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
-    const uint32_t tmem = *tmem_slot;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
     const int units = s_before[kThreads] * a.q_heads;          // the host has checked that it fits
 
     // The grid has a block for each unit that there can be; a block that is done with its own takes one that has not begun (it
     // cancels that block's launch), so that all SMs end together however the units differ.  Warp 0 does this, one unit ahead of the
     // tensor core, and hands what it has worked out to the others.
-    const auto take = [&](uint32_t n, Unit& u) {                // the n-th unit of this block, for a whole warp; false: no more, or given up
-        bool ok = mbar_wait(u_full + 8 * (n & 1), (n >> 1) & 1, abort_flag, a.status, 0x301u);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) return false;
-        u = s_unit[n & 1];
+    // The n-th unit of this block, for a whole warp until it gives it back; null: no more of them, or given up.
+    const auto take = [&](uint32_t n) -> const Unit* {
+        const bool ok = mbar_wait(u_full + 8 * (n & 1), (n >> 1) & 1, abort_flag, a.status, 0x301u);
+        return __all_sync(0xffffffffu, ok) && s_unit[n & 1].lq > 0 ? &s_unit[n & 1] : nullptr;
+    };
+    const auto give_back = [&](uint32_t n) {
         __syncwarp();
         if (lane == 0) mbar_arrive(u_empty + 8 * (n & 1));
-        return u.lq > 0;
     };
 
     // 128 x 72 + 256 x 216 registers, all of the 384 x 168 that the block was launched with
@@ -247,41 +283,42 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                         answered();
                     }
                     if (!ok || !(ok = mbar_wait(u_empty + 8 * (n & 1), ((n >> 1) & 1) ^ 1, abort_flag, a.status, 0x314u))) break;
-                    Unit u = {};
-                    if (index >= 0) u = unit_of(a, s_before, chunk, index);
-                    s_unit[n & 1] = u;
+                    Unit& u = s_unit[n & 1];
+                    if (index >= 0) unit_of(a, s_before, chunk, index, u);
+                    else u.lq = 0;
                     mbar_arrive(u_full + 8 * (n & 1));
                     if (index < 0) break;
-                    if (u.last() > u.first()) {
+                    const int begin = u.begin, end = u.end;
+                    if (end > begin) {
                         if (!(ok = mbar_wait(q_empty, (used & 1) ^ 1, abort_flag, a.status, 0x310u))) break;
                         ++used;
-                        const bool two[2] = {u.hi[0] > u.lo[0], u.hi[1] > u.lo[1]};
-                        mbar_arrive_expect_tx(q_full, (two[0] + two[1]) * P::kTileBytes);
+                        const bool one = u.hi[0] > u.lo[0], two = u.hi[1] > u.lo[1];
+                        const int kv_head = u.head / a.group, k0 = u.k0;
+                        mbar_arrive_expect_tx(q_full, (one + two) * P::kTileBytes);
 #pragma unroll
-                        for (int t = 0; t < 2; ++t)
-                            if (two[t])
-#pragma unroll
-                                for (int h = 0; h < D / 64; ++h)
-                                    tma_load_3d(sQ + t * P::kTileBytes + h * P::kSlab, &tmQ, 64 * h, u.head, u.q0 + u.row + t * kTile, q_full);
-                        for (int j = u.first(); j < u.last(); ++j, ++it) {
+                        for (int h = 0; h < D / 64; ++h) {
+                            if (one) tma_load_3d(sQ + h * P::kSlabQ, &tmQ, 64 * h, u.head, u.q0 + u.row, q_full);
+                            if (two) tma_load_3d(sQ + P::kTileBytes + h * P::kSlabQ, &tmQ, 64 * h, u.head, u.q0 + u.row + kTile, q_full);
+                        }
+                        for (int j = begin; j < end; ++j, ++it) {
                             const uint32_t s = it % ST, use = it / ST;
                             // the next unit is asked for as late as its answer still comes in time: asked for at this one's start, a
                             // long unit's block takes a second one that others would begin earlier (8192 tokens of 8 heads 165 -> 208 us)
-                            if (j == u.last() - 1) ask();
+                            if (j == end - 1) ask();
                             if (!(ok = mbar_wait(k_empty + 8 * s, (use & 1) ^ 1, abort_flag, a.status, 0x311u))) break;
-                            mbar_arrive_expect_tx(k_full + 8 * s, P::kTileBytes);
+                            mbar_arrive_expect_tx(k_full + 8 * s, P::kStageBytes);
 #pragma unroll
                             for (int h = 0; h < D / 64; ++h)
-                                tma_load_3d(sK + s * P::kTileBytes + h * P::kSlab, &tmK, 64 * h, u.head / a.group, u.k0 + j * kTile, k_full + 8 * s);
+                                tma_load_3d(sK + s * P::kStageBytes + h * P::kSlab, &tmK, 64 * h, kv_head, k0 + j * kKeys, k_full + 8 * s);
                             if (!(ok = mbar_wait(v_empty + 8 * s, (use & 1) ^ 1, abort_flag, a.status, 0x312u))) break;
-                            mbar_arrive_expect_tx(v_full + 8 * s, P::kTileBytes);
+                            mbar_arrive_expect_tx(v_full + 8 * s, P::kStageBytes);
 #pragma unroll
                             for (int h = 0; h < D / 64; ++h)
-                                tma_load_3d(sV + s * P::kTileBytes + h * P::kSlab, &tmV, 64 * h, u.head / a.group, u.k0 + j * kTile, v_full + 8 * s);
+                                tma_load_3d(sV + s * P::kStageBytes + h * P::kSlab, &tmV, 64 * h, kv_head, k0 + j * kKeys, v_full + 8 * s);
                         }
                     }
                     if (!ok) break;
-                    if (u.last() <= u.first()) ask();
+                    if (end <= begin) ask();
                     answered();
                 }
                 if (!ok) {
@@ -289,93 +326,89 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                     while (clock64() - t0 < (1ll << 22)) { }
                 }
             }
-        } else if (warp == 1) {
-            if (lane == 0) {
-                constexpr uint32_t kQK = idesc_bf16(kTile, kTile, false), kPV = idesc_bf16(kTile, D, true);
-                uint32_t it = 0, used = 0, weights = 0, checked = 0;            // the latter two: a phase bit for each tile, for each stage
-                bool ok = true;
-                for (uint32_t n = 0; ok; ++n) {
-                    if (!(ok = mbar_wait(u_full + 8 * (n & 1), (n >> 1) & 1, abort_flag, a.status, 0x302u))) break;
-                    const Unit u = s_unit[n & 1];
-                    mbar_arrive(u_empty + 8 * (n & 1));
-                    if (u.lq == 0) break;
-                    const int first = u.first(), last = u.last();
-                    if (last <= first) continue;
-                    if (!(ok = mbar_wait(q_full, used & 1, abort_flag, a.status, 0x320u))) break;
-                    ++used;
-                    for (int j = first; ok && j <= last; ++j) {
-                        const uint32_t i = it + (j - first), s = i % ST, use = i / ST;           // of step j
-                        const uint32_t sp = (i - 1) % ST, usep = (i - 1) / ST;                   // of step j - 1
-                        bool odd = false;
-                        if (j < last && !(ok = mbar_wait(k_full + 8 * s, use & 1, abort_flag, a.status, 0x321u))) break;
-                        if (j > first) {
-                            if (u.hides(0, j - 1) || u.hides(1, j - 1)) {
-                                if (!(ok = mbar_wait(v_ok + 8 * sp, (checked >> sp) & 1, abort_flag, a.status, 0x322u))) break;
-                                checked ^= 1u << sp;
-                                odd = v_odd[2 * sp] || v_odd[2 * sp + 1];
-                            }
-                            if (!(ok = mbar_wait(v_full + 8 * sp, usep & 1, abort_flag, a.status, 0x323u))) break;
+        } else if (warp < 3) {
+            // A tile's products, in a warp of their own: while one waits for a barrier, which takes a few hundred cycles even if it has long
+            // been arrived on, the tensor core has the other's to do.  The whole warp goes through this together, and one thread issues: where
+            // one thread alone runs the loop, the compiler does not know an instruction's operands to be the warp's, and each takes some
+            // 100 cycles to issue (16384 tokens of 8 heads, both tiles from one thread: 888 us; from one warp: 682).
+            constexpr uint32_t kQK = idesc_bf16(kTile, kKeys, false), kPV = idesc_bf16(kTile, D, true);
+            const int t = warp - 1;
+            const bool leader = elect_one();
+            const auto same = [](int v) { return __shfl_sync(0xffffffffu, v, 0); };
+            const auto wait = [&](uint32_t bar, uint32_t parity, unsigned code) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, a.status, code)); };
+            const uint64_t dq = smem_desc_sw128(sQ + t * P::kTileBytes), dk0 = smem_desc_sw128(sK), dv0 = smem_desc_mn_sw128(sV, P::kSlab);
+            const uint32_t sums = tmem + kO + t * D;
+            uint32_t it = 0, used = 0, weights = 0;                // steps, units with any, a phase bit for each buffer
+            bool ok = true;
+            for (uint32_t n = 0; ok; ++n) {
+                const Unit* u = take(n);
+                if (!u) break;
+                const int first = same(u->begin), last = same(u->end), lo = same(u->lo[t]), hi = same(u->hi[t]), all_lo = same(u->all_lo[t]), all_hi = same(u->all_hi[t]);
+                give_back(n);
+                if (last <= first) continue;
+                if (!(ok = wait(q_full, used & 1, 0x320u))) break;
+                ++used;
+                // step j's scores, and the sums of step j - 2, whose weights are where those scores go
+                for (int j = first; j < last + 2; ++j) {
+                    const uint32_t i = it + (j - first), s = i % ST, sp = (i - 2) % ST, parity = ((i - 2) / ST) & 1, buffer = j & 1;
+                    const uint32_t scores = tmem + kS + t * kTile + buffer * kKeys;
+                    const bool sums_due = j - 2 >= lo && j - 2 < hi, scores_due = j >= lo && j < hi;
+                    bool by_hand = false;
+                    if (j < last && !(ok = wait(k_full + 8 * s, (i / ST) & 1, 0x321u))) break;
+                    if (j >= first + 2 && !(ok = wait(v_full + 8 * sp, parity, 0x322u))) break;
+                    if (sums_due) {
+                        if ((j - 2) * kKeys < all_lo || (j - 1) * kKeys > all_hi) {
+                            if (!(ok = wait(v_ok + 8 * sp, parity, 0x323u))) break;
+                            by_hand = v_odd[sp];
                         }
-#pragma unroll 1
-                        for (int t = 0; t < 2; ++t) {                                            // (unrolled it takes more registers than there are)
-                            const int lo = t ? u.lo[1] : u.lo[0], hi = t ? u.hi[1] : u.hi[0];
-                            if (j > lo && j <= hi) {
-                                if (!(ok = mbar_wait(p_full + 8 * t, (weights >> t) & 1, abort_flag, a.status, 0x324u))) break;
-                                weights ^= 1u << t;
-                                tc_fence_after_sync();
-                                if (!(odd && (t ? u.hides(1, j - 1) : u.hides(0, j - 1)))) {
-                                    const uint64_t dv = smem_desc_mn_sw128(sV + sp * P::kTileBytes, P::kSlab);
-                                    const uint32_t to = tmem + kO + t * D, from = tmem + kS + t * kTile;
+                        // last of all, for from here to the scores there is a softmax warp that waits
+                        if (!(ok = wait(p_full + 16 * t + 8 * buffer, (weights >> buffer) & 1, 0x324u))) break;
+                        weights ^= 1u << buffer;
+                    }
+                    tc_fence_after_sync();
+                    if (leader) {
+                        if (sums_due && !by_hand) {
+                            const uint64_t dv = dv0 + sp * (P::kStageBytes / 16);
 #pragma unroll
-                                    for (int k = 0; k < kTile / 16; ++k) mma_bf16_ts(to, from + 8 * k, dv + k * (16 * 128 / 16), kPV, k > 0 || j - 1 > lo);
-                                }
-                                if (j == hi) mma_commit(o_full + 8 * t);
-                            }
-                            if (j >= lo && j < hi) {
-                                tc_fence_after_sync();
-                                const uint64_t dq = smem_desc_sw128(sQ + t * P::kTileBytes), dk = smem_desc_sw128(sK + s * P::kTileBytes);
-                                const uint32_t to = tmem + kS + t * kTile;
-#pragma unroll
-                                for (int k = 0; k < D / 16; ++k) {
-                                    const uint64_t at = (k % 4) * 2 + (k / 4) * (P::kSlab / 16);
-                                    mma_bf16(to, dq + at, dk + at, kQK, k > 0);
-                                }
-                                mma_commit(s_full + 8 * t);
-                            }
+                            for (int k = 0; k < kKeys / 16; ++k) mma_bf16_ts(sums, scores + 8 * k, dv + k * (16 * 128 / 16), kPV, k > 0 || j - 2 > lo);
                         }
-                        if (!ok) break;
-                        if (j > first) mma_commit(v_empty + 8 * sp);
+                        if (scores_due) {
+                            const uint64_t dk = dk0 + s * (P::kStageBytes / 16);
+#pragma unroll
+                            for (int k = 0; k < D / 16; ++k)
+                                mma_bf16(scores, dq + (k % 4) * 2 + (k / 4) * (P::kSlabQ / 16), dk + (k % 4) * 2 + (k / 4) * (P::kSlab / 16), kQK, k > 0);
+                            mma_commit(s_full + 16 * t + 8 * buffer);
+                        }
+                        if (sums_due) mma_commit(o_full + 16 * t + 8 * buffer);
+                        if (j >= first + 2) mma_commit(v_empty + 8 * sp);
                         if (j < last) mma_commit(k_empty + 8 * s);
                         if (j == last - 1) mma_commit(q_empty);
                     }
-                    it += last - first;
+                    __syncwarp();
                 }
+                it += last - first;
             }
         } else {
-            // rows (warp - 2) * 64 .. + 64 of V where a step hides something
+            // V where a step hides something.  Every step is waited for and confirmed, for a wait must not be more than one phase behind its
+            // barrier.
             uint32_t it = 0;
             bool ok = true;
-            Unit u;
-                for (uint32_t n = 0; ok && take(n, u); ++n) {
-                const int first = u.first(), last = u.last();
-                for (int j = first; j < last; ++j) {
-                    // every step is waited for and let go, for a wait must not be more than one phase behind its barrier
-                    const uint32_t i = it + (j - first), s = i % ST, use = i / ST;
-                    ok = mbar_wait(v_full + 8 * s, use & 1, abort_flag, a.status, 0x330u);
+            for (uint32_t n = 0; ok; ++n) {
+                const Unit* u = take(n);
+                if (!u) break;
+                for (int j = u->begin; j < u->end; ++j, ++it) {
+                    const uint32_t s = it % ST;
+                    ok = mbar_wait(v_full + 8 * s, (it / ST) & 1, abort_flag, a.status, 0x330u);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
-                    if (!u.hides(0, j) && !u.hides(1, j)) {
-                        if (lane == 0) mbar_arrive(v_empty + 8 * s);
-                        continue;
-                    }
-                    const int live = u.lk - j * kTile;             // rows of the sequence
-                    uint32_t odd = 0;
-                    // a lane takes a 16-byte piece of every fourth row: 8 lanes are a row of 64 values
-#pragma unroll
-                    for (int h = 0; h < D / 64; ++h) {
-                        for (int x = 0; x < 64; x += 4) {
-                            const int row = (warp - 2) * 64 + x + (lane >> 3);
-                            uint4* p = reinterpret_cast<uint4*>(smem + (2 + ST + s) * P::kTileBytes + h * P::kSlab + row * 128 + (lane & 7) * 16);
+                    if (u->hides(0, j) || u->hides(1, j)) {
+                        const int live = u->lk - j * kKeys;        // rows of the sequence
+                        uint32_t odd = 0;
+                        // a lane takes a 16-byte piece of every fourth row: 8 lanes are a row of 64 values
+#pragma unroll 4
+                        for (int x = 0; x < D; x += 4) {
+                            const int row = x % 64 + (lane >> 3);
+                            uint4* p = reinterpret_cast<uint4*>(smem + 2 * P::kTileBytes + (ST + s) * P::kStageBytes + x / 64 * P::kSlab + row * 128 + (lane & 7) * 16);
                             if (row >= live) {
                                 *p = make_uint4(0, 0, 0, 0);
                             } else {
@@ -384,71 +417,79 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                                        ((v.w & 0x7f807f80u) + 0x00800080u);
                             }
                         }
+                        const bool any = __any_sync(0xffffffffu, (odd & 0x80008000u) != 0);
+                        fence_proxy_async_smem();
+                        if (lane == 0) v_odd[s] = any;
                     }
-                    const bool any = __any_sync(0xffffffffu, (odd & 0x80008000u) != 0);
-                    fence_proxy_async_smem();
-                    if (lane == 0) v_odd[2 * s + warp - 2] = any;
                     __syncwarp();
                     if (lane == 0) {
                         mbar_arrive(v_ok + 8 * s);
                         mbar_arrive(v_empty + 8 * s);
                     }
                 }
-                it += max(0, last - first);
+                give_back(n);
             }
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-        const int t = (warp - 4) >> 2, quarter = warp & 3;
+        const int t = (warp - 4) >> 2, quarter = warp & 3;         // a row a thread
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-        const uint32_t s_at = tmem + kS + t * kTile + lanes, o_at = tmem + kO + t * D + lanes;
-        uint32_t it = 0, scores = 0, outs = 0, checked = 0;
+        const uint32_t o_at = tmem + kO + t * D + lanes;
+        uint32_t it = 0, phases = 0;                               // steps of all, a phase bit for each buffer
         bool ok = true;
-        Unit u;
-            for (uint32_t n = 0; ok && take(n, u); ++n) {
-            const int first = u.first(), last = u.last();
-            // (arrays that t picks from would live in local memory, which has next to no L1 here: 900 us for 8192 tokens of 8 heads against 165)
-            const int lo_t = t ? u.lo[1] : u.lo[0], hi_t = t ? u.hi[1] : u.hi[0];
-            const int all_lo = t ? u.all_lo[1] : u.all_lo[0], all_hi = t ? u.all_hi[1] : u.all_hi[0];
-            const int row = u.row + t * kTile + quarter * 32 + lane, off = u.lk - u.lq;
-            const int mine = min(row, u.lq - 1);               // rows behind the last one only must not get in the way
-            const int see_hi = a.causal ? min(u.lk, mine + off + 1) : u.lk, see_lo = a.window ? max(0, mine + off + 1 - a.window) : 0;
+        // PV(j) of the last step but one or the last so far is complete.  (The one before it with this buffer is known to be: S(j + 2), or the
+        // end of the unit before, said so; a barrier is never two phases ahead of one who waits for it.)
+        const auto sums_of = [&](int j) {
+            return mbar_wait(o_full + 16 * t + 8 * (j & 1), ((phases >> (j & 1)) & 1) ^ 1, abort_flag, a.status, 0x342u);
+        };
+        for (uint32_t n = 0; ok; ++n, give_back(n - 1)) {
+            const Unit* u = take(n);
+            if (!u) break;
+            const int lo_t = u->lo[t], hi_t = u->hi[t], all_lo = u->all_lo[t], all_hi = u->all_hi[t];
+            const int row = u->row + t * kTile + quarter * 32 + lane;
+            // of the keys, this row sees no more than the first `reach`, and of those the last `window`; rows behind the last one must not
+            // get in the way
+            const int reach = min(row, u->lq - 1) + u->lk - u->lq + 1;
+            const int see_hi = a.causal ? min(u->lk, reach) : u->lk, see_lo = a.window ? max(0, reach - a.window) : 0;
+            const uint32_t it0 = it - u->begin;                    // steps before step 0
+            it += u->end - u->begin;
             float top = -INFINITY, total = 0.0f;
-            for (int j = first; j < last; ++j) {
-                const uint32_t sl = (it + (j - first)) % ST;
-                const bool some = u.hides(0, j) || u.hides(1, j);
-                const uint32_t phase = (checked >> sl) & 1;
-                if (some) checked ^= 1u << sl;
-                if (j < lo_t || j >= hi_t) continue;
-                ok = mbar_wait(s_full + 8 * t, scores & 1, abort_flag, a.status, 0x340u);
+            for (int j = lo_t; j < hi_t; ++j) {
+                const uint32_t s_at = tmem + kS + t * kTile + (j & 1) * kKeys + lanes;
+                ok = mbar_wait(s_full + 16 * t + 8 * (j & 1), (phases >> (j & 1)) & 1, abort_flag, a.status, 0x340u);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                ++scores;
+                phases ^= 1u << (j & 1);
                 tc_fence_after_sync();
-                const bool hides = j * kTile < all_lo || (j + 1) * kTile > all_hi;
-                const int lo = see_lo - j * kTile, hi = see_hi - j * kTile;                  // columns that this row sees
-                float m = -INFINITY;
+                const bool hides = j * kKeys < all_lo || (j + 1) * kKeys > all_hi;
+                const int lo = see_lo - j * kKeys, hi = see_hi - j * kKeys;                  // columns that this row sees
+                uint32_t s[2][32];
+                tmem_ld_32x32(s_at, s[0]);
+                tmem_ld_32x32(s_at + 32, s[1]);
+                tmem_ld_wait();
+                float m = -INFINITY, m2 = -INFINITY;
 #pragma unroll
-                for (int x = 0; x < 4; x += 2) {
-                    uint32_t s[2][32];
-                    tmem_ld_32x32(s_at + 32 * x, s[0]);
-                    tmem_ld_32x32(s_at + 32 * x + 32, s[1]);
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        tmem_arrived(s[y]);
-                        if (hides) hide(s[y], lo - 32 * (x + y), hi - 32 * (x + y));
-#pragma unroll
-                        for (int c = 0; c < 32; c += 2) m = max3(m, __uint_as_float(s[y][c]), __uint_as_float(s[y][c + 1]));
-                    }
+                for (int x = 0; x < 2; ++x) {
+                    tmem_arrived(s[x]);
+                    if (hides) hide(s[x], lo - 32 * x, hi - 32 * x);
                 }
-                m *= a.scale2;
+#pragma unroll
+                for (int c = 0; c < 32; c += 2) {
+                    m = max3(m, __uint_as_float(s[0][c]), __uint_as_float(s[0][c + 1]));
+                    m2 = max3(m2, __uint_as_float(s[1][c]), __uint_as_float(s[1][c + 1]));
+                }
+                m = max3(m, m, m2) * a.scale2;
                 const bool move = m > top + kRescale;
                 if (__any_sync(0xffffffffu, move)) {
                     const float to = fmaxf(top, m), by = top == -INFINITY ? 0.0f : exp2a(top - to);
                     top = to;
                     total *= by;
                     if (j > lo_t) {
+                        // (that S(j) is there says that PV(j - 2) is complete)
+                        ok = sums_of(j - 1);
+                        ok = __all_sync(0xffffffffu, ok);
+                        if (!ok) break;
+                        tc_fence_after_sync();
 #pragma unroll
                         for (int c0 = 0; c0 < D; c0 += 32) {
                             uint32_t o[32];
@@ -463,36 +504,30 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 }
                 const float minus = top == -INFINITY ? 0.0f : -top;
                 uint64_t sum = 0;
-                // S is read a second time, 32 columns ahead of their use, rather than kept: all 128 with what the weights need do not
-                // fit into the registers (900 us for 8192 tokens of 8 heads, when what did not fit went to local memory)
-                uint32_t s[2][32];
-                tmem_ld_32x32(s_at, s[0]);
+                // hidden columns, and scores that are no numbers or infinite, take the exponential unit throughout
+                const bool plain = __any_sync(0xffffffffu, hides || !(fabsf(m) < INFINITY) || top == -INFINITY);
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    tmem_ld_wait();
-                    tmem_arrived(s[x & 1]);
-                    if (x < 3) tmem_ld_32x32(s_at + 32 * (x + 1), s[(x + 1) & 1]);
-                    if (hides) hide(s[x & 1], lo - 32 * x, hi - 32 * x);
+                for (int x = 0; x < 2; ++x) {
                     uint32_t p[16];
-#pragma unroll
-                    for (int c = 0; c < 32; c += 2) {
-                        float e0, e1;
-                        unpack2(fma2(pack2(s[x & 1][c], s[x & 1][c + 1]), both(a.scale2), both(minus)), e0, e1);
-                        e0 = exp2a(e0);
-                        e1 = exp2a(e1);
-                        sum = add2(sum, pack2f(e0, e1));
-                        p[c / 2] = bf16x2(e0, e1);             // a weight is off by at most 2^-9 of itself
-                    }
-                    tmem_st_32x16(s_at + 16 * x, p);           // over columns that have been read
+                    if (plain) weights_of<false>(s[x], a.scale2, minus, sum, p);
+                    else weights_of<true>(s[x], a.scale2, minus, sum, p);
+                    tmem_st_32x16(s_at + 16 * x, p);
                 }
                 total += sum2(sum);
                 tmem_st_wait();
-                if (some) {
-                    ok = mbar_wait(v_ok + 8 * sl, phase, abort_flag, a.status, 0x341u);
+                if (hides) {
+                    const uint32_t sl = (it0 + j) % ST;
+                    ok = mbar_wait(v_ok + 8 * sl, ((it0 + j) / ST) & 1, abort_flag, a.status, 0x341u);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
-                    if (hides && (v_odd[2 * sl] || v_odd[2 * sl + 1])) {
+                    if (v_odd[sl]) {
                         // some of V is no number, and this tile hides some of it: the product by hand, of what each row sees
+                        if (j > lo_t) {
+                            ok = sums_of(j - 1);
+                            ok = __all_sync(0xffffffffu, ok);
+                            if (!ok) break;
+                            tc_fence_after_sync();
+                        }
                         for (int c0 = 0; c0 < D; c0 += 32) {
                             uint32_t o[32];
                             if (j > lo_t) {
@@ -503,13 +538,13 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
 #pragma unroll
                                 for (int c = 0; c < 32; ++c) o[c] = 0;
                             }
-                            for (int k = 0; k < kTile; ++k) {
+                            for (int k = 0; k < kKeys; ++k) {
                                 uint32_t two = tmem_ld_32x1(s_at + k / 2);
                                 tmem_ld_wait();
                                 asm volatile("" : "+r"(two));
                                 const float w = __uint_as_float((k & 1) ? two & 0xffff0000u : two << 16);
                                 const bool seen = k >= lo && k < hi;
-                                const uint8_t* v = smem + (2 + ST + sl) * P::kTileBytes + (c0 / 64) * P::kSlab + k * 128;
+                                const uint8_t* v = smem + 2 * P::kTileBytes + (ST + sl) * P::kStageBytes + (c0 / 64) * P::kSlab + k * 128;
 #pragma unroll
                                 for (int x = 0; x < 4; ++x) {
                                     const uint4 q = *reinterpret_cast<const uint4*>(v + ((((c0 % 64) / 8 + x) ^ (k & 7)) << 4));
@@ -530,30 +565,28 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 }
                 tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_full + 8 * t);
+                if (lane == 0) mbar_arrive(p_full + 16 * t + 8 * (j & 1));
             }
             if (!ok) break;
-            it += max(0, last - first);
-            if (u.row + t * kTile >= u.lq) continue;           // the whole tile
-            const bool some = hi_t > lo_t;
-            if (some) {
-                ok = mbar_wait(o_full + 8 * t, outs & 1, abort_flag, a.status, 0x342u);
+            if (u->row + t * kTile >= u->lq) continue;             // the whole tile
+            const bool any = hi_t > lo_t;
+            if (any) {
+                ok = sums_of(hi_t - 1);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                ++outs;
                 tc_fence_after_sync();
             }
             const float by = total == 0.0f ? 0.0f : 1.0f / total;
-            __nv_bfloat16* to = a.y + (long long)(u.q0 + row) * a.ldy + u.head * D;
+            __nv_bfloat16* to = a.y + (long long)(u->q0 + row) * a.ldy + u->head * D;
 #pragma unroll
             for (int c0 = 0; c0 < D; c0 += 32) {
                 uint32_t o[32];
-                if (some) {
+                if (any) {
                     tmem_ld_32x32(o_at + c0, o);
                     tmem_ld_wait();
                     tmem_arrived(o);
                 }
-                if (row >= u.lq) continue;
+                if (row >= u->lq) continue;
 #pragma unroll
                 for (int x = 0; x < 32; x += 8) {
                     uint32_t w[4];
@@ -562,7 +595,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                     *reinterpret_cast<uint4*>(to + c0 + x) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
-            tc_fence_before_sync();                            // the next unit's first PV comes after this warp's next p_full
+            tc_fence_before_sync();                                // the next unit's first PV comes after this warp's next p_full
         }
     }
 
@@ -579,8 +612,8 @@ typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void
                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 // Heads of bf16 values as a 3-D tensor (values, heads, tokens), a token `pitch` elements after the other: boxes of 64 values of one head
-// x 128 tokens in the 128-byte swizzle.
-int encode_heads(CUtensorMap* map, const void* base, int64_t dim, int64_t heads, int64_t tokens, int64_t pitch) {
+// x box_tokens tokens in the 128-byte swizzle.
+int encode_heads(CUtensorMap* map, const void* base, int64_t dim, int64_t heads, int64_t tokens, int64_t pitch, int box_tokens) {
     static EncodeFn fn = nullptr;
     if (!fn) {
         void* sym = nullptr;
@@ -592,7 +625,7 @@ int encode_heads(CUtensorMap* map, const void* base, int64_t dim, int64_t heads,
         fn = reinterpret_cast<EncodeFn>(sym);
     }
     const cuuint64_t dims[3] = {(cuuint64_t)dim, (cuuint64_t)heads, (cuuint64_t)(tokens > 0 ? tokens : 1)}, strides[2] = {(cuuint64_t)dim * 2, (cuuint64_t)pitch * 2};
-    const cuuint32_t box[3] = {64, 1, kTile}, each[3] = {1, 1, 1};
+    const cuuint32_t box[3] = {64, 1, (cuuint32_t)box_tokens}, each[3] = {1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? NQ_OK : NQ_ERR_CUDA;
 }
@@ -600,10 +633,10 @@ int encode_heads(CUtensorMap* map, const void* base, int64_t dim, int64_t heads,
 template <int D>
 int launch_prompt(const nq_prompt_desc* d, const void* Q, const void* K, const void* V, const PromptArgs& a, int64_t most, cudaStream_t s) {
     CUtensorMap tmQ, tmK, tmV;
-    int st = encode_heads(&tmQ, Q, D, d->q_heads, d->rows_q, d->ldq);
+    int st = encode_heads(&tmQ, Q, D, d->q_heads, d->rows_q, d->ldq, kTile);
     // (no keys at all: nothing is loaded, but a map needs an address)
-    if (st == NQ_OK) st = encode_heads(&tmK, d->rows_k > 0 ? K : Q, D, d->kv_heads, d->rows_k, d->rows_k > 0 ? d->ldk : d->kv_heads * (int64_t)D);
-    if (st == NQ_OK) st = encode_heads(&tmV, d->rows_k > 0 ? V : Q, D, d->kv_heads, d->rows_k, d->rows_k > 0 ? d->ldv : d->kv_heads * (int64_t)D);
+    if (st == NQ_OK) st = encode_heads(&tmK, d->rows_k > 0 ? K : Q, D, d->kv_heads, d->rows_k, d->rows_k > 0 ? d->ldk : d->kv_heads * (int64_t)D, kKeys);
+    if (st == NQ_OK) st = encode_heads(&tmV, d->rows_k > 0 ? V : Q, D, d->kv_heads, d->rows_k, d->rows_k > 0 ? d->ldv : d->kv_heads * (int64_t)D, kKeys);
     if (st != NQ_OK) return st;
     if (cudaFuncSetAttribute(prompt_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem) != cudaSuccess) {
         (void)cudaGetLastError();
