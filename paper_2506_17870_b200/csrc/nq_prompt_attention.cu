@@ -140,31 +140,30 @@ __device__ __forceinline__ void hide(uint32_t (&s)[32], int lo, int hi) {
 }
 
 // Weights 2^(s scale + minus) of 32 scores, their sum, and as pairs of bf16 (a weight is off by at most 2^-9 of itself).
-// The exponential unit takes 4 a cycle and scheduler, which alone would be as long as both products.  So (MIXED) 3 of 8 come from the
-// other pipes: 2^y = 2^n 2^f, n = y rounded (y + 1.5 * 2^23 holds it in its low bits), f in [-1/2, 1/2] by a polynomial of degree 3, fitted
-// to 2^f for the least relative error on that interval: 7.5e-5 (2^-13.7), where a weight's rounding is 2^-9.  y under -126 counts as that.
-template <bool MIXED>
+// The exponential unit takes 4 a cycle and scheduler, which alone would be as long as both products.  So 3 of 8 come from the other
+// pipes: 2^y = 2^n 2^f, n = y rounded (y + 1.5 * 2^23 holds it in its low bits), f in [-1/2, 1/2] by a polynomial of degree 3, fitted
+// to 2^f for the least relative error on that interval: 7.5e-5 (2^-13.7), where a weight's rounding is 2^-9.  y under -127 counts as that,
+// whose 2^n is made as 0; a NaN stays one.
 __device__ __forceinline__ void weights_of(const uint32_t (&s)[32], float scale, float minus, uint64_t& sum, uint32_t (&p)[16]) {
     constexpr float kBig = 12582912.0f;
 #pragma unroll
     for (int c = 0; c < 32; c += 2) {
-        uint64_t y = fma2(pack2(s[c], s[c + 1]), both(scale), both(minus));
+        const uint64_t y = fma2(pack2(s[c], s[c + 1]), both(scale), both(minus));
         float e0, e1;
         unpack2(y, e0, e1);
-        if (MIXED && (c / 2) % 8 >= 5) {
-            y = pack2f(fmaxf(e0, -126.0f), fmaxf(e1, -126.0f));
-            const uint64_t big = add2(y, both(kBig)), f = fma2(add2(big, both(-kBig)), both(-1.0f), y);
+        uint64_t e;
+        if ((c / 2) % 8 >= 5) {
+            const uint64_t z = pack2f(max3(e0, e0, -127.0f), max3(e1, e1, -127.0f));
+            const uint64_t big = add2(z, both(kBig)), f = fma2(add2(big, both(-kBig)), both(-1.0f), z);
             const uint64_t q = fma2(fma2(fma2(both(0.0551716793f), f, both(0.2426111685f)), f, both(0.6932609878f)), f, both(0.9999280708f));
             float n0, n1;
             unpack2(big, n0, n1);
-            unpack2(q, e0, e1);
-            e0 = __uint_as_float(__float_as_uint(e0) + (__float_as_uint(n0) << 23));
-            e1 = __uint_as_float(__float_as_uint(e1) + (__float_as_uint(n1) << 23));
+            e = mul2(q, pack2((__float_as_uint(n0) << 23) + 0x3f800000u, (__float_as_uint(n1) << 23) + 0x3f800000u));
         } else {
-            e0 = exp2a(e0);
-            e1 = exp2a(e1);
+            e = pack2f(exp2a(e0), exp2a(e1));
         }
-        sum = add2(sum, pack2f(e0, e1));
+        sum = add2(sum, e);
+        unpack2(e, e0, e1);
         p[c / 2] = bf16x2(e0, e1);
     }
 }
@@ -335,7 +334,16 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             const int t = warp - 1;
             const bool leader = elect_one();
             const auto same = [](int v) { return __shfl_sync(0xffffffffu, v, 0); };
-            const auto wait = [&](uint32_t bar, uint32_t parity, unsigned code) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, a.status, code)); };
+            // A barrier's answer takes 100 cycles and more to come, so those of a step are asked together.  (Each of them holds its phase until
+            // this warp has gone on.)
+            const auto wait = [&](uint32_t b0, uint32_t p0, uint32_t b1, uint32_t p1, uint32_t b2, uint32_t p2, unsigned code) {
+                bool all = mbar_try_wait(b0, p0);
+                all &= mbar_try_wait(b1, p1);
+                all &= mbar_try_wait(b2, p2);
+                if (__all_sync(0xffffffffu, all)) return true;
+                all = mbar_wait(b0, p0, abort_flag, a.status, code) && mbar_wait(b1, p1, abort_flag, a.status, code + 1) && mbar_wait(b2, p2, abort_flag, a.status, code + 2);
+                return (bool)__all_sync(0xffffffffu, all);
+            };
             const uint64_t dq = smem_desc_sw128(sQ + t * P::kTileBytes), dk0 = smem_desc_sw128(sK), dv0 = smem_desc_mn_sw128(sV, P::kSlab);
             const uint32_t sums = tmem + kO + t * D;
             uint32_t it = 0, used = 0, weights = 0;                // steps, units with any, a phase bit for each buffer
@@ -346,7 +354,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 const int first = same(u->begin), last = same(u->end), lo = same(u->lo[t]), hi = same(u->hi[t]), all_lo = same(u->all_lo[t]), all_hi = same(u->all_hi[t]);
                 give_back(n);
                 if (last <= first) continue;
-                if (!(ok = wait(q_full, used & 1, 0x320u))) break;
+                if (!(ok = wait(q_full, used & 1, q_full, used & 1, q_full, used & 1, 0x320u))) break;
                 ++used;
                 // step j's scores, and the sums of step j - 2, whose weights are where those scores go
                 for (int j = first; j < last + 2; ++j) {
@@ -354,16 +362,19 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                     const uint32_t scores = tmem + kS + t * kTile + buffer * kKeys;
                     const bool sums_due = j - 2 >= lo && j - 2 < hi, scores_due = j >= lo && j < hi;
                     bool by_hand = false;
-                    if (j < last && !(ok = wait(k_full + 8 * s, (i / ST) & 1, 0x321u))) break;
-                    if (j >= first + 2 && !(ok = wait(v_full + 8 * sp, parity, 0x322u))) break;
-                    if (sums_due) {
+                    // the step's keys, and the values and weights of step j - 2, each where there is such a step
+                    const bool keys = j < last, values = j >= first + 2;
+                    const uint32_t kb = k_full + 8 * s, kp = (i / ST) & 1, vb = v_full + 8 * sp;
+                    if (sums_due) {                            // (then there are values)
+                        if (!(ok = wait(p_full + 16 * t + 8 * buffer, (weights >> buffer) & 1, vb, parity, keys ? kb : vb, keys ? kp : parity, 0x323u))) break;
+                        weights ^= 1u << buffer;
                         if ((j - 2) * kKeys < all_lo || (j - 1) * kKeys > all_hi) {
-                            if (!(ok = wait(v_ok + 8 * sp, parity, 0x323u))) break;
+                            const uint32_t ob = v_ok + 8 * sp;
+                            if (!(ok = wait(ob, parity, ob, parity, ob, parity, 0x326u))) break;
                             by_hand = v_odd[sp];
                         }
-                        // last of all, for from here to the scores there is a softmax warp that waits
-                        if (!(ok = wait(p_full + 16 * t + 8 * buffer, (weights >> buffer) & 1, 0x324u))) break;
-                        weights ^= 1u << buffer;
+                    } else if (keys || values) {
+                        if (!(ok = wait(keys ? kb : vb, keys ? kp : parity, values ? vb : kb, values ? parity : kp, keys ? kb : vb, keys ? kp : parity, 0x329u))) break;
                     }
                     tc_fence_after_sync();
                     if (leader) {
@@ -454,11 +465,14 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             const uint32_t it0 = it - u->begin;                    // steps before step 0
             it += u->end - u->begin;
             float top = -INFINITY, total = 0.0f;
+            bool there = false;                                    // the next step's scores, as far as is known
             for (int j = lo_t; j < hi_t; ++j) {
                 const uint32_t s_at = tmem + kS + t * kTile + (j & 1) * kKeys + lanes;
-                ok = mbar_wait(s_full + 16 * t + 8 * (j & 1), (phases >> (j & 1)) & 1, abort_flag, a.status, 0x340u);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
+                if (!__all_sync(0xffffffffu, there)) {
+                    ok = mbar_wait(s_full + 16 * t + 8 * (j & 1), (phases >> (j & 1)) & 1, abort_flag, a.status, 0x340u);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                }
                 phases ^= 1u << (j & 1);
                 tc_fence_after_sync();
                 const bool hides = j * kKeys < all_lo || (j + 1) * kKeys > all_hi;
@@ -467,18 +481,20 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 tmem_ld_32x32(s_at, s[0]);
                 tmem_ld_32x32(s_at + 32, s[1]);
                 tmem_ld_wait();
-                float m = -INFINITY, m2 = -INFINITY;
+                float m = -INFINITY, m1 = -INFINITY, m2 = -INFINITY, m3 = -INFINITY;
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     tmem_arrived(s[x]);
                     if (hides) hide(s[x], lo - 32 * x, hi - 32 * x);
                 }
 #pragma unroll
-                for (int c = 0; c < 32; c += 2) {
+                for (int c = 0; c < 32; c += 4) {
                     m = max3(m, __uint_as_float(s[0][c]), __uint_as_float(s[0][c + 1]));
+                    m1 = max3(m1, __uint_as_float(s[0][c + 2]), __uint_as_float(s[0][c + 3]));
                     m2 = max3(m2, __uint_as_float(s[1][c]), __uint_as_float(s[1][c + 1]));
+                    m3 = max3(m3, __uint_as_float(s[1][c + 2]), __uint_as_float(s[1][c + 3]));
                 }
-                m = max3(m, m, m2) * a.scale2;
+                m = max3(m, m1, max3(m2, m2, m3)) * a.scale2;
                 const bool move = m > top + kRescale;
                 if (__any_sync(0xffffffffu, move)) {
                     const float to = fmaxf(top, m), by = top == -INFINITY ? 0.0f : exp2a(top - to);
@@ -490,7 +506,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                         ok = __all_sync(0xffffffffu, ok);
                         if (!ok) break;
                         tc_fence_after_sync();
-#pragma unroll
+#pragma unroll 1
                         for (int c0 = 0; c0 < D; c0 += 32) {
                             uint32_t o[32];
                             tmem_ld_32x32(o_at + c0, o);
@@ -504,16 +520,14 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 }
                 const float minus = top == -INFINITY ? 0.0f : -top;
                 uint64_t sum = 0;
-                // hidden columns, and scores that are no numbers or infinite, take the exponential unit throughout
-                const bool plain = __any_sync(0xffffffffu, hides || !(fabsf(m) < INFINITY) || top == -INFINITY);
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     uint32_t p[16];
-                    if (plain) weights_of<false>(s[x], a.scale2, minus, sum, p);
-                    else weights_of<true>(s[x], a.scale2, minus, sum, p);
+                    weights_of(s[x], a.scale2, minus, sum, p);
                     tmem_st_32x16(s_at + 16 * x, p);
                 }
                 total += sum2(sum);
+                there = j + 1 < hi_t && mbar_try_wait(s_full + 16 * t + 8 * ((j + 1) & 1), (phases >> ((j + 1) & 1)) & 1);
                 tmem_st_wait();
                 if (hides) {
                     const uint32_t sl = (it0 + j) % ST;
@@ -528,6 +542,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                             if (!ok) break;
                             tc_fence_after_sync();
                         }
+#pragma unroll 1
                         for (int c0 = 0; c0 < D; c0 += 32) {
                             uint32_t o[32];
                             if (j > lo_t) {
@@ -538,6 +553,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
 #pragma unroll
                                 for (int c = 0; c < 32; ++c) o[c] = 0;
                             }
+#pragma unroll 1
                             for (int k = 0; k < kKeys; ++k) {
                                 uint32_t two = tmem_ld_32x1(s_at + k / 2);
                                 tmem_ld_wait();
@@ -578,7 +594,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             }
             const float by = total == 0.0f ? 0.0f : 1.0f / total;
             __nv_bfloat16* to = a.y + (long long)(u->q0 + row) * a.ldy + u->head * D;
-#pragma unroll
+#pragma unroll 1
             for (int c0 = 0; c0 < D; c0 += 32) {
                 uint32_t o[32];
                 if (any) {
