@@ -12,7 +12,7 @@
 namespace nq {
 namespace {
 
-// The cache is read once, 16 tokens of one kv head (a "step") at a time by one warp, straight into the registers of the matrix
+// The cache is read once, 16 or 32 tokens of one kv head (a "step") at a time by one warp, straight into the registers of the matrix
 // instruction: no shared memory, no barrier, nothing between warps until they have their sums.  Both products have the tokens or
 // the head's channels as their 16 rows and the query heads of the kv head as their 8 columns:
 //   S^T [16 tokens, 8 heads] = K Q^T       a lane's 16-byte pieces of two tokens are the operand as they come: the channels are
@@ -25,8 +25,12 @@ namespace {
 // a second kernel, in a fixed order.
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr float kRescale = 8.0f;         // the running maximum moves when a score passes it by 2^8 (fp32 sums have room)
-constexpr float kShift = 7.0f;           // f16 weights are held times 2^7: at most 2^15, and exact down to 2^-21 of the largest
+// f16 weights are held times 2^7: at most 2^15 (a weight is at most 2^8), normal down to 2^-21 of the one at the maximum.
 constexpr float kTiny = 1.17549435e-38f;
+
+// Tokens of a step: as many as bring 8 KB (4 KB of 8-bit heads of 64) to a warp.  Two groups of 16 at once also halve what a step costs
+// beside its products (e4m3, 131072 tokens of 8 heads of 128, 16 at once: 79 us).
+__host__ __device__ constexpr int step_tokens(int dim, int cache) { return dim == 128 && cache == NQ_BF16 ? 16 : 32; }
 
 struct TokenArgs {
     Pages c;
@@ -96,13 +100,20 @@ __device__ __forceinline__ void codes4(uint32_t w, uint32_t& lo, uint32_t& hi) {
 }
 
 // Steps of a sequence, its tokens and the number of its first step (behind a window it is not 0).
+template <int TOKENS>
 __device__ __forceinline__ int steps_of(const TokenArgs& a, int seq, int& length, int& first) {
     length = min(a.lengths[seq], a.table_tokens);
-    first = a.window > 0 && length > a.window ? (length - a.window) >> 4 : 0;
-    return length <= 0 ? 0 : ((length + 15) >> 4) - first;
+    first = a.window > 0 && length > a.window ? (length - a.window) / TOKENS : 0;
+    return length <= 0 ? 0 : (length - 1) / TOKENS + 1 - first;
+}
+
+// (a 64-bit division takes several hundred cycles; what fits takes the short one)
+__device__ __forceinline__ long long divide(long long a, long long b) {
+    return ((unsigned long long)a | (unsigned long long)b) >> 32 ? a / b : (long long)((unsigned)a / (unsigned)b);
 }
 
 // Where a warp is in the long row.
+template <int TOKENS>
 struct Place {
     int seq, head, block, step;              // sequence, kv head, block of columns, step among the sequence's
     int steps, length, first;                // of the sequence
@@ -115,7 +126,7 @@ struct Place {
         head = 0;
         do {
             if (++seq >= a.seqs) return;
-            steps = steps_of(a, seq, length, first);
+            steps = steps_of<TOKENS>(a, seq, length, first);
         } while (steps == 0);
     }
 };
@@ -126,13 +137,14 @@ __device__ __forceinline__ void zero_row(const TokenArgs& a, int seq, int column
 }
 
 template <int D, int CACHE, int NT>
-__global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) token_kernel(const TokenArgs a) {
+__global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ_BF16) ? 3 : 2) token_kernel(const TokenArgs a) {
     constexpr bool kCodes = CACHE != NQ_BF16;
     constexpr int kRow = D * (kCodes ? 1 : 2);                       // bytes of a token's head
     constexpr int kKPieces = kRow / 64;                              // 16-byte pieces of a K row in a lane (4 lanes a row)
     constexpr int kVBytes = kRow / 8 > 16 ? 16 : kRow / 8;           // piece of a V row in a lane (8 lanes a row)
     constexpr int kVPieces = kRow / 8 / kVBytes, kVWords = kVBytes / 4;
     constexpr int kSteps = D / 16;                                   // matrix instructions of 16 channels
+    constexpr int kSub = step_tokens(D, CACHE) / 16, kTokens = 16 * kSub;
     constexpr int kSlot = kSlotFloats<D, NT>;
     extern __shared__ __align__(16) float s_parts[];                 // [2 * kWarps][kSlot]
     __shared__ long long s_before[kThreads + 1];
@@ -149,7 +161,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) token_kernel(const 
     long long mine = 0;
     for (int s = threadIdx.x * chunk; s < min(a.seqs, (int)(threadIdx.x + 1) * chunk); ++s) {
         int length, first;
-        mine += steps_of(a, s, length, first);
+        mine += steps_of<kTokens>(a, s, length, first);
     }
     long long sum = mine;
 #pragma unroll
@@ -170,14 +182,14 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) token_kernel(const 
 
     // ---- this block's and this warp's part of it
     const long long blocks = min((long long)gridDim.x, (total + kWarps - 1) / kWarps);
-    const long long begin = blockIdx.x < blocks ? total * blockIdx.x / blocks : 0, end = blockIdx.x < blocks ? total * (blockIdx.x + 1) / blocks : 0;
+    const long long begin = blockIdx.x < blocks ? divide(total * blockIdx.x, blocks) : 0, end = blockIdx.x < blocks ? divide(total * (blockIdx.x + 1), blocks) : 0;
     const long long from = begin + (end - begin) * warp / kWarps;
     int left = (int)(begin + (end - begin) * (warp + 1) / kWarps - from);
     int part = 2 * warp;                                             // next part to fill
     if (left > 0) {
-        Place at;
+        Place<kTokens> at;
         {
-            const long long step = from / units;                     // sequences' steps before `at` are no more than this
+            const long long step = divide(from, units);                     // sequences' steps before `at` are no more than this
             int lo = 0, hi = kThreads;
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
@@ -185,12 +197,12 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) token_kernel(const 
             }
             long long rest = from - s_before[lo] * units;
             at.seq = lo * chunk;
-            at.steps = steps_of(a, at.seq, at.length, at.first);
+            at.steps = steps_of<kTokens>(a, at.seq, at.length, at.first);
             while (rest >= (long long)at.steps * units) {
                 rest -= (long long)at.steps * units;
-                at.steps = steps_of(a, ++at.seq, at.length, at.first);
+                at.steps = steps_of<kTokens>(a, ++at.seq, at.length, at.first);
             }
-            const int unit = (int)(rest / at.steps);
+            const int unit = (int)divide(rest, at.steps);
             at.step = (int)(rest - (long long)unit * at.steps);
             at.head = unit / a.head_blocks;
             at.block = unit - at.head * a.head_blocks;
@@ -198,77 +210,88 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) token_kernel(const 
         const int per_page = a.c.page_size >> 4;
         const long long page_rows = (long long)a.c.kv_heads * a.c.page_size;
 
-        uint4 kw[2][kKPieces];                                       // K of tokens i, i + 8
-        uint32_t vw[4][kVPieces][kVWords];                           // V of tokens 2 j, 2 j + 1, 2 j + 8, 2 j + 9
-        float ks[2] = {1.0f, 1.0f}, vs[2] = {1.0f, 1.0f};            // scales of tokens i, i + 8
-        long long my_row = -1;                                       // lane's page of step pages_from + lane: its first row for head 0, -1: none
+        uint4 kw[kSub][2][kKPieces];                                 // K of tokens i, i + 8 of 16
+        uint32_t vw[kSub][4][kVPieces][kVWords];                     // V of tokens 2 j, 2 j + 1, 2 j + 8, 2 j + 9 of 16
+        float ks[kSub][2], vs[kSub][2];                              // scales of tokens i, i + 8
+        long long row[kSub];                                         // of the first of 16 tokens in the cache, -1: no such page
+        long long my_row = -1;                                       // lane's page of 16 tokens number pages_from + lane: its first row for head 0, -1: none
         int pages_seq = -1, pages_from = 0;
 
-        auto row_of = [&](const Place& p) -> long long {             // row of the step's first token in the cache, -1: none
-            const int number = p.first + p.step;
-            if (p.seq != pages_seq || number < pages_from || number >= pages_from + 32) {
+        auto find_rows = [&](const Place<kTokens>& p) {
+            const int number = (p.first + p.step) * kSub;
+            if (p.seq != pages_seq || number < pages_from || number + kSub > pages_from + 32) {
                 pages_seq = p.seq;
                 pages_from = number;
                 const int n = number + lane;
                 my_row = -1;
-                if (n < p.first + p.steps) {
+                if (n * 16 < p.length) {
                     const int nth = n / per_page, page = a.table[p.seq * a.ld_table + nth];
                     if (page >= 0 && page < a.c.pages) my_row = page * page_rows + (n - nth * per_page) * 16;
                 }
             }
-            const long long row = __shfl_sync(0xffffffffu, my_row, number - pages_from);
-            return row < 0 ? -1 : row + (long long)p.head * a.c.page_size;
-        };
-        auto load_k = [&](long long row) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-#pragma unroll
-                for (int p = 0; p < kKPieces; ++p)
-                    kw[t][p] = row < 0 ? make_uint4(0, 0, 0, 0) : load16(a.c.k + (row + i + 8 * t) * kRow + 16 * (j + 4 * p));
-                if (kCodes && row >= 0) ks[t] = a.c.ks[row + i + 8 * t];
+            for (int u = 0; u < kSub; ++u) {
+                const long long r = __shfl_sync(0xffffffffu, my_row, number + u - pages_from);
+                row[u] = r < 0 ? -1 : r + (long long)p.head * a.c.page_size;
             }
         };
-        auto load_v = [&](long long row) {
+        auto load_k = [&] {
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const int token = 2 * j + (t & 1) + 8 * (t >> 1);
+            for (int u = 0; u < kSub; ++u)
 #pragma unroll
-                for (int p = 0; p < kVPieces; ++p) {
-                    const uint8_t* src = a.c.v + (row + token) * kRow + kVBytes * (i + 8 * p);
-                    if (row < 0) {
+                for (int t = 0; t < 2; ++t) {
+                    const uint8_t* src = a.c.k + (row[u] + i + 8 * t) * kRow + 16 * j;
 #pragma unroll
-                        for (int w = 0; w < kVWords; ++w) vw[t][p][w] = 0;
-                    } else if (kVWords == 4) {
-                        const uint4 v = load16(src);
-                        vw[t][p][0] = v.x; vw[t][p][1] = v.y; vw[t][p][2 % kVWords] = v.z; vw[t][p][3 % kVWords] = v.w;
-                    } else {
-                        asm volatile("ld.global.L1::no_allocate.v2.b32 {%0, %1}, [%2];" : "=r"(vw[t][p][0]), "=r"(vw[t][p][1]) : "l"(src) : "memory");
+                    for (int p = 0; p < kKPieces; ++p) kw[u][t][p] = row[u] < 0 ? make_uint4(0, 0, 0, 0) : load16(src + 64 * p);
+                    if (kCodes && row[u] >= 0) ks[u][t] = a.c.ks[row[u] + i + 8 * t];
+                }
+        };
+        auto load_v = [&] {
+#pragma unroll
+            for (int u = 0; u < kSub; ++u) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const uint8_t* src = a.c.v + (row[u] + 2 * j + (t & 1) + 8 * (t >> 1)) * kRow + kVBytes * i;
+#pragma unroll
+                    for (int p = 0; p < kVPieces; ++p) {
+                        if (row[u] < 0) {
+#pragma unroll
+                            for (int w = 0; w < kVWords; ++w) vw[u][t][p][w] = 0;
+                        } else if (kVWords == 4) {
+                            const uint4 v = load16(src + 8 * kVBytes * p);
+                            vw[u][t][p][0] = v.x; vw[u][t][p][1] = v.y; vw[u][t][p][2 % kVWords] = v.z; vw[u][t][p][3 % kVWords] = v.w;
+                        } else {
+                            asm volatile("ld.global.L1::no_allocate.v2.b32 {%0, %1}, [%2];" : "=r"(vw[u][t][p][0]), "=r"(vw[u][t][p][1]) : "l"(src) : "memory");
+                        }
                     }
                 }
-            }
-            if (kCodes && row >= 0) {
-                vs[0] = a.c.vs[row + i];
-                vs[1] = a.c.vs[row + i + 8];
+                if (kCodes && row[u] >= 0) {
+                    vs[u][0] = a.c.vs[row[u] + i];
+                    vs[u][1] = a.c.vs[row[u] + i + 8];
+                }
             }
         };
 
         uint32_t qf[NT][kSteps][2];
         float q_scale[NT][2];                                        // of heads 2 j, 2 j + 1: what a product of codes is multiplied by
-        float o[NT][kSteps][4], top[NT][2], weight[NT][2], largest = kTiny;
+        float o[NT][kSteps][4], top[NT][2], weight[NT][2], largest = kTiny, unit_inv = 0.0f;     // the largest scale of a value so far, and its inverse
         int begun = 0;
 
-        long long row = row_of(at);
-        load_k(row);
-        load_v(row);
+        find_rows(at);
+        load_k();
+        load_v();
         bool fresh = true;
         while (left > 0) {
-            const Place cur = at;
-            const bool there = row >= 0;
+            const Place<kTokens> cur = at;
+            bool there[kSub];
+#pragma unroll
+            for (int u = 0; u < kSub; ++u) there[u] = row[u] >= 0;
             const int block = cur.block, kv_head = cur.head;
             if (fresh) {                                             // another sequence or head
                 fresh = false;
                 begun = cur.step == 0;
                 largest = kTiny;
+                unit_inv = 1.0f / kTiny;
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     const int h = (block * NT + n) * 8 + i;
@@ -318,87 +341,114 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) token_kernel(const 
             }
 
             // ---- scores
-            float sc[NT][4];
+            float sc[kSub][NT][4];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.0f;
+            for (int u = 0; u < kSub; ++u)
 #pragma unroll
-            for (int p = 0; p < kKPieces; ++p) {
-                const uint32_t w0[4] = {kw[0][p].x, kw[0][p].y, kw[0][p].z, kw[0][p].w}, w1[4] = {kw[1][p].x, kw[1][p].y, kw[1][p].z, kw[1][p].w};
-                if (!kCodes) {
+                for (int n = 0; n < NT; ++n) sc[u][n][0] = sc[u][n][1] = sc[u][n][2] = sc[u][n][3] = 0.0f;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
+            for (int p = 0; p < kKPieces; ++p)
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) mma<false>(sc[n], w0[2 * h], w1[2 * h], w0[2 * h + 1], w1[2 * h + 1], qf[n][2 * p + h][0], qf[n][2 * p + h][1]);
-                } else {
+                for (int u = 0; u < kSub; ++u) {
+                    const uint4 x = kw[u][0][p], y = kw[u][1][p];
+                    const uint32_t w0[4] = {x.x, x.y, x.z, x.w}, w1[4] = {y.x, y.y, y.z, y.w};
+                    if (!kCodes) {
 #pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        uint32_t a0, a1, a2, a3;
-                        codes4<CACHE>(w0[h], a0, a2);
-                        codes4<CACHE>(w1[h], a1, a3);
+                        for (int h = 0; h < 2; ++h)
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) mma<true>(sc[n], a0, a1, a2, a3, qf[n][4 * p + h][0], qf[n][4 * p + h][1]);
+                            for (int n = 0; n < NT; ++n) mma<false>(sc[u][n], w0[2 * h], w1[2 * h], w0[2 * h + 1], w1[2 * h + 1], qf[n][2 * p + h][0], qf[n][2 * p + h][1]);
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) {
+                            uint32_t a0, a1, a2, a3;
+                            codes4<CACHE>(w0[h], a0, a2);
+                            codes4<CACHE>(w1[h], a1, a3);
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) mma<true>(sc[u][n], a0, a1, a2, a3, qf[n][4 * p + h][0], qf[n][4 * p + h][1]);
+                        }
                     }
                 }
-            }
-            const float kscale[2] = {ks[0], ks[1]}, vscale[2] = {vs[0], vs[1]};
+            float kscale[kSub][2], vscale[kSub][2];
+#pragma unroll
+            for (int u = 0; u < kSub; ++u)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    kscale[u][t] = kCodes ? ks[u][t] : 1.0f;
+                    vscale[u][t] = kCodes ? vs[u][t] : 1.0f;
+                }
             --left;
             at.next(a);
             const bool closes = left == 0 || at.step == 0;           // the warp's last step of this sequence and head
             if (left > 0) {
-                row = row_of(at);
-                load_k(row);
+                find_rows(at);
+                load_k();
             }
             // ---- masks: only a sequence's first and last steps have any
-            const int length = cur.length, token0 = (cur.first + cur.step) * 16;
+            const int length = cur.length, token0 = (cur.first + cur.step) * kTokens;
             const int lo = a.window > 0 ? length - a.window : 0;
-            const bool edge = token0 + 16 > length || token0 < lo || !there;
-            bool seen[2] = {true, true};
-            float vscale_used[2] = {vscale[0], vscale[1]};
+            bool edge = token0 + kTokens > length || token0 < lo;
+#pragma unroll
+            for (int u = 0; u < kSub; ++u) edge |= !there[u];
+            bool seen[kSub][2];
+#pragma unroll
+            for (int u = 0; u < kSub; ++u) seen[u][0] = seen[u][1] = true;
             if (edge) {
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const int token = token0 + i + 8 * t;
-                    seen[t] = there && token < length && token >= lo;
-                    if (!seen[t]) vscale_used[t] = 0.0f;
-                }
+                for (int u = 0; u < kSub; ++u) {
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const int token = token0 + 2 * j + (t & 1) + 8 * (t >> 1);
-                    if (there && token < length && token >= lo) continue;
+                    for (int t = 0; t < 2; ++t) {
+                        const int token = token0 + 16 * u + i + 8 * t;
+                        seen[u][t] = there[u] && token < length && token >= lo;
+                        if (!seen[u][t]) vscale[u][t] = 0.0f;
+                    }
 #pragma unroll
-                    for (int p = 0; p < kVPieces; ++p)
+                    for (int t = 0; t < 4; ++t) {
+                        const int token = token0 + 16 * u + 2 * j + (t & 1) + 8 * (t >> 1);
+                        if (there[u] && token < length && token >= lo) continue;
 #pragma unroll
-                        for (int w = 0; w < kVWords; ++w) vw[t][p][w] = 0;
+                        for (int p = 0; p < kVPieces; ++p)
+#pragma unroll
+                            for (int w = 0; w < kVWords; ++w) vw[u][t][p][w] = 0;
+                    }
                 }
             }
             // ---- weights
             bool move = false;
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int u = 0; u < kSub; ++u)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float s = sc[n][e] * q_scale[n][e & 1];
-                    if (kCodes) s *= kscale[e >> 1];
-                    s = seen[e >> 1] ? s : -INFINITY;
-                    sc[n][e] = s;
-                    move |= s > top[n][e & 1] + kRescale;
-                }
-            if (kCodes) move |= fabsf(vscale_used[0]) > largest || fabsf(vscale_used[1]) > largest;
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float s = sc[u][n][e] * q_scale[n][e & 1];
+                        if (kCodes) s *= kscale[u][e >> 1];
+                        s = seen[u][e >> 1] ? s : -INFINITY;
+                        sc[u][n][e] = s;
+                        move |= s > top[n][e & 1] + kRescale;
+                    }
+            if (kCodes)
+#pragma unroll
+                for (int u = 0; u < kSub; ++u) move |= fabsf(vscale[u][0]) > largest || fabsf(vscale[u][1]) > largest;
             if (__any_sync(0xffffffffu, move)) {
                 float shrink = 1.0f;
                 if (kCodes) {
-                    float m = fmaxf(largest, fmaxf(fabsf(vscale_used[0]), fabsf(vscale_used[1])));
+                    float m = largest;
+#pragma unroll
+                    for (int u = 0; u < kSub; ++u) m = fmaxf(m, fmaxf(fabsf(vscale[u][0]), fabsf(vscale[u][1])));
 #pragma unroll
                     for (int x = 4; x < 32; x *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
                     shrink = largest / m;
                     largest = m;
+                    unit_inv = 1.0f / m;
                 }
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     float by[2];
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        float m = fmaxf(top[n][c], fmaxf(sc[n][c], sc[n][2 + c]));
+                        float m = top[n][c];
+#pragma unroll
+                        for (int u = 0; u < kSub; ++u) m = fmaxf(m, fmaxf(sc[u][n][c], sc[u][n][2 + c]));
 #pragma unroll
                         for (int x = 4; x < 32; x *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
                         by[c] = top[n][c] == -INFINITY ? 0.0f : exp2a(top[n][c] - m);
@@ -412,62 +462,67 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) token_kernel(const 
                     }
                 }
             }
-            uint32_t pf[NT][2];
-            float value[2] = {1.0f, 1.0f};
-            if (kCodes) {
-                const float inv = 1.0f / largest;
-                value[0] = vscale_used[0] * inv * 128.0f;            // 2^kShift
-                value[1] = vscale_used[1] * inv * 128.0f;
-            }
+            uint32_t pf[kSub][NT][2];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                float p[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float m = top[n][e & 1];
-                    p[e] = exp2a(sc[n][e] - (m == -INFINITY ? 0.0f : m));
-                    weight[n][e & 1] += p[e];
-                    if (kCodes) p[e] *= value[e >> 1];
-                }
+            for (int u = 0; u < kSub; ++u) {
                 if (kCodes) {
-                    const __half2 x = __floats2half2_rn(p[0], p[1]), y = __floats2half2_rn(p[2], p[3]);
-                    pf[n][0] = transpose8x8(*reinterpret_cast<const uint32_t*>(&x));
-                    pf[n][1] = transpose8x8(*reinterpret_cast<const uint32_t*>(&y));
-                } else {
-                    // bf16 has fp32's range: a weight is off by at most 2^-9 of itself
-                    const __nv_bfloat162 x = __floats2bfloat162_rn(p[0], p[1]), y = __floats2bfloat162_rn(p[2], p[3]);
-                    pf[n][0] = transpose8x8(*reinterpret_cast<const uint32_t*>(&x));
-                    pf[n][1] = transpose8x8(*reinterpret_cast<const uint32_t*>(&y));
+                    vscale[u][0] = vscale[u][0] * unit_inv * 128.0f;
+                    vscale[u][1] = vscale[u][1] * unit_inv * 128.0f;
                 }
-            }
-            // ---- values
-            if (!kCodes) {
 #pragma unroll
-                for (int s = 0; s < kSteps; ++s) {
-                    // two pieces of 8 channels: rows 0-7 of tile s are channel s of piece i, rows 8-15 of piece i + 8; one piece: channels 2 s, 2 s + 1
-                    const int w = kVPieces == 2 ? s / 2 : s;
-                    const uint32_t lo0 = kVPieces == 2 ? ((s & 1) ? 0x7632u : 0x5410u) : 0x5410u, hi0 = kVPieces == 2 ? lo0 : 0x7632u;
-                    const uint32_t a0 = prmt(vw[0][0][w], vw[1][0][w], lo0), a1 = prmt(vw[0][kVPieces - 1][w], vw[1][kVPieces - 1][w], hi0);
-                    const uint32_t a2 = prmt(vw[2][0][w], vw[3][0][w], lo0), a3 = prmt(vw[2][kVPieces - 1][w], vw[3][kVPieces - 1][w], hi0);
+                for (int n = 0; n < NT; ++n) {
+                    float p[4];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) mma<false>(o[n][s], a0, a1, a2, a3, pf[n][0], pf[n][1]);
-                }
-            } else {
-#pragma unroll
-                for (int w = 0; w < kVWords; ++w) {                  // four channels: two tiles, channels 2 s, 2 s + 1 of the lane's piece
-                    uint32_t x[4], y[4];
-                    codes4<CACHE>(prmt(vw[0][0][w], vw[1][0][w], 0x5140), x[0], x[1]);
-                    codes4<CACHE>(prmt(vw[0][0][w], vw[1][0][w], 0x7362), x[2], x[3]);
-                    codes4<CACHE>(prmt(vw[2][0][w], vw[3][0][w], 0x5140), y[0], y[1]);
-                    codes4<CACHE>(prmt(vw[2][0][w], vw[3][0][w], 0x7362), y[2], y[3]);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        mma<true>(o[n][2 * w], x[0], x[1], y[0], y[1], pf[n][0], pf[n][1]);
-                        mma<true>(o[n][2 * w + 1], x[2], x[3], y[2], y[3], pf[n][0], pf[n][1]);
+                    for (int e = 0; e < 4; ++e) {
+                        const float m = top[n][e & 1];
+                        p[e] = exp2a(sc[u][n][e] - (m == -INFINITY ? 0.0f : m));
+                        weight[n][e & 1] += p[e];
+                        if (kCodes) p[e] *= vscale[u][e >> 1];
+                    }
+                    if (kCodes) {
+                        const __half2 x = __floats2half2_rn(p[0], p[1]), y = __floats2half2_rn(p[2], p[3]);
+                        pf[u][n][0] = transpose8x8(*reinterpret_cast<const uint32_t*>(&x));
+                        pf[u][n][1] = transpose8x8(*reinterpret_cast<const uint32_t*>(&y));
+                    } else {
+                        // bf16 has fp32's range: a weight is off by at most 2^-9 of itself
+                        const __nv_bfloat162 x = __floats2bfloat162_rn(p[0], p[1]), y = __floats2bfloat162_rn(p[2], p[3]);
+                        pf[u][n][0] = transpose8x8(*reinterpret_cast<const uint32_t*>(&x));
+                        pf[u][n][1] = transpose8x8(*reinterpret_cast<const uint32_t*>(&y));
                     }
                 }
             }
-            if (left > 0) load_v(row);
+            // ---- values
+#pragma unroll
+            for (int u = 0; u < kSub; ++u) {
+                const uint32_t (&v)[4][kVPieces][kVWords] = vw[u];
+                if (!kCodes) {
+#pragma unroll
+                    for (int s = 0; s < kSteps; ++s) {
+                        // two pieces of 8 channels: rows 0-7 of tile s are channel s of piece i, rows 8-15 of piece i + 8; one piece: channels 2 s, 2 s + 1
+                        const int w = kVPieces == 2 ? s / 2 : s;
+                        const uint32_t lo0 = kVPieces == 2 ? ((s & 1) ? 0x7632u : 0x5410u) : 0x5410u, hi0 = kVPieces == 2 ? lo0 : 0x7632u;
+                        const uint32_t a0 = prmt(v[0][0][w], v[1][0][w], lo0), a1 = prmt(v[0][kVPieces - 1][w], v[1][kVPieces - 1][w], hi0);
+                        const uint32_t a2 = prmt(v[2][0][w], v[3][0][w], lo0), a3 = prmt(v[2][kVPieces - 1][w], v[3][kVPieces - 1][w], hi0);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) mma<false>(o[n][s], a0, a1, a2, a3, pf[u][n][0], pf[u][n][1]);
+                    }
+                } else {
+#pragma unroll
+                    for (int w = 0; w < kVWords; ++w) {              // four channels: two tiles, channels 2 s, 2 s + 1 of the lane's piece
+                        uint32_t x[4], y[4];
+                        codes4<CACHE>(prmt(v[0][0][w], v[1][0][w], 0x5140), x[0], x[1]);
+                        codes4<CACHE>(prmt(v[0][0][w], v[1][0][w], 0x7362), x[2], x[3]);
+                        codes4<CACHE>(prmt(v[2][0][w], v[3][0][w], 0x5140), y[0], y[1]);
+                        codes4<CACHE>(prmt(v[2][0][w], v[3][0][w], 0x7362), y[2], y[3]);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            mma<true>(o[n][2 * w], x[0], x[1], y[0], y[1], pf[u][n][0], pf[u][n][1]);
+                            mma<true>(o[n][2 * w + 1], x[2], x[3], y[2], y[3], pf[u][n][0], pf[u][n][1]);
+                        }
+                    }
+                }
+            }
+            if (left > 0) load_v();
 
             if (closes) {
                 fresh = true;
@@ -574,7 +629,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) token_kernel(const 
         if (begins && !ends) {
             // the last step of it is `rest` steps behind this block's end
             const long long x = end - 1 + rest;
-            record = make_int4(first.x, first.y, (int)(((x + 1) * blocks - 1) / total), 0);
+            record = make_int4(first.x, first.y, (int)divide((x + 1) * blocks - 1, total), 0);
         }
         p = last + 1;
     }
@@ -614,8 +669,8 @@ int tiles(int group) { return group <= 8 ? 1 : 2; }
 // Thread blocks: as many as the GPU holds at once, no more than there can be work for.
 int64_t block_count(const nq_kv_pages* c, int64_t q_heads, int64_t seqs, int64_t table_cols) {
     const int group = (int)(q_heads / c->kv_heads), nt = tiles(group);
-    const int64_t per = (group + 8 * nt - 1) / (8 * nt) * c->kv_heads * table_cols * (c->page_size / 16);     // steps of the longest sequence
-    const int64_t most = (nt == 1 ? 3 : 2) * (int64_t)sm_count();
+    const int64_t per = (group + 8 * nt - 1) / (8 * nt) * c->kv_heads * ((table_cols * c->page_size + step_tokens(c->head_dim, c->dtype) - 1) / step_tokens(c->head_dim, c->dtype));     // steps of the longest sequence
+    const int64_t most = (nt == 1 && !(c->head_dim == 128 && c->dtype != NQ_BF16) ? 3 : 2) * (int64_t)sm_count();
     if (per >= most * kWarps || seqs >= most * kWarps) return most;
     const int64_t need = (per * seqs + kWarps - 1) / kWarps;
     return need < 1 ? 1 : need < most ? need : most;

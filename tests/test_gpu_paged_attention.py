@@ -16,7 +16,19 @@ def definition(q, cache, table, lengths, window, scale):
             t = torch.arange(n, device="cuda")
             seen = (t >= n - window)[None] if window else torch.ones(1, n, dtype=torch.bool, device="cuda")
             y[i:i + 1], bound[i:i + 1] = attend(q[i:i + 1], sequence(cache, table[i], n, 0), sequence(cache, table[i], n, 1), seen, scale)
+            if cache[3] is not None:
+                bound[i] += held_as_f16(cache, table[i], n, seen[0], q.shape[1])
     return y, bound
+
+
+def held_as_f16(cache, row, n, seen, heads):
+    """What weights of 8-bit values lose beside bf16's half step.  A weight w (of the one at the running maximum, which is 1 and not above
+    the largest) is held as f16(2^7 w vs / R), R the largest scale so far: under 2^-14 that is off by half of f16's least step, 2^-25, so
+    the sum by at most 2^-25 2^-7 R sum |code|, and the sum of weights it is divided by is 1 at least."""
+    codes = sequence((cache[0], cache[1], None, None), row, n, 1).abs()
+    scales = sequence((cache[0], cache[3][..., None], None, None), row, n, 1)
+    codes, scales = torch.where(seen[:, None, None], codes, 0.0), torch.where(seen[:, None, None], scales, 0.0)
+    return (2.0 ** -32 * scales.abs().amax(0) * codes.sum(0)).repeat_interleave(heads // codes.shape[1], 0)
 
 
 def case(lengths, group, kv_heads, dim, page, kind, window=0, seed=1, q_scale=1.0, scale=None):
@@ -113,6 +125,8 @@ def test_pages_outside_the_cache_are_hidden(kind):
             assert bool((y[i] == 0).all())
             continue
         want, bound = attend(q[i:i + 1], sequence(cache, table[i], length, 0), sequence(cache, table[i], length, 1), seen[None], 0.125)
+        if cache[3] is not None:
+            bound[0] += held_as_f16(cache, table[i], length, seen, 4)
         check(y[i:i + 1], want, bound)
 
 
