@@ -43,12 +43,14 @@ __device__ __forceinline__ void row_scale(uint32_t amax_bits, float most, float&
     inv = __frcp_rn(s);
 }
 
-// Four values to INT8, `a` in the lowest byte: nearest even, clamped to +-127 (fl(x * inv) can pass 127 by a rounding), a NaN as 0.
+// Four values to INT8, `a` in the lowest byte: nearest even, a NaN as 0.  (Within +-127.5, as x * inv is, nothing comes out as -128.)
 __device__ __forceinline__ uint32_t i8x4(float a, float b, float c, float d) {
-    const float v[4] = {a, b, c, d};
-    uint32_t r = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r |= (uint32_t)(min(max(__float2int_rn(v[i]), -127), 127) & 0xff) << (8 * i);
+    uint32_t w[4], r;
+    asm("cvt.rni.sat.s8.f32 %0, %1;" : "=r"(w[0]) : "f"(a));
+    asm("cvt.rni.sat.s8.f32 %0, %1;" : "=r"(w[1]) : "f"(b));
+    asm("cvt.rni.sat.s8.f32 %0, %1;" : "=r"(w[2]) : "f"(c));
+    asm("cvt.rni.sat.s8.f32 %0, %1;" : "=r"(w[3]) : "f"(d));
+    asm("{\n\t.reg .b32 x, y;\n\tprmt.b32 x, %1, %2, 0x0040;\n\tprmt.b32 y, %3, %4, 0x0040;\n\tprmt.b32 %0, x, y, 0x5410;\n\t}" : "=r"(r) : "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]));
     return r;
 }
 
