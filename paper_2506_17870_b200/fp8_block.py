@@ -112,37 +112,18 @@ def block_norm(x: torch.Tensor, y: Optional[torch.Tensor], post_weight: Optional
     return _BlockNorm.apply(*tensors, how, dict(h_dtype=h_dtype, h_scale=h_scale))
 
 
-class MlpBlock(torch.nn.Module):
-    """norm -> up -> activation -> down; its output meets the stream in the next block's (or the final) norm, which
-    applies this block's post norm, gate and residual scale."""
+class ServedBlock(torch.nn.Module):
+    """A block whose linears (`linears`: their names) are laid out as Fp8Weights for serving, and refused once they have changed."""
+    linears: Tuple[str, ...] = ()
 
-    def __init__(self, width: int, hidden: int, device="cuda"):
+    def __init__(self):
         super().__init__()
-        new = lambda *shape: torch.nn.Parameter(torch.empty(*shape, device=device))
-        self.pre_weight, self.post_weight, self.gate = new(width), new(width), new(1, width)
-        self.up, self.down, self.up_bias = new(hidden, width), new(width, hidden), new(hidden)
-        with torch.no_grad():
-            self.pre_weight.fill_(1.0)
-            self.post_weight.fill_(1.0)
-            self.gate.fill_(0.5)
-            self.up_bias.zero_()
-            self.up.normal_(std=width ** -0.5)
-            self.down.normal_(std=hidden ** -0.5)
-        self.served: Optional[Tuple[Fp8Weight, Fp8Weight]] = None
-        self._served_from = None                               # what up and down were when they were laid out
-
-    def forward(self, h: torch.Tensor) -> torch.Tensor:
-        y = fp8_linear(torch.nn.functional.gelu(fp8_linear(h, self.up, self.up_bias)), self.down)
-        if y.requires_grad and (self.up.requires_grad or self.down.requires_grad):
-            y.register_hook(self._backward_came)
-        return y
-
-    def _backward_came(self, _) -> None:
-        self._served_from = None                               # a fused optimiser's step is not counted as a write
+        self.served: Optional[Tuple[Fp8Weight, ...]] = None
+        self._served_from = None                               # what the linears were when they were laid out
 
     def _weights(self):
-        """The two weights, where they lie and how often they were written (not counting writes through .data)."""
-        return [(w, w.data_ptr(), 0 if w.is_inference() else w._version) for w in (self.up, self.down)]
+        """The linears, where they lie and how often they were written (not counting writes through .data)."""
+        return [(w, w.data_ptr(), 0 if w.is_inference() else w._version) for w in (getattr(self, name) for name in self.linears)]
 
     def _served_as_they_are(self) -> bool:
         return self._served_from is not None and all(a is b and rest == now for (a, *rest), (b, *now) in zip(self._served_from, self._weights()))
@@ -161,13 +142,44 @@ class MlpBlock(torch.nn.Module):
     def freeze(self) -> None:
         """Lays the weights out for serving; to be called again after a backward pass or a change of the weights.  (Not noticed
         by serve(): writes through .data, and a fused optimiser's step on gradients from before this call.)"""
-        self.served, self._served_from = (quantize_weight(self.up), quantize_weight(self.down)), self._weights()
+        self.served, self._served_from = tuple(quantize_weight(getattr(self, name)) for name in self.linears), self._weights()
+
+    def _laid_out(self) -> Tuple[Fp8Weight, ...]:
+        if not self._served_as_they_are():
+            raise RuntimeError("the weights were not laid out for serving, or were trained or changed since: call freeze()")
+        return self.served
+
+
+class MlpBlock(ServedBlock):
+    """norm -> up -> activation -> down; its output meets the stream in the next block's (or the final) norm, which
+    applies this block's post norm, gate and residual scale."""
+    linears = ("up", "down")
+
+    def __init__(self, width: int, hidden: int, device="cuda"):
+        super().__init__()
+        new = lambda *shape: torch.nn.Parameter(torch.empty(*shape, device=device))
+        self.pre_weight, self.post_weight, self.gate = new(width), new(width), new(1, width)
+        self.up, self.down, self.up_bias = new(hidden, width), new(width, hidden), new(hidden)
+        with torch.no_grad():
+            self.pre_weight.fill_(1.0)
+            self.post_weight.fill_(1.0)
+            self.gate.fill_(0.5)
+            self.up_bias.zero_()
+            self.up.normal_(std=width ** -0.5)
+            self.down.normal_(std=hidden ** -0.5)
+
+    def forward(self, h: torch.Tensor) -> torch.Tensor:
+        y = fp8_linear(torch.nn.functional.gelu(fp8_linear(h, self.up, self.up_bias)), self.down)
+        if y.requires_grad and (self.up.requires_grad or self.down.requires_grad):
+            y.register_hook(self._backward_came)
+        return y
+
+    def _backward_came(self, _) -> None:
+        self._served_from = None                               # a fused optimiser's step is not counted as a write
 
     @torch.no_grad()
     def serve(self, h: torch.Tensor, hs: torch.Tensor) -> torch.Tensor:
-        if not self._served_as_they_are():
-            raise RuntimeError("the weights were not laid out for serving, or were trained or changed since: call freeze()")
-        up, down = self.served
+        up, down = self._laid_out()
         a = torch.nn.functional.gelu(nq.nq_fp8_gemm(h, hs, up.q, up.s, bias=self.up_bias))
         q, s, _, _ = nq.nq_fp8_quantize(a)
         return nq.nq_fp8_gemm(q, s, down.q, down.s)
@@ -200,8 +212,8 @@ class MlpStack(torch.nn.Module):
             b.freeze()
 
     @torch.no_grad()
-    def serve(self, x: torch.Tensor) -> torch.Tensor:
-        """The same for one token or many, with the norms' outputs as e4m3 operands."""
+    def serve(self, x: torch.Tensor, *more) -> torch.Tensor:
+        """The same for one token or many, with the norms' outputs as e4m3 operands; `more` goes to each block."""
         y = None
         for i in range(len(self.blocks) + 1):
             post, gate, pre, how = self._between(i)
@@ -211,7 +223,7 @@ class MlpStack(torch.nn.Module):
                                         h_dtype=torch.bfloat16 if final else torch.float8_e4m3fn, **how)
             x = x if r is None else r
             if not final:
-                y = self.blocks[i].serve(h, hs)
+                y = self.blocks[i].serve(h, hs, *more)
         return h
 
 
