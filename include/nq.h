@@ -481,7 +481,7 @@ NQ_API int nq_kv_cache_write(const nq_kv_pages *cache, const void *K, int64_t ld
 /*
  * ... and back, as packed rows: token t of sequence s to row starts[s] + t of K, V (device, out) [rows, kv_heads * head_dim] of
  * y_dtype (NQ_F32, NQ_BF16).  starts (device) int32 [seqs + 1], not decreasing: sequence s has starts[s + 1] - starts[s] tokens.
- * Rows before starts[0] and from starts[seqs] on are left as they were; starts past `rows` are not followed.
+ * Rows before starts[0] and from starts[seqs] on are left as they were; starts past `rows` are not followed.  K, V must not overlap the cache.
  */
 NQ_API int nq_kv_cache_read(const nq_kv_pages *cache, const int32_t *table, int64_t ld_table, int64_t table_cols, const int32_t *starts,
                             int64_t seqs, void *K, int64_t ldk, void *V, int64_t ldv, int y_dtype, int64_t rows, void *stream);
@@ -491,7 +491,8 @@ NQ_API int nq_kv_cache_read(const nq_kv_pages *cache, const int32_t *table, int6
  *   y_h = sum_t w_t v_t,  w = softmax over t of (scale * q_h . k_t),  t in [max(0, n - window), n), n = min(lengths[s], what the
  *   table's columns hold); window == 0: all of them.
  *   scale > 0.  A sequence that sees nothing (n <= 0, or no page in the cache), or whose scores are all -infinity, gets zeros.
- *   Q (device) bf16 [seqs, q_heads * head_dim], pitch ldq; Y (device, out) likewise, pitch ldy (multiples of 8, 16-byte aligned)
+ *   Q (device) bf16 [seqs, q_heads * head_dim], pitch ldq; Y (device, out) likewise, pitch ldy (multiples of 8, 16-byte aligned); Y must not
+ *   overlap Q or the cache
  *   table (device) int32 [seqs, table_cols], lengths (device) int32 [seqs]
  *   Sums, maxima and weights are fp32.  A weight is rounded to bf16 (bf16 cache) or f16 (8-bit caches, times the value's scale)
  *   for its product with the values, which is exact in both; queries meet 8-bit keys as f16, scaled by a power of two.  As f16, a

@@ -389,7 +389,8 @@ __global__ void __launch_bounds__(kThreads, 3) read_kernel(const ReadArgs a) {
                 break;
             }
         }
-        const int t = (int)(row - from), of = t / a.c.page_size, within = t - of * a.c.page_size;
+        const long long t = row - from;                       // (a start far below 0 leaves no page: all tokens of a table have numbers under 2^31)
+        const int of = t > 0x7fffffffll ? 0x7fffffff : (int)t / a.c.page_size, within = t > 0x7fffffffll ? 0 : (int)t - of * a.c.page_size;
         if (of != nth) {
             nth = of;
             page = of < a.table_cols ? a.table[seq * a.ld_table + of] : -1;

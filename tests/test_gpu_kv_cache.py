@@ -184,3 +184,27 @@ def test_offsets_past_32_bits():
     assert torch.equal(k[page - 1], x[0]) and torch.equal(k[0], x[2]) and torch.equal(v[page], -x[1])
     y = nq.nq_paged_attention(x[:2].contiguous(), c, table, torch.tensor([1, 1], dtype=torch.int32, device="cuda"))
     assert torch.equal(y[0], -x[2]) and torch.equal(y[1], -x[1])
+
+
+def test_starts_far_below_zero_have_no_pages():
+    cache = empty(2, 1, 16, 64, BF16, 1.0)
+    table = torch.tensor([[0, 1]], dtype=torch.int32, device="cuda")
+    starts = torch.tensor([-(1 << 31), 5], dtype=torch.int32, device="cuda")
+    k, v = nq.nq_kv_cache_read(nq.nq_kv_pages(*cache), table, starts, 5)
+    assert bool((k == 0).all()) and bool((v == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_queries_in_place(dtype):
+    import ctypes
+    x = torch.randn(600, (8 + 2 * 2) * 128, device="cuda").to(dtype)
+    angles = angles_of(700, 128)
+    positions = torch.arange(600, dtype=torch.int32, device="cuda")
+    want, _ = nq.nq_qk_norm_rotate(x, angles, positions, q_heads=8, kv_heads=2, y_dtype=dtype)
+    before = x.clone()
+    code = nq.NQ_BF16 if dtype is BF16 else nq.NQ_F32
+    k = torch.empty(600, 256, dtype=dtype, device="cuda")
+    d = nq.nq_qk_desc(600, 1536, 1536, 256, 700, code, code, 8, 2, 128, 128, nq.NQ_NORM_RMS, 0, 1e-6)
+    assert nq.lib().nq_qk_norm_rotate(ctypes.addressof(d), x.data_ptr(), None, None, angles.data_ptr(), positions.data_ptr(), x.data_ptr(), k.data_ptr(),
+                                      None, None, torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(x[:, :1024].view(600, 8, 128), want) and torch.equal(x[:, 1024:], before[:, 1024:])

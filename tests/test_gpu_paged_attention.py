@@ -205,3 +205,31 @@ def test_two_streams_at_once():
                 got[i] = nq.nq_paged_attention(qs[i], c, table, n)
         torch.cuda.synchronize()
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("kind", [F8, I8])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_a_key_of_infinite_scale_is_no_number_whatever_its_score(kind, sign):
+    cache, table, n = filled([20], 1, 16, 64, kind, 2)
+    q = torch.full((1, 4, 64), sign, device="cuda").bfloat16()
+    page = int(table[0, 0])
+    cache[0][page, 0, 5] = torch.ones(64, device="cuda").to(kind)
+    cache[2][page, 0, 5] = float("inf")
+    assert torch.isnan(nq.nq_paged_attention(q, nq.nq_kv_pages(*cache), table, n)).all()
+
+
+@pytest.mark.parametrize("kind", [BF16, F8])
+def test_calls_one_behind_another_share_nothing(kind):
+    """Many calls of different sizes in a row, each launched while the one before still runs."""
+    made = [filled(lengths, 2, 16, 64, kind, seed) for seed, lengths in enumerate([[3000, 5], [1] * 300, [0, 700, 0], [17]])]
+    qs = [torch.randn(len(m[2]), 8, 64, device="cuda").bfloat16() for m in made]
+    call = lambda i: nq.nq_paged_attention(qs[i], nq.nq_kv_pages(*made[i][0]), made[i][1], made[i][2])
+    want = []
+    for i in range(4):
+        want.append(call(i))
+        torch.cuda.synchronize()
+    for _ in range(30):
+        got = [call(i) for i in (0, 1, 2, 3, 1, 0)]
+    torch.cuda.synchronize()
+    for i, y in zip((0, 1, 2, 3, 1, 0), got):
+        assert torch.equal(y, want[i])
