@@ -906,26 +906,33 @@ class nq_kv_pages(ctypes.Structure):
                 [(k, ctypes.c_int32) for k in ("page_size", "kv_heads", "head_dim", "dtype")])
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, ks: Optional[torch.Tensor] = None, vs: Optional[torch.Tensor] = None):
-        code = _CACHE_TYPES.get(k.dtype)
+        kind, shape, index = k.dtype, k.shape, k.get_device()
+        code = _CACHE_TYPES.get(kind)
         if code is None:
-            raise ValueError(f"a cache is bfloat16, float8_e4m3fn or int8, got {k.dtype}")
-        if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype:
-            raise ValueError(f"k and v must be [pages, kv_heads, page_size, head_dim] of one type, got {list(k.shape)} {k.dtype} and {list(v.shape)} {v.dtype}")
+            raise ValueError(f"a cache is bfloat16, float8_e4m3fn or int8, got {kind}")
+        if len(shape) != 4 or v.shape != shape or v.dtype is not kind:
+            raise ValueError(f"k and v must be [pages, kv_heads, page_size, head_dim] of one type, got {list(shape)} {kind} and {list(v.shape)} {v.dtype}")
         if (code == NQ_BF16) != (ks is None) or (code == NQ_BF16) != (vs is None):
             raise ValueError("ks and vs go with a float8_e4m3fn or int8 cache")
-        index = k.get_device()
-        shape = k.shape
-        for name, t in (("k", k), ("v", v), ("ks", ks), ("vs", vs)):
-            if t is None:
-                continue
-            _on(t, name, index)
-            if name in ("ks", "vs") and (t.dtype is not torch.float32 or t.shape != shape[:3]):
-                raise ValueError(f"{name} must be float32 {list(shape[:3])}, got {t.dtype} {list(t.shape)}")
-            if not t.is_contiguous():
-                raise ValueError(f"{name} must be contiguous")
-        super().__init__(k.data_ptr(), v.data_ptr(), None if ks is None else ks.data_ptr(), None if vs is None else vs.data_ptr(),
-                         shape[0], shape[2], shape[1], shape[3], code)
+        _cache_tensor(k, "k", index)
+        _cache_tensor(v, "v", index)
+        ks_ptr = vs_ptr = None
+        if ks is not None:
+            for name, t in (("ks", ks), ("vs", vs)):
+                if t.dtype is not torch.float32 or t.shape != shape[:3]:
+                    raise ValueError(f"{name} must be float32 {list(shape[:3])}, got {t.dtype} {list(t.shape)}")
+                _cache_tensor(t, name, index)
+            ks_ptr, vs_ptr = ks.data_ptr(), vs.data_ptr()
+        pages, heads, page, dim = shape
+        super().__init__(k.data_ptr(), v.data_ptr(), ks_ptr, vs_ptr, pages, page, heads, dim, code)
         self.tensors, self.index = (k, v, ks, vs), index
+
+
+def _cache_tensor(t: torch.Tensor, name: str, index: int) -> None:
+    if t.get_device() != index or index < 0:
+        _on(t, name, index)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
 
 
 def _pages_on(cache: nq_kv_pages, index: int) -> int:
@@ -945,7 +952,10 @@ def _heads(t: torch.Tensor, name: str, index: int, heads: int, dim: int) -> int:
     """Checks [tokens, heads, dim] on the GPU of this index, a token's heads dense; -> its pitch of tokens."""
     if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
         raise ValueError(f"{name} must be [tokens, {heads}, {dim}], got {list(t.shape)}")
-    _on(t, name, index)
+    if t.get_device() != index or index < 0:
+        _on(t, name, index)
+    if t.is_contiguous():
+        return heads * dim
     ld, between, step = t.stride()
     if t.numel() > 0 and ((step != 1 and dim > 1) or (between != dim and heads > 1)):
         raise ValueError(f"{name} must have dense heads in a token (strides {list(t.stride())})")
@@ -957,6 +967,8 @@ def _heads(t: torch.Tensor, name: str, index: int, heads: int, dim: int) -> int:
 
 
 def _table(t: torch.Tensor, seqs: int, index: int) -> int:
+    if t.dtype is torch.int32 and t.is_contiguous() and t.dim() == 2 and t.shape[0] == seqs and t.get_device() == index >= 0:
+        return t.shape[1] or 1
     return _matrix(t, "table", index, torch.int32, (seqs, t.shape[-1]))
 
 
@@ -1025,11 +1037,16 @@ def nq_kv_cache_read(cache: nq_kv_pages, table: torch.Tensor, starts: torch.Tens
     if rows < 0:
         raise ValueError("rows must not be negative")
     if k_out is None:
-        make = lambda: torch.empty_strided((rows, heads, dim), (heads * dim, dim, 1), dtype=y_dtype, device=table.device)
-        k_out, v_out = make(), make()
-    if k_out.dtype not in _FLOATS or v_out.dtype is not k_out.dtype or k_out.shape[0] != rows or v_out.shape[0] != rows:
-        raise ValueError(f"k and v must be float32 or bfloat16 with {rows} rows, got {k_out.dtype} {list(k_out.shape)} and {v_out.dtype} {list(v_out.shape)}")
-    ldk, ldv = _heads(k_out, "k_out", index, heads, dim), _heads(v_out, "v_out", index, heads, dim)
+        if y_dtype not in _FLOATS:
+            raise ValueError(f"the output must be float32 or bfloat16, got {y_dtype}")
+        shape, strides, device = (rows, heads, dim), (heads * dim, dim, 1), table.device
+        k_out = torch.empty_strided(shape, strides, dtype=y_dtype, device=device)
+        v_out = torch.empty_strided(shape, strides, dtype=y_dtype, device=device)
+        ldk = ldv = heads * dim
+    else:
+        if k_out.dtype not in _FLOATS or v_out.dtype is not k_out.dtype or k_out.shape[0] != rows or v_out.shape[0] != rows:
+            raise ValueError(f"k and v must be float32 or bfloat16 with {rows} rows, got {k_out.dtype} {list(k_out.shape)} and {v_out.dtype} {list(v_out.shape)}")
+        ldk, ldv = _heads(k_out, "k_out", index, heads, dim), _heads(v_out, "v_out", index, heads, dim)
     seqs = table.shape[0]
     _check(lib().nq_kv_cache_read(_pages_on(cache, index), table.data_ptr(), _table(table, seqs, index), table.shape[-1], _ints(starts, "starts", seqs + 1, index),
                                   seqs, k_out.data_ptr(), ldk, v_out.data_ptr(), ldv, _FLOATS[k_out.dtype], rows, _raw_stream(table)), "nq_kv_cache_read")

@@ -93,7 +93,7 @@ template <typename T, typename Y, int D, int CACHE, bool PLAIN>
 __global__ void __launch_bounds__(kThreads) heads_kernel(const HeadsArgs a) {
     constexpr int kLanes = D / 16, kGroups = 32 / kLanes, kTurns = sizeof(T) == 2 ? 4 : 2;
     const int lane = threadIdx.x & 31, p = lane % kLanes, group = lane / kLanes;
-    const long long warp = ((long long)blockIdx.x * kThreads + threadIdx.x) >> 5;
+    const long long warp = (long long)blockIdx.x * (kThreads / 32) + __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0);    // (known to be the warp's)
     const long long token = warp / a.parts;
     const int turn0 = (int)(warp - token * a.parts) * a.per_part;
     if (token >= a.tokens) return;
@@ -112,8 +112,8 @@ __global__ void __launch_bounds__(kThreads) heads_kernel(const HeadsArgs a) {
     Eight<T> raw[kTurns][2];
     const auto load = [&](Eight<T> (&to)[2], int turn) {
         const int kind = kind_of(turn), h = head_of(turn, kind);
-        if (h >= (kind == 0 ? a.q_heads : a.kv_heads)) return;
-        const T* src = (kind == 0 ? from[0] : kind == 1 ? from[1] : from[2]) + h * D;
+        // (behind the last head: that one again, which nobody stores)
+        const T* src = (kind == 0 ? from[0] : kind == 1 ? from[1] : from[2]) + min(h, (kind == 0 ? a.q_heads : a.kv_heads) - 1) * D;
         to[0].load(src + 8 * c0);
         to[1].load(src + 8 * c1);
     };
@@ -154,13 +154,8 @@ __global__ void __launch_bounds__(kThreads) heads_kernel(const HeadsArgs a) {
             const int kind = kind_of(turn), h = head_of(turn, kind);
             const bool live = h < (kind == 0 ? a.q_heads : a.kv_heads);
             uint64_t f[8];
-            if (live) {
-                raw[u][0].to(f);
-                raw[u][1].to(f + 4);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] = 0;
-            }
+            raw[u][0].to(f);
+            raw[u][1].to(f + 4);
             if (turn + kTurns < end) load(raw[u], turn + kTurns);    // kTurns turns are on their way at any time
             if (!PLAIN) {
                 if (a.rms && kind < 2) {
