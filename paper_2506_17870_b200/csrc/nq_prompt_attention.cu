@@ -15,14 +15,18 @@ namespace {
 
 using namespace sm100;
 
-// A unit of work is 256 rows of queries of one head, as two tiles of 128; a thread block works through units, one block an SM.
-// For each 128 keys ("step") and tile:  S = Q K^T into tensor memory (128 columns), the tile's four softmax warps read a row a
-// thread, keep its maximum and sum, write the weights back as bf16 over S, and O += P V takes them from there (P as the operand in
-// tensor memory, V as it lies, N-major).  While one tile's weights are being computed the tensor core works for the other:
-//   PV(0, j - 1)  QK(0, j)  PV(1, j - 1)  QK(1, j)  ...
+// A unit of work is two tiles of 128 rows of queries that read the same keys: 256 rows of a head, or 128 of two heads; a thread block works
+// through units, one block an SM.
+// For each 64 keys ("step") and tile:  S = Q K^T into one of the tile's two score buffers in tensor memory (64 columns), the tile's four
+// softmax warps read a row a thread, keep its maximum and sum, write the weights back as bf16 over S, and O += P V takes them from there
+// (P as the operand in tensor memory, V as it lies, N-major).  A tile's products go  PV(j - 2)  QK(j)  into the same buffer, while the
+// softmax is at step j - 1 in the other.  (Steps of 128 keys and one buffer, tiles taking turns: each waits out the other's round trip,
+// 16384 tokens of 8 heads 552 us.)
+// Measured: 16384 tokens, 8 / 2 heads of 128, causal: 421 us as a burst, 1.31 PFLOP/s (0.78 of the measured bf16 rate), some 520 back to back under
+// the power limit; tensor pipe, exponentials and issue are each about half busy, what bounds a step is the round trip.
 // The running maximum moves only when a score passes it by 2^8, so the sums in tensor memory are seldom rescaled (by the softmax warps:
-// S(j) being there says that PV(j - 1) is complete, for the tensor core works in order).
-// Two warps look after V where a step has hidden keys (the last of a sequence, the diagonal, a window's edge): rows of V behind the
+// S(j) being there says that PV(j - 2) is complete, for the tensor core works in order; PV(j - 1) has a barrier).
+// A warp looks after V where a step has hidden keys (the last of a sequence, the diagonal, a window's edge): rows of V behind the
 // sequence are zeroed, since 0 x NaN is NaN in the product, and where the sequence's own rows hold infinities or NaN, the tiles that
 // hide some of the step take their weights times V by themselves, only what each row sees.
 constexpr int kThreads = 384;            // warp 0 TMA and units, warps 1 and 2 MMA of the tiles (1 also TMEM), warp 3 looks after V, warps 4-7 and 8-11 softmax of the tiles
@@ -40,7 +44,9 @@ struct Shape {
 
 struct PromptArgs {
     const int *starts_q, *starts_k;
-    int seqs, rows_q, rows_k, q_heads, group, causal, window;
+    int seqs, rows_q, rows_k, group, causal, window;
+    int heads;                           // query heads, or pairs of them: what a unit is made for
+    int per_unit, span, next_row;        // a unit is 128 rows (`span`) of two heads that share their keys, or 256 of one, whose second tile starts next_row on
     float scale2;                        // score scale * log2(e)
     __nv_bfloat16* y;
     long long ldy;
@@ -49,8 +55,8 @@ struct PromptArgs {
 
 struct Unit {
     int q0, k0;                          // rows of the tensors: the sequence's first query and key
-    int lq, lk, row;                     // its lengths, and the unit's first row in it
-    int head;
+    int lq, lk;                          // its lengths
+    int row[2], head[2];                 // of each tile: its first row in the sequence, and its query head
     int lo[2], hi[2];                    // steps of each tile (hi <= lo: none)
     int all_lo[2], all_hi[2];            // keys that all rows of the tile see
     int begin, end;                      // steps of either
@@ -62,8 +68,8 @@ __device__ __forceinline__ int clamp_start(int v, int low, int high) { return mi
 
 // `before`: units (of one head) before each chunk of sequences
 __device__ __forceinline__ void unit_of(const PromptArgs& a, const int* before, int chunk, int index, Unit& u) {
-    const int pair = before[kThreads] - 1 - index / a.q_heads;     // the longest rows of a causal prompt first
-    u.head = index % a.q_heads;
+    const int pair = before[kThreads] - 1 - index / a.heads;       // the longest rows of a causal prompt first
+    const int head = index % a.heads * a.per_unit;
     int lo = 0, hi = kThreads;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -73,17 +79,18 @@ __device__ __forceinline__ void unit_of(const PromptArgs& a, const int* before, 
     for (;; ++s) {
         u.q0 = clamp_start(a.starts_q[s], 0, a.rows_q);
         u.lq = clamp_start(a.starts_q[s + 1], u.q0, a.rows_q) - u.q0;
-        const int n = (u.lq + 2 * kTile - 1) / (2 * kTile);
+        const int n = (u.lq + a.span - 1) / a.span;
         if (rest < n) break;
         rest -= n;
     }
     u.k0 = clamp_start(a.starts_k[s], 0, a.rows_k);
     u.lk = clamp_start(a.starts_k[s + 1], u.k0, a.rows_k) - u.k0;
-    u.row = rest * 2 * kTile;
     const int off = u.lk - u.lq;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        const int a0 = u.row + t * kTile, b0 = min(a0 + kTile, u.lq);              // rows [a0, b0)
+        u.row[t] = rest * a.span + t * a.next_row;
+        u.head[t] = head + t * (a.per_unit - 1);
+        const int a0 = u.row[t], b0 = min(a0 + kTile, u.lq);                       // rows [a0, b0)
         u.lo[t] = u.hi[t] = u.all_lo[t] = u.all_hi[t] = 0;
         if (a0 >= b0) continue;
         const int seen_hi = a.causal ? min(u.lk, b0 + off) : u.lk, seen_lo = a.window ? max(0, a0 + off + 1 - a.window) : 0;
@@ -141,10 +148,10 @@ __device__ __forceinline__ void hide(uint32_t (&s)[32], int lo, int hi) {
 }
 
 // Weights 2^(s scale + minus) of 32 scores, their sum, and as pairs of bf16 (a weight is off by at most 2^-9 of itself).
-// The exponential unit takes 4 a cycle and scheduler, which alone would be as long as both products.  So one of 4 comes from the other
+// The exponential unit takes 4 a cycle and scheduler, which alone would be as long as both products.  So 3 of 8 come from the other
 // pipes: 2^y = 2^n 2^f, n = y rounded (y + 1.5 * 2^23 holds it in its low bits), f in [-1/2, 1/2] by a polynomial of degree 3, fitted
 // to 2^f for the least relative error on that interval: 7.5e-5 (2^-13.7), where a weight's rounding is 2^-9.  y under -127 counts as that,
-// whose 2^n is made as 0; a NaN stays one.  (16384 tokens of 8 heads: none 492 us, one of 8 476, one of 4 433, 3 of 8 440.)
+// whose 2^n is made as 0; a NaN stays one.  (16384 tokens of 8 heads: none 492 us, one of 8 476, one of 4 428, 3 of 8 421.)
 __device__ __forceinline__ void weights_of(const uint32_t (&s)[32], float scale, float minus, uint64_t& sum, uint32_t (&p)[16]) {
     constexpr float kBig = 12582912.0f;
 #pragma unroll
@@ -153,7 +160,7 @@ __device__ __forceinline__ void weights_of(const uint32_t (&s)[32], float scale,
         float e0, e1;
         unpack2(y, e0, e1);
         uint64_t e;
-        if ((c / 2) % 4 == 3) {
+        if ((c / 2) % 8 >= 5) {
             const uint64_t z = pack2f(max3(e0, e0, -127.0f), max3(e1, e1, -127.0f));
             const uint64_t big = add2(z, both(kBig)), f = fma2(add2(big, both(-kBig)), both(-1.0f), z);
             const uint64_t q = fma2(fma2(fma2(both(0.0551716793f), f, both(0.2426111685f)), f, both(0.6932609878f)), f, both(0.9999280708f));
@@ -221,13 +228,13 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     start_next();
     wait_previous();
 
-    // units of one head before each chunk of sequences
+    // units of one head (or pair) before each chunk of sequences
     const int chunk = (a.seqs + kThreads - 1) / kThreads;
     {
         int sum = 0;
         for (int s = threadIdx.x * chunk; s < min(a.seqs, (int)(threadIdx.x + 1) * chunk); ++s) {
             const int from = clamp_start(a.starts_q[s], 0, a.rows_q);
-            sum += (clamp_start(a.starts_q[s + 1], from, a.rows_q) - from + 2 * kTile - 1) / (2 * kTile);
+            sum += (clamp_start(a.starts_q[s + 1], from, a.rows_q) - from + a.span - 1) / a.span;
         }
 #pragma unroll
         for (int m = 1; m < 32; m *= 2) {
@@ -244,7 +251,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
-    const int units = s_before[kThreads] * a.q_heads;          // the host has checked that it fits
+    const int units = s_before[kThreads] * a.heads;          // the host has checked that it fits
 
     // The grid has a block for each unit that there can be; a block that is done with its own takes one that has not begun (it
     // cancels that block's launch), so that all SMs end together however the units differ.  Warp 0 does this, one unit ahead of the
@@ -293,12 +300,12 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                         if (!(ok = mbar_wait(q_empty, (used & 1) ^ 1, abort_flag, a.status, 0x310u))) break;
                         ++used;
                         const bool one = u.hi[0] > u.lo[0], two = u.hi[1] > u.lo[1];
-                        const int kv_head = u.head / a.group, k0 = u.k0;
+                        const int kv_head = u.head[0] / a.group, k0 = u.k0;
                         mbar_arrive_expect_tx(q_full, (one + two) * P::kTileBytes);
 #pragma unroll
                         for (int h = 0; h < D / 64; ++h) {
-                            if (one) tma_load_3d(sQ + h * P::kSlabQ, &tmQ, 64 * h, u.head, u.q0 + u.row, q_full);
-                            if (two) tma_load_3d(sQ + P::kTileBytes + h * P::kSlabQ, &tmQ, 64 * h, u.head, u.q0 + u.row + kTile, q_full);
+                            if (one) tma_load_3d(sQ + h * P::kSlabQ, &tmQ, 64 * h, u.head[0], u.q0 + u.row[0], q_full);
+                            if (two) tma_load_3d(sQ + P::kTileBytes + h * P::kSlabQ, &tmQ, 64 * h, u.head[1], u.q0 + u.row[1], q_full);
                         }
                         for (int j = begin; j < end; ++j, ++it) {
                             const uint32_t s = it % ST, use = it / ST;
@@ -415,16 +422,17 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                     if (!ok) break;
                     if (u->hides(0, j) || u->hides(1, j)) {
                         const int live = u->lk - j * kKeys;        // rows of the sequence
-                        uint32_t odd = 0;
+                        uint8_t* v0 = smem + 2 * P::kTileBytes + (ST + s) * P::kStageBytes + (lane >> 3) * 128 + (lane & 7) * 16;
                         // a lane takes a 16-byte piece of every fourth row: 8 lanes are a row of 64 values
-#pragma unroll 4
-                        for (int x = 0; x < D; x += 4) {
-                            const int row = x % 64 + (lane >> 3);
-                            uint4* p = reinterpret_cast<uint4*>(smem + 2 * P::kTileBytes + (ST + s) * P::kStageBytes + x / 64 * P::kSlab + row * 128 + (lane & 7) * 16);
-                            if (row >= live) {
-                                *p = make_uint4(0, 0, 0, 0);
-                            } else {
-                                const uint4 v = *p;
+                        for (int x = max(0, live) & ~3; x < kKeys; x += 4)
+                            if (x + (lane >> 3) >= live)
+#pragma unroll
+                                for (int h = 0; h < D / 64; ++h) *reinterpret_cast<uint4*>(v0 + h * P::kSlab + x * 128) = make_uint4(0, 0, 0, 0);
+                        uint32_t odd = 0;
+                        if (a.causal || a.window) {                // (otherwise all that is left is seen by all)
+#pragma unroll 16
+                            for (int x = 0; x < D; x += 4) {       // rows x % 64 of slab x / 64
+                                const uint4 v = *reinterpret_cast<const uint4*>(v0 + x / 64 * P::kSlab + x % 64 * 128);
                                 odd |= ((v.x & 0x7f807f80u) + 0x00800080u) | ((v.y & 0x7f807f80u) + 0x00800080u) | ((v.z & 0x7f807f80u) + 0x00800080u) |
                                        ((v.w & 0x7f807f80u) + 0x00800080u);
                             }
@@ -458,7 +466,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             const Unit* u = take(n);
             if (!u) break;
             const int lo_t = u->lo[t], hi_t = u->hi[t], all_lo = u->all_lo[t], all_hi = u->all_hi[t];
-            const int row = u->row + t * kTile + quarter * 32 + lane;
+            const int row = u->row[t] + quarter * 32 + lane;
             // of the keys, this row sees no more than the first `reach`, and of those the last `window`; rows behind the last one must not
             // get in the way
             const int reach = min(row, u->lq - 1) + u->lk - u->lq + 1;
@@ -585,7 +593,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 if (lane == 0) mbar_arrive(p_full + 16 * t + 8 * (j & 1));
             }
             if (!ok) break;
-            if (u->row + t * kTile >= u->lq) continue;             // the whole tile
+            if (u->row[t] >= u->lq) continue;             // the whole tile
             const bool any = hi_t > lo_t;
             if (any) {
                 ok = sums_of(hi_t - 1);
@@ -597,8 +605,8 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             // 32 channels at once go through shared memory, so that four lanes write 64 bytes of a row (a row a lane, 16 bytes at once, took
             // 3500 cycles of 64 channels' unit).  Pieces are rotated by row / 2, so that neither way meets bank conflicts.
             uint8_t* stage = smem + 2 * P::kTileBytes + 2 * ST * P::kStageBytes + (warp - 4) * P::kOut;
-            const int rows = min(32, u->lq - u->row - t * kTile - quarter * 32), piece = lane & 3;
-            __nv_bfloat16* to = a.y + (long long)(u->q0 + u->row + t * kTile + quarter * 32) * a.ldy + u->head * D + 8 * piece;
+            const int rows = min(32, u->lq - u->row[t] - quarter * 32), piece = lane & 3;
+            __nv_bfloat16* to = a.y + (long long)(u->q0 + u->row[t] + quarter * 32) * a.ldy + u->head[t] * D + 8 * piece;
 #pragma unroll 1
             for (int c0 = 0; c0 < D; c0 += 32) {
                 uint32_t o[32];
@@ -690,11 +698,15 @@ extern "C" int nq_prompt_attention(const nq_prompt_desc* d, const void* Q, const
     const auto off = [](const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; };
     if (off(Q, 16) || off(Y, 16) || (d->ldq & 7) || (d->ldy & 7) || off(starts_q, 4) || off(starts_k, 4)) return NQ_ERR_ALIGNMENT;
     if (d->rows_k > 0 && (off(K, 16) || off(V, 16) || (d->ldk & 7) || (d->ldv & 7))) return NQ_ERR_ALIGNMENT;
-    const int64_t most = (d->rows_q / 256 + (d->seqs < d->rows_q ? d->seqs : d->rows_q)) * d->q_heads;      // units
+    // Heads that share keys go in pairs where there is an even number of them: both tiles of a unit then see the same keys, and short
+    // prompts fill both (the five packed ones: 144 us with 256 rows of a head).
+    const bool paired = d->q_heads / d->kv_heads % 2 == 0;
+    const int64_t heads = paired ? d->q_heads / 2 : d->q_heads;
+    const int64_t most = (d->rows_q / (paired ? 128 : 256) + (d->seqs < d->rows_q ? d->seqs : d->rows_q)) * heads;      // units
     if (most > 0x7fff0000ll || d->ldq >= 1ll << 38 || d->ldk >= 1ll << 38 || d->ldv >= 1ll << 38) return NQ_ERR_UNSUPPORTED;
     nq::PromptArgs a = {};
     a.starts_q = starts_q; a.starts_k = starts_k; a.seqs = (int)d->seqs; a.rows_q = (int)d->rows_q; a.rows_k = (int)d->rows_k;
-    a.q_heads = d->q_heads; a.group = d->q_heads / d->kv_heads; a.causal = d->causal != 0; a.window = d->window;
+    a.heads = (int)heads; a.per_unit = paired ? 2 : 1; a.span = paired ? 128 : 256; a.next_row = paired ? 0 : 128; a.group = d->q_heads / d->kv_heads; a.causal = d->causal != 0; a.window = d->window;
     a.scale2 = d->scale * 1.44269504088896341f;
     a.y = static_cast<__nv_bfloat16*>(Y); a.ldy = d->ldy;
     a.status = nq::status_word();

@@ -215,3 +215,27 @@ def test_two_streams_at_once():
                 got[i] = nq.nq_prompt_attention(*sets[i], starts)
         torch.cuda.synchronize()
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 70), (False, 200)])
+@pytest.mark.parametrize("lq,lk", [([1], [1]), ([257, 128, 0, 129], [257, 128, 0, 129]), ([700], [900]), ([300, 40], [100, 290]), ([513], [513])])
+def test_heads_that_do_not_pair(lq, lk, causal, window, dim):
+    """An odd number of query heads a key head: a unit of work is 256 rows of one head."""
+    case(lq, lk, 3, 1, dim, causal, window)
+    case(lq, lk, 2, 2, dim, causal, window)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_hidden_values_where_heads_do_not_pair(bad):
+    lengths = [300, 140]
+    q, k, v = inputs(440, 440, 3, 3, 64)
+    v[260], v[410] = bad, bad
+    y = nq.nq_prompt_attention(q, k, v, starts_of(lengths))
+    nq.nq_device_status()
+    clean = v.clone()
+    clean[260], clean[410] = 0.0, 0.0
+    want, bound = definition(q, k, clean, lengths, lengths, True, 0, 0.125)
+    for rows in (slice(0, 260), slice(300, 410)):
+        check(y[rows], want[rows], bound[rows])
+    assert not torch.isfinite(y[260:300]).all(-1).any() and not torch.isfinite(y[410:]).all(-1).any()
