@@ -85,7 +85,7 @@ __device__ __forceinline__ uint32_t i8x4(uint64_t ab, uint64_t cd) {
 // p + rotary / 16 of the rotated part, and of the rest (`free` lanes of it) chunk p + rotary / 16 and the one (D - rotary) / 16 on.
 // So a pair of values never leaves its lane, for either order of pairs, and D / 16 lanes are a head.  A token's angles stay in
 // registers for all the heads that a warp takes; heads are dealt to 32 / (D / 16) lane groups in turn.
-// Four turns (two in fp32) are on their way to a warp at any time.  16384 tokens of 32 + 8 heads of 128 73 us (0.72 of the copy rate), 96 into
+// Four turns (two in fp32) are on their way to a warp at any time.  16384 tokens of 32 + 8 heads of 128 67 us (0.78 of the copy rate), 88 into
 // an e4m3 cache; 87 with a head's kind looked up lane by lane, all loads waited for together and scalar products.  Bound by the latency
 // of the loads and by issue in about equal parts (16 warps of 128 registers); for few tokens a token is cut into `parts` warps, so that a
 // turn or two of loads is all a warp does (3 tokens 3 us).
