@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ
     constexpr int kSub = step_tokens(D, CACHE) / 16, kTokens = 16 * kSub;
     constexpr int kSlot = kSlotFloats<D, NT>;
     extern __shared__ __align__(16) float s_parts[];                 // [2 * kWarps][kSlot]
-    __shared__ long long s_before[kThreads + 1];
+    __shared__ __align__(16) long long s_before[kThreads + 1];
     __shared__ long long s_warp[kWarps];
     __shared__ float s_factor[2 * kWarps][8 * NT], s_total[8 * NT];
     __shared__ int4 s_meta[2 * kWarps];                              // of each part: sequence (-1: none), unit, whether it holds the first (1) and the last (2) step
@@ -199,12 +199,11 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ
     if (left > 0) {
         Place<kTokens> at;
         {
-            const long long step = divide(from, units);                     // sequences' steps before `at` are no more than this
-            int lo = 0, hi = kThreads;
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (s_before[mid] <= step) lo = mid; else hi = mid;
-            }
+            // the last chunk that starts at or before `from`
+            int lo = 0;
+#pragma unroll
+            for (int x = 0; x < kThreads / 32; ++x) lo += s_before[kThreads / 32 * lane + x] * units <= from;
+            lo = __reduce_add_sync(0xffffffffu, lo) - 1;
             long long rest = from - s_before[lo] * units;
             at.seq = lo * chunk;
             at.steps = steps_of<kTokens>(a, at.seq, at.length, at.first);
@@ -214,7 +213,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ
             }
             const int unit = (int)divide(rest, at.steps);
             at.step = (int)(rest - (long long)unit * at.steps);
-            at.head = unit / a.head_blocks;
+            at.head = a.head_blocks == 1 ? unit : unit / a.head_blocks;
             at.block = unit - at.head * a.head_blocks;
         }
         const int per_page = a.c.page_size >> 4;
@@ -287,6 +286,11 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ
         float o[NT][kSteps][4], top[NT][2], weight[NT][2], largest = kTiny, unit_inv = 0.0f;     // the largest scale of a value so far, and its inverse
         int begun = 0;
 
+        {
+            // the first queries on their way while the table is asked
+            const char* src = reinterpret_cast<const char*>(a.q + at.seq * a.ldq + (long long)(at.head * a.group + at.block * 8 * NT) * D) + 128 * lane;
+            if (128 * lane < 2 * D * min(8 * NT, a.group - at.block * 8 * NT)) asm volatile("prefetch.global.L1 [%0];" ::"l"(src));
+        }
         find_rows(at);
         load_k();
         load_v();
@@ -596,40 +600,42 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ
 
     // ---- the block's parts: neighbours of one sequence and head are joined; all of it: out; otherwise to the block's slots
     int4 record = make_int4(-1, 0, 0, 0);
-    for (int p = 0; p < 2 * kWarps;) {
-        const int4 first = s_meta[p];
-        if (first.x < 0) {
-            ++p;
-            continue;
-        }
-        int last = p, ends = first.z & 2, rest = first.w;
-        for (int x = p + 1; x < 2 * kWarps; ++x) {
-            const int4 m = s_meta[x];
-            if (m.x < 0) continue;
-            if (m.x != first.x || m.y != first.y) break;
-            last = x;
-            ends |= m.z & 2;
-            rest = m.w;
-        }
+    const int4 meta = lane < 2 * kWarps ? s_meta[lane] : make_int4(-1, 0, 0, 0);
+    const auto of = [](int v, int from) { return __shfl_sync(0xffffffffu, v, from); };
+    for (unsigned parts = __ballot_sync(0xffffffffu, meta.x >= 0); parts;) {
+        const int p = __ffs(parts) - 1;
+        const int4 first = make_int4(of(meta.x, p), of(meta.y, p), of(meta.z, p), 0);
+        const unsigned these = __ballot_sync(0xffffffffu, meta.x == first.x && meta.y == first.y);
+        const int rest = of(meta.w, 31 - __clz(these));
+        const bool ends = __any_sync(0xffffffffu, (these >> lane & 1u) && (meta.z & 2));
+        parts &= ~these;
         const bool begins = first.z & 1;
-        const int block = first.y % a.head_blocks, kv_head = first.y / a.head_blocks;
+        const int kv_head = a.head_blocks == 1 ? first.y : first.y / a.head_blocks, block = first.y - kv_head * a.head_blocks;
         float* slot = a.slots + (2ll * blockIdx.x + (begins ? 1 : 0)) * kSlot;
-        if (threadIdx.x < 8 * NT) {                                  // what each part counts for, by column
-            const int column = threadIdx.x;
-            float m = -INFINITY, sum_w = 0.0f;
-            for (int x = p; x <= last; ++x)
-                if (s_meta[x].x >= 0) m = fmaxf(m, s_parts[x * kSlot + 8 * NT * D + column]);
-            for (int x = p; x <= last; ++x) {
-                if (s_meta[x].x < 0) continue;
-                const float t = s_parts[x * kSlot + 8 * NT * D + column], by = t == -INFINITY && m == -INFINITY ? 1.0f : exp2a(t - m);
-                s_factor[x][column] = by;
-                sum_w += by * s_parts[x * kSlot + 8 * NT * (D + 1) + column];
+        if (threadIdx.x < 8 * NT * 2 * kWarps) {                     // what each part counts for, by column: eight parts side by side
+            const int column = threadIdx.x / (2 * kWarps), x = threadIdx.x % (2 * kWarps);
+            const bool one = these >> x & 1u;
+            const float t = one ? s_parts[x * kSlot + 8 * NT * D + column] : -INFINITY;
+            float m = t;
+#pragma unroll
+            for (int y = 1; y < 2 * kWarps; y *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, y));
+            const float by = t == -INFINITY && m == -INFINITY ? 1.0f : exp2a(t - m);
+            float sum_w = one ? by * s_parts[x * kSlot + 8 * NT * (D + 1) + column] : 0.0f;
+#pragma unroll
+            for (int y = 1; y < 2 * kWarps; y *= 2) sum_w += __shfl_xor_sync(0xffffffffu, sum_w, y);
+            s_factor[x][column] = by;
+            if (x == 0) {
+                s_total[column] = sum_w;
+                if (!(begins && ends)) {
+                    slot[8 * NT * D + column] = m;
+                    slot[8 * NT * (D + 1) + column] = sum_w;
+                }
             }
-            s_total[column] = sum_w;
-            if (!(begins && ends)) {
-                slot[8 * NT * D + column] = m;
-                slot[8 * NT * (D + 1) + column] = sum_w;
-            }
+        }
+        if (threadIdx.x == kThreads - 1 && begins && !ends) {
+            // the last step of it is `rest` steps behind this block's end
+            const long long x = end - 1 + rest, large = more * (per + 1);
+            record = make_int4(first.x, first.y, (int)(x < large ? divide(x, per + 1) : more + divide(x - large, per)), 0);
         }
         __syncthreads();
         for (int e = threadIdx.x; e < 8 * NT * D / 4; e += kThreads) {
@@ -637,7 +643,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ
             float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
             for (int x = 0; x < 2 * kWarps; ++x) {
-                if (x < p || x > last || s_meta[x].x < 0) continue;
+                if (!(these >> x & 1u)) continue;
                 const float4 v = *reinterpret_cast<const float4*>(s_parts + x * kSlot + 4 * e);
                 const float by = s_factor[x][column];
                 sum.x += by * v.x; sum.y += by * v.y; sum.z += by * v.z; sum.w += by * v.w;
@@ -646,14 +652,8 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ
             else if (h < a.group) store_row4(a.y + first.x * a.ldy + (long long)(kv_head * a.group + h) * D + 4 * (e % (D / 4)), sum, s_total[column]);
         }
         __syncthreads();
-        if (begins && !ends) {
-            // the last step of it is `rest` steps behind this block's end
-            const long long x = end - 1 + rest, large = more * (per + 1);
-            record = make_int4(first.x, first.y, (int)(x < large ? divide(x, per + 1) : more + divide(x - large, per)), 0);
-        }
-        p = last + 1;
     }
-    if (threadIdx.x == 0) a.records[blockIdx.x] = record;
+    if (threadIdx.x == kThreads - 1) a.records[blockIdx.x] = record;
 }
 
 // A sequence and head that begins in block blockIdx.x and goes on in others: their parts joined, blockIdx.y: four columns of it.  What each
@@ -691,24 +691,51 @@ __global__ void __launch_bounds__(kJoin) join_kernel(const TokenArgs a) {
         }
         return v;
     };
-    float4 m = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY), sum_w = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int x = threadIdx.x; x < n; x += kJoin) {
-        const float4 t = *reinterpret_cast<const float4*>(part(x) + 8 * NT * D + column0);
+    const int column = threadIdx.x / (D / 4) % 4, piece = threadIdx.x % (D / 4), first = threadIdx.x / D;
+    // all that a thread needs at first, asked for at once: a part's maximum and weights, and its values of kEarly parts
+    constexpr int kEarly = 8;
+    const float4 none = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    const auto top_of = [&](int x) { return *reinterpret_cast<const float4*>(part(x) + 8 * NT * D + column0); };
+    const auto weight_of = [&](int x) { return *reinterpret_cast<const float4*>(part(x) + 8 * NT * (D + 1) + column0); };
+    const auto value_of = [&](int x) { return *reinterpret_cast<const float4*>(part(x) + (column0 + column) * D + 4 * piece); };
+    float4 m = none, sum_w = make_float4(0.0f, 0.0f, 0.0f, 0.0f), early[kEarly];
+    float early_top[kEarly];
+    if (threadIdx.x < n) {
+        m = top_of(threadIdx.x);
+        sum_w = weight_of(threadIdx.x);
+    }
+#pragma unroll
+    for (int e = 0; e < kEarly; ++e)
+        if (first + e * kAtOnce < n) {
+            early[e] = value_of(first + e * kAtOnce);
+            early_top[e] = part(first + e * kAtOnce)[8 * NT * D + column0 + column];
+        }
+    const float4 mine = m;
+    for (int x = threadIdx.x + kJoin; x < n; x += kJoin) {
+        const float4 t = top_of(x);
         m = make_float4(fmaxf(m.x, t.x), fmaxf(m.y, t.y), fmaxf(m.z, t.z), fmaxf(m.w, t.w));
     }
     m = over_block(m, true);
     const auto by = [](float t, float top) { return t == -INFINITY && top == -INFINITY ? 1.0f : exp2a(t - top); };
-    for (int x = threadIdx.x; x < n; x += kJoin) {
-        const float4 t = *reinterpret_cast<const float4*>(part(x) + 8 * NT * D + column0), w = *reinterpret_cast<const float4*>(part(x) + 8 * NT * (D + 1) + column0);
+    if (threadIdx.x < n) {
+        sum_w.x *= by(mine.x, m.x); sum_w.y *= by(mine.y, m.y); sum_w.z *= by(mine.z, m.z); sum_w.w *= by(mine.w, m.w);
+    }
+    for (int x = threadIdx.x + kJoin; x < n; x += kJoin) {
+        const float4 t = top_of(x), w = weight_of(x);
         sum_w.x += by(t.x, m.x) * w.x; sum_w.y += by(t.y, m.y) * w.y; sum_w.z += by(t.z, m.z) * w.z; sum_w.w += by(t.w, m.w) * w.w;
     }
     sum_w = over_block(sum_w, false);
-    const int column = threadIdx.x / (D / 4) % 4, piece = threadIdx.x % (D / 4), first = threadIdx.x / D;
     const float top = column == 0 ? m.x : column == 1 ? m.y : column == 2 ? m.z : m.w;
     float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int e = 0; e < kEarly; ++e)
+        if (first + e * kAtOnce < n) {
+            const float f = by(early_top[e], top);
+            sum.x += f * early[e].x; sum.y += f * early[e].y; sum.z += f * early[e].z; sum.w += f * early[e].w;
+        }
 #pragma unroll 8
-    for (int x = first; x < n; x += kAtOnce) {
-        const float4 v = *reinterpret_cast<const float4*>(part(x) + (column0 + column) * D + 4 * piece);
+    for (int x = first + kEarly * kAtOnce; x < n; x += kAtOnce) {
+        const float4 v = value_of(x);
         const float f = by(part(x)[8 * NT * D + column0 + column], top);
         sum.x += f * v.x; sum.y += f * v.y; sum.z += f * v.z; sum.w += f * v.w;
     }
