@@ -286,11 +286,6 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ
         float o[NT][kSteps][4], top[NT][2], weight[NT][2], largest = kTiny, unit_inv = 0.0f;     // the largest scale of a value so far, and its inverse
         int begun = 0;
 
-        {
-            // the first queries on their way while the table is asked
-            const char* src = reinterpret_cast<const char*>(a.q + at.seq * a.ldq + (long long)(at.head * a.group + at.block * 8 * NT) * D) + 128 * lane;
-            if (128 * lane < 2 * D * min(8 * NT, a.group - at.block * 8 * NT)) asm volatile("prefetch.global.L1 [%0];" ::"l"(src));
-        }
         find_rows(at);
         load_k();
         load_v();
