@@ -23,8 +23,9 @@ namespace {
 // The sequences' steps (of all kv heads) lie in one long row that is cut evenly over the warps of a full GPU, however the
 // lengths fall.  What a warp has of a sequence and head, if not all of it, is joined in its thread block, and over thread blocks by
 // a second kernel, in a fixed order.
-// Bound by HBM: 64 sequences of up to 8192 tokens, 32 / 8 heads of 128, bf16 196 us (0.95 of the copy rate), e4m3 125 (0.77); one of 131072 e4m3 tokens
-// 62 (0.68: some 15 us go to the cut, the first loads and the joins); one of 1501 INT8 tokens 15, all latency.
+// Bound by HBM: 64 sequences of up to 8192 tokens, 32 / 8 heads of 128, bf16 193 us (0.97 of the copy rate), e4m3 120 (0.80); one of 131072 e4m3 tokens
+// 58 (0.72: some 11 us go to the cut, the first loads and the joins); one of 1501 INT8 tokens 10.5, all latency (15 with a search for the
+// place, a block's parts weighed one after the other, and a join that asked for maxima, weights and values in turn).
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr float kRescale = 8.0f;         // the running maximum moves when a score passes it by 2^8 (fp32 sums have room)
 // f16 weights are held times 2^7: at most 2^15 (a weight is at most 2^8), normal down to 2^-21 of the one at the maximum.
