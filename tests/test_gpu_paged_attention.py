@@ -233,3 +233,11 @@ def test_calls_one_behind_another_share_nothing(kind):
     torch.cuda.synchronize()
     for i, y in zip((0, 1, 2, 3, 1, 0), got):
         assert torch.equal(y, want[i])
+
+
+@pytest.mark.parametrize("kind", [BF16, F8, I8])
+@pytest.mark.parametrize("lengths,group,dim,window", [([40007], 4, 128, 0), ([40007, 60], 16, 64, 0), ([9001, 1, 700], 40, 128, 0), ([50000], 3, 128, 39001)])
+def test_one_head_is_split_over_all_thread_blocks(lengths, group, dim, window, kind):
+    """More parts of a head than the joining kernel has threads; a group of several blocks of heads."""
+    q, cache, table, n, y = case(lengths, group, 1, dim, 16, kind, window=window)
+    assert torch.equal(y, nq.nq_paged_attention(q, nq.nq_kv_pages(*cache), table, n, window=window))
