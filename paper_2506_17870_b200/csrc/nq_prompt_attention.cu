@@ -7,6 +7,7 @@
 #include "../../include/nq.h"
 #include "nq_fp8.cuh"
 #include "nq_internal.cuh"
+#include "nq_ranges.cuh"
 #include "nq_sm100.cuh"
 #include "nq_sm100_bf16.cuh"
 
@@ -93,9 +94,9 @@ __device__ __forceinline__ void unit_of(const PromptArgs& a, const int* before, 
         const int a0 = u.row[t], b0 = min(a0 + kTile, u.lq);                       // rows [a0, b0)
         u.lo[t] = u.hi[t] = u.all_lo[t] = u.all_hi[t] = 0;
         if (a0 >= b0) continue;
-        const int seen_hi = a.causal ? min(u.lk, b0 + off) : u.lk, seen_lo = a.window ? max(0, a0 + off + 1 - a.window) : 0;
+        const int seen_hi = a.causal ? min(u.lk, b0 + off) : u.lk, seen_lo = window_start(a.window, a0 + off + 1);
         u.all_hi[t] = a.causal ? min(u.lk, a0 + off + 1) : u.lk;
-        u.all_lo[t] = a.window ? max(0, b0 + off - a.window) : 0;
+        u.all_lo[t] = window_start(a.window, b0 + off);
         if (seen_hi > seen_lo) {
             u.lo[t] = seen_lo / kKeys;
             u.hi[t] = (seen_hi + kKeys - 1) / kKeys;
@@ -469,8 +470,8 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             const int row = u->row[t] + quarter * 32 + lane;
             // of the keys, this row sees no more than the first `reach`, and of those the last `window`; rows behind the last one must not
             // get in the way
-            const int reach = min(row, u->lq - 1) + u->lk - u->lq + 1;
-            const int see_hi = a.causal ? min(u->lk, reach) : u->lk, see_lo = a.window ? max(0, reach - a.window) : 0;
+            const int reach = u->lk - (u->lq - 1 - min(row, u->lq - 1));
+            const int see_hi = a.causal ? min(u->lk, reach) : u->lk, see_lo = window_start(a.window, reach);
             const uint32_t it0 = it - u->begin;                    // steps before step 0
             it += u->end - u->begin;
             float top = -INFINITY, total = 0.0f;
