@@ -966,6 +966,13 @@ def _heads(t: torch.Tensor, name: str, index: int, heads: int, dim: int) -> int:
     return heads * dim
 
 
+def _window(window: int) -> int:
+    """A window as the library's int holds it: what passes 32 bits would arrive as another number."""
+    if not -(1 << 31) <= window < 1 << 31:
+        raise ValueError(f"window must be under 2^31, got {window}")
+    return window
+
+
 def _table(t: torch.Tensor, seqs: int, index: int) -> int:
     if t.dtype is torch.int32 and t.is_contiguous() and t.dim() == 2 and t.shape[0] == seqs and t.get_device() == index >= 0:
         return t.shape[1] or 1
@@ -1088,7 +1095,7 @@ def nq_paged_attention(q: torch.Tensor, cache: nq_kv_pages, table: torch.Tensor,
             raise ValueError("workspace must be contiguous")
         _on(workspace, "workspace", index)
     _check(lib().nq_paged_attention(pages, q.data_ptr(), ldq, heads, table.data_ptr(), ld_table, cols, _ints(lengths, "lengths", seqs, index), seqs,
-                                    window, dim ** -0.5 if scale is None else scale, y_out.data_ptr(), ldy, workspace.data_ptr(),
+                                    _window(window), dim ** -0.5 if scale is None else scale, y_out.data_ptr(), ldy, workspace.data_ptr(),
                                     workspace.numel() * workspace.element_size(), _raw_stream(q)), "nq_paged_attention")
     return y_out
 
@@ -1119,7 +1126,7 @@ def nq_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, start
         if y_out.dtype is not torch.bfloat16 or y_out.shape != q.shape:
             raise ValueError(f"y_out must be bfloat16 {list(q.shape)}, got {y_out.dtype} {list(y_out.shape)}")
         ldy = _heads(y_out, "y_out", index, heads, dim)
-    d = nq_prompt_desc(seqs, rows, k.shape[0], ldq, ldk, ldv, ldy, heads, kv_heads, dim, causal, window, dim ** -0.5 if scale is None else scale)
+    d = nq_prompt_desc(seqs, rows, k.shape[0], ldq, ldk, ldv, ldy, heads, kv_heads, dim, causal, _window(window), dim ** -0.5 if scale is None else scale)
     _check(lib().nq_prompt_attention(ctypes.addressof(d), q.data_ptr(), k.data_ptr(), v.data_ptr(), _ints(starts_q, "starts_q", seqs + 1, index),
                                      _ints(starts_k, "starts_k", seqs + 1, index), y_out.data_ptr(), _raw_stream(q)), "nq_prompt_attention")
     return y_out
