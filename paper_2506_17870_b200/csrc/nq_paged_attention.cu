@@ -8,6 +8,7 @@
 
 #include "../../include/nq.h"
 #include "nq_kv_cache.cuh"
+#include "nq_ranges.cuh"
 
 namespace nq {
 namespace {
@@ -234,7 +235,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ
                 pages_from = number;
                 const int n = number + lane;
                 my_row = -1;
-                if (n * 16 < p.length) {
+                if (group_in(n, p.length)) {
                     const int nth = n / per_page, page = a.table[p.seq * a.ld_table + nth];
                     if (page >= 0 && page < a.c.pages) my_row = page * page_rows + (n - nth * per_page) * 16;
                 }
@@ -396,7 +397,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ
             // ---- masks: only a sequence's first and last steps have any
             const int length = cur.length, token0 = (cur.first + cur.step) * kTokens;
             const int lo = a.window > 0 ? length - a.window : 0;
-            bool edge = token0 + kTokens > length || token0 < lo;
+            bool edge = length - token0 < kTokens || token0 < lo;       // (token0 + kTokens may pass 32 bits)
 #pragma unroll
             for (int u = 0; u < kSub; ++u) edge |= !there[u];
             bool seen[kSub][2];

@@ -14,4 +14,8 @@ namespace nq {
 // queries where a sequence has fewer keys than those, and a window may be 2^31 - 1: their difference is taken only where it is positive.
 NQ_BOTH int window_start(int window, int reach) { return window > 0 && reach > window ? reach - window : 0; }
 
+// Whether group `n` of 16 tokens has any of a sequence's `length`, for groups that may lie behind all that a table can name (whose
+// first token's number, 16 n, does not fit 32 bits).
+NQ_BOTH bool group_in(int n, int length) { return length > 0 && n <= (length - 1) >> 4; }
+
 }  // namespace nq

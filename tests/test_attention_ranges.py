@@ -16,6 +16,7 @@ def ranges(tmp_path_factory):
     source.write_text(f'''#include "{HEADER}"
 extern "C" {{
 int window_start(int window, int reach) {{ return nq::window_start(window, reach); }}
+int group_in(int n, int length) {{ return nq::group_in(n, length); }}
 }}
 ''')
     subprocess.run(["g++", "-O2", "-ftrapv", "-shared", "-fPIC", "-o", str(library), str(source)], check=True)
@@ -26,3 +27,19 @@ int window_start(int window, int reach) {{ return nq::window_start(window, reach
 def test_window_start(ranges, window):
     for reach in (-MOST + 4096, -200, -1, 0, 1, 99, 100, 101, MOST - 4096, MOST):
         assert ranges.window_start(window, reach) == (max(0, reach - window) if window else 0)
+
+
+@pytest.mark.parametrize("page", [16, 32, 48, 64, 128, 256, 512])
+@pytest.mark.parametrize("tokens", [16, 32])
+def test_no_page_is_asked_for_behind_the_table(ranges, page, tokens):
+    """A warp of the single-token kernel asks for the pages of 32 groups of 16 tokens, from the one that its step starts at.  In the largest table
+    that is accepted, the last sequence's last steps ask for none behind its columns, and for all that there are."""
+    columns = MOST // page
+    for length in (columns * page, columns * page - 1, columns * page - 17, 33):
+        last = (length - 1) // 16
+        for first in range(max(0, last - 40) // (tokens // 16) * (tokens // 16), last + 1, tokens // 16):
+            for n in range(first, first + 32):
+                asked = bool(ranges.group_in(n, length))
+                assert asked == (16 * n < length)
+                assert not asked or n // (page // 16) < columns
+    assert not ranges.group_in(0, 0) and not ranges.group_in(0, -5) and ranges.group_in(0, 1)
