@@ -257,9 +257,10 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     // The grid has a block for each unit that there can be; a block that is done with its own takes one that has not begun (it
     // cancels that block's launch), so that all SMs end together however the units differ.  Warp 0 does this, one unit ahead of the
     // tensor core, and hands what it has worked out to the others.
-    // The n-th unit of this block, for a whole warp until it gives it back; null: no more of them, or given up.
-    const auto take = [&](uint32_t n) -> const Unit* {
-        const bool ok = mbar_wait(u_full + 8 * (n & 1), (n >> 1) & 1, abort_flag, a.status, 0x301u);
+    // The n-th unit of this block, for a whole warp until it gives it back; null: no more of them, or given up.  `idle`: steps of the unit before
+    // that this warp had no part in.
+    const auto take = [&](uint32_t n, int idle) -> const Unit* {
+        const bool ok = mbar_wait(u_full + 8 * (n & 1), (n >> 1) & 1, abort_flag, a.status, 0x301u, wait_limit(kWaitLimitCycles, idle));
         return __all_sync(0xffffffffu, ok) && s_unit[n & 1].lq > 0 ? &s_unit[n & 1] : nullptr;
     };
     const auto give_back = [&](uint32_t n) {
@@ -358,7 +359,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             uint32_t it = 0, used = 0, weights = 0;                // steps, units with any, a phase bit for each buffer
             bool ok = true;
             for (uint32_t n = 0; ok; ++n) {
-                const Unit* u = take(n);
+                const Unit* u = take(n, 0);
                 if (!u) break;
                 const int first = same(u->begin), last = same(u->end), lo = same(u->lo[t]), hi = same(u->hi[t]), all_lo = same(u->all_lo[t]), all_hi = same(u->all_hi[t]);
                 give_back(n);
@@ -414,7 +415,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             uint32_t it = 0;
             bool ok = true;
             for (uint32_t n = 0; ok; ++n) {
-                const Unit* u = take(n);
+                const Unit* u = take(n, 0);
                 if (!u) break;
                 for (int j = u->begin; j < u->end; ++j, ++it) {
                     const uint32_t s = it % ST;
@@ -463,9 +464,13 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         const auto sums_of = [&](int j) {
             return mbar_wait(o_full + 16 * t + 8 * (j & 1), ((phases >> (j & 1)) & 1) ^ 1, abort_flag, a.status, 0x342u);
         };
+        // A tile without rows (the second one of a head's last rows) is done at once, and its warps wait for the next unit as long as the
+        // other tile has steps: with 10^8 keys that is longer than a step's limit.
+        int idle = 0;
         for (uint32_t n = 0; ok; ++n, give_back(n - 1)) {
-            const Unit* u = take(n);
+            const Unit* u = take(n, idle);
             if (!u) break;
+            idle = u->end - u->begin - (u->hi[t] - u->lo[t]);
             const int lo_t = u->lo[t], hi_t = u->hi[t], all_lo = u->all_lo[t], all_hi = u->all_hi[t];
             const int row = u->row[t] + quarter * 32 + lane;
             // of the keys, this row sees no more than the first `reach`, and of those the last `window`; rows behind the last one must not

@@ -18,4 +18,8 @@ NQ_BOTH int window_start(int window, int reach) { return window > 0 && reach > w
 // first token's number, 16 n, does not fit 32 bits).
 NQ_BOTH bool group_in(int n, int length) { return length > 0 && n <= (length - 1) >> 4; }
 
+// How long (SM cycles) to wait for something that comes only when another role is through with `steps` steps of its own, where one step's limit
+// is `one`: 2^14 cycles for each beside it, ten times what a step of the prompt kernel takes (some 1650).
+NQ_BOTH long long wait_limit(long long one, int steps) { return steps > 0 ? one + ((long long)steps << 14) : one; }
+
 }  // namespace nq

@@ -62,14 +62,14 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
 
 // Bounded wait.  Returns false when the wait gave up: either its own limit expired (then the
 // status word gets `code`, first writer wins, and the block-wide abort flag is raised) or another
-// role of the block raised the abort flag.
+// role of the block raised the abort flag.  (`limit`: for who has to wait for more than a step of another role's.)
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag,
-                                          unsigned int* status, unsigned int code) {
+                                          unsigned int* status, unsigned int code, long long limit = kWaitLimitCycles) {
     if (mbar_try_wait(bar, parity)) return true;
     const long long t0 = clock64();
     while (!mbar_try_wait(bar, parity)) {
         if (*abort_flag) return false;
-        if (clock64() - t0 > kWaitLimitCycles) {
+        if (clock64() - t0 > limit) {
             *abort_flag = 1;
             if (atomicCAS(status, 0u, code) == 0u) status[1] = blockIdx.x;
             return false;

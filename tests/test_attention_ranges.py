@@ -17,10 +17,13 @@ def ranges(tmp_path_factory):
 extern "C" {{
 int window_start(int window, int reach) {{ return nq::window_start(window, reach); }}
 int group_in(int n, int length) {{ return nq::group_in(n, length); }}
+long long wait_limit(long long one, int steps) {{ return nq::wait_limit(one, steps); }}
 }}
 ''')
     subprocess.run(["g++", "-O2", "-ftrapv", "-shared", "-fPIC", "-o", str(library), str(source)], check=True)
-    return ctypes.CDLL(str(library))
+    loaded = ctypes.CDLL(str(library))
+    loaded.wait_limit.restype, loaded.wait_limit.argtypes = ctypes.c_longlong, (ctypes.c_longlong, ctypes.c_int)
+    return loaded
 
 
 @pytest.mark.parametrize("window", [0, 1, 100, MOST - 200, MOST - 1, MOST])
@@ -43,3 +46,13 @@ def test_no_page_is_asked_for_behind_the_table(ranges, page, tokens):
                 assert asked == (16 * n < length)
                 assert not asked or n // (page // 16) < columns
     assert not ranges.group_in(0, 0) and not ranges.group_in(0, -5) and ranges.group_in(0, 1)
+
+
+def test_a_wait_for_many_steps_outlasts_them(ranges):
+    """The tile without rows of a unit waits for the other's steps: 64 keys each, some 1650 cycles."""
+    one = 2 ** 31
+    for keys in (0, 64, 10 ** 6, 10 ** 8, MOST - 4096):
+        steps = -(-keys // 64)
+        assert ranges.wait_limit(one, steps) >= one // 2 + 5 * 1650 * steps
+    assert ranges.wait_limit(one, 0) == ranges.wait_limit(one, -3) == one
+    assert ranges.wait_limit(one, 8) < one + one // 1000                 # what is stuck is still given up after about a second
