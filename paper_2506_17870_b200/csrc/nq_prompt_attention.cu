@@ -470,7 +470,6 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         for (uint32_t n = 0; ok; ++n, give_back(n - 1)) {
             const Unit* u = take(n, idle);
             if (!u) break;
-            idle = u->end - u->begin - (u->hi[t] - u->lo[t]);
             const int lo_t = u->lo[t], hi_t = u->hi[t], all_lo = u->all_lo[t], all_hi = u->all_hi[t];
             const int row = u->row[t] + quarter * 32 + lane;
             // of the keys, this row sees no more than the first `reach`, and of those the last `window`; rows behind the last one must not
@@ -599,7 +598,11 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 if (lane == 0) mbar_arrive(p_full + 16 * t + 8 * (j & 1));
             }
             if (!ok) break;
-            if (u->row[t] >= u->lq) continue;             // the whole tile
+            if (u->row[t] >= u->lq) {                     // the whole tile
+                idle = u->end - u->begin;
+                continue;
+            }
+            idle = 0;
             const bool any = hi_t > lo_t;
             if (any) {
                 ok = sums_of(hi_t - 1);
