@@ -496,7 +496,8 @@ NQ_API int nq_kv_cache_read(const nq_kv_pages *cache, const int32_t *table, int6
  *   table (device) int32 [seqs, table_cols], lengths (device) int32 [seqs]
  *   Sums, maxima and weights are fp32.  A weight is rounded to bf16 (bf16 cache) or f16 (8-bit caches, times the value's scale)
  *   for its product with the values, which is exact in both; queries meet 8-bit keys as f16, scaled by a power of two.  As f16, a
- *   weight is good to 2^-11 of itself down to 2^-21 of the largest, and under 2^-32 of it is lost.
+ *   weight times its value's scale is good to 2^-11 of itself down to 2^-21 of the largest such product of its sequence and head, and under
+ *   2^-32 of that is lost.
  *   workspace (device) nq_paged_attention_workspace_bytes() bytes, 16-byte aligned: parts of sequences that several thread blocks
  *   share.  Two calls that may run at the same time need two.  No atomics: results repeat bit for bit.
  */

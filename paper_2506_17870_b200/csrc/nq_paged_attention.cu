@@ -29,8 +29,15 @@ namespace {
 // place, a block's parts weighed one after the other, and a join that asked for maxima, weights and values in turn).
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr float kRescale = 8.0f;         // the running maximum moves when a score passes it by 2^8 (fp32 sums have room)
-// f16 weights are held times 2^7: at most 2^15 (a weight is at most 2^8), normal down to 2^-21 of the one at the maximum.
-constexpr float kTiny = 1.17549435e-38f;
+// 8-bit caches: what is rounded to f16 is a weight times its value's scale, times a power of two of the column's own (`held`): the largest such
+// product so far is 2^7 to 2^8 when that power is set and may rise to 2^15 before it is set anew, so f16 is normal down to 2^-21 of it, and what is
+// lost is under 2^-32 of it.  (In units of the largest scale, whatever its weight, one token of a large value and no weight took the bits of
+// all others.)  When the running maximum moves, by 2^8 or more, the power moves against it, and the sums grow by 2 at most.  It is at most
+// 2^125, so that its inverse is a normal number (products under 2^-118 are then held to 2^-150), and weights are at most 1 (2^-8 for the one that
+// moved the maximum), so that no scale takes a product past fp32.  (One sequence of 131072 e4m3 tokens 58.1 us, in units of the largest scale 57.5; 64
+// of up to 8192 120 - 128 against 131.)
+constexpr float kLift = 8.0f, kMostHeld = 32768.0f;
+constexpr int kHeld = 7, kMostPower = 125;
 
 // Tokens of a step: as many as bring 8 KB (4 KB of 8-bit heads of 64) to a warp.  Two groups of 16 at once also halve what a step costs
 // beside its products (e4m3, 131072 tokens of 8 heads of 128, 16 at once: 79 us).
@@ -61,6 +68,9 @@ __device__ __forceinline__ float exp2a(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// of a positive normal number: the exponent of the power of two at or below it; and back
+__device__ __forceinline__ int log2_of(float x) { return (__float_as_int(x) >> 23) - 127; }
+__device__ __forceinline__ float power_of_two(int e) { return __int_as_float((e + 127) << 23); }
 __device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t s) {
     uint32_t r;
     asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(s));
@@ -285,7 +295,8 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ
 
         uint32_t qf[NT][kSteps][2];
         float q_scale[NT][2];                                        // of heads 2 j, 2 j + 1: what a product of codes is multiplied by
-        float o[NT][kSteps][4], top[NT][2], weight[NT][2], largest = kTiny, unit_inv = 0.0f;     // the largest scale of a value so far, and its inverse
+        float o[NT][kSteps][4], top[NT][2], weight[NT][2];
+        float held[NT][2];                                           // of heads 2 j, 2 j + 1: what a weight times its value's scale is multiplied by
         int begun = 0;
 
         find_rows(at);
@@ -301,8 +312,6 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ
             if (fresh) {                                             // another sequence or head
                 fresh = false;
                 begun = cur.step == 0;
-                largest = kTiny;
-                unit_inv = 1.0f / kTiny;
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     const int h = (block * NT + n) * 8 + i;
@@ -310,6 +319,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ
                     const __nv_bfloat16* src = a.q + cur.seq * a.ldq + (long long)(kv_head * a.group + (live ? h : 0)) * D;
                     top[n][0] = top[n][1] = -INFINITY;
                     weight[n][0] = weight[n][1] = 0.0f;
+                    held[n][0] = held[n][1] = 1.0f;
 #pragma unroll
                     for (int s = 0; s < kSteps; ++s) o[n][s][0] = o[n][s][1] = o[n][s][2] = o[n][s][3] = 0.0f;
                     if (!kCodes) {
@@ -385,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     kscale[u][t] = kCodes ? ks[u][t] + (ks[u][t] - ks[u][t]) : 1.0f;                 // an infinite scale's values are no numbers
-                    vscale[u][t] = kCodes ? vs[u][t] : 1.0f;
+                    vscale[u][t] = kCodes ? vs[u][t] + (vs[u][t] - vs[u][t]) : 1.0f;
                 }
             --left;
             at.next(a);
@@ -435,23 +445,9 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ
                         if (kCodes) s *= kscale[u][e >> 1];
                         s = seen[u][e >> 1] ? s : -INFINITY;
                         sc[u][n][e] = s;
-                        move |= s > top[n][e & 1] + kRescale;
+                        move |= s > top[n][e & 1] + (kCodes ? 0.0f : kRescale);
                     }
-            if (kCodes)
-#pragma unroll
-                for (int u = 0; u < kSub; ++u) move |= fabsf(vscale[u][0]) > largest || fabsf(vscale[u][1]) > largest;
             if (__any_sync(0xffffffffu, move)) {
-                float shrink = 1.0f;
-                if (kCodes) {
-                    float m = largest;
-#pragma unroll
-                    for (int u = 0; u < kSub; ++u) m = fmaxf(m, fmaxf(fabsf(vscale[u][0]), fabsf(vscale[u][1])));
-#pragma unroll
-                    for (int x = 4; x < 32; x *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-                    shrink = largest / m;
-                    largest = m;
-                    unit_inv = 1.0f / m;
-                }
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     float by[2];
@@ -462,10 +458,52 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ
                         for (int u = 0; u < kSub; ++u) m = fmaxf(m, fmaxf(sc[u][n][c], sc[u][n][2 + c]));
 #pragma unroll
                         for (int x = 4; x < 32; x *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-                        by[c] = top[n][c] == -INFINITY ? 0.0f : exp2a(top[n][c] - m);
+                        if (kCodes) m = m > top[n][c] ? m + kLift : m;
+                        const float d = top[n][c] == -INFINITY ? -INFINITY : top[n][c] - m;
+                        by[c] = exp2a(d);
                         top[n][c] = m;
                         weight[n][c] *= by[c];
-                        by[c] *= shrink;
+                        if (kCodes) {
+                            const float up = fminf(ceilf(-d), (float)(kMostPower - log2_of(held[n][c])));
+                            by[c] = exp2a(d + up);
+                            held[n][c] = power_of_two(log2_of(held[n][c]) + (int)up);
+                        }
+                    }
+#pragma unroll
+                    for (int s = 0; s < kSteps; ++s) {
+                        o[n][s][0] *= by[0]; o[n][s][1] *= by[1]; o[n][s][2] *= by[0]; o[n][s][3] *= by[1];
+                    }
+                }
+            }
+            bool grow = false;
+#pragma unroll
+            for (int u = 0; u < kSub; ++u)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float m = top[n][e & 1], p = exp2a(sc[u][n][e] - (m == -INFINITY ? 0.0f : m));
+                        weight[n][e & 1] += p;
+                        sc[u][n][e] = kCodes ? p * vscale[u][e >> 1] : p;
+                        if (kCodes) grow |= fabsf(sc[u][n][e]) * held[n][e & 1] > kMostHeld;
+                    }
+            if (kCodes && __any_sync(0xffffffffu, grow)) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    float by[2];
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        float m = 0.0f;
+#pragma unroll
+                        for (int u = 0; u < kSub; ++u) m = fmaxf(m, fmaxf(fabsf(sc[u][n][c]), fabsf(sc[u][n][2 + c])));
+#pragma unroll
+                        for (int x = 4; x < 32; x *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+                        by[c] = 1.0f;
+                        if (m * held[n][c] > kMostHeld) {
+                            const int old = log2_of(held[n][c]), now = kHeld - log2_of(m);
+                            by[c] = exp2a((float)(now - old));
+                            held[n][c] = power_of_two(now);
+                        }
                     }
 #pragma unroll
                     for (int s = 0; s < kSteps; ++s) {
@@ -475,23 +513,12 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ
             }
             uint32_t pf[kSub][NT][2];
 #pragma unroll
-            for (int u = 0; u < kSub; ++u) {
-                if (kCodes) {
-                    vscale[u][0] = vscale[u][0] * unit_inv * 128.0f;
-                    vscale[u][1] = vscale[u][1] * unit_inv * 128.0f;
-                }
+            for (int u = 0; u < kSub; ++u)
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    float p[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float m = top[n][e & 1];
-                        p[e] = exp2a(sc[u][n][e] - (m == -INFINITY ? 0.0f : m));
-                        weight[n][e & 1] += p[e];
-                        if (kCodes) p[e] *= vscale[u][e >> 1];
-                    }
+                    const float (&p)[4] = sc[u][n];
                     if (kCodes) {
-                        const __half2 x = __floats2half2_rn(p[0], p[1]), y = __floats2half2_rn(p[2], p[3]);
+                        const __half2 x = __floats2half2_rn(p[0] * held[n][0], p[1] * held[n][1]), y = __floats2half2_rn(p[2] * held[n][0], p[3] * held[n][1]);
                         pf[u][n][0] = transpose8x8(*reinterpret_cast<const uint32_t*>(&x));
                         pf[u][n][1] = transpose8x8(*reinterpret_cast<const uint32_t*>(&y));
                     } else {
@@ -501,7 +528,6 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ
                         pf[u][n][1] = transpose8x8(*reinterpret_cast<const uint32_t*>(&y));
                     }
                 }
-            }
             // ---- values
 #pragma unroll
             for (int u = 0; u < kSub; ++u) {
@@ -538,7 +564,6 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ
             if (closes) {
                 fresh = true;
                 const int ended = cur.step + 1 == cur.steps;
-                const float unit = kCodes ? largest * (1.0f / 128.0f) : 1.0f;
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -552,14 +577,16 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         const int column = n * 8 + 2 * j + c, h = block * NT * 8 + column;
-                        const float by = begun && ended ? (weight[n][c] > 0.0f || weight[n][c] != weight[n][c] ? unit / weight[n][c] : 0.0f) : unit;
+                        // (the two factors one after the other: their product can be too small a number)
+                        const float by = begun && ended ? (weight[n][c] > 0.0f || weight[n][c] != weight[n][c] ? 1.0f / weight[n][c] : 0.0f) : 1.0f;
+                        const float back = kCodes ? power_of_two(-log2_of(held[n][c])) : 1.0f;
                         constexpr int kRuns = !kCodes && kVPieces == 2 ? 2 : 1, kRun = D / 8 / kRuns;
 #pragma unroll
                         for (int r = 0; r < kRuns; ++r) {
                             const int channel = kRun * (i + 8 * r);
                             float v[kRun];
 #pragma unroll
-                            for (int x = 0; x < kRun; ++x) v[x] = by * (kRuns == 2 ? o[n][x % kSteps][2 * r + c] : o[n][x / 2][2 * (x & 1) + c]);
+                            for (int x = 0; x < kRun; ++x) v[x] = by == 0.0f ? 0.0f : by * (kRuns == 2 ? o[n][x % kSteps][2 * r + c] : o[n][x / 2][2 * (x & 1) + c]) * back;
                             if (begun && ended) {
                                 if (h < a.group) {
                                     __nv_bfloat16* to = a.y + cur.seq * a.ldy + (long long)(kv_head * a.group + h) * D + channel;
