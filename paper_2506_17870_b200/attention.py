@@ -35,16 +35,19 @@ class Batch(NamedTuple):
     rows_all: int
     single: bool                       # one new token each
     fresh: bool                        # nobody has earlier tokens
+    longest: int = 0                   # tokens of the longest sequence, the new ones included
 
 
 class PageTable:
     """Which pages of a cache (or of the caches of several layers) each sequence holds.  Kept on the host; extend() hands out what a
-    pass over new tokens needs on the device."""
+    pass over new tokens needs on the device.  positions: how many tokens a sequence may have (None: as many as there are pages for)."""
 
-    def __init__(self, pages: int, page_size: int, device="cuda"):
+    def __init__(self, pages: int, page_size: int, device="cuda", positions: Optional[int] = None):
         if pages < 0 or page_size < 1:
             raise ValueError(f"{pages} pages of {page_size} tokens")
-        self.page_size, self.device = page_size, device
+        if positions is not None and positions < 0:
+            raise ValueError(f"{positions} positions")
+        self.page_size, self.device, self.positions = page_size, device, positions
         self._free = list(range(pages - 1, -1, -1))
         self._held: dict = {}                                  # sequence -> its pages
         self._length: dict = {}
@@ -69,12 +72,15 @@ class PageTable:
         del self._length[sequence]
 
     def extend(self, sequences: Sequence[int], counts: Sequence[int]) -> Batch:
-        """Room for counts[i] new tokens of each sequence.  Raises before anything changes when there are not enough pages."""
+        """Room for counts[i] new tokens of each sequence.  Raises before anything changes when there are not enough pages or positions."""
         if len(sequences) != len(counts) or len(set(sequences)) != len(sequences):
             raise ValueError("one count for each sequence, and each sequence once")
         if any(c < 0 for c in counts):
             raise ValueError("counts must not be negative")
         ps = self.page_size
+        longest = max((self._length[s] + c for s, c in zip(sequences, counts)), default=0)
+        if self.positions is not None and longest > self.positions:
+            raise RuntimeError(f"{longest} tokens of a sequence, there are {self.positions} positions")
         need = [-(-(self._length[s] + c) // ps) - len(self._held[s]) for s, c in zip(sequences, counts)]
         if sum(need) > len(self._free):
             raise RuntimeError(f"{sum(need)} pages needed, {len(self._free)} free")
@@ -97,7 +103,7 @@ class PageTable:
         table = [self._held[s] + [-1] * (columns - len(self._held[s])) for s in sequences]
         ints = lambda v, *shape: torch.tensor(v, dtype=torch.int32).reshape(*shape).to(self.device)
         return Batch(ints(positions, -1), ints(slots, -1), ints(starts, -1), ints(starts_all, -1), ints(table, len(sequences), columns), ints(lengths, -1),
-                     starts_all[-1], all(c == 1 for c in counts), fresh)
+                     starts_all[-1], all(c == 1 for c in counts), fresh, longest)
 
 
 class AttentionBlock(ServedBlock):
@@ -132,6 +138,8 @@ class AttentionBlock(ServedBlock):
 
     @torch.no_grad()
     def serve(self, h: torch.Tensor, hs: torch.Tensor, batch: Batch, angles: torch.Tensor) -> torch.Tensor:
+        if batch.longest > angles.shape[0]:                    # their keys would be NaN, and stay in the cache
+            raise ValueError(f"{batch.longest} tokens of a sequence, angles of {angles.shape[0]} positions")
         qkv, out = self._laid_out()
         if self.pages is None:
             raise RuntimeError("the layer has no cache: call cache()")
@@ -175,7 +183,7 @@ class DecoderStack(MlpStack):
         for b in self.blocks:
             if isinstance(b, AttentionBlock):
                 b.cache(pages, page_size, dtype)
-        return PageTable(pages, page_size, self.final_weight.device)
+        return PageTable(pages, page_size, self.final_weight.device, self.angles.shape[0])
 
     def serve(self, x: torch.Tensor, batch: Batch) -> torch.Tensor:
         """New tokens' stream [tokens, width], packed as the batch says -> the final norm's output."""
