@@ -175,6 +175,14 @@ class DecoderStack(MlpStack):
             self.blocks.append(_Mlp(width, hidden, device))
         self.angles = rotary_angles(positions, head_dim, device=device)
 
+    def _apply(self, *args, **kwargs):
+        super()._apply(*args, **kwargs)
+        device = self.final_weight.device                      # the angles go where the weights go, and stay fp32
+        if self.angles.is_meta and device.type != "meta":
+            self.angles = rotary_angles(*self.angles.shape, device=device)
+        self.angles = self.angles.to(device)
+        return self
+
     def forward(self, x):
         raise RuntimeError("a DecoderStack is for serving: call serve()")
 
