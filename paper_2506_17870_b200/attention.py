@@ -11,6 +11,7 @@ from __future__ import annotations
 
 from typing import List, NamedTuple, Optional, Sequence
 
+import numpy as np
 import torch
 
 from . import binding as nq
@@ -40,7 +41,8 @@ class Batch(NamedTuple):
 
 class PageTable:
     """Which pages of a cache (or of the caches of several layers) each sequence holds.  Kept on the host; extend() hands out what a
-    pass over new tokens needs on the device.  positions: how many tokens a sequence may have (None: as many as there are pages for)."""
+    pass over new tokens needs on the device.  positions: how many tokens a sequence may have (None: as many as there are pages for).  Where they are given, a batch's table has
+    columns for all of them, so that a captured pass over its tensors follows sequences into new pages."""
 
     def __init__(self, pages: int, page_size: int, device="cuda", positions: Optional[int] = None):
         if pages < 0 or page_size < 1:
@@ -48,6 +50,7 @@ class PageTable:
         if positions is not None and positions < 0:
             raise ValueError(f"{positions} positions")
         self.page_size, self.device, self.positions = page_size, device, positions
+        self.columns = None if positions is None else max(1, min(pages, -(-positions // page_size)))
         self._free = list(range(pages - 1, -1, -1))
         self._held: dict = {}                                  # sequence -> its pages
         self._length: dict = {}
@@ -99,10 +102,12 @@ class PageTable:
             lengths.append(at + c)
             starts.append(starts[-1] + c)
             starts_all.append(starts_all[-1] + at + c)
-        columns = max([1] + [len(self._held[s]) for s in sequences])
-        table = [self._held[s] + [-1] * (columns - len(self._held[s])) for s in sequences]
+        columns = self.columns or max([1] + [len(self._held[s]) for s in sequences])
+        table = np.full((len(sequences), columns), -1, np.int32)
+        for row, s in zip(table, sequences):
+            row[:len(self._held[s])] = self._held[s]
         ints = lambda v, *shape: torch.tensor(v, dtype=torch.int32).reshape(*shape).to(self.device)
-        return Batch(ints(positions, -1), ints(slots, -1), ints(starts, -1), ints(starts_all, -1), ints(table, len(sequences), columns), ints(lengths, -1),
+        return Batch(ints(positions, -1), ints(slots, -1), ints(starts, -1), ints(starts_all, -1), torch.from_numpy(table).to(self.device), ints(lengths, -1),
                      starts_all[-1], all(c == 1 for c in counts), fresh, longest)
 
 
