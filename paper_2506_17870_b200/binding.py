@@ -928,6 +928,28 @@ class nq_kv_pages(ctypes.Structure):
         self.tensors, self.index = (k, v, ks, vs), index
 
 
+class _NoGradient(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, what, y, *operands):
+        ctx.what = what
+        ctx.mark_dirty(y)
+        return y
+
+    @staticmethod
+    def backward(ctx, _):
+        raise RuntimeError(f"{ctx.what} has no gradient: call it under torch.no_grad(), or on detached tensors")
+
+
+def _serving(what: str, y: torch.Tensor, *operands: Optional[torch.Tensor]) -> torch.Tensor:
+    """The attention calls have no gradients.  Where one is wanted of an operand, autograd would take their output for a constant: it is tied
+    to a node that refuses to be differentiated."""
+    if torch.is_grad_enabled():
+        for t in operands:
+            if t is not None and t.requires_grad:
+                return _NoGradient.apply(what, y, *operands)
+    return y
+
+
 def _cache_tensor(t: torch.Tensor, name: str, index: int) -> None:
     if t.get_device() != index or index < 0:
         _on(t, name, index)
@@ -1017,12 +1039,12 @@ def nq_qk_norm_rotate(x: torch.Tensor, angles: Optional[torch.Tensor], positions
                                    None if angles is None else angles.data_ptr(), None if positions is None else _ints(positions, "positions", tokens, index),
                                    q.data_ptr(), None if k is None else k.data_ptr(), None if cache is None else _pages_on(cache, index),
                                    None if slots is None else _ints(slots, "slots", tokens, index), _raw_stream(x)), "nq_qk_norm_rotate")
-    return q, k
+    return _serving("nq_qk_norm_rotate", q, x, q_weight), None if k is None else _serving("nq_qk_norm_rotate", k, x, k_weight)
 
 
 def nq_kv_cache_write(cache: nq_kv_pages, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
     """Stores k, v [tokens, kv_heads, head_dim] (fp32 or bf16) in the slots int32 [tokens], quantised as the cache holds them; a slot
-    outside the cache (-1, say) is passed over."""
+    outside the cache (-1, say) is passed over.  The cache holds values: no gradient leads back through it."""
     index = k.get_device()
     heads, dim = cache.kv_heads, cache.head_dim
     if k.dtype not in _FLOATS or v.dtype is not k.dtype or v.shape != k.shape:
@@ -1097,7 +1119,7 @@ def nq_paged_attention(q: torch.Tensor, cache: nq_kv_pages, table: torch.Tensor,
     _check(lib().nq_paged_attention(pages, q.data_ptr(), ldq, heads, table.data_ptr(), ld_table, cols, _ints(lengths, "lengths", seqs, index), seqs,
                                     _window(window), dim ** -0.5 if scale is None else scale, y_out.data_ptr(), ldy, workspace.data_ptr(),
                                     workspace.numel() * workspace.element_size(), _raw_stream(q)), "nq_paged_attention")
-    return y_out
+    return _serving("nq_paged_attention", y_out, q)
 
 
 def nq_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts_q: torch.Tensor, starts_k: Optional[torch.Tensor] = None, *,
@@ -1129,7 +1151,7 @@ def nq_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, start
     d = nq_prompt_desc(seqs, rows, k.shape[0], ldq, ldk, ldv, ldy, heads, kv_heads, dim, causal, _window(window), dim ** -0.5 if scale is None else scale)
     _check(lib().nq_prompt_attention(ctypes.addressof(d), q.data_ptr(), k.data_ptr(), v.data_ptr(), _ints(starts_q, "starts_q", seqs + 1, index),
                                      _ints(starts_k, "starts_k", seqs + 1, index), y_out.data_ptr(), _raw_stream(q)), "nq_prompt_attention")
-    return y_out
+    return _serving("nq_prompt_attention", y_out, q, k, v)
 
 
 def nq_i8_mma_ceiling(stage_iters: int) -> float:
