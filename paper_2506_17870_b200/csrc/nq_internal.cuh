@@ -45,6 +45,9 @@ int sm_count();
 // Defined in nq_runtime.cu; kernels get its address through status_word().
 unsigned int* status_word();
 
+// The driver's cuTensorMapEncodeTiled, null where it has none.  (As the two above: safe to call from several threads.)
+void* tensor_map_encoder();
+
 // The paper's 64-bit packed words -> sliced layout (kernel beside the codec, whose slice cutter it uses).
 int word64_to_sliced_launch(const uint64_t* words, int bits, int64_t rows, int64_t cols, uint8_t* packed, cudaStream_t s);
 

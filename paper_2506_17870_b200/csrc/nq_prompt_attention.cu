@@ -659,16 +659,8 @@ typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void
 // Heads of bf16 values as a 3-D tensor (values, heads, tokens), a token `pitch` elements after the other: boxes of 64 values of one head
 // x box_tokens tokens in the 128-byte swizzle.
 int encode_heads(CUtensorMap* map, const void* base, int64_t dim, int64_t heads, int64_t tokens, int64_t pitch, int box_tokens) {
-    static EncodeFn fn = nullptr;
-    if (!fn) {
-        void* sym = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &q) != cudaSuccess || !sym || q != cudaDriverEntryPointSuccess) {
-            (void)cudaGetLastError();
-            return NQ_ERR_CUDA;
-        }
-        fn = reinterpret_cast<EncodeFn>(sym);
-    }
+    const EncodeFn fn = reinterpret_cast<EncodeFn>(tensor_map_encoder());
+    if (!fn) return NQ_ERR_CUDA;
     const cuuint64_t dims[3] = {(cuuint64_t)dim, (cuuint64_t)heads, (cuuint64_t)(tokens > 0 ? tokens : 1)}, strides[2] = {(cuuint64_t)dim * 2, (cuuint64_t)pitch * 2};
     const cuuint32_t box[3] = {64, 1, (cuuint32_t)box_tokens}, each[3] = {1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,

@@ -2,6 +2,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/nq.h"
 #include "nq_internal.cuh"
 
@@ -10,27 +12,41 @@ namespace nq {
 __device__ unsigned int g_status_word[4];
 
 int sm_count() {
-    static int cached[64] = {0};
+    static std::atomic<int> cached[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
-    if (cached[dev] == 0) {
-        int n = 0;
+    int n = cached[dev].load(std::memory_order_relaxed);
+    if (n == 0) {
         if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) n = 148;
-        cached[dev] = n;
+        cached[dev].store(n, std::memory_order_relaxed);
     }
-    return cached[dev];
+    return n;
 }
 
 unsigned int* status_word() {
-    static unsigned int* cached[64] = {nullptr};
+    static std::atomic<void*> cached[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
-    if (!cached[dev]) {
-        void* p = nullptr;
+    void* p = cached[dev].load(std::memory_order_relaxed);
+    if (!p) {
         if (cudaGetSymbolAddress(&p, g_status_word) != cudaSuccess) return nullptr;
-        cached[dev] = static_cast<unsigned int*>(p);
+        cached[dev].store(p, std::memory_order_relaxed);
     }
-    return cached[dev];
+    return static_cast<unsigned int*>(p);
+}
+
+void* tensor_map_encoder() {
+    static std::atomic<void*> cached;
+    void* p = cached.load(std::memory_order_relaxed);
+    if (!p) {
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || !p || q != cudaDriverEntryPointSuccess) {
+            (void)cudaGetLastError();
+            return nullptr;
+        }
+        cached.store(p, std::memory_order_relaxed);
+    }
+    return p;
 }
 
 }  // namespace nq
