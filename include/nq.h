@@ -495,9 +495,9 @@ NQ_API int nq_kv_cache_read(const nq_kv_pages *cache, const int32_t *table, int6
  *   overlap Q or the cache
  *   table (device) int32 [seqs, table_cols], lengths (device) int32 [seqs]
  *   Sums, maxima and weights are fp32.  A weight is rounded to bf16 (bf16 cache) or f16 (8-bit caches, times the value's scale)
- *   for its product with the values, which is exact in both; queries meet 8-bit keys as f16, scaled by a power of two.  As f16, a
- *   weight times its value's scale is good to 2^-11 of itself down to 2^-21 of the largest such product of its sequence and head, and under
- *   2^-32 of that is lost.
+ *   for its product with the values, which is exact in both; queries meet 8-bit keys as f16, scaled by a power of two (exact but for values
+ *   under 2^-17 of the head's largest).  As f16, a weight times its value's scale is good to 2^-11 of itself down to 2^-21 of the largest such
+ *   product of its sequence and head, and under 2^-32 of that is lost.
  *   workspace (device) nq_paged_attention_workspace_bytes() bytes, 16-byte aligned: parts of sequences that several thread blocks
  *   share.  Two calls that may run at the same time need two.  No atomics: results repeat bit for bit.
  */
@@ -514,8 +514,9 @@ NQ_API int nq_paged_attention(const nq_kv_pages *cache, const void *Q, int64_t l
  *   What a row does not see has no part in it, infinities and NaN in its keys or values included.
  *   Q, Y bf16 [rows_q, q_heads * head_dim], K, V bf16 [rows_k, kv_heads * head_dim] (device), pitches multiples of 8, 16-byte aligned
  *   starts (device) int32 [seqs + 1], not decreasing, in [0, rows]: read when the kernel runs.  Rows of Y outside the sequences are left as they were.
- *   Products on the tensor core (exact products, fp32 sums); maxima, sums and weights are fp32; a weight is rounded to bf16 for its product with
- *   the values.  scale > 0.  Needs no workspace; results repeat bit for bit.
+ *   Products on the tensor core (exact products, fp32 sums); maxima, sums and weights are fp32, a weight good to 2^-13.7 of itself (part of the
+ *   exponentials come from a polynomial), and rounded to bf16 for its product with the values.  scale > 0.  Needs no workspace; results repeat
+ *   bit for bit.  Y must not overlap Q, K or V.
  */
 typedef struct {
     int64_t seqs, rows_q, rows_k, ldq, ldk, ldv, ldy;

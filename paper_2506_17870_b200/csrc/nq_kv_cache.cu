@@ -530,7 +530,7 @@ extern "C" int nq_kv_cache_read(const nq_kv_pages* cache, const int32_t* table, 
     a.parts = (turns + a.per_part - 1) / a.per_part;
     // two rows a warp, as long as each SM gets 64 warps or more
     const long long each = rows / (64ll * nq::sm_count());
-    a.tokens = a.parts > 1 || each < 1 ? 1 : each < 2 ? (int)each : 2;
+    a.tokens = a.parts > 1 || each < 2 ? 1 : 2;
     const cudaStream_t s = (cudaStream_t)stream;
     using bf16 = __nv_bfloat16;
     if (cache->head_dim == 64)

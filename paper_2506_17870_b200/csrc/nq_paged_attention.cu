@@ -4,8 +4,6 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
-#include <type_traits>
-
 #include "../../include/nq.h"
 #include "nq_kv_cache.cuh"
 #include "nq_ranges.cuh"
@@ -90,8 +88,7 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// Two codes (in the low 16 bits) to f16 exactly.
-template <int CACHE>
+// Two e4m3 codes (in the low 16 bits) to f16 exactly.
 __device__ __forceinline__ uint32_t codes2(uint32_t two) {
     uint32_t h;
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((unsigned short)two));
@@ -101,8 +98,8 @@ __device__ __forceinline__ uint32_t codes2(uint32_t two) {
 template <int CACHE>
 __device__ __forceinline__ void codes4(uint32_t w, uint32_t& lo, uint32_t& hi) {
     if (CACHE == NQ_E4M3) {
-        lo = codes2<CACHE>(w);
-        hi = codes2<CACHE>(w >> 16);
+        lo = codes2(w);
+        hi = codes2(w >> 16);
     } else {
         const uint32_t u = w ^ 0x80808080u;
         const __half2 off = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));
@@ -330,8 +327,8 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ
                         }
                         q_scale[n][0] = q_scale[n][1] = a.scale2;
                     } else {
-                        // bf16 to f16, times a power of two that puts the head's largest into [1, 2): exact but for values below
-                        // 2^-13 of it, which lose bits under 2^-24 of it
+                        // bf16 to f16, times a power of two that puts the head's largest into [1, 2): exact but for values below 2^-17 of it,
+                        // whose 8 bits go under f16's last, 2^-24
                         uint4 v[2 * kKPieces];
                         uint32_t m = 0;
 #pragma unroll
@@ -346,7 +343,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ
                         m = max(m >> 16, m & 0xffffu);
                         m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
                         m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-                        const int e = min(max((int)(m >> 7), 1), 253);               // 254, 255 (infinity, NaN): infinite in f16, as they should be
+                        const int e = min(max((int)(m >> 7), 1), 253);               // 254: [2, 4); 255 (infinity, NaN): no finite number in f16 either
                         const float up = __int_as_float((254 - e) << 23), down = __int_as_float(e << 23);
 #pragma unroll
                         for (int w = 0; w < 8 * kKPieces; ++w) {
@@ -522,7 +519,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !(D == 128 && CACHE != NQ
                         pf[u][n][0] = transpose8x8(*reinterpret_cast<const uint32_t*>(&x));
                         pf[u][n][1] = transpose8x8(*reinterpret_cast<const uint32_t*>(&y));
                     } else {
-                        // bf16 has fp32's range: a weight is off by at most 2^-9 of itself
+                        // bf16 has fp32's range: a weight is off by at most 2^-8 of itself
                         const __nv_bfloat162 x = __floats2bfloat162_rn(p[0], p[1]), y = __floats2bfloat162_rn(p[2], p[3]);
                         pf[u][n][0] = transpose8x8(*reinterpret_cast<const uint32_t*>(&x));
                         pf[u][n][1] = transpose8x8(*reinterpret_cast<const uint32_t*>(&y));

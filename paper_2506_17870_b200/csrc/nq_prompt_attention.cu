@@ -148,10 +148,10 @@ __device__ __forceinline__ void hide(uint32_t (&s)[32], int lo, int hi) {
     for (int c = 0; c < 32; ++c) s[c] = (keep >> c) & 1u ? s[c] : 0xff800000u;
 }
 
-// Weights 2^(s scale + minus) of 32 scores, their sum, and as pairs of bf16 (a weight is off by at most 2^-9 of itself).
+// Weights 2^(s scale + minus) of 32 scores, their sum, and as pairs of bf16 (a weight is off by at most 2^-8 of itself).
 // The exponential unit takes 4 a cycle and scheduler, which alone would be as long as both products.  So 3 of 8 come from the other
 // pipes: 2^y = 2^n 2^f, n = y rounded (y + 1.5 * 2^23 holds it in its low bits), f in [-1/2, 1/2] by a polynomial of degree 3, fitted
-// to 2^f for the least relative error on that interval: 7.5e-5 (2^-13.7), where a weight's rounding is 2^-9.  y under -127 counts as that,
+// to 2^f for the least relative error on that interval: 7.5e-5 (2^-13.7), where a weight's rounding is 2^-8.  y under -127 counts as that,
 // whose 2^n is made as 0; a NaN stays one.  (16384 tokens of 8 heads: none 492 us, one of 8 476, one of 4 428, 3 of 8 421.)
 __device__ __forceinline__ void weights_of(const uint32_t (&s)[32], float scale, float minus, uint64_t& sum, uint32_t (&p)[16]) {
     constexpr float kBig = 12582912.0f;
