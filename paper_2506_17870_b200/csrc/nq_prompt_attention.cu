@@ -33,6 +33,10 @@ using namespace sm100;
 constexpr int kThreads = 384;            // warp 0 TMA and units, warps 1 and 2 MMA of the tiles (1 also TMEM), warp 3 looks after V, warps 4-7 and 8-11 softmax of the tiles
 constexpr int kTile = 128, kKeys = 64;   // rows of a tile, keys of a step
 constexpr float kRescale = 8.0f;
+// The tensor core cuts each product off some 25 bits below the running sum that it is added to, towards zero: over n keys whose values have one sign
+// that takes n 2^-27 of a sum (measured: 0.8 % of 2^20 keys, 10 % of 2^24).  So every kFold steps (a part: 2^15 keys) a row's sums go to fp32 sums of
+// the thread's own, in local memory, and start anew; its sum of weights likewise.
+constexpr int kFold = 512;               // (a power of two)
 
 template <int D>
 struct Shape {
@@ -177,7 +181,28 @@ __device__ __forceinline__ void weights_of(const uint32_t (&s)[32], float scale,
     }
 }
 
+// A row's sums in tensor memory and those of its parts so far (none: !more), the latter times `then`, together: to the parts, or back.  (A function
+// of its own: in the place of its calls it slowed down every step, 16384 tokens of 8 heads 433 -> 443 us and, at a step's end, 467.)
 template <int D>
+__device__ __noinline__ void fold(uint32_t o_at, float* far, bool more, float then, bool back) {
+#pragma unroll 1
+    for (int c0 = 0; c0 < D; c0 += 32) {
+        uint32_t o[32];
+        tmem_ld_32x32(o_at + c0, o);
+        tmem_ld_wait();
+        tmem_arrived(o);
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+            const float x = __uint_as_float(o[c]) + (more ? far[c0 + c] * then : 0.0f);
+            if (back) o[c] = __float_as_uint(x); else far[c0 + c] = x;
+        }
+        if (back) tmem_st_32x32(o_at + c0, o);
+    }
+    tmem_st_wait();
+}
+
+// LONG: a sequence may have more than kFold steps of keys.
+template <int D, bool LONG>
 __global__ void __launch_bounds__(kThreads, 1)
 prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const PromptArgs a) {
     using P = Shape<D>;
@@ -391,7 +416,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                         if (sums_due && !by_hand) {
                             const uint64_t dv = dv0 + sp * (P::kStageBytes / 16);
 #pragma unroll
-                            for (int k = 0; k < kKeys / 16; ++k) mma_bf16_ts(sums, scores + 8 * k, dv + k * (16 * 128 / 16), kPV, k > 0 || j - 2 > lo);
+                            for (int k = 0; k < kKeys / 16; ++k) mma_bf16_ts(sums, scores + 8 * k, dv + k * (16 * 128 / 16), kPV, k > 0 || (LONG ? ((j - 2 - lo) & (kFold - 1)) != 0 : j - 2 > lo));
                         }
                         if (scores_due) {
                             const uint64_t dk = dk0 + s * (P::kStageBytes / 16);
@@ -467,6 +492,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         // A tile without rows (the second one of a head's last rows) is done at once, and its warps wait for the next unit as long as the
         // other tile has steps: with 10^8 keys that is longer than a step's limit.
         int idle = 0;
+        float far[LONG ? D + 2 : 1];                               // sums of the parts so far, the maximum that they go with, the sum of their weights
         for (uint32_t n = 0; ok; ++n, give_back(n - 1)) {
             const Unit* u = take(n, idle);
             if (!u) break;
@@ -480,123 +506,140 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
             it += u->end - u->begin;
             float top = -INFINITY, total = 0.0f;
             bool there = false;                                    // the next step's scores, as far as is known
-            for (int j = lo_t; j < hi_t; ++j) {
-                const uint32_t s_at = tmem + kS + t * kTile + (j & 1) * kKeys + lanes;
-                if (!__all_sync(0xffffffffu, there)) {
-                    ok = mbar_wait(s_full + 16 * t + 8 * (j & 1), (phases >> (j & 1)) & 1, abort_flag, a.status, 0x340u);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                }
-                phases ^= 1u << (j & 1);
-                tc_fence_after_sync();
-                const bool hides = j * kKeys < all_lo || (j + 1) * kKeys > all_hi;
-                const int lo = see_lo - j * kKeys, hi = see_hi - j * kKeys;                  // columns that this row sees
-                uint32_t s[2][32];
-                tmem_ld_32x32(s_at, s[0]);
-                tmem_ld_32x32(s_at + 32, s[1]);
-                tmem_ld_wait();
-                float m = -INFINITY, m1 = -INFINITY, m2 = -INFINITY, m3 = -INFINITY;
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    tmem_arrived(s[x]);
-                    if (hides) hide(s[x], lo - 32 * x, hi - 32 * x);
-                }
-#pragma unroll
-                for (int c = 0; c < 32; c += 4) {
-                    m = max3(m, __uint_as_float(s[0][c]), __uint_as_float(s[0][c + 1]));
-                    m1 = max3(m1, __uint_as_float(s[0][c + 2]), __uint_as_float(s[0][c + 3]));
-                    m2 = max3(m2, __uint_as_float(s[1][c]), __uint_as_float(s[1][c + 1]));
-                    m3 = max3(m3, __uint_as_float(s[1][c + 2]), __uint_as_float(s[1][c + 3]));
-                }
-                m = max3(m, m1, max3(m2, m2, m3)) * a.scale2;
-                const bool move = m > top + kRescale;
-                if (__any_sync(0xffffffffu, move)) {
-                    const float to = fmaxf(top, m), by = top == -INFINITY ? 0.0f : exp2a(top - to);
-                    top = to;
-                    total *= by;
-                    if (j > lo_t) {
-                        // (that S(j) is there says that PV(j - 2) is complete)
-                        ok = sums_of(j - 1);
+            int from, upto = lo_t;                                 // steps of the sums in tensor memory
+            do {
+                from = upto;
+                upto = LONG ? min(from + kFold, hi_t) : hi_t;
+                for (int j = from; j < upto; ++j) {
+                    const uint32_t s_at = tmem + kS + t * kTile + (j & 1) * kKeys + lanes;
+                    if (!__all_sync(0xffffffffu, there)) {
+                        ok = mbar_wait(s_full + 16 * t + 8 * (j & 1), (phases >> (j & 1)) & 1, abort_flag, a.status, 0x340u);
                         ok = __all_sync(0xffffffffu, ok);
                         if (!ok) break;
-                        tc_fence_after_sync();
-#pragma unroll 1
-                        for (int c0 = 0; c0 < D; c0 += 32) {
-                            uint32_t o[32];
-                            tmem_ld_32x32(o_at + c0, o);
-                            tmem_ld_wait();
-                            tmem_arrived(o);
-#pragma unroll
-                            for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * by);
-                            tmem_st_32x32(o_at + c0, o);
-                        }
                     }
-                }
-                const float minus = top == -INFINITY ? 0.0f : -top;
-                uint64_t sum = 0;
+                    phases ^= 1u << (j & 1);
+                    tc_fence_after_sync();
+                    const bool hides = j * kKeys < all_lo || (j + 1) * kKeys > all_hi;
+                    const int lo = see_lo - j * kKeys, hi = see_hi - j * kKeys;                  // columns that this row sees
+                    uint32_t s[2][32];
+                    tmem_ld_32x32(s_at, s[0]);
+                    tmem_ld_32x32(s_at + 32, s[1]);
+                    tmem_ld_wait();
+                    float m = -INFINITY, m1 = -INFINITY, m2 = -INFINITY, m3 = -INFINITY;
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    uint32_t p[16];
-                    weights_of(s[x], a.scale2, minus, sum, p);
-                    tmem_st_32x16(s_at + 16 * x, p);
-                }
-                total += sum2(sum);
-                there = j + 1 < hi_t && mbar_try_wait(s_full + 16 * t + 8 * ((j + 1) & 1), (phases >> ((j + 1) & 1)) & 1);
-                tmem_st_wait();
-                if (hides) {
-                    const uint32_t sl = (it0 + j) % ST;
-                    ok = mbar_wait(v_ok + 8 * sl, ((it0 + j) / ST) & 1, abort_flag, a.status, 0x341u);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                    if (v_odd[sl]) {
-                        // some of V is no number, and this tile hides some of it: the product by hand, of what each row sees
-                        if (j > lo_t) {
+                    for (int x = 0; x < 2; ++x) {
+                        tmem_arrived(s[x]);
+                        if (hides) hide(s[x], lo - 32 * x, hi - 32 * x);
+                    }
+#pragma unroll
+                    for (int c = 0; c < 32; c += 4) {
+                        m = max3(m, __uint_as_float(s[0][c]), __uint_as_float(s[0][c + 1]));
+                        m1 = max3(m1, __uint_as_float(s[0][c + 2]), __uint_as_float(s[0][c + 3]));
+                        m2 = max3(m2, __uint_as_float(s[1][c]), __uint_as_float(s[1][c + 1]));
+                        m3 = max3(m3, __uint_as_float(s[1][c + 2]), __uint_as_float(s[1][c + 3]));
+                    }
+                    m = max3(m, m1, max3(m2, m2, m3)) * a.scale2;
+                    const bool move = m > top + kRescale;
+                    if (__any_sync(0xffffffffu, move)) {
+                        const float to = fmaxf(top, m), by = top == -INFINITY ? 0.0f : exp2a(top - to);
+                        top = to;
+                        total *= by;
+                        if (j > from) {
+                            // (that S(j) is there says that PV(j - 2) is complete)
                             ok = sums_of(j - 1);
                             ok = __all_sync(0xffffffffu, ok);
                             if (!ok) break;
                             tc_fence_after_sync();
-                        }
 #pragma unroll 1
-                        for (int c0 = 0; c0 < D; c0 += 32) {
-                            uint32_t o[32];
-                            if (j > lo_t) {
+                            for (int c0 = 0; c0 < D; c0 += 32) {
+                                uint32_t o[32];
                                 tmem_ld_32x32(o_at + c0, o);
                                 tmem_ld_wait();
                                 tmem_arrived(o);
-                            } else {
 #pragma unroll
-                                for (int c = 0; c < 32; ++c) o[c] = 0;
+                                for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * by);
+                                tmem_st_32x32(o_at + c0, o);
+                            }
+                        }
+                    }
+                    const float minus = top == -INFINITY ? 0.0f : -top;
+                    uint64_t sum = 0;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        uint32_t p[16];
+                        weights_of(s[x], a.scale2, minus, sum, p);
+                        tmem_st_32x16(s_at + 16 * x, p);
+                    }
+                    total += sum2(sum);
+                    there = j + 1 < hi_t && mbar_try_wait(s_full + 16 * t + 8 * ((j + 1) & 1), (phases >> ((j + 1) & 1)) & 1);
+                    tmem_st_wait();
+                    if (hides) {
+                        const uint32_t sl = (it0 + j) % ST;
+                        ok = mbar_wait(v_ok + 8 * sl, ((it0 + j) / ST) & 1, abort_flag, a.status, 0x341u);
+                        ok = __all_sync(0xffffffffu, ok);
+                        if (!ok) break;
+                        if (v_odd[sl]) {
+                            // some of V is no number, and this tile hides some of it: the product by hand, of what each row sees
+                            if (j > from) {
+                                ok = sums_of(j - 1);
+                                ok = __all_sync(0xffffffffu, ok);
+                                if (!ok) break;
+                                tc_fence_after_sync();
                             }
 #pragma unroll 1
-                            for (int k = 0; k < kKeys; ++k) {
-                                uint32_t two = tmem_ld_32x1(s_at + k / 2);
-                                tmem_ld_wait();
-                                asm volatile("" : "+r"(two));
-                                const float w = __uint_as_float((k & 1) ? two & 0xffff0000u : two << 16);
-                                const bool seen = k >= lo && k < hi;
-                                const uint8_t* v = smem + 2 * P::kTileBytes + (ST + sl) * P::kStageBytes + (c0 / 64) * P::kSlab + k * 128;
+                            for (int c0 = 0; c0 < D; c0 += 32) {
+                                uint32_t o[32];
+                                if (j > from) {
+                                    tmem_ld_32x32(o_at + c0, o);
+                                    tmem_ld_wait();
+                                    tmem_arrived(o);
+                                } else {
 #pragma unroll
-                                for (int x = 0; x < 4; ++x) {
-                                    const uint4 q = *reinterpret_cast<const uint4*>(v + ((((c0 % 64) / 8 + x) ^ (k & 7)) << 4));
-                                    const uint32_t words[4] = {q.x, q.y, q.z, q.w};
+                                    for (int c = 0; c < 32; ++c) o[c] = 0;
+                                }
+#pragma unroll 1
+                                for (int k = 0; k < kKeys; ++k) {
+                                    uint32_t two = tmem_ld_32x1(s_at + k / 2);
+                                    tmem_ld_wait();
+                                    asm volatile("" : "+r"(two));
+                                    const float w = __uint_as_float((k & 1) ? two & 0xffff0000u : two << 16);
+                                    const bool seen = k >= lo && k < hi;
+                                    const uint8_t* v = smem + 2 * P::kTileBytes + (ST + sl) * P::kStageBytes + (c0 / 64) * P::kSlab + k * 128;
 #pragma unroll
-                                    for (int y = 0; y < 4; ++y) {
-                                        float& e0 = reinterpret_cast<float&>(o[8 * x + 2 * y]);
-                                        float& e1 = reinterpret_cast<float&>(o[8 * x + 2 * y + 1]);
-                                        e0 = seen ? fmaf(w, __uint_as_float(words[y] << 16), e0) : e0;
-                                        e1 = seen ? fmaf(w, __uint_as_float(words[y] & 0xffff0000u), e1) : e1;
+                                    for (int x = 0; x < 4; ++x) {
+                                        const uint4 q = *reinterpret_cast<const uint4*>(v + ((((c0 % 64) / 8 + x) ^ (k & 7)) << 4));
+                                        const uint32_t words[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                                        for (int y = 0; y < 4; ++y) {
+                                            float& e0 = reinterpret_cast<float&>(o[8 * x + 2 * y]);
+                                            float& e1 = reinterpret_cast<float&>(o[8 * x + 2 * y + 1]);
+                                            e0 = seen ? fmaf(w, __uint_as_float(words[y] << 16), e0) : e0;
+                                            e1 = seen ? fmaf(w, __uint_as_float(words[y] & 0xffff0000u), e1) : e1;
+                                        }
                                     }
                                 }
+                                tmem_st_32x32(o_at + c0, o);
                             }
-                            tmem_st_32x32(o_at + c0, o);
+                            tmem_st_wait();
                         }
-                        tmem_st_wait();
                     }
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(p_full + 16 * t + 8 * (j & 1));
                 }
-                tc_fence_before_sync();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(p_full + 16 * t + 8 * (j & 1));
-            }
+                if (!ok) break;
+                if (LONG && upto < hi_t) {
+                    ok = sums_of(upto - 1);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    tc_fence_after_sync();
+                    const float then = from > lo_t && far[D] != -INFINITY ? exp2a(far[D] - top) : 0.0f;
+                    fold<D>(o_at, far, from > lo_t, then, false);
+                    far[D + 1] = total + (from > lo_t ? far[D + 1] * then : 0.0f);
+                    far[D] = top;
+                    total = 0.0f;
+                }
+            } while (LONG && upto < hi_t);
             if (!ok) break;
             if (u->row[t] >= u->lq) {                     // the whole tile
                 idle = u->end - u->begin;
@@ -609,6 +652,11 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after_sync();
+            }
+            if (LONG && from > lo_t) {
+                const float then = far[D] != -INFINITY ? exp2a(far[D] - top) : 0.0f;
+                total += far[D + 1] * then;
+                fold<D>(o_at, far, true, then, true);
             }
             const float by = total == 0.0f ? 0.0f : 1.0f / total;
             // 32 channels at once go through shared memory, so that four lanes write 64 bytes of a row (a row a lane, 16 bytes at once, took
@@ -675,11 +723,14 @@ int launch_prompt(const nq_prompt_desc* d, const void* Q, const void* K, const v
     if (st == NQ_OK) st = encode_heads(&tmK, d->rows_k > 0 ? K : Q, D, d->kv_heads, d->rows_k, d->rows_k > 0 ? d->ldk : d->kv_heads * (int64_t)D, kKeys);
     if (st == NQ_OK) st = encode_heads(&tmV, d->rows_k > 0 ? V : Q, D, d->kv_heads, d->rows_k, d->rows_k > 0 ? d->ldv : d->kv_heads * (int64_t)D, kKeys);
     if (st != NQ_OK) return st;
-    if (cudaFuncSetAttribute(prompt_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem) != cudaSuccess) {
+    // No sequence has more keys than there are rows of them: up to one part there is nothing to fold (64 images of heads of 64 41.2 us, with the code
+    // for it 42.2; heads of 128 the same with and without).
+    const auto kernel = d->rows_k > kFold * kKeys ? prompt_kernel<D, true> : prompt_kernel<D, false>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem) != cudaSuccess) {
         (void)cudaGetLastError();
         return NQ_ERR_CUDA;
     }
-    return launch_chained(prompt_kernel<D>, (unsigned)most, kThreads, Shape<D>::kSmem, 1, s, tmQ, tmK, tmV, a);
+    return launch_chained(kernel, (unsigned)most, kThreads, Shape<D>::kSmem, 1, s, tmQ, tmK, tmV, a);
 }
 
 }  // namespace
