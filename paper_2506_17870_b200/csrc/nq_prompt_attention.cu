@@ -34,9 +34,9 @@ constexpr int kThreads = 384;            // warp 0 TMA and units, warps 1 and 2 
 constexpr int kTile = 128, kKeys = 64;   // rows of a tile, keys of a step
 constexpr float kRescale = 8.0f;
 // The tensor core cuts each product off some 25 bits below the running sum that it is added to, towards zero: over n keys whose values have one sign
-// that takes n 2^-27 of a sum (measured: 0.8 % of 2^20 keys, 10 % of 2^24).  So every kFold steps (a part: 2^15 keys) a row's sums go to fp32 sums of
+// that takes n 2^-27 of a sum (measured: 0.8 % of 2^20 keys, 10 % of 2^24).  So every kFold steps (a part: 2^16 keys) a row's sums go to fp32 sums of
 // the thread's own, in local memory, and start anew; its sum of weights likewise.
-constexpr int kFold = 512;               // (a power of two)
+constexpr int kFold = 1024;              // (a power of two)
 
 template <int D>
 struct Shape {
@@ -633,9 +633,10 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
                     tc_fence_after_sync();
-                    const float then = from > lo_t && far[D] != -INFINITY ? exp2a(far[D] - top) : 0.0f;
-                    fold<D>(o_at, far, from > lo_t, then, false);
-                    far[D + 1] = total + (from > lo_t ? far[D + 1] * then : 0.0f);
+                    const bool more = from > u->lo[t];             // (asked again: kept in a register, it slows the steps down by 2.5 %)
+                    const float then = more && far[D] != -INFINITY ? exp2a(far[D] - top) : 0.0f;
+                    fold<D>(o_at, far, more, then, false);
+                    far[D + 1] = total + (more ? far[D + 1] * then : 0.0f);
                     far[D] = top;
                     total = 0.0f;
                 }
@@ -653,7 +654,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
                 if (!ok) break;
                 tc_fence_after_sync();
             }
-            if (LONG && from > lo_t) {
+            if (LONG && from > u->lo[t]) {
                 const float then = far[D] != -INFINITY ? exp2a(far[D] - top) : 0.0f;
                 total += far[D + 1] * then;
                 fold<D>(o_at, far, true, then, true);
@@ -724,7 +725,7 @@ int launch_prompt(const nq_prompt_desc* d, const void* Q, const void* K, const v
     if (st == NQ_OK) st = encode_heads(&tmV, d->rows_k > 0 ? V : Q, D, d->kv_heads, d->rows_k, d->rows_k > 0 ? d->ldv : d->kv_heads * (int64_t)D, kKeys);
     if (st != NQ_OK) return st;
     // No sequence has more keys than there are rows of them: up to one part there is nothing to fold (64 images of heads of 64 41.2 us, with the code
-    // for it 42.2; heads of 128 the same with and without).
+    // for it 42.2; 64 queries of 32 heads of 128 behind 131072 keys 1671 us, without it 1655).
     const auto kernel = d->rows_k > kFold * kKeys ? prompt_kernel<D, true> : prompt_kernel<D, false>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem) != cudaSuccess) {
         (void)cudaGetLastError();

@@ -27,7 +27,7 @@ def one_query_a_head(q, k, v, scale):
 def test_values_of_one_sign_lose_nothing_to_their_number(size, dim, heads, keys):
     """Weights and result are rounded to bf16, half a step of 2^-8 each, which is 2^-8 of the result, for the weights' roundings have both signs: their
     mean over 2^10 keys that hold the weight would be off by 2^-8 2^-5 three times as often as not.  Beside that, sums of n products in parts of
-    2^15: n 2^-27 of the part at most, 2^-12, and the parts' own additions, 2^-24 each."""
+    2^16: n 2^-27 of the part at most, 2^-11, and the parts' own additions, 2^-24 each."""
     g = torch.Generator(device="cuda").manual_seed(3)
     q, k, _ = inputs(3, keys, *heads, dim)
     q = (size * q.float()).bfloat16()
@@ -42,8 +42,8 @@ def test_values_of_one_sign_lose_nothing_to_their_number(size, dim, heads, keys)
 
 @pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("heads", [(2, 1), (1, 1)])
-@pytest.mark.parametrize("keys", [32768, 32769, 32768 + 64, 32768 + 65, 65536 + 1, 100000])
-@pytest.mark.parametrize("causal,window", [(True, 0), (True, 40000), (False, 0)])
+@pytest.mark.parametrize("keys", [65536 - 40, 65536, 65537, 65536 + 64, 65536 + 65, 131072 + 1, 140000])
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 70000), (False, 0)])
 def test_where_the_parts_meet(causal, window, keys, heads, dim):
     rows = 150
     q, k, v = inputs(rows + 20, keys + 20, *heads, dim, keys)
@@ -59,21 +59,21 @@ def test_where_the_parts_meet(causal, window, keys, heads, dim):
 @pytest.mark.parametrize("slope", [1.0, -1.0, 0.0])
 def test_maxima_that_move_between_the_parts(slope, dim):
     """Scores that rise or fall by some hundreds along the keys, and a row whose first part sees nothing but minus infinity."""
-    keys = 100000
+    keys = 150000
     q, k, v = inputs(2, keys, 1, 1, dim)
     k = (0.1 * k.float() + (slope * torch.arange(keys, device="cuda") / keys * 400 / dim ** 0.5)[:, None, None]).bfloat16()
     q = torch.ones_like(q)
     if slope == 0.0:
-        k[:40000, :, 0] = -math.inf
+        k[:70000, :, 0] = -math.inf
     y = nq.nq_prompt_attention(q, k, v, starts_of([2]), starts_of([keys]), causal=False)
-    at = slice(40000, None) if slope == 0.0 else slice(None)
+    at = slice(70000, None) if slope == 0.0 else slice(None)
     want, bound = attend(q, k[at], v[at], torch.ones(2, len(k[at]), dtype=torch.bool, device="cuda"), dim ** -0.5)
     check(y, want, bound)
 
 
 @pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
-@pytest.mark.parametrize("keys", [32768 + 40, 32768 + 64, 65536 + 33])
+@pytest.mark.parametrize("keys", [65536 + 40, 65536 + 64, 131072 + 33])
 def test_no_numbers_hidden_in_the_first_step_of_a_part(keys, bad, dim):
     """The step that starts a part is the one that hides keys, so its product is made by hand."""
     rows = 30
