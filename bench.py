@@ -15,7 +15,8 @@ reported under rows.model_switch, and configs 3 and 5 run layer by layer through
 stack at batch 128, the ViT-B/16 linears at 256 x 197 tokens): rows.resnet101_stack_int8_6, rows.vit_b16_linears_int8_4.
 `value` is the integer-op throughput of the whole step (2*M*N*K per contraction; the codec kernels
 add time but no ops) in TOPS, summed over ranks.  Per-row numbers (TOPS per mode, GB/s per codec
-kernel) are reported under "rows".
+kernel) come as a line of their own, {"rows": ...}, on standard error: with them the result's line is 20 KB long, and what keeps
+no more than the end of a program's output lost its beginning.
 
     python bench.py [--gpus N] [--steps K] [--warmup W] [--impl ours|reference] [--sizes 4096,8192]
 
@@ -1141,6 +1142,7 @@ def main():
             import torch.distributed as dist
             dist.destroy_process_group()
     if line is not None:
+        print(json.dumps({"rows": line.pop("rows")}), file=sys.stderr, flush=True)
         print(json.dumps(line), flush=True)
 
 
