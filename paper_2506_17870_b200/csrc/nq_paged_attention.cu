@@ -22,7 +22,7 @@ namespace {
 // The sequences' steps (of all kv heads) lie in one long row that is cut evenly over the warps of a full GPU, however the
 // lengths fall.  What a warp has of a sequence and head, if not all of it, is joined in its thread block, and over thread blocks by
 // a second kernel, in a fixed order.
-// The matrix instruction cuts products off 24 bits below the running sum that they are added to, towards zero: a warp's sum over n tokens of values of
+// The matrix instruction cuts products off 25 bits below the running sum that they are added to, towards zero: a warp's sum over n tokens of values of
 // one sign loses n 2^-27.  Cut over 1184 warps or more, that stays under half a bf16 step up to a cache of some 6 10^8 tokens times heads.
 // Bound by HBM: 64 sequences of up to 8192 tokens, 32 / 8 heads of 128, bf16 193 us (0.97 of the copy rate), e4m3 120 (0.80); one of 131072 e4m3 tokens
 // 58 (0.72: some 11 us go to the cut, the first loads and the joins); one of 1501 INT8 tokens 10.5, all latency (15 with a search for the
