@@ -514,9 +514,9 @@ NQ_API int nq_paged_attention(const nq_kv_pages *cache, const void *Q, int64_t l
  *   What a row does not see has no part in it, infinities and NaN in its keys or values included.
  *   Q, Y bf16 [rows_q, q_heads * head_dim], K, V bf16 [rows_k, kv_heads * head_dim] (device), pitches multiples of 8, 16-byte aligned
  *   starts (device) int32 [seqs + 1], not decreasing, in [0, rows]: read when the kernel runs.  Rows of Y outside the sequences are left as they were.
- *   Products on the tensor core (exact products, fp32 sums of up to 2^16 keys, then fp32 sums of those); maxima, sums and weights are fp32, a weight good to 2^-13.7 of itself (part of the
- *   exponentials come from a polynomial), and rounded to bf16 for its product with the values.  scale > 0.  Needs no workspace; results repeat
- *   bit for bit.  Y must not overlap Q, K or V.
+ *   Products on the tensor core (exact products, fp32 sums of up to 2^16 keys, then fp32 sums of those); maxima, sums and weights are fp32, a
+ *   weight good to 2^-13.7 of itself (part of the exponentials come from a polynomial), and rounded to bf16 for its product with the values.
+ *   scale > 0.  Needs no workspace; results repeat bit for bit.  Y must not overlap Q, K or V.
  */
 typedef struct {
     int64_t seqs, rows_q, rows_k, ldq, ldk, ldv, ldy;
